@@ -463,7 +463,7 @@ def _plain_distill(st):
     case = st["case"]
     n, v, tau, alpha = case["rows"], case["classes"], case["temperature"], case["alpha"]
     z = st["z"].float()
-    there = (st["idx"] >= 0) & (st["idx"] < v)
+    there = (st["idx"] >= 0) & (st["idx"] < v) & (st["top"] != -math.inf)
     at = torch.where(there, st["idx"], 0).long()
     t = torch.where(there, st["top"], -math.inf) / tau
     t = t - t.max(1, keepdim=True)[0]
@@ -511,7 +511,7 @@ def _exact_distill(st):
         r = slice(i, min(n, i + step))
         z = st["z"][r].double().requires_grad_(True)
         idx = st["idx"][r].long()
-        there = (idx >= 0) & (idx < v)
+        there = (idx >= 0) & (idx < v) & (st["top"][r] != -math.inf)
         p = torch.softmax(torch.where(there, st["top"][r].double() / tau, -1e30), 1) * there
         logq = torch.log_softmax(z / tau, 1)
         logq = torch.gather(logq, 1, idx.clamp(0, v - 1))
