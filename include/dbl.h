@@ -18,7 +18,8 @@
  *    weights are KRSC, master weights and gradients are fp32.  Every tensor
  *    base address must be 16-byte aligned and every NHWC channel count a
  *    multiple of 8 (a 16-byte pixel row); violations return DBL_ERR_INVALID
- *    before anything is launched.  There is no slow fallback path.
+ *    before anything is launched.  There is no slow fallback path.  (The
+ *    operators of models over tokens take any size; see there.)
  *  - Kernels that wait on an asynchronous copy give up after a bounded time,
  *    record DBL_ERR_TIMEOUT in a device-side status word and return; read it
  *    with dbl_device_status().
@@ -57,7 +58,7 @@ enum {
     DBL_ERR_WORKSPACE = -5    /* ws_bytes smaller than *_workspace_bytes()           */
 };
 
-enum { DBL_F32 = 0, DBL_BF16 = 1 }; /* element types for dbl_progressive_resize */
+enum { DBL_F32 = 0, DBL_BF16 = 1 }; /* element types, where a call takes either */
 
 /* Text of the last error raised on the calling thread ("" if none). Host. */
 DBL_API const char* dbl_last_error(void);
@@ -509,6 +510,137 @@ DBL_API int dbl_zero_f32_2d(float* base, int64_t rows, int64_t cols, int64_t ld,
 
 /* Host: the integer taps above for one axis (i0, i1, lambda: [out] each). */
 DBL_API int dbl_resize_taps(int32_t in, int32_t out, int32_t* i0, int32_t* i1, float* lambda);
+
+/* ========================================================================
+ * Operators of models over tokens, trained by the same server and workers:
+ * layer norm, a gated linear recurrence along the sequence, and the
+ * distillation loss.  The paper trains a ResNet-18 only; the scheme (Sec. 3
+ * and 4) asks nothing of the model but its gradients, and these are the
+ * layers of a sequence model that the calls above do not provide (its
+ * products are dbl_conv_* with 1x1 filters).
+ *
+ * Beside the conventions at the top of this file:
+ *  - dtype is DBL_BF16 (the library's 16-bit format) or DBL_F32, for every
+ *    tensor given as void*; the arithmetic, statistics, states and sums are
+ *    fp32 in both, and each output is rounded once.
+ *  - Any channel count or class count is taken, odd ones included, and base
+ *    addresses need only the alignment of their element type.  Rows of a
+ *    multiple of 16 bytes at 16-byte aligned addresses are the fastest.
+ *  - ld_* are the elements from one row to the next (0: rows are dense).
+ *    Elements between the rows are not written.
+ *  - Unless stated, an output may not overlap an input.
+ *  - Sums are added in an order that depends on the sizes, the alignment and
+ *    the device alone: the same call gives the same bits.
+ * ======================================================================== */
+
+/* Layer norm over the last dimension, with the residual addition before it:
+ *   s = x [+ res],  mean = sum_c s / c,  var = sum_c (s - mean)^2 / c,
+ *   invstd = 1/sqrt(var + eps),  y = (s - mean)*invstd [*gamma] [+ beta].
+ * x, res, sum, y: [rows, c] of dtype; gamma, beta: [c] fp32 (NULL: 1 and 0);
+ * save_mean, save_invstd: [rows] fp32, for the backward pass (both NULL:
+ * not kept).  sum (or NULL): s rounded to dtype, the residual stream's new
+ * value; y is computed from s before that rounding.
+ * ld_in is the row stride of the tensors read (x, res; dy, dskip, x below),
+ * ld_out that of the tensors written (y, sum; dx below). */
+typedef struct {
+    int64_t rows;
+    int32_t c;
+    int32_t dtype;
+    int64_t ld_in, ld_out;
+    float eps;
+} dbl_ln_shape;
+DBL_API int dbl_layer_norm_fwd(const dbl_ln_shape* shape, const void* x, const void* res /* or NULL */,
+                               const float* gamma /* or NULL */, const float* beta /* or NULL */,
+                               void* sum /* or NULL */, void* y, float* save_mean, float* save_invstd, void* stream);
+
+/* Its backward pass, x being the normalised tensor (sum, where there is a
+ * residual):  xhat = (x - mean)*invstd, g = dy*gamma,
+ *   dx = invstd*(g - sum_c g / c - xhat * sum_c (g*xhat) / c) [+ dskip],
+ *   dgamma = sum_rows dy*xhat,  dbeta = sum_rows dy   ([c] fp32, overwritten).
+ * dskip (or NULL): the gradient that reaches x past the norm (the residual
+ * stream's).  dgamma and dbeta may both be NULL (the parameters are not
+ * trained); then no workspace is used. */
+DBL_API size_t dbl_layer_norm_workspace_bytes(const dbl_ln_shape* shape);
+DBL_API int dbl_layer_norm_bwd(const dbl_ln_shape* shape, const void* dy, const void* dskip /* or NULL */,
+                               const void* x, const float* gamma /* or NULL */, const float* save_mean,
+                               const float* save_invstd, void* dx, float* dgamma, float* dbeta, void* ws,
+                               size_t ws_bytes, void* stream);
+
+/* Gated linear recurrence along a sequence, each channel by itself:
+ *   a_i = 1/(1 + exp(-gate_i)),  h_i = a_i*h_{i-1} + (1 - a_i)*x_i,  i = 1..t.
+ * x, gate, h: [n, t, c] of dtype, step (b, i) at row b*t + i; h0 (or NULL: 0)
+ * and h_last (or NULL): [n, c] fp32, the states before the first and after
+ * the last step; h_last may be h0's buffer (a sequence continued call by call:
+ * t = 1 is the form for single tokens).  The state is fp32 throughout; only
+ * what is written to h is rounded.
+ * lengths (or NULL): [n] int32 on the device; sequence b has its first
+ * lengths[b] steps only (taken as 0 below 0 and as t above t).  The steps
+ * past it are neither read nor counted: h is 0 there, and h_last the state
+ * after the last step that counts (h0 where there is none).
+ * states (or NULL): [n, ceil(t/DBL_SCAN_CHUNK), c] fp32, the state before
+ * step DBL_SCAN_CHUNK*j + 1 of each sequence, which the backward pass starts
+ * from.  ld_x is the row stride of x and gate (dx and dgate below), so that
+ * both can be halves of one projection's output; ld_h that of h (dh below). */
+#define DBL_SCAN_CHUNK 64
+typedef struct {
+    int32_t n, t, c;
+    int32_t dtype;
+    int64_t ld_x, ld_h;
+} dbl_scan_shape;
+DBL_API size_t dbl_gated_scan_states_bytes(const dbl_scan_shape* shape);
+/* pass: DBL_PASS_FWD or DBL_PASS_DGRAD (0 for any other). */
+DBL_API size_t dbl_gated_scan_workspace_bytes(const dbl_scan_shape* shape, int pass);
+DBL_API int dbl_gated_scan_fwd(const dbl_scan_shape* shape, const void* x, const void* gate,
+                               const float* h0 /* or NULL */, const int32_t* lengths /* or NULL */, void* h,
+                               float* h_last /* or NULL */, float* states /* or NULL */, void* ws, size_t ws_bytes,
+                               void* stream);
+
+/* Its backward pass.  dh: the gradient of h; dh_last (or NULL: 0): that of
+ * h_last.  With G_i the whole gradient of h_i, G_i = dh_i + a_{i+1}*G_{i+1}
+ * (dh_last added at the last step that counts),
+ *   dx_i = (1 - a_i)*G_i,  dgate_i = G_i*(h_{i-1} - x_i)*a_i*(1 - a_i),
+ *   dh0 = a_1*G_1 (or NULL; dh_last where no step counts).
+ * dx and dgate are 0 past lengths.  h is recomputed in fp32 from states. */
+DBL_API int dbl_gated_scan_bwd(const dbl_scan_shape* shape, const void* dh, const float* dh_last /* or NULL */,
+                               const void* x, const void* gate, const float* states,
+                               const int32_t* lengths /* or NULL */, void* dx, void* dgate,
+                               float* dh0 /* or NULL */, void* ws, size_t ws_bytes, void* stream);
+
+/* Distillation from a teacher's largest logits, with the labels' cross-entropy
+ * beside it, forward and backward in one call.  Row r has logits z (dtype,
+ * [rows, classes], row stride ld), the teacher's k logits t and their classes
+ * ([rows, k] fp32 and int32, dense; k = 0: both NULL) and a label:
+ *   p = softmax over the k entries of t/T,  q = softmax(z/T) over all classes,
+ *   loss_r = alpha*T^2 * sum_j p_j*(log p_j - log q[class_j])
+ *            + (1 - alpha) * (logsumexp(z) - z[label]),
+ *   loss = sum_r w_r*loss_r,
+ *   dlogits_r = S*w_r*( alpha*T*(q - p) + (1 - alpha)*(softmax(z) - onehot) ).
+ * An entry with a class outside [0, classes), or with a logit of -infinity, is
+ * absent; a row with no entry has no first term, one whose label is outside
+ * [0, classes), or given labels = NULL, no second.  A class named by several
+ * entries gets the sum of their p.  A student logit of -infinity is a masked
+ * class (q = 0); a row of nothing else, or with NaN or +infinity in it, has no
+ * distribution, and its loss and gradient are NaN.
+ * row_weight (or NULL: 1/rows, the batch mean): w, [rows] fp32; a row of
+ * weight 0 has loss and gradient 0 whatever it holds.  loss_scale (or NULL:
+ * 1): S, one fp32 on the device; the losses are reported unscaled.
+ * row_loss: loss_r, [rows] fp32; loss (or NULL): one fp32.  dlogits (or NULL:
+ * the losses alone): [rows, classes] of dtype, row stride ld_grad; it may be
+ * the logits' own buffer (with ld_grad = ld), which is then overwritten. */
+#define DBL_DISTILL_MAX_K 1024
+typedef struct {
+    int64_t rows;
+    int32_t classes, k;
+    int32_t dtype;
+    float temperature; /* T > 0 */
+    float alpha;       /* in [0, 1] */
+    int64_t ld, ld_grad;
+} dbl_distill_shape;
+DBL_API int dbl_distill_fwd_bwd(const dbl_distill_shape* shape, const void* logits, const float* teacher_logits,
+                                const int32_t* teacher_classes, const int32_t* labels /* or NULL */,
+                                const float* row_weight /* or NULL */, const float* loss_scale /* or NULL */,
+                                float* row_loss, float* loss /* or NULL */, void* dlogits /* or NULL */,
+                                void* stream);
 
 /* ========================================================================
  * Host-side planner of dual-batch learning (Sec. 3.3-3.4).

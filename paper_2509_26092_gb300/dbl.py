@@ -62,6 +62,27 @@ class MergeParams(ctypes.Structure):
                 ("f_small", ctypes.c_float), ("order", ctypes.c_int32)]
 
 
+class LnShape(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("c", ctypes.c_int32), ("dtype", ctypes.c_int32), ("ld_in", ctypes.c_int64),
+                ("ld_out", ctypes.c_int64), ("eps", ctypes.c_float)]
+
+
+class ScanShape(ctypes.Structure):
+    _fields_ = [("n", ctypes.c_int32), ("t", ctypes.c_int32), ("c", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("ld_x", ctypes.c_int64), ("ld_h", ctypes.c_int64)]
+
+
+DBL_SCAN_CHUNK = 64
+
+
+class DistillShape(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("classes", ctypes.c_int32), ("k", ctypes.c_int32),
+                ("dtype", ctypes.c_int32), ("temperature", ctypes.c_float), ("alpha", ctypes.c_float),
+                ("ld", ctypes.c_int64), ("ld_grad", ctypes.c_int64)]
+
+
+DBL_DISTILL_MAX_K = 1024
+
 _libs = {}
 _precision = contextvars.ContextVar("dbl_precision", default="bf16")
 PRECISIONS = ("bf16", "f16")
@@ -149,6 +170,14 @@ def lib(p=None):
             "dbl_progressive_resize_stem_u8": (ctypes.c_int, [_V, _I32, _I32, _I32, _I32, ctypes.POINTER(ctypes.c_float),
                                                               ctypes.POINTER(ctypes.c_float), _V, _I32, _I32, _I32,
                                                               _I32, _I32, _I32, _I32, _I32, _V]),
+            "dbl_layer_norm_fwd": (ctypes.c_int, [ctypes.POINTER(LnShape)] + [_V] * 9),
+            "dbl_layer_norm_workspace_bytes": (_SZ, [ctypes.POINTER(LnShape)]),
+            "dbl_layer_norm_bwd": (ctypes.c_int, [ctypes.POINTER(LnShape)] + [_V] * 10 + [_SZ, _V]),
+            "dbl_gated_scan_states_bytes": (_SZ, [ctypes.POINTER(ScanShape)]),
+            "dbl_gated_scan_workspace_bytes": (_SZ, [ctypes.POINTER(ScanShape), ctypes.c_int]),
+            "dbl_gated_scan_fwd": (ctypes.c_int, [ctypes.POINTER(ScanShape)] + [_V] * 8 + [_SZ, _V]),
+            "dbl_gated_scan_bwd": (ctypes.c_int, [ctypes.POINTER(ScanShape)] + [_V] * 10 + [_SZ, _V]),
+            "dbl_distill_fwd_bwd": (ctypes.c_int, [ctypes.POINTER(DistillShape)] + [_V] * 10),
             "dbl_update_factor": (_D, [_D, _D, ctypes.c_int]),
             "dbl_plan": (ctypes.c_int, [_D, _D, _I32, _I32, _D, _D, _D, ctypes.c_int] + [ctypes.POINTER(_D)] * 4),
         }
@@ -434,6 +463,68 @@ def dbl_progressive_resize_stem_u8(inp, n, h_in, w_in, c, scale, bias, out, h_ou
 
 def dbl_zero_f32_2d(base, rows, cols, ld, stream=None):
     _check(lib().dbl_zero_f32_2d(_ptr(base), rows, cols, ld, _stream(stream)))
+
+
+def ln_shape(rows, c, eps=1e-5, dtype=DBL_BF16, ld_in=0, ld_out=0):
+    """dbl_ln_shape; ld_in / ld_out: row strides in elements of what is read / written (0: dense)."""
+    return LnShape(rows, c, dtype, ld_in, ld_out, eps)
+
+
+def dbl_layer_norm_fwd(shape, x, res, gamma, beta, sum, y, save_mean, save_invstd, stream=None):
+    """y = layer norm of x [+ res]; sum (or None) gets x + res; save_mean / save_invstd for the backward pass."""
+    _check(lib().dbl_layer_norm_fwd(ctypes.byref(shape), _ptr(x), _ptr(res), _ptr(gamma), _ptr(beta), _ptr(sum),
+                                    _ptr(y), _ptr(save_mean), _ptr(save_invstd), _stream(stream)))
+
+
+def dbl_layer_norm_workspace_bytes(shape):
+    return lib().dbl_layer_norm_workspace_bytes(ctypes.byref(shape))
+
+
+def dbl_layer_norm_bwd(shape, dy, dskip, x, gamma, save_mean, save_invstd, dx, dgamma, dbeta, ws, ws_bytes,
+                       stream=None):
+    """x: the normalised tensor (the forward pass's sum, where there is a residual); dx gets dskip added."""
+    _check(lib().dbl_layer_norm_bwd(ctypes.byref(shape), _ptr(dy), _ptr(dskip), _ptr(x), _ptr(gamma),
+                                    _ptr(save_mean), _ptr(save_invstd), _ptr(dx), _ptr(dgamma), _ptr(dbeta),
+                                    _ptr(ws), ws_bytes, _stream(stream)))
+
+
+def scan_shape(n, t, c, dtype=DBL_BF16, ld_x=0, ld_h=0):
+    """dbl_scan_shape; ld_x / ld_h: row strides in elements of x, gate (and their gradients) / of h (0: dense)."""
+    return ScanShape(n, t, c, dtype, ld_x, ld_h)
+
+
+def dbl_gated_scan_states_bytes(shape):
+    return lib().dbl_gated_scan_states_bytes(ctypes.byref(shape))
+
+
+def dbl_gated_scan_workspace_bytes(shape, pass_):
+    return lib().dbl_gated_scan_workspace_bytes(ctypes.byref(shape), pass_)
+
+
+def dbl_gated_scan_fwd(shape, x, gate, h0, lengths, h, h_last, states, ws=None, ws_bytes=0, stream=None):
+    _check(lib().dbl_gated_scan_fwd(ctypes.byref(shape), _ptr(x), _ptr(gate), _ptr(h0), _ptr(lengths), _ptr(h),
+                                    _ptr(h_last), _ptr(states), _ptr(ws), ws_bytes, _stream(stream)))
+
+
+def dbl_gated_scan_bwd(shape, dh, dh_last, x, gate, states, lengths, dx, dgate, dh0, ws=None, ws_bytes=0,
+                       stream=None):
+    _check(lib().dbl_gated_scan_bwd(ctypes.byref(shape), _ptr(dh), _ptr(dh_last), _ptr(x), _ptr(gate), _ptr(states),
+                                    _ptr(lengths), _ptr(dx), _ptr(dgate), _ptr(dh0), _ptr(ws), ws_bytes,
+                                    _stream(stream)))
+
+
+def distill_shape(rows, classes, k, temperature=1.0, alpha=1.0, dtype=DBL_BF16, ld=0, ld_grad=0):
+    """dbl_distill_shape; ld / ld_grad: row strides in elements of the logits / their gradient (0: dense)."""
+    return DistillShape(rows, classes, k, dtype, temperature, alpha, ld, ld_grad)
+
+
+def dbl_distill_fwd_bwd(shape, logits, teacher_logits, teacher_classes, labels, row_weight, loss_scale, row_loss,
+                        loss, dlogits, stream=None):
+    """dlogits=None: the losses alone.  teacher_classes, labels: int32; labels, row_weight, loss_scale, loss may
+    be None."""
+    _check(lib().dbl_distill_fwd_bwd(ctypes.byref(shape), _ptr(logits), _ptr(teacher_logits), _ptr(teacher_classes),
+                                     _ptr(labels), _ptr(row_weight), _ptr(loss_scale), _ptr(row_loss), _ptr(loss),
+                                     _ptr(dlogits), _stream(stream)))
 
 
 def dbl_resize_taps(n_in, n_out):
