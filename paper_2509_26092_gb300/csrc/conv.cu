@@ -3908,7 +3908,9 @@ int dbl_device_status(int32_t* status)
     int v = 0, zero = 0;
     if ((rc = cuda_check(cudaMemcpyFromSymbol(&v, g_conv_status, sizeof(int)), "device_status read"))) return rc;
     if ((rc = cuda_check(cudaMemcpyToSymbol(g_conv_status, &zero, sizeof(int)), "device_status clear"))) return rc;
-    *status = v;
+    int other = 0;
+    if ((rc = scan_device_status(&other))) return rc;
+    *status = v != DBL_OK ? v : other;
     return DBL_OK;
 }
 
