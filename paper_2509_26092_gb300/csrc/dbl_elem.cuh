@@ -61,7 +61,61 @@ __device__ __forceinline__ float block_max(float v, float* red)
     return s;
 }
 
+// From a 16-byte boundary to one, a multiple of 16 bytes; counted on the barrier.
+__device__ __forceinline__ void bulk_load(uint32_t dst, uintptr_t src, uint32_t bytes, uint64_t* bar)
+{
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src),
+                 "r"(bytes), "r"(smem_u32(bar))
+                 : "memory");
+}
+__device__ __forceinline__ void bulk_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
+__device__ __forceinline__ void bulk_wait_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
+
+// Waits for a phase, for what blocks of the cluster wrote before it too.  Bounded, like every wait of the library: a
+// block that gives up says so in the status word and does not wait again.
+__device__ __forceinline__ bool bounded_try(uint64_t* bar, uint32_t parity)
+{
+    uint32_t ok;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok)
+        : "r"(smem_u32(bar)), "r"(parity)
+        : "memory");
+    return ok != 0;
+}
+__device__ __forceinline__ void bounded_wait(uint64_t* bar, uint32_t parity, volatile int* abort, int* status)
+{
+    if (bounded_try(bar, parity)) return;
+    const uint64_t t0 = globaltimer();
+    for (uint32_t i = 0; i < kWaitLimitPolls; ++i) {
+        if (bounded_try(bar, parity)) return;
+        if ((i & 63u) == 63u && (*abort || globaltimer() - t0 > kWaitLimitNs)) break;
+    }
+    *abort = 1;
+    atomicExch(status, DBL_ERR_TIMEOUT);
+}
+
+// Before a block's end: one that gave up leaves the copies that it started some time to land.
+__device__ __forceinline__ void linger(volatile int* abort)
+{
+    if (!*abort) return;
+    const uint64_t t0 = globaltimer();
+    for (uint32_t i = 0; i < kWaitLimitPolls && globaltimer() - t0 < kWaitLimitNs / 8; ++i) {}
+}
+
 }  // namespace dev
+
+// Reads a device-side status word, and clears it if it is set (the device being idle).
+template <class S>
+int take_status(S& word, int* status)
+{
+    const int zero = 0;
+    int rc = cuda_check(cudaMemcpyFromSymbol(status, word, sizeof(int)), "device_status read");
+    if (rc == DBL_OK && *status != DBL_OK) rc = cuda_check(cudaMemcpyToSymbol(word, &zero, sizeof(int)), "device_status clear");
+    return rc;
+}
 #endif
 
 }  // namespace dbl

@@ -104,7 +104,8 @@ int current_context_id(unsigned long long* id);
 int bn_fwd_finalize(int64_t count, int C, float eps, const float* sum, const float* sumsq, float* save_mean,
                     float* save_invstd, cudaStream_t st);
 
-// Reads and clears the status word of scan.cu's kernels (DBL_OK or DBL_ERR_TIMEOUT), the device being idle.
+// Read and clear the status words of these files' kernels (DBL_OK or DBL_ERR_TIMEOUT), the device being idle.
+int ln_device_status(int* status);
 int scan_device_status(int* status);
 
 }  // namespace dbl

@@ -1,5 +1,11 @@
 // ln.cu -- layer norm over the last dimension, forward (with the residual addition before it) and backward (with
 // the skip path's gradient and the sums over rows for gamma and beta).
+//
+// Bound by memory.  A group of threads takes a row, 8 or 16 columns a thread, and goes on to another until there are
+// none; a group's next rows are on their way into shared memory meanwhile, each by one bulk copy, so that what is in
+// flight does not go by the registers (loads into registers a row ahead reached 0.4 of the copy rate).  A row is read
+// once and written once; the variance is taken of the deviations from the mean, so that an offset of the row costs no
+// digits.
 #include <math.h>
 
 #include <algorithm>
@@ -11,22 +17,395 @@ namespace {
 using namespace dbl;
 using namespace dbl::dev;
 
-constexpr int kThreads = 256;
-constexpr int kMaxParts = 304;  // blocks of rows whose column sums are kept apart
+constexpr int kMaxGroup = 512;     // threads of a row
+constexpr int kBlock = 256;        // threads of a block of several groups
+constexpr int kMaxDepth = 4;       // rows of a group on their way
+constexpr int kWide = 256;         // threads of the kernels for rows wider than a group
+constexpr int kSumThreads = 1024;
+constexpr size_t kRingBytes = 200 * 1024;  // shared memory for them on an SM
+
+__device__ int g_ln_status;
 
 struct LnArgs {
     const void *x, *res, *dy;
     const float *gamma, *beta;
     void *sum, *y;
     float *mean, *invstd;
+    float* parts;
     int64_t rows, ld_in, ld_out;
     int c;
     float eps;
+    int group, depth, slot;  // threads of a row, rows on their way, bytes of one in shared memory
 };
 
-// One row per block, read once per step.
+// This thread's columns of a row, in pairs: J accesses of 16 bytes where rows allow it (VEC; FULL: every thread has all
+// of its columns), otherwise of 4 bytes.
+template <class T, bool VEC, bool FULL, int N>
+struct Cols {
+    static constexpr int A = VEC ? 16 / (int)sizeof(T) : 2, J = N / A, P = A / 2;  // columns, accesses, pairs of one
+    // first column of access j, and how far the second of its (first) pair is: single fp32 columns lie side by side in
+    // a warp, 16-bit ones in a thread, which can store them at once in rows that begin at a word
+    static __device__ __forceinline__ int col(int j, int g, int G) { return !VEC && sizeof(T) == 4 ? j * 2 * G + g : (j * G + g) * A; }
+    static __device__ __forceinline__ int mate(int G) { return !VEC && sizeof(T) == 4 ? G : 1; }
+    static __device__ __forceinline__ float2 pair(const T* p) { return make_float2(elem_f(p[0]), elem_f(p[1])); }
+    // access j of a row in shared memory that begins `off` elements after row; zeros past its end
+    static __device__ __forceinline__ void read(float2* f, const char* row, int off, int c, int g, int G, int j)
+    {
+        const int i = col(j, g, G);
+        if constexpr (VEC) {
+            uint4 r = make_uint4(0, 0, 0, 0);
+            if (FULL || i < c) r = reinterpret_cast<const uint4*>(row)[j * G + g];
+            const T* p = reinterpret_cast<const T*>(&r);
+#pragma unroll
+            for (int k = 0; k < P; ++k) f[k] = pair(p + 2 * k);
+        } else {
+            const T* p = reinterpret_cast<const T*>(row) + off + i;
+            f[0] = make_float2(i < c ? elem_f(p[0]) : 0.f, i + mate(G) < c ? elem_f(p[mate(G)]) : 0.f);
+        }
+    }
+    static __device__ __forceinline__ void write(T* row, const float2* f, int c, int g, int G, int j)
+    {
+        const int i = col(j, g, G);
+        if constexpr (VEC) {
+            uint4 o;
+            T* p = reinterpret_cast<T*>(&o);
+#pragma unroll
+            for (int k = 0; k < P; ++k) {
+                if constexpr (sizeof(T) == 2)
+                    reinterpret_cast<uint32_t*>(&o)[k] = act::pack2_u32(f[k].x, f[k].y);
+                else
+                    p[2 * k] = f[k].x, p[2 * k + 1] = f[k].y;
+            }
+            if (FULL || i < c) *reinterpret_cast<uint4*>(row + i) = o;
+        } else {
+            if (sizeof(T) == 2 && i + 1 < c && (reinterpret_cast<uintptr_t>(row) & 3) == 0) {
+                *reinterpret_cast<uint32_t*>(row + i) = act::pack2_u32(f[0].x, f[0].y);
+            } else {
+                if (i < c) row[i] = elem_from<T>(f[0].x);
+                if (i + mate(G) < c) row[i + mate(G)] = elem_from<T>(f[0].y);
+            }
+        }
+    }
+    // parameters of the same columns (`other` where there are none, and past the row's end)
+    static __device__ __forceinline__ void param(float2* f, const float* p, float other, int c, int g, int G, int j)
+    {
+        const int i = col(j, g, G);
+#pragma unroll
+        for (int k = 0; k < P; ++k) {
+            f[k] = make_float2(other, other);
+            if constexpr (VEC) {
+                if (p && (FULL || i < c)) {
+                    const float4 q = __ldg(reinterpret_cast<const float4*>(p + i) + k / 2);
+                    f[k] = k & 1 ? make_float2(q.z, q.w) : make_float2(q.x, q.y);
+                }
+            } else if (p) {
+                if (i < c) f[k].x = __ldg(p + i);
+                if (i + mate(G) < c) f[k].y = __ldg(p + i + mate(G));
+            }
+        }
+    }
+};
+
+__device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
+
+// A block's groups: their places, barriers and rows in shared memory.
+template <class T, bool VEC, int TENSORS>
+struct Groups {
+    int G, g, id, n, warp, warps, depth, slot, c;
+    uint64_t* bars;  // of this group, one per row on its way
+    float2* red;     // of this group: [2][warps]
+    char* ring;      // of this group: [depth][TENSORS][slot]
+    int* abort;
+    int64_t rows, ld;
+    unsigned phase;
+
+    static __host__ __device__ size_t head(int warps) { return 128 + (size_t)warps * (kMaxDepth * sizeof(uint64_t) + 4 * sizeof(float2)); }
+
+    __device__ __forceinline__ void set(const LnArgs& a, char* smem)
+    {
+        G = a.group, g = threadIdx.x % G, id = threadIdx.x / G, n = blockDim.x / G, warp = g >> 5, warps = G >> 5;
+        depth = a.depth, slot = a.slot, c = a.c, rows = a.rows, ld = a.ld_in, phase = 0;
+        const int all = blockDim.x >> 5;
+        abort = reinterpret_cast<int*>(smem);
+        bars = reinterpret_cast<uint64_t*>(smem + 128) + id * kMaxDepth;
+        red = reinterpret_cast<float2*>(smem + 128 + (size_t)all * kMaxDepth * sizeof(uint64_t)) + id * warps * 4;
+        ring = smem + (head(all) + 127) / 128 * 128 + (size_t)id * depth * TENSORS * slot;
+        if (threadIdx.x == 0) *abort = 0;
+        if (g == 0) {
+            for (int k = 0; k < depth; ++k) mbar_init(&bars[k], 1);
+            fence_mbar_init();
+        }
+        __syncthreads();
+    }
+    __device__ __forceinline__ void sync() const
+    {
+        if (warps == 1)
+            __syncwarp();
+        else
+            asm volatile("bar.sync %0, %1;" ::"r"(id + 1), "r"(G) : "memory");
+    }
+    // One thread's work: row r of every tensor into place k.
+    __device__ __forceinline__ void fetch(const T* const (&from)[TENSORS], int k, int64_t r) const
+    {
+        char* const to = ring + (size_t)k * TENSORS * slot;
+        if constexpr (VEC) {
+            const uint32_t bytes = c * sizeof(T);
+            mbar_arrive_expect_tx(&bars[k], (from[TENSORS - 1] ? TENSORS : TENSORS - 1) * bytes);
+#pragma unroll
+            for (int t = 0; t < TENSORS; ++t)
+                if (t < TENSORS - 1 || from[t]) bulk_load(smem_u32(to + t * slot), reinterpret_cast<uintptr_t>(from[t] + r * ld), bytes, &bars[k]);
+        } else {
+            Span sp[TENSORS];
+            uint32_t sum = 0;
+#pragma unroll
+            for (int t = 0; t < TENSORS; ++t) sp[t] = span(from[t], r), sum += sp[t].bytes;
+            mbar_arrive_expect_tx(&bars[k], sum);
+#pragma unroll
+            for (int t = 0; t < TENSORS; ++t)
+                if (sp[t].bytes) bulk_load(smem_u32(to + t * slot), sp[t].lo, sp[t].bytes, &bars[k]);
+        }
+    }
+    struct Span {
+        uintptr_t lo;
+        uint32_t bytes;
+    };
+    // A row from the 16-byte boundary at or before its first element to that at or after its last; nothing where that
+    // would leave the tensor.
+    __device__ __forceinline__ Span span(const T* from, int64_t r) const
+    {
+        const uintptr_t p = reinterpret_cast<uintptr_t>(from + r * ld), e = (p + c * sizeof(T) + 15) & ~(uintptr_t)15, lo = p & ~(uintptr_t)15;
+        const bool whole = lo >= reinterpret_cast<uintptr_t>(from) && e <= reinterpret_cast<uintptr_t>(from + (rows - 1) * ld + c);
+        return {lo, from && whole ? (uint32_t)(e - lo) : 0u};
+    }
+    // elements from the 16-byte boundary to a row's first one
+    __device__ __forceinline__ int offset(const T* from, int64_t r) const
+    {
+        if constexpr (VEC) return 0;
+        constexpr uint32_t E = 16 / sizeof(T);
+        return (int)(((uint32_t)reinterpret_cast<uintptr_t>(from) / sizeof(T) + (uint32_t)r * (uint32_t)ld) % E);
+    }
+    __device__ __forceinline__ const char* row(int k, int t) const { return ring + ((size_t)k * TENSORS + t) * slot; }
+    __device__ __forceinline__ void wait(const T* const (&from)[TENSORS], int k, int64_t r)
+    {
+        bounded_wait(&bars[k], phase >> k & 1, abort, &g_ln_status);
+        phase ^= 1u << k;
+        if (VEC || (r >= 16 && r < rows - 16)) return;  // of 16 rows the 16 bytes before or after are the tensor's
+        // rows at the tensor's ends, where no bulk copy has brought them
+#pragma unroll
+        for (int t = 0; t < TENSORS; ++t) {
+            if (!from[t] || span(from[t], r).bytes) continue;
+            T* to = reinterpret_cast<T*>(ring + ((size_t)k * TENSORS + t) * slot) + offset(from[t], r);
+            for (int i = g; i < c; i += G) to[i] = from[t][r * ld + i];
+        }
+        sync();
+    }
+    // Sums over the group, the same bits in all its threads; which: 0 or 1, not the same twice in a row.
+    __device__ __forceinline__ float2 total(float2 v, int which) const
+    {
+        v = make_float2(warp_sum(v.x), warp_sum(v.y));
+        if (warps == 1) return v;
+        float2* p = red + which * warps;
+        if ((threadIdx.x & 31) == 0) p[warp] = v;
+        sync();
+        v = (threadIdx.x & 31) < warps ? p[threadIdx.x & 31] : make_float2(0.f, 0.f);
+        return make_float2(warp_sum(v.x), warp_sum(v.y));
+    }
+    __device__ __forceinline__ float total(float v, int which) const
+    {
+        v = warp_sum(v);
+        if (warps == 1) return v;
+        float2* p = red + which * warps;
+        if ((threadIdx.x & 31) == 0) p[warp].x = v;
+        sync();
+        return warp_sum((threadIdx.x & 31) < warps ? p[threadIdx.x & 31].x : 0.f);
+    }
+};
+
+template <class T, bool VEC, bool FULL, int N, int THREADS, int BLOCKS>
+__global__ void __launch_bounds__(THREADS, BLOCKS) ln_fwd_kernel(LnArgs a)
+{
+    typedef Cols<T, VEC, FULL, N> C;
+    constexpr int P = C::P;
+    extern __shared__ __align__(128) char smem[];
+    Groups<T, VEC, 2> w;
+    w.set(a, smem);
+    const T* const from[2] = {static_cast<const T*>(a.x), static_cast<const T*>(a.res)};
+    const int g = w.g, G = w.G;
+    const int64_t hop = (int64_t)gridDim.x * w.n;
+    int64_t r = (int64_t)blockIdx.x * w.n + w.id;
+    if (g == 0)
+        for (int k = 0; k < w.depth; ++k)
+            if (r + k * hop < a.rows) w.fetch(from, k, r + k * hop);
+    constexpr bool KEEP = N <= 16;  // the parameters, from row to row
+    float2 ga[KEEP ? N / 2 : P], be[KEEP ? N / 2 : P];
+    if (KEEP) {
+#pragma unroll
+        for (int j = 0; j < C::J; ++j) {
+            C::param(ga + (KEEP ? j * P : 0), a.gamma, 1.f, a.c, g, G, j);
+            C::param(be + (KEEP ? j * P : 0), a.beta, 0.f, a.c, g, G, j);
+        }
+    }
+    const float inv_c = 1.f / a.c;
+    for (int k = 0; r < a.rows; r += hop, k = k + 1 == w.depth ? 0 : k + 1) {
+        float2 v[N / 2], s = both(0.f);
+        w.wait(from, k, r);
+        const int off = w.offset(from[0], r), off_r = w.offset(from[1], r);
+#pragma unroll
+        for (int j = 0; j < C::J; ++j) C::read(v + j * P, w.row(k, 0), off, a.c, g, G, j);
+        if (a.res) {
+#pragma unroll
+            for (int j = 0; j < C::J; ++j) {
+                float2 u[P];
+                C::read(u, w.row(k, 1), off_r, a.c, g, G, j);
+#pragma unroll
+                for (int i = 0; i < P; ++i) v[j * P + i] = __fadd2_rn(v[j * P + i], u[i]);
+            }
+        }
+        if (a.sum) {
+#pragma unroll
+            for (int j = 0; j < C::J; ++j) C::write(static_cast<T*>(a.sum) + r * a.ld_out, v + j * P, a.c, g, G, j);
+        }
+#pragma unroll
+        for (int i = 0; i < N / 2; ++i) s = __fadd2_rn(s, v[i]);
+        const float mean = w.total(s.x + s.y, 0) * inv_c;
+        if (w.warps == 1) __syncwarp();
+        if (g == 0 && r + w.depth * hop < a.rows) w.fetch(from, k, r + w.depth * hop);  // the group has read the place
+        s = both(0.f);
+#pragma unroll
+        for (int j = 0; j < C::J; ++j) {
+            const int i0 = C::col(j, g, G);
+#pragma unroll
+            for (int i = j * P; i < (j + 1) * P; ++i) {
+                v[i] = __fadd2_rn(v[i], both(-mean));
+                if (VEC) {
+                    if (FULL || i0 < a.c) s = __ffma2_rn(v[i], v[i], s);
+                } else {
+                    if (i0 < a.c) s.x = fmaf(v[i].x, v[i].x, s.x);
+                    if (i0 + C::mate(G) < a.c) s.y = fmaf(v[i].y, v[i].y, s.y);
+                }
+            }
+        }
+        const float inv = 1.f / sqrtf(fmaf(w.total(s.x + s.y, 1), inv_c, a.eps));
+#pragma unroll
+        for (int j = 0; j < C::J; ++j) {
+            float2* f = v + j * P;
+            if (!KEEP) {
+                C::param(ga, a.gamma, 1.f, a.c, g, G, j);
+                C::param(be, a.beta, 0.f, a.c, g, G, j);
+            }
+#pragma unroll
+            for (int i = 0; i < P; ++i)
+                f[i] = __ffma2_rn(__fmul2_rn(f[i], both(inv)), ga[(KEEP ? j * P : 0) + i], be[(KEEP ? j * P : 0) + i]);
+            C::write(static_cast<T*>(a.y) + r * a.ld_out, f, a.c, g, G, j);
+        }
+        if (g == 0 && a.mean) {
+            a.mean[r] = mean;
+            a.invstd[r] = inv;
+        }
+    }
+    linger(w.abort);
+}
+
+// x: the normalised tensor, res: dskip, y: dx.  A thread also adds up dy*xhat and dy of its columns over the rows
+// that its group takes; a block leaves these sums in parts[block][2][c].
+template <class T, bool VEC, bool FULL, int N, int THREADS, int BLOCKS>
+__global__ void __launch_bounds__(THREADS, BLOCKS) ln_bwd_kernel(LnArgs a)
+{
+    typedef Cols<T, VEC, FULL, N> C;
+    constexpr int P = C::P;
+    extern __shared__ __align__(128) char smem[];
+    Groups<T, VEC, 3> w;
+    w.set(a, smem);
+    const T* const from[3] = {static_cast<const T*>(a.x), static_cast<const T*>(a.dy), static_cast<const T*>(a.res)};
+    const int g = w.g, G = w.G;
+    const int64_t hop = (int64_t)gridDim.x * w.n;
+    int64_t r = (int64_t)blockIdx.x * w.n + w.id;
+    float mean = 0.f, inv = 0.f;
+    if (r < a.rows) {
+        if (g == 0)
+            for (int k = 0; k < w.depth; ++k)
+                if (r + k * hop < a.rows) w.fetch(from, k, r + k * hop);
+        mean = a.mean[r], inv = a.invstd[r];
+    }
+    grid_dependency_trigger();
+    float2 dg[N / 2], db[N / 2];
+#pragma unroll
+    for (int i = 0; i < N / 2; ++i) dg[i] = db[i] = both(0.f);
+    const float inv_c = 1.f / a.c;
+    bool first = true;
+    int par = 0;
+    for (int k = 0; r < a.rows; r += hop, k = k + 1 == w.depth ? 0 : k + 1, par ^= 1) {
+        float2 h[N / 2], d[N / 2], tx = both(0.f), ty = tx;
+        w.wait(from, k, r);
+        const int off_x = w.offset(from[0], r), off_d = w.offset(from[1], r);
+        const float is = inv, mu = mean;
+        if (r + hop < a.rows) mean = a.mean[r + hop], inv = a.invstd[r + hop];
+#pragma unroll
+        for (int j = 0; j < C::J; ++j) {
+            float2 ga[P];
+            C::read(h + j * P, w.row(k, 0), off_x, a.c, g, G, j);
+            C::read(d + j * P, w.row(k, 1), off_d, a.c, g, G, j);
+            C::param(ga, a.gamma, 1.f, a.c, g, G, j);
+#pragma unroll
+            for (int q = 0; q < P; ++q) {  // past the row's end d is 0
+                const int i = j * P + q;
+                h[i] = __fmul2_rn(__fadd2_rn(h[i], both(-mu)), both(is));
+                dg[i] = __ffma2_rn(d[i], h[i], dg[i]);
+                db[i] = __fadd2_rn(db[i], d[i]);
+                d[i] = __fmul2_rn(d[i], ga[q]);
+                tx = __fadd2_rn(tx, d[i]);
+                ty = __ffma2_rn(d[i], h[i], ty);
+            }
+        }
+        const float2 t = w.total(make_float2(tx.x + tx.y, ty.x + ty.y), par);
+        if (w.warps == 1) __syncwarp();
+        // the row before this one has been read by all of the group: its place is free
+        if (g == 0 && !first && r + (w.depth - 1) * hop < a.rows) w.fetch(from, (k ? k : w.depth) - 1, r + (w.depth - 1) * hop);
+        first = false;
+        tx = both(-t.x * inv_c * is), ty = both(-t.y * inv_c * is);
+        const int off_s = w.offset(from[2], r);
+#pragma unroll
+        for (int i = 0; i < N / 2; ++i) d[i] = __ffma2_rn(h[i], ty, __ffma2_rn(d[i], both(is), tx));
+#pragma unroll
+        for (int j = 0; j < C::J; ++j) {
+            if (a.res) {
+                float2 u[P];
+                C::read(u, w.row(k, 2), off_s, a.c, g, G, j);
+#pragma unroll
+                for (int q = 0; q < P; ++q) d[j * P + q] = __fadd2_rn(d[j * P + q], u[q]);
+            }
+            C::write(static_cast<T*>(a.y) + r * a.ld_out, d + j * P, a.c, g, G, j);
+        }
+    }
+    linger(w.abort);
+    if (!a.parts) return;
+    // groups of one block: through shared memory, all rows being done
+    float* out = a.parts + (int64_t)blockIdx.x * 2 * a.c;
+    float* sums = reinterpret_cast<float*>(w.ring - (size_t)w.id * w.depth * 3 * w.slot);
+    if (w.n > 1) {
+        __syncthreads();
+        out = sums + w.id * 2 * a.c;
+    }
+#pragma unroll
+    for (int j = 0; j < C::J; ++j)
+#pragma unroll
+        for (int q = 0; q < P; ++q) {
+            const int i = C::col(j, g, G) + 2 * q, m = i + C::mate(G);
+            if (i < a.c) out[i] = dg[j * P + q].x, out[a.c + i] = db[j * P + q].x;
+            if (m < a.c) out[m] = dg[j * P + q].y, out[a.c + m] = db[j * P + q].y;
+        }
+    if (w.n == 1) return;
+    __syncthreads();
+    for (int i = threadIdx.x; i < 2 * a.c; i += blockDim.x) {
+        float t = 0.f;
+        for (int k = 0; k < w.n; ++k) t += sums[k * 2 * a.c + i];
+        a.parts[(int64_t)blockIdx.x * 2 * a.c + i] = t;
+    }
+}
+
+// Rows of more columns than a block holds: a block per row, which it reads once per step (from L2 but for the first).
 template <class T>
-__global__ void __launch_bounds__(kThreads) ln_fwd_kernel(LnArgs a)
+__global__ void __launch_bounds__(kWide) ln_fwd_wide_kernel(LnArgs a)
 {
     __shared__ float red[32];
     for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
@@ -34,15 +413,15 @@ __global__ void __launch_bounds__(kThreads) ln_fwd_kernel(LnArgs a)
         const T* res = a.res ? static_cast<const T*>(a.res) + r * a.ld_in : nullptr;
         auto at = [&](int i) { return res ? elem_f(x[i]) + elem_f(res[i]) : elem_f(x[i]); };
         float s = 0.f;
-        for (int i = threadIdx.x; i < a.c; i += kThreads) s += at(i);
+        for (int i = threadIdx.x; i < a.c; i += kWide) s += at(i);
         const float mean = block_sum(s, red) / a.c;
         s = 0.f;
-        for (int i = threadIdx.x; i < a.c; i += kThreads) {
+        for (int i = threadIdx.x; i < a.c; i += kWide) {
             const float d = at(i) - mean;
             s = fmaf(d, d, s);
         }
         const float inv = 1.f / sqrtf(block_sum(s, red) / a.c + a.eps);
-        for (int i = threadIdx.x; i < a.c; i += kThreads) {
+        for (int i = threadIdx.x; i < a.c; i += kWide) {
             const float v = at(i), h = (v - mean) * inv;
             if (a.sum) static_cast<T*>(a.sum)[r * a.ld_out + i] = elem_from<T>(v);
             static_cast<T*>(a.y)[r * a.ld_out + i] = elem_from<T>(fmaf(h, a.gamma ? a.gamma[i] : 1.f,
@@ -55,9 +434,8 @@ __global__ void __launch_bounds__(kThreads) ln_fwd_kernel(LnArgs a)
     }
 }
 
-// x: the normalised tensor, res: dskip, y: dx
 template <class T>
-__global__ void __launch_bounds__(kThreads) ln_bwd_kernel(LnArgs a)
+__global__ void __launch_bounds__(kWide) ln_bwd_wide_kernel(LnArgs a)
 {
     __shared__ float red[32];
     for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
@@ -65,14 +443,14 @@ __global__ void __launch_bounds__(kThreads) ln_bwd_kernel(LnArgs a)
         const T* dy = static_cast<const T*>(a.dy) + r * a.ld_in;
         const float mean = a.mean[r], inv = a.invstd[r];
         float s0 = 0.f, s1 = 0.f;
-        for (int i = threadIdx.x; i < a.c; i += kThreads) {
+        for (int i = threadIdx.x; i < a.c; i += kWide) {
             const float g = elem_f(dy[i]) * (a.gamma ? a.gamma[i] : 1.f);
             s0 += g;
             s1 = fmaf(g, (elem_f(x[i]) - mean) * inv, s1);
         }
         s0 = block_sum(s0, red) / a.c;
         s1 = block_sum(s1, red) / a.c;
-        for (int i = threadIdx.x; i < a.c; i += kThreads) {
+        for (int i = threadIdx.x; i < a.c; i += kWide) {
             const float g = elem_f(dy[i]) * (a.gamma ? a.gamma[i] : 1.f), h = (elem_f(x[i]) - mean) * inv;
             float d = inv * (g - s0 - h * s1);
             if (a.res) d += elem_f(static_cast<const T*>(a.res)[r * a.ld_in + i]);
@@ -81,31 +459,42 @@ __global__ void __launch_bounds__(kThreads) ln_bwd_kernel(LnArgs a)
     }
 }
 
-// parts[block][2][c]: each block's sums of dy*xhat and of dy over its rows
+// The column sums of such rows: a block of columns over a part of the rows.
 template <class T>
-__global__ void __launch_bounds__(kThreads) ln_params_kernel(LnArgs a, float* parts)
+__global__ void __launch_bounds__(kWide) ln_params_wide_kernel(LnArgs a)
 {
-    for (int i = threadIdx.x; i < a.c; i += kThreads) {
-        float dg = 0.f, db = 0.f;
-        for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
-            const float d = elem_f(static_cast<const T*>(a.dy)[r * a.ld_in + i]);
-            const float h = (elem_f(static_cast<const T*>(a.x)[r * a.ld_in + i]) - a.mean[r]) * a.invstd[r];
-            dg = fmaf(d, h, dg);
-            db += d;
-        }
-        parts[(int64_t)blockIdx.x * 2 * a.c + i] = dg;
-        parts[((int64_t)blockIdx.x * 2 + 1) * a.c + i] = db;
+    grid_dependency_trigger();
+    const int i = blockIdx.x * kWide + threadIdx.x;
+    if (i >= a.c) return;
+    float dg = 0.f, db = 0.f;
+    for (int64_t r = blockIdx.y; r < a.rows; r += gridDim.y) {
+        const float d = elem_f(static_cast<const T*>(a.dy)[r * a.ld_in + i]);
+        const float h = (elem_f(static_cast<const T*>(a.x)[r * a.ld_in + i]) - a.mean[r]) * a.invstd[r];
+        dg = fmaf(d, h, dg);
+        db += d;
     }
+    a.parts[(int64_t)blockIdx.y * 2 * a.c + i] = dg;
+    a.parts[((int64_t)blockIdx.y * 2 + 1) * a.c + i] = db;
 }
 
-__global__ void __launch_bounds__(kThreads) ln_params_sum_kernel(const float* parts, int nparts, int c, float* dgamma,
-                                                                float* dbeta)
+// Sums of the parts, 32 columns a block: 32 threads per column, each every 32nd part.
+__global__ void __launch_bounds__(kSumThreads) ln_params_sum_kernel(const float* parts, int nparts, int c, float* dgamma,
+                                                                   float* dbeta)
 {
-    const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-    if (i >= 2 * (int64_t)c) return;
+    __shared__ float red[32][33];
+    const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
+    const int i = blockIdx.x * 32 + lane;  // of 2*c
+    grid_dependency_wait();
     float s = 0.f;
-    for (int p = 0; p < nparts; ++p) s += parts[(int64_t)p * 2 * c + i];
-    (i < c ? dgamma : dbeta - c)[i] = s;
+    if (i < 2 * c) {
+#pragma unroll 8
+        for (int p = w; p < nparts; p += 32) s += parts[(int64_t)p * 2 * c + i];
+    }
+    red[w][lane] = s;
+    __syncthreads();
+    s = warp_sum(red[lane][w]);
+    const int o = blockIdx.x * 32 + w;
+    if (lane == 0 && o < 2 * c) (o < c ? dgamma : dbeta - c)[o] = s;
 }
 
 int check(const dbl_ln_shape* s, const char* what)
@@ -129,9 +518,112 @@ LnArgs args(const dbl_ln_shape* s)
     return a;
 }
 
-int parts_of(const dbl_ln_shape* s) { return (int)std::min<int64_t>(std::max<int64_t>(s->rows, 1), kMaxParts); }
+// Whether every row of every tensor starts and ends at a multiple of 16 bytes.
+bool vec_of(const LnArgs& a, size_t e)
+{
+    return a.c * e % 16 == 0 && a.ld_in * e % 16 == 0 && a.ld_out * e % 16 == 0 && aligned16(a.x) && aligned16(a.res) &&
+           aligned16(a.dy) && aligned16(a.sum) && aligned16(a.y) && aligned16(a.gamma) && aligned16(a.beta);
+}
+
+// Groups, blocks and shared memory for n columns a thread and `tensors` rows to read, `resident` threads on an SM.
+struct Plan {
+    int threads, blocks;
+    size_t smem;
+};
+Plan plan_of(LnArgs& a, int n, int tensors, int resident, size_t least, size_t e)
+{
+    Plan p;
+    a.group = ((a.c + n - 1) / n + 31) / 32 * 32;
+    const int groups = std::max(1, kBlock / a.group);
+    p.threads = a.group * groups;
+    const int on_sm = std::max(1, resident / p.threads);
+    a.slot = (int)((a.c * e + 16 + 127) / 128 * 128);
+    a.depth = (int)std::min<size_t>(kMaxDepth, std::max<size_t>(least, kRingBytes / on_sm / ((size_t)groups * tensors * a.slot)));
+    p.smem = (Groups<float, true, 1>::head(p.threads / 32) + 127) / 128 * 128 +
+             std::max((size_t)groups * a.depth * tensors * a.slot, groups > 1 ? (size_t)groups * 2 * a.c * sizeof(float) : 0);
+    p.blocks = (int)std::max<int64_t>(1, std::min<int64_t>((a.rows + groups - 1) / groups, (int64_t)on_sm * sm_count()));
+    return p;
+}
+
+// Whether rows of this width are held by a group, in two places of a ring at least.
+bool held(const LnArgs& a, int tensors, size_t e)
+{
+    return a.c <= 32 * kMaxGroup && 2 * tensors * (a.c * e + 144) <= kRingBytes;
+}
+
+// The backward pass's blocks, each of which leaves a row of partial column sums.  By the sizes alone, as the
+// workspace is.
+Plan bwd_plan(LnArgs& a, size_t e)
+{
+    if (!held(a, 3, e)) return {kWide, (int)std::max<int64_t>(1, std::min<int64_t>((a.rows + 15) / 16, 64)), 0};
+    if (a.c <= 256) return plan_of(a, 8, 3, 3 * kBlock, 2, e);
+    if (a.c <= 16 * kBlock) return plan_of(a, 16, 3, 2 * kBlock, 2, e);
+    return plan_of(a, a.c <= 16 * kMaxGroup ? 16 : 32, 3, kMaxGroup, 2, e);
+}
+
+template <auto KERNEL>
+int launch(const LnArgs& a, const Plan& p, cudaStream_t st, const char* what)
+{
+    const int rc = cuda_check(cudaFuncSetAttribute(KERNEL, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)p.smem), what);
+    if (rc != DBL_OK) return rc;
+    KERNEL<<<p.blocks, p.threads, p.smem, st>>>(a);
+    return launch_check(what);
+}
+
+template <class T, bool VEC, int N, int THREADS, int BLOCKS>
+int run_fwd_held(LnArgs& a, cudaStream_t st, const char* what)
+{
+    const Plan p = plan_of(a, N, 2, THREADS * BLOCKS, 2, sizeof(T));
+    if (VEC && a.c == a.group * N) return launch<ln_fwd_kernel<T, VEC, VEC, N, THREADS, BLOCKS>>(a, p, st, what);
+    return launch<ln_fwd_kernel<T, VEC, false, N, THREADS, BLOCKS>>(a, p, st, what);
+}
+
+template <class T, bool VEC>
+int run_fwd(LnArgs a, cudaStream_t st)
+{
+    const char* what = "layer_norm_fwd";
+    if (held(a, 2, sizeof(T))) {
+        if (a.c <= 256) return run_fwd_held<T, VEC, 8, kBlock, 4>(a, st, what);
+        if (a.c <= 16 * kBlock) return run_fwd_held<T, VEC, 16, kBlock, 3>(a, st, what);
+        if (a.c <= 16 * kMaxGroup) return run_fwd_held<T, VEC, 16, kMaxGroup, 1>(a, st, what);
+        return run_fwd_held<T, VEC, 32, kMaxGroup, 1>(a, st, what);
+    }
+    ln_fwd_wide_kernel<T><<<(int)std::min<int64_t>(a.rows, 1 << 20), kWide, 0, st>>>(a);
+    return launch_check(what);
+}
+
+template <class T, bool VEC, int N, int THREADS, int BLOCKS>
+int run_bwd_held(const LnArgs& a, const Plan& p, cudaStream_t st, const char* what)
+{
+    if (VEC && a.c == a.group * N) return launch<ln_bwd_kernel<T, VEC, VEC, N, THREADS, BLOCKS>>(a, p, st, what);
+    return launch<ln_bwd_kernel<T, VEC, false, N, THREADS, BLOCKS>>(a, p, st, what);
+}
+
+template <class T, bool VEC>
+int run_bwd(const LnArgs& a, const Plan& p, cudaStream_t st)
+{
+    const char* what = "layer_norm_bwd";
+    if (a.rows == 0) return DBL_OK;
+    if (held(a, 3, sizeof(T))) {
+        if (a.c <= 256) return run_bwd_held<T, VEC, 8, kBlock, 3>(a, p, st, what);
+        if (a.c <= 16 * kBlock) return run_bwd_held<T, VEC, 16, kBlock, 2>(a, p, st, what);
+        if (a.c <= 16 * kMaxGroup) return run_bwd_held<T, VEC, 16, kMaxGroup, 1>(a, p, st, what);
+        return run_bwd_held<T, VEC, 32, kMaxGroup, 1>(a, p, st, what);
+    }
+    ln_bwd_wide_kernel<T><<<(int)std::min<int64_t>(a.rows, 1 << 20), kWide, 0, st>>>(a);
+    const int rc = launch_check(what);
+    if (rc != DBL_OK || !a.parts) return rc;
+    ln_params_wide_kernel<T><<<dim3((a.c + kWide - 1) / kWide, p.blocks), kWide, 0, st>>>(a);
+    return launch_check(what);
+}
 
 }  // namespace
+
+namespace dbl {
+
+int ln_device_status(int* status) { return take_status(g_ln_status, status); }
+
+}  // namespace dbl
 
 extern "C" {
 
@@ -149,18 +641,16 @@ int dbl_layer_norm_fwd(const dbl_ln_shape* s, const void* x, const void* res, co
     if (s->rows == 0) return DBL_OK;
     LnArgs a = args(s);
     a.x = x, a.res = res, a.gamma = gamma, a.beta = beta, a.sum = sum, a.y = y, a.mean = save_mean, a.invstd = save_invstd;
-    const int grid = (int)std::min<int64_t>(s->rows, 1 << 20);
-    if (s->dtype == DBL_F32)
-        ln_fwd_kernel<float><<<grid, kThreads, 0, as_stream(stream)>>>(a);
-    else
-        ln_fwd_kernel<act_t><<<grid, kThreads, 0, as_stream(stream)>>>(a);
-    return launch_check("layer_norm_fwd");
+    cudaStream_t st = as_stream(stream);
+    if (s->dtype == DBL_F32) return vec_of(a, e) ? run_fwd<float, true>(a, st) : run_fwd<float, false>(a, st);
+    return vec_of(a, e) ? run_fwd<act_t, true>(a, st) : run_fwd<act_t, false>(a, st);
 }
 
 size_t dbl_layer_norm_workspace_bytes(const dbl_ln_shape* s)
 {
     if (check(s, "layer_norm_workspace_bytes") != DBL_OK) return 0;
-    return (size_t)parts_of(s) * 2 * s->c * sizeof(float);
+    LnArgs a = args(s);
+    return (size_t)bwd_plan(a, elem_bytes(s->dtype)).blocks * 2 * s->c * sizeof(float);
 }
 
 int dbl_layer_norm_bwd(const dbl_ln_shape* s, const void* dy, const void* dskip, const void* x, const float* gamma,
@@ -176,35 +666,35 @@ int dbl_layer_norm_bwd(const dbl_ln_shape* s, const void* dy, const void* dskip,
     if (!aligned_to(dy, e) || !aligned_to(dskip, e) || !aligned_to(x, e) || !aligned_to(dx, e) || !aligned_to(gamma, 4) ||
         !aligned_to(save_mean, 4) || !aligned_to(save_invstd, 4) || !aligned_to(dgamma, 4) || !aligned_to(dbeta, 4))
         return set_error(DBL_ERR_INVALID, "layer_norm_bwd: a pointer is not aligned to its element type");
+    LnArgs a = args(s);
+    const Plan p = bwd_plan(a, e);
     if (dgamma) {
-        if (!ws || ws_bytes < dbl_layer_norm_workspace_bytes(s))
+        if (!ws || ws_bytes < (size_t)p.blocks * 2 * s->c * sizeof(float))
             return set_error(DBL_ERR_WORKSPACE, "layer_norm_bwd: workspace too small");
         if (!aligned16(ws)) return set_error(DBL_ERR_INVALID, "layer_norm_bwd: workspace must be 16-byte aligned");
     }
     cudaStream_t st = as_stream(stream);
-    LnArgs a = args(s);
-    a.x = x, a.res = dskip, a.dy = dy, a.gamma = gamma, a.y = dx;
+    a.x = x, a.res = dskip, a.dy = dy, a.gamma = gamma, a.y = dx, a.parts = dgamma ? static_cast<float*>(ws) : nullptr;
     a.mean = const_cast<float*>(save_mean), a.invstd = const_cast<float*>(save_invstd);
-    if (s->rows > 0) {
-        const int grid = (int)std::min<int64_t>(s->rows, 1 << 20);
-        if (s->dtype == DBL_F32)
-            ln_bwd_kernel<float><<<grid, kThreads, 0, st>>>(a);
-        else
-            ln_bwd_kernel<act_t><<<grid, kThreads, 0, st>>>(a);
-        rc = launch_check("layer_norm_bwd");
-    }
-    if (rc != DBL_OK || !dgamma) return rc;
-    const int np = parts_of(s);
-    float* parts = static_cast<float*>(ws);
     if (s->dtype == DBL_F32)
-        ln_params_kernel<float><<<np, kThreads, 0, st>>>(a, parts);
+        rc = vec_of(a, e) ? run_bwd<float, true>(a, p, st) : run_bwd<float, false>(a, p, st);
     else
-        ln_params_kernel<act_t><<<np, kThreads, 0, st>>>(a, parts);
-    rc = launch_check("layer_norm_bwd");
-    if (rc != DBL_OK) return rc;
-    ln_params_sum_kernel<<<(int)((2 * (int64_t)s->c + kThreads - 1) / kThreads), kThreads, 0, st>>>(parts, np, s->c, dgamma,
-                                                                                                dbeta);
-    return launch_check("layer_norm_bwd sums");
+        rc = vec_of(a, e) ? run_bwd<act_t, true>(a, p, st) : run_bwd<act_t, false>(a, p, st);
+    if (rc != DBL_OK || !dgamma) return rc;
+    // its launch overlaps the end of the kernel before it
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.gridDim = dim3((unsigned)((2 * (int64_t)s->c + 31) / 32));
+    cfg.blockDim = dim3(kSumThreads);
+    cfg.stream = st;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    const cudaError_t err = cudaLaunchKernelEx(&cfg, ln_params_sum_kernel, (const float*)a.parts, s->rows ? p.blocks : 0, s->c,
+                                               dgamma, dbeta);
+    rc = launch_check("layer_norm_bwd sums");
+    return err == cudaSuccess ? rc : cuda_check(err, "layer_norm_bwd sums");
 }
 
 }  // extern "C"

@@ -225,15 +225,6 @@ __device__ __forceinline__ void tma_store_3d(const void* tmap, const void* src, 
                  "r"(smem_u32(src)), "r"(c0), "r"(c1), "r"(c2)
                  : "memory");
 }
-__device__ __forceinline__ void bulk_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
-__device__ __forceinline__ void bulk_wait_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
-__device__ __forceinline__ void bulk_load(uint32_t dst, uintptr_t src, uint32_t bytes, uint64_t* bar)
-{
-    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src),
-                 "r"(bytes), "r"(smem_u32(bar))
-                 : "memory");
-}
-
 constexpr int kBlock = 8;  // steps worked on at once
 
 template <class T, bool ALIGNED, int LANES, int R>
@@ -364,31 +355,7 @@ __device__ __forceinline__ void st_async2(uint32_t addr, uint32_t bar, float2 v)
                  : "memory");
 }
 
-__device__ __forceinline__ bool link_try(uint64_t* bar, uint32_t parity)
-{
-    uint32_t ok;
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
-        "selp.u32 %0, 1, 0, p;\n\t}"
-        : "=r"(ok)
-        : "r"(smem_u32(bar)), "r"(parity)
-        : "memory");
-    return ok != 0;
-}
-
-// Bounded, like every wait of the library: a block that gives up says so in the status word and does not wait again.
-__device__ __forceinline__ void link_wait(uint64_t* bar, uint32_t parity, volatile int* abort)
-{
-    if (link_try(bar, parity)) return;
-    const uint64_t t0 = globaltimer();
-    for (uint32_t i = 0; i < kWaitLimitPolls; ++i) {
-        if (link_try(bar, parity)) return;
-        if ((i & 63u) == 63u && (*abort || globaltimer() - t0 > kWaitLimitNs)) break;
-    }
-    *abort = 1;
-    atomicExch(&g_scan_status, DBL_ERR_TIMEOUT);
-}
+__device__ __forceinline__ void link_wait(uint64_t* bar, uint32_t parity, int* abort) { bounded_wait(bar, parity, abort, &g_scan_status); }
 
 // A block stays until the others no longer write to its shared memory (also where one has given up).
 __device__ __forceinline__ void cluster_leave()
@@ -584,6 +551,7 @@ __global__ void __launch_bounds__(kThreads, BLOCKS) scan_fwd_kernel(ScanArgs a, 
         if (a.states) keep += (int64_t)(step / kChunk) * a.c;
     }
     if (ALIGNED) bulk_wait_read();
+    linger(&sm.links.abort);
     if (w.S > 1) cluster_leave();
     if (a.last && last && w.one && w.rank == w.S - 1) st_state(a.last + w.b * a.c + w.ch, end, w.two);
 }
@@ -802,6 +770,7 @@ __global__ void __launch_bounds__(kThreads, BLOCKS) scan_bwd_kernel(ScanArgs a, 
         row -= step;
     }
     if (ALIGNED) bulk_wait_read();
+    linger(&sm.links.abort);
     if (w.S > 1) cluster_leave();
     if (a.last && last && w.one && w.rank == 0) st_state(a.last + w.b * a.c + w.ch, end, w.two);
 }
@@ -949,14 +918,7 @@ int pass_through(const dbl_scan_shape* s, const float* from, float* to, cudaStre
 
 namespace dbl {
 
-// The device-side status word of this file's kernels, cleared as it is read (the device is synchronised).
-int scan_device_status(int* status)
-{
-    int zero = 0;
-    int rc = cuda_check(cudaMemcpyFromSymbol(status, g_scan_status, sizeof(int)), "device_status read");
-    if (rc == DBL_OK && *status != DBL_OK) rc = cuda_check(cudaMemcpyToSymbol(g_scan_status, &zero, sizeof(int)), "device_status clear");
-    return rc;
-}
+int scan_device_status(int* status) { return take_status(g_scan_status, status); }
 
 }  // namespace dbl
 
