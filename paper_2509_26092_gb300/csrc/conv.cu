@@ -3908,7 +3908,7 @@ int dbl_device_status(int32_t* status)
     int v = 0, zero = 0;
     if ((rc = cuda_check(cudaMemcpyFromSymbol(&v, g_conv_status, sizeof(int)), "device_status read"))) return rc;
     if ((rc = cuda_check(cudaMemcpyToSymbol(g_conv_status, &zero, sizeof(int)), "device_status clear"))) return rc;
-    for (auto take : {ln_device_status, scan_device_status}) {
+    for (auto take : {ln_device_status, scan_device_status, distill_device_status}) {
         int other = 0;
         if ((rc = take(&other))) return rc;
         if (v == DBL_OK) v = other;

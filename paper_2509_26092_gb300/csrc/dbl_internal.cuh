@@ -107,6 +107,7 @@ int bn_fwd_finalize(int64_t count, int C, float eps, const float* sum, const flo
 // Read and clear the status words of these files' kernels (DBL_OK or DBL_ERR_TIMEOUT), the device being idle.
 int ln_device_status(int* status);
 int scan_device_status(int* status);
+int distill_device_status(int* status);
 
 }  // namespace dbl
 
