@@ -11,6 +11,22 @@ inline size_t elem_bytes(int dtype) { return dtype == DBL_F32 ? sizeof(float) : 
 inline bool aligned_to(const void* p, size_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
 
 #if defined(__CUDACC__)
+// Lets KERNEL be launched with up to `bytes` of dynamic shared memory, the same for all its launches, and in clusters of
+// more than eight blocks where asked.  Once per device.
+template <auto KERNEL>
+int allow_launch(size_t bytes, bool large_clusters, const char* what)
+{
+    static std::atomic<bool> done[64] = {};
+    int dev = 0;
+    int rc = cuda_check(cudaGetDevice(&dev), what);
+    if (rc != DBL_OK || (dev >= 0 && dev < 64 && done[dev])) return rc;
+    rc = cuda_check(cudaFuncSetAttribute(KERNEL, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes), what);
+    if (rc == DBL_OK && large_clusters)
+        rc = cuda_check(cudaFuncSetAttribute(KERNEL, cudaFuncAttributeNonPortableClusterSizeAllowed, 1), what);
+    if (rc == DBL_OK && dev >= 0 && dev < 64) done[dev] = true;
+    return rc;
+}
+
 namespace dev {
 
 __device__ __forceinline__ float elem_f(float v) { return v; }

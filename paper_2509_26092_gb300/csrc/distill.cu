@@ -17,9 +17,13 @@ namespace {
 using namespace dbl;
 using namespace dbl::dev;
 
-constexpr int kMaxThreads = 512;
+constexpr int kMaxThreads = 256;             // that pass over the row; a warp more takes the teacher's entries
+constexpr int kFewK = 64;                    // and up to this many, looks for classes that are named twice
 constexpr int kMaxK = DBL_DISTILL_MAX_K;
 constexpr int kMaxCluster = 16;
+constexpr int kWarpRows = 4;                 // rows of a block, a warp each, where they have
+constexpr size_t kWarpBytes = 16384 + 16, kWarpBytesFew = 4096 + 16;  // this many bytes at the most
+constexpr int kWarpK = 128;                  // and the teacher this many entries
 constexpr int kStream = 256;                 // threads of the kernel for rows that no cluster holds
 constexpr size_t kPartBytes = 68 * 1024;     // of a row, to a block: three blocks on an SM
 constexpr size_t kMaxPartBytes = 200 * 1024;
@@ -38,7 +42,7 @@ struct DistillArgs {
     void* dz;
     int64_t rows, ld, ld_grad;
     int v, k;
-    float tau, alpha;
+    float tau, alpha, one;  // one: the weight of a row where none are given
 };
 
 __device__ __forceinline__ float exp2_ftz(float x)
@@ -94,100 +98,171 @@ struct Unit {
     }
 };
 
-// The teacher's distribution of row r, by one warp: p[j] (0 where the entry is absent) and its class (or -1).
-// Returns log(sum) + largest/T, so that log p = t/T less that; NaN where there is no entry.
-__device__ __forceinline__ float teacher(const DistillArgs& a, int64_t r, float* p, int* cls, bool& some)
+// What a row's group keeps in shared memory beside its logits: of the teacher's k entries the classes (-1: absent, and
+// past the end to a multiple of 4), p, t/T, the student's logits, and their gradients.
+struct Entries {
+    int* cls;
+    float *p, *lt, *zc, *fix;
+    static __host__ __device__ size_t bytes(int k) { return (size_t)((k + 3) / 4 * 4) * 20; }
+    __device__ __forceinline__ Entries(char* at, int k)
+    {
+        const int n = (k + 3) / 4 * 4;
+        cls = reinterpret_cast<int*>(at);
+        p = reinterpret_cast<float*>(cls + n), lt = p + n, zc = lt + n, fix = zc + n;
+    }
+};
+
+// Row r's entries and the student's logits z of their classes, by `threads` threads.
+template <class T>
+__device__ __forceinline__ void load_entries(const DistillArgs& a, int64_t r, const T* z, const Entries& en, int tid, int threads)
+{
+    const float inv_tau = 1.f / a.tau;
+#pragma unroll 4
+    for (int j = tid; j < (a.k + 3) / 4 * 4; j += threads) {
+        const int c = j < a.k ? __ldg(a.cls + r * a.k + j) : -1;
+        const float t = j < a.k ? __ldg(a.top + r * a.k + j) : 0.f;
+        const bool there = c >= 0 && c < a.v && t != -INFINITY && a.alpha > 0.f;  // a term of weight 0 is absent
+        en.cls[j] = there ? c : -1;
+        en.lt[j] = t * inv_tau;
+        en.zc[j] = there ? elem_f(z[c]) : 0.f;
+    }
+}
+
+// The teacher's distribution, by one warp.  log_t: log p = t/T less that.  False where there is no entry.
+__device__ __forceinline__ bool teacher(const DistillArgs& a, const Entries& en, float& log_t)
 {
     const int lane = threadIdx.x & 31;
-    const float inv_tau = 1.f / a.tau;
-    float tm = -INFINITY;
+    float tm = -INFINITY, sum = 0.f;
     bool any = false;
-    for (int j = lane; j < a.k; j += 32) {
-        const int c = a.cls[r * a.k + j];
-        const float t = a.top[r * a.k + j];
-        const bool there = c >= 0 && c < a.v && t != -INFINITY && a.alpha > 0.f;  // a term of weight 0 is absent
-        cls[j] = there ? c : -1;
-        p[j] = t;
-        if (there) any = true, tm = fmaxf(tm, t);
-    }
-    some = __any_sync(0xffffffffu, any);
+    for (int j = lane; j < a.k; j += 32)
+        if (en.cls[j] >= 0) any = true, tm = fmaxf(tm, en.lt[j]);
     tm = warp_max(tm);
-    float sum = 0.f;
     for (int j = lane; j < a.k; j += 32) {
-        const float e = cls[j] >= 0 ? expf((p[j] - tm) * inv_tau) : 0.f;
-        p[j] = e;
+        const float e = en.cls[j] >= 0 ? expf(en.lt[j] - tm) : 0.f;
+        en.p[j] = e;
         sum += e;
     }
     sum = warp_sum(sum);
     const float inv = 1.f / sum;
-    for (int j = lane; j < a.k; j += 32) p[j] = cls[j] >= 0 ? p[j] * inv : 0.f;
-    return logf(sum) + tm * inv_tau;
+    for (int j = lane; j < a.k; j += 32) en.p[j] = en.cls[j] >= 0 ? en.p[j] * inv : 0.f;
+    log_t = logf(sum) + tm;
+    return __any_sync(0xffffffffu, any);
 }
 
-// The first term of row r's loss over alpha*T^2, by one warp, from the logits z of the entries' classes.
-__device__ __forceinline__ float divergence(const DistillArgs& a, int64_t r, const float* p, const int* cls, const float* zc, float log_t,
-                                            float m, float log_q)
+// Whether another entry names the class of entry j.
+__device__ __forceinline__ bool again(const DistillArgs& a, const Entries& en, int j)
+{
+    const int c = en.cls[j];
+    int count = 0;
+#pragma unroll 4
+    for (int i = 0; i < a.k; i += 4) {
+        const int4 q = *reinterpret_cast<const int4*>(en.cls + i);
+        count += (q.x == c) + (q.y == c) + (q.z == c) + (q.w == c);
+    }
+    return count > 1;
+}
+
+// The first term of a row's loss over alpha*T^2, by one warp.
+__device__ __forceinline__ float divergence(const DistillArgs& a, const Entries& en, float log_t, float m, float log_q)
 {
     const float inv_tau = 1.f / a.tau;
     float loss = 0.f;
     for (int j = threadIdx.x & 31; j < a.k; j += 32)
-        if (cls[j] >= 0 && p[j] != 0.f)
-            loss += p[j] * ((a.top[r * a.k + j] * inv_tau - log_t) - ((zc[j] - m) * inv_tau - log_q));
+        if (en.cls[j] >= 0 && en.p[j] != 0.f) loss += en.p[j] * ((en.lt[j] - log_t) - ((en.zc[j] - m) * inv_tau - log_q));
     return warp_sum(loss);
 }
 
+// The whole probability of class c, which several entries may name.
+__device__ __forceinline__ float named(const DistillArgs& a, const Entries& en, int c)
+{
+    float s = 0.f;
+    for (int i = 0; i < a.k; i += 4) {
+        const int4 q = *reinterpret_cast<const int4*>(en.cls + i);
+        if (q.x == c) s += en.p[i];
+        if (q.y == c) s += en.p[i + 1];
+        if (q.z == c) s += en.p[i + 2];
+        if (q.w == c) s += en.p[i + 3];
+    }
+    return s;
+}
+
 struct Smem {
+    float4 part[kMaxCluster];            // (maximum, sum at T, sum at 1) of every block of the cluster
+    float4 warp[kMaxThreads / 32];       // of every warp
     uint64_t full;
     int abort, some;
-    float log_t, zl;
-    float red[32];
-    float2 red2[32];
-    float4 part[kMaxCluster];  // (maximum, sum at T, sum at 1) of every block of the cluster
+    float log_t;
 };
 
-// and p, cls, the entries' logits and gradients ([k] each)
-__host__ __device__ inline size_t head_bytes(int k) { return ((sizeof(Smem) + 15) / 16 * 16 + (size_t)k * 16 + 127) / 128 * 128; }
+__host__ __device__ inline size_t head_bytes(int k) { return ((sizeof(Smem) + 15) / 16 * 16 + Entries::bytes(k) + 127) / 128 * 128; }
 
-// One row, or a cluster's part of it, per block.
-template <class T>
-__global__ void __launch_bounds__(kMaxThreads, 3) distill_kernel(DistillArgs a)
+// (maximum, sums) of the parts of a row as one.
+__device__ __forceinline__ float4 join(const float4* part, int n, float cA)
+{
+    float4 t = make_float4(-INFINITY, 0.f, 0.f, 0.f);
+#pragma unroll 4
+    for (int i = 0; i < n; ++i) t.x = fmaxf(t.x, part[i].x);
+    const float m = t.x == -INFINITY ? 0.f : t.x;  // nothing but minus infinities: sums of 0, or NaN
+#pragma unroll 4
+    for (int i = 0; i < n; ++i) {
+        const float4 q = part[i];
+        t.y = fmaf(q.y, exp2_ftz((q.x - m) * cA), t.y);
+        t.z = fmaf(q.z, exp2_ftz((q.x - m) * kLog2e), t.z);
+    }
+    return t;
+}
+
+// One row, or a cluster's part of it, per block; WARP: a row per warp.
+template <class T, bool WARP>
+__global__ void __launch_bounds__(WARP ? 32 * kWarpRows : kMaxThreads + 32, WARP ? 10 : 3) distill_kernel(DistillArgs a, int bytes_of_group)
 {
     typedef Unit<T> U;
     constexpr int E = U::E, P = U::P;
     extern __shared__ __align__(128) char smem_raw[];
-    Smem& sm = *reinterpret_cast<Smem*>(smem_raw);
-    float* p = reinterpret_cast<float*>(smem_raw + (sizeof(Smem) + 15) / 16 * 16);
-    int* cls = reinterpret_cast<int*>(p + a.k);
-    float *zc = reinterpret_cast<float*>(cls + a.k), *fix = zc + a.k;
-    const size_t head = head_bytes(a.k);
-    uint4* units = reinterpret_cast<uint4*>(smem_raw + head);
+    char* const base = smem_raw + (WARP ? (threadIdx.x >> 5) * bytes_of_group : 0);
+    Smem& sm = *reinterpret_cast<Smem*>(base);
+    const Entries en(base + (sizeof(Smem) + 15) / 16 * 16, a.k);
+    uint4* units = reinterpret_cast<uint4*>(base + head_bytes(a.k));
     T* elems = reinterpret_cast<T*>(units);
 
-    uint32_t nrank;
-    asm("mov.u32 %0, %%cluster_nctaid.x;" : "=r"(nrank));
-    const int S = (int)nrank, rank = (int)cluster_ctarank(), tid = threadIdx.x, threads = blockDim.x;
-    const int64_t r = blockIdx.x / S;
+    int S = 1, rank = 0;
+    if (!WARP) {
+        uint32_t n;
+        asm("mov.u32 %0, %%cluster_nctaid.x;" : "=r"(n));
+        S = (int)n, rank = (int)cluster_ctarank();
+    }
+    const int tid = WARP ? threadIdx.x & 31 : threadIdx.x, threads = WARP ? 32 : blockDim.x - 32;
+    const bool side = !WARP && tid >= threads;  // the warp beside those that pass over the row
+    auto sync = [] {
+        if (WARP)
+            __syncwarp();
+        else
+            __syncthreads();
+    };
+    const int64_t r = WARP ? (int64_t)blockIdx.x * kWarpRows + (threadIdx.x >> 5) : S == 1 ? blockIdx.x : blockIdx.x / (unsigned)S;
+    grid_dependency_trigger();
+    if (r >= a.rows) return;
     const T* z = static_cast<const T*>(a.z) + r * a.ld;
     T* dz = a.dz ? static_cast<T*>(a.dz) + r * a.ld_grad : nullptr;
     // the row in units of 16 bytes, from the boundary at or before its first element; this block's part of them
     const uintptr_t p0 = reinterpret_cast<uintptr_t>(z), p1 = p0 + (size_t)a.v * sizeof(T);
     const int lead = (int)(p0 & 15) / (int)sizeof(T);
-    const int all = (int)(((p1 + 15) >> 4) - (p0 >> 4)), per = (all + S - 1) / S;
+    const int all = (int)(((p1 + 15) >> 4) - (p0 >> 4)), per = S == 1 ? all : (int)((unsigned)(all + S - 1) / (unsigned)S);
     const int u0 = min(rank * per, all), n = min(per, all - u0);
     const int first = u0 * E - lead;  // the element that is elems[0]
     const int e0 = max(first, 0), e1 = min(first + n * E, a.v);
-    const float w = a.weight ? a.weight[r] : 1.f / (float)a.rows;
-    const int lab = a.labels && a.alpha < 1.f ? a.labels[r] : -1;
+    const float w = a.weight ? __ldg(a.weight + r) : a.one;
+    const int lab = a.labels && a.alpha < 1.f ? __ldg(a.labels + r) : -1;
+    const float scale = a.scale ? __ldg(a.scale) : 1.f;
     const bool given = lab >= 0 && lab < a.v;
 
-    grid_dependency_trigger();
     auto zeros = [&] {
         const T zero = elem_from<T>(0.f);
         const int mis = (int)(reinterpret_cast<uintptr_t>(dz + e0) & 15) / (int)sizeof(T), b0 = min(e0 + (mis ? E - mis : 0), e1);
-        const int b1 = b0 + (e1 - b0) / E * E;
-        for (int i = e0 + tid; i < b0; i += threads) dz[i] = zero;
-        for (int i = b0 + tid * E; i < b1; i += threads * E) *reinterpret_cast<uint4*>(dz + i) = make_uint4(0, 0, 0, 0);
-        for (int i = b1 + tid; i < e1; i += threads) dz[i] = zero;
+        const int b1 = b0 + (e1 - b0) / E * E, step = WARP ? 32 : blockDim.x;
+        for (int i = e0 + tid; i < b0; i += step) dz[i] = zero;
+        for (int i = b0 + tid * E; i < b1; i += step * E) *reinterpret_cast<uint4*>(dz + i) = make_uint4(0, 0, 0, 0);
+        for (int i = b1 + tid; i < e1; i += step) dz[i] = zero;
     };
     if (w == 0.f) {
         if (rank == 0 && tid == 0) a.row_loss[r] = 0.f;
@@ -204,49 +279,39 @@ __global__ void __launch_bounds__(kMaxThreads, 3) distill_kernel(DistillArgs a)
         mbar_arrive_expect_tx(&sm.full, bytes);
         if (bytes) bulk_load(smem_u32(units + c0), (p0 & ~(uintptr_t)15) + (uintptr_t)(u0 + c0) * 16, bytes, &sm.full);
     }
-    for (int i = tid; i < 2 * E; i += threads) {
-        const int u = i < E ? 0 : c1, at = u * E + i % E;
-        if (n > 0 && (i < E ? c0 == 1 : c1 < n)) {
-            const int el = first + at;
-            elems[at] = el >= 0 && el < a.v ? z[el] : elem_from<T>(-INFINITY);
-        }
+    if ((c0 || c1 < n) && tid < 2 * E && n > 0 && (tid < E ? c0 == 1 : c1 < n)) {
+        const int at = (tid < E ? 0 : c1 * E) + tid % E, el = first + at;
+        elems[at] = el >= 0 && el < a.v ? z[el] : elem_from<T>(-INFINITY);
     }
-    if (tid < 32) {
-        bool some;
-        const float log_t = teacher(a, r, p, cls, some);
-        if (tid == 0) {
-            sm.log_t = log_t, sm.some = some;
-            sm.zl = given ? elem_f(z[lab]) : 0.f;
-        }
-        if (rank == 0)
-            for (int j = tid; j < a.k; j += 32) zc[j] = cls[j] >= 0 ? elem_f(z[cls[j]]) : 0.f;
+    const float zl = given ? elem_f(z[lab]) : 0.f;
+    sync();
+    if (WARP || side) {  // while the row is on its way
+        load_entries(a, r, z, en, tid & 31, 32);
+        __syncwarp();
+        float log_t;
+        const bool some = teacher(a, en, log_t);
+        if ((tid & 31) == 0) sm.log_t = log_t, sm.some = some;
+        if (a.k <= kFewK)
+            for (int j = tid & 31; j < a.k; j += 32) en.fix[j] = again(a, en, j) ? 1.f : 0.f;
     }
-    __syncthreads();
-    const bool some = sm.some;
-    bounded_wait(&sm.full, 0, &sm.abort, &g_distill_status);
-    if (!some && !given) {
-        linger(&sm.abort);
-        if (rank == 0 && tid == 0) a.row_loss[r] = 0.f;
-        if (dz) zeros();
-        return;
-    }
-    // maximum
-    const uint32_t lowest = sizeof(T) == 4 ? 0xff800000u : act::kF16 ? 0xfc00fc00u : 0xff80ff80u;  // minus infinity
-    uint4 mx = make_uint4(lowest, lowest, lowest, lowest);
-#pragma unroll 4
-    for (int i = tid; i < n; i += threads) U::max(mx, units[i]);
+    // Two kinds of exponential where there may be two terms and T is not 1.
+    const bool kl = a.k > 0 && a.alpha > 0.f, two = kl && given && a.tau != 1.f;
+    const float cA = kl ? kLog2e / a.tau : kLog2e;
     float2 f[P];
-    U::floats(f, mx);
-    float m = -INFINITY;
+    float4 t = make_float4(-INFINITY, 0.f, 0.f, 0.f);
+    if (!side) {
+        bounded_wait(&sm.full, 0, &sm.abort, &g_distill_status);
+        const uint32_t lowest = sizeof(T) == 4 ? 0xff800000u : act::kF16 ? 0xfc00fc00u : 0xff80ff80u;  // minus infinity
+        uint4 mx = make_uint4(lowest, lowest, lowest, lowest);
+#pragma unroll 4
+        for (int i = tid; i < n; i += threads) U::max(mx, units[i]);
+        U::floats(f, mx);
+        float m = -INFINITY;
 #pragma unroll
-    for (int i = 0; i < P; ++i) m = fmaxf(m, fmaxf(f[i].x, f[i].y));
-    m = block_max(m, sm.red);
-    // sums; one kind of exponential where there is one term, or T = 1
-    const bool two = some && given && a.tau != 1.f;
-    const float cA = some ? kLog2e / a.tau : kLog2e;
-    float2 sA = both(0.f), sB = both(0.f);
-    if (m != -INFINITY) {  // otherwise nothing here
-        const float2 nm = both(-m);
+        for (int i = 0; i < P; ++i) m = fmaxf(m, fmaxf(f[i].x, f[i].y));
+        m = warp_max(m);
+        float2 sA = both(0.f), sB = both(0.f);
+        const float2 nm = both(m == -INFINITY ? 0.f : -m);  // nothing but minus infinities: sums of 0
         if (two) {
 #pragma unroll 2
             for (int i = tid; i < n; i += threads) {
@@ -266,35 +331,36 @@ __global__ void __launch_bounds__(kMaxThreads, 3) distill_kernel(DistillArgs a)
                 for (int q = 0; q < P; ++q) sA = __fadd2_rn(sA, exp2_2(__fmul2_rn(__fadd2_rn(f[q], nm), both(cA))));
             }
         }
+        t = make_float4(m, warp_sum(sA.x + sA.y), two ? warp_sum(sB.x + sB.y) : 0.f, 0.f);
+        if (!WARP && (tid & 31) == 0) sm.warp[tid >> 5] = t;
     }
-    float tA = warp_sum(sA.x + sA.y), tB = warp_sum(sB.x + sB.y);
-    if ((tid & 31) == 0) sm.red2[tid >> 5] = make_float2(tA, tB);
-    __syncthreads();
-    tA = tB = 0.f;
-    for (int i = 0; i < threads >> 5; ++i) tA += sm.red2[i].x, tB += sm.red2[i].y;
-    if (S > 1) {
-        if (tid < S)
-            st_cluster_v4(mapa_shared(smem_u32(&sm.part[rank]), tid), __float_as_uint(m), __float_as_uint(tA), __float_as_uint(tB), 0);
-        // also: no block writes a gradient to the logits' place before the others have read what they need there
-        cluster_sync_all();
-        m = sm.part[0].x;
-        for (int i = 1; i < S; ++i) m = fmaxf(m, sm.part[i].x);
-        tA = tB = 0.f;
-        for (int i = 0; i < S; ++i) {
-            const float4 q = sm.part[i];
-            tA += q.y * exp2_ftz((q.x - m) * cA);
-            tB += q.z * exp2_ftz((q.x - m) * kLog2e);
+    sync();
+    if (!WARP) {
+        t = join(sm.warp, threads >> 5, cA);
+        if (S > 1) {
+            if (tid < S)
+                st_cluster_v4(mapa_shared(smem_u32(&sm.part[rank]), tid), __float_as_uint(t.x), __float_as_uint(t.y), __float_as_uint(t.z), 0);
+            // also: no block writes a gradient to the logits' place before the others have read what they need there
+            cluster_sync_all();
+            t = join(sm.part, S, cA);
         }
     }
-    if (!two) tB = tA;
-    if (rank == 0 && tid < 32) {
-        float loss = some ? divergence(a, r, p, cls, zc, sm.log_t, m, logf(tA)) * (a.alpha * a.tau * a.tau) : 0.f;
-        if (given) loss += (1.f - a.alpha) * (logf(tB) - (sm.zl - m));
-        if (tid == 0) a.row_loss[r] = loss;
-    }
     linger(&sm.abort);
+    const bool some = sm.some;
+    if (!some && !given) {
+        if (rank == 0 && tid == 0) a.row_loss[r] = 0.f;
+        if (dz) zeros();
+        return;
+    }
+    const float m = t.x, bad = m == -INFINITY ? NAN : 0.f;  // no distribution
+    const float tA = t.y + bad, tB = two ? t.z + bad : tA;
+    if (rank == 0 && (WARP || side)) {
+        float loss = some ? divergence(a, en, sm.log_t, m, logf(tA)) * (a.alpha * a.tau * a.tau) : 0.f;
+        if (given) loss += (1.f - a.alpha) * (logf(tB) - (zl - m));
+        if ((tid & 31) == 0) a.row_loss[r] = loss;
+    }
     if (!dz) return;
-    const float fw = a.scale ? w * *a.scale : w;
+    const float fw = w * scale;
     const float gt = some ? fw * a.alpha * a.tau : 0.f, gl = given ? fw * (1.f - a.alpha) : 0.f;
     // exponentials' factors: the two terms', or both in one
     const float fA = two ? gt / tA : (gt + gl) / tA, fB = gl / tB;
@@ -303,54 +369,48 @@ __global__ void __launch_bounds__(kMaxThreads, 3) distill_kernel(DistillArgs a)
         const float2 g = __fmul2_rn(exp2_2(__fmul2_rn(d, both(cA))), both(fA));
         return two ? __ffma2_rn(exp2_2(__fmul2_rn(d, both(kLog2e))), both(fB), g) : g;
     };
-    // the classes of the teacher and the label, before their logits are overwritten
-    auto fix_of = [&](int c, float pj) {
-        const float g = grad(both(elem_f(elems[c - first]))).x;
-        return g - gt * pj - (c == lab && given ? gl : 0.f);
-    };
-    for (int j = tid; j < a.k; j += threads) {
-        if (cls[j] < e0 || cls[j] >= e1) continue;
-        float pj = 0.f;
-        for (int i = 0; i < a.k; ++i)
-            if (cls[i] == cls[j]) pj += p[i];  // a class may be named again
-        fix[j] = fix_of(cls[j], pj);
-    }
+    // the classes of the teacher and the label, from their logits as they were
+    const bool lab_here = given && lab >= e0 && lab < e1 && tid == threads - 1;
     float fix_lab = 0.f;
-    bool lab_here = given && tid == threads - 1 && lab >= e0 && lab < e1;
-    if (lab_here) {
-        float pj = 0.f;
-        for (int i = 0; i < a.k; ++i)
-            if (cls[i] == lab) pj += p[i];
-        fix_lab = fix_of(lab, pj);
-    }
-    __syncthreads();
-    if (two) {
-#pragma unroll 2
-        for (int i = tid; i < n; i += threads) {
-            U::floats(f, units[i]);
-#pragma unroll
-            for (int q = 0; q < P; ++q) f[q] = grad(f[q]);
-            units[i] = U::pack(f);
+    if (!side) {
+        for (int j = tid; j < a.k; j += threads) {
+            const int c = en.cls[j];
+            if (c < e0 || c >= e1) continue;
+            const float pj = (a.k <= kFewK ? en.fix[j] != 0.f : again(a, en, j)) ? named(a, en, c) : en.p[j];
+            en.fix[j] = grad(both(en.zc[j])).x - gt * pj - (c == lab && given ? gl : 0.f);
         }
-    } else {
-        const float2 nm = both(-m);
+        if (lab_here) fix_lab = grad(both(zl)).x - gt * named(a, en, lab) - gl;
+        if (two) {
 #pragma unroll 2
-        for (int i = tid; i < n; i += threads) {
-            U::floats(f, units[i]);
+            for (int i = tid; i < n; i += threads) {
+                U::floats(f, units[i]);
 #pragma unroll
-            for (int q = 0; q < P; ++q) f[q] = __fmul2_rn(exp2_2(__fmul2_rn(__fadd2_rn(f[q], nm), both(cA))), both(fA));
-            units[i] = U::pack(f);
+                for (int q = 0; q < P; ++q) f[q] = grad(f[q]);
+                units[i] = U::pack(f);
+            }
+        } else {
+            const float2 nm = both(-m);
+#pragma unroll 2
+            for (int i = tid; i < n; i += threads) {
+                U::floats(f, units[i]);
+#pragma unroll
+                for (int q = 0; q < P; ++q) f[q] = __fmul2_rn(exp2_2(__fmul2_rn(__fadd2_rn(f[q], nm), both(cA))), both(fA));
+                units[i] = U::pack(f);
+            }
         }
     }
-    __syncthreads();
-    for (int j = tid; j < a.k; j += threads)
-        if (cls[j] >= e0 && cls[j] < e1) elems[cls[j] - first] = elem_from<T>(fix[j]);
-    if (lab_here) elems[lab - first] = elem_from<T>(fix_lab);
+    sync();
+    if (!side) {
+        for (int j = tid; j < a.k; j += threads)
+            if (en.cls[j] >= e0 && en.cls[j] < e1) elems[en.cls[j] - first] = elem_from<T>(en.fix[j]);
+        if (lab_here) elems[lab - first] = elem_from<T>(fix_lab);
+    }
     const bool same = ((reinterpret_cast<uintptr_t>(dz) ^ p0) & 15) == 0;  // rows begin at the same place of a unit
     if (same) fence_async_shared();
-    __syncthreads();
+    sync();
+    const int step = WARP ? 32 : blockDim.x;
     if (!same) {
-        for (int i = e0 + tid; i < e1; i += threads) dz[i] = elems[i - first];
+        for (int i = e0 + tid; i < e1; i += step) dz[i] = elems[i - first];
         return;
     }
     if (tid == 0 && c1 > c0) {
@@ -359,8 +419,8 @@ __global__ void __launch_bounds__(kMaxThreads, 3) distill_kernel(DistillArgs a)
                      : "memory");
         bulk_commit();
     }
-    for (int i = e0 + tid; i < min(first + c0 * E, e1); i += threads) dz[i] = elems[i - first];
-    for (int i = max(first + c1 * E, e0) + tid; i < e1; i += threads) dz[i] = elems[i - first];
+    for (int i = e0 + tid; i < min(first + c0 * E, e1); i += step) dz[i] = elems[i - first];
+    for (int i = max(first + c1 * E, e0) + tid; i < e1; i += step) dz[i] = elems[i - first];
     if (tid == 0) bulk_wait_read();
 }
 
@@ -369,20 +429,21 @@ template <class T>
 __global__ void __launch_bounds__(kStream) distill_stream_kernel(DistillArgs a)
 {
     __shared__ float red[32];
-    __shared__ float p[kMaxK], zc[kMaxK];
-    __shared__ int cls[kMaxK];
+    __shared__ __align__(16) char entries[kMaxK * 20];
+    const Entries en(entries, a.k);
     __shared__ int some_s;
     __shared__ float log_ts;
     for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
         const T* z = static_cast<const T*>(a.z) + r * a.ld;
         T* dz = a.dz ? static_cast<T*>(a.dz) + r * a.ld_grad : nullptr;
-        const float w = a.weight ? a.weight[r] : 1.f / (float)a.rows;
+        const float w = a.weight ? a.weight[r] : a.one;
         const int lab = a.labels && a.alpha < 1.f ? a.labels[r] : -1;
         const bool given = lab >= 0 && lab < a.v;
         if (threadIdx.x < 32) {
-            bool some;
-            const float log_t = teacher(a, r, p, cls, some);
-            for (int j = threadIdx.x; j < a.k; j += 32) zc[j] = cls[j] >= 0 ? elem_f(z[cls[j]]) : 0.f;
+            float log_t;
+            load_entries(a, r, z, en, threadIdx.x, 32);
+            __syncwarp();
+            const bool some = teacher(a, en, log_t);
             if (threadIdx.x == 0) some_s = some, log_ts = log_t;
         }
         __syncthreads();
@@ -410,7 +471,7 @@ __global__ void __launch_bounds__(kStream) distill_stream_kernel(DistillArgs a)
         const float tA = block_sum((sA[0] + sA[1]) + (sA[2] + sA[3]), red), tB = block_sum((sB[0] + sB[1]) + (sB[2] + sB[3]), red);
         const float zl = given ? elem_f(z[lab]) : 0.f;
         if (threadIdx.x < 32) {
-            float loss = some ? divergence(a, r, p, cls, zc, log_ts, m, logf(tA)) * (a.alpha * a.tau * a.tau) : 0.f;
+            float loss = some ? divergence(a, en, log_ts, m, logf(tA)) * (a.alpha * a.tau * a.tau) : 0.f;
             if (given) loss += (1.f - a.alpha) * (logf(tB) - (zl - m));
             if (threadIdx.x == 0) a.row_loss[r] = loss;
         }
@@ -428,18 +489,10 @@ __global__ void __launch_bounds__(kStream) distill_stream_kernel(DistillArgs a)
         for (int i = threadIdx.x; i < a.v; i += kStream) dz[i] = elem_from<T>(grad(elem_f(z[i])));
         __syncthreads();
         for (int j = threadIdx.x; j < a.k; j += kStream) {
-            if (cls[j] < 0) continue;
-            float pj = 0.f;
-            for (int i = 0; i < a.k; ++i)
-                if (cls[i] == cls[j]) pj += p[i];
-            dz[cls[j]] = elem_from<T>(grad(zc[j]) - gt * pj - (cls[j] == lab && given ? gl : 0.f));
+            const int c = en.cls[j];
+            if (c >= 0) dz[c] = elem_from<T>(grad(en.zc[j]) - gt * named(a, en, c) - (c == lab && given ? gl : 0.f));
         }
-        if (given && threadIdx.x == 0) {
-            float pj = 0.f;
-            for (int i = 0; i < a.k; ++i)
-                if (cls[i] == lab) pj += p[i];
-            if (pj == 0.f) dz[lab] = elem_from<T>(grad(zl) - gl);  // not among the entries (or of no weight there)
-        }
+        if (given && threadIdx.x == 0) dz[lab] = elem_from<T>(grad(zl) - gt * named(a, en, lab) - gl);
         __syncthreads();
     }
 }
@@ -451,6 +504,7 @@ __global__ void __launch_bounds__(1024) distill_loss_kernel(const float* row_los
     __shared__ float red[32];
     grid_dependency_wait();
     float s = 0.f;
+#pragma unroll 8
     for (int64_t r = threadIdx.x; r < rows; r += 1024) s += weight ? weight[r] * row_loss[r] : row_loss[r];
     s = block_sum(s, red);
     if (threadIdx.x == 0) *loss = weight ? s : s / (float)rows;
@@ -459,15 +513,27 @@ __global__ void __launch_bounds__(1024) distill_loss_kernel(const float* row_los
 template <class T>
 int launch(const DistillArgs& a, cudaStream_t st, const char* what)
 {
-    constexpr auto kernel = distill_kernel<T>;
+    constexpr auto kernel = distill_kernel<T, false>;
+    constexpr auto kernel_w = distill_kernel<T, true>;
     const size_t head = head_bytes(a.k);
     const size_t row = ((size_t)a.v * sizeof(T) + 15) / 16 * 16 + 16;
     auto part = [&](int S) { return (row / 16 + S - 1) / S * 16; };
+    // Many rows go by the rows in flight on an SM (8000 x 8000 in bf16: 85 us a warp each, 120 us a block each; 8000 x
+    // 4000 48 and 73 us), few by the threads of each.
+    if (row <= (a.rows >= 4 * sm_count() ? kWarpBytes : kWarpBytesFew) && a.k <= kWarpK) {
+        const size_t group = (head + row + 127) / 128 * 128;
+        const int64_t grid = (a.rows + kWarpRows - 1) / kWarpRows;
+        if (grid > 0x7fffffff) return set_error(DBL_ERR_UNSUPPORTED, "%s: more than 2^31 blocks", what);
+        const int rc = allow_launch<kernel_w>(kWarpRows * (kWarpBytes + head_bytes(kWarpK) + 128), false, what);
+        if (rc != DBL_OK) return rc;
+        kernel_w<<<(unsigned)grid, 32 * kWarpRows, group * kWarpRows, st>>>(a, (int)group);
+        return launch_check(what);
+    }
     // as many blocks to a row as bring three on an SM, and for few rows, as fill the SMs with parts of 8 KB and more
     int S = 1;
     while (S < kMaxCluster && part(S) > kPartBytes) S *= 2;
     while (S < kMaxCluster && a.rows * S * 2 <= sm_count() && part(2 * S) >= 8192) S *= 2;
-    while (S > 1 && !cluster_held<kernel>(S, kMaxThreads, kMaxPartBytes + head_bytes(kMaxK))) S /= 2;
+    while (S > 1 && !cluster_held<kernel>(S, kMaxThreads + 32, kMaxPartBytes + head_bytes(kMaxK))) S /= 2;
     if (part(S) > kMaxPartBytes) {
         distill_stream_kernel<T><<<(int)std::min<int64_t>(a.rows, 1 << 20), kStream, 0, st>>>(a);
         return launch_check(what);
@@ -476,9 +542,7 @@ int launch(const DistillArgs& a, cudaStream_t st, const char* what)
     const size_t smem = head + part(S);
     int threads = 64;  // four units of 16 bytes a thread and pass, or more
     while (threads < kMaxThreads && (size_t)threads * 64 < part(S)) threads *= 2;
-    int rc = cuda_check(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem), what);
-    if (rc == DBL_OK && S > 8)
-        rc = cuda_check(cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1), what);
+    int rc = allow_launch<kernel>(kMaxPartBytes + head_bytes(kMaxK), true, what);
     if (rc != DBL_OK) return rc;
     cudaLaunchConfig_t cfg = {};
     cudaLaunchAttribute at[1];
@@ -486,12 +550,12 @@ int launch(const DistillArgs& a, cudaStream_t st, const char* what)
     at[0].val.clusterDim.x = S;
     at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
     cfg.gridDim = dim3((unsigned)(a.rows * S));
-    cfg.blockDim = dim3(threads);
+    cfg.blockDim = dim3(threads + 32);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = st;
     cfg.attrs = at;
     cfg.numAttrs = 1;
-    const cudaError_t err = cudaLaunchKernelEx(&cfg, kernel, a);
+    const cudaError_t err = cudaLaunchKernelEx(&cfg, kernel, a, 0);
     rc = launch_check(what);
     return err == cudaSuccess ? rc : cuda_check(err, what);
 }
@@ -526,7 +590,7 @@ extern "C" int dbl_distill_fwd_bwd(const dbl_distill_shape* s, const void* logit
         return set_error(DBL_ERR_INVALID, "%s: a pointer is not aligned to its element type", w);
     DistillArgs a = {logits, teacher_logits, teacher_classes, labels, row_weight, loss_scale, row_loss, dlogits, s->rows,
                      s->ld ? s->ld : s->classes, s->ld_grad ? s->ld_grad : s->classes, s->classes, s->k, s->temperature,
-                     s->alpha};
+                     s->alpha, s->rows > 0 ? 1.f / (float)s->rows : 0.f};
     if (logits && dlogits == logits && a.ld != a.ld_grad)
         return set_error(DBL_ERR_INVALID, "%s: a gradient in the logits' place needs their row stride", w);
     cudaStream_t st = as_stream(stream);

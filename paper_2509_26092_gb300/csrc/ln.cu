@@ -564,7 +564,7 @@ Plan bwd_plan(LnArgs& a, size_t e)
 template <auto KERNEL>
 int launch(const LnArgs& a, const Plan& p, cudaStream_t st, const char* what)
 {
-    const int rc = cuda_check(cudaFuncSetAttribute(KERNEL, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)p.smem), what);
+    const int rc = allow_launch<KERNEL>(kRingBytes + 16 * 1024, false, what);
     if (rc != DBL_OK) return rc;
     KERNEL<<<p.blocks, p.threads, p.smem, st>>>(a);
     return launch_check(what);

@@ -846,7 +846,7 @@ int launch_tiles(ScanArgs a, cudaStream_t st, const char* what)
     // clusters take turns (backward, 8 x 8192 x 1024: 1, 2 and 4 blocks 147, 132 and 136 us; forward, 4 x 8192 x 1024:
     // 2, 4 and 8 blocks 64, 48 and 54 us; 185 x 196 x 256: 1 and 2 blocks 24 and 30 us).
     int S = (int)std::max<int64_t>(1, std::min<int64_t>({kMaxCluster, 2 * sm_count() / cols, (a.t + subs * R - 1) / (subs * R)}));
-    while (S > 1 && !cluster_held<kernel>(S, kThreads, smem_of(S))) --S;
+    while (S > 1 && !cluster_held<kernel>(S, kThreads, smem_of(kMaxCluster))) --S;
     if (cols * S > 0x7fffffff) return set_error(DBL_ERR_UNSUPPORTED, "%s: more than 2^31 blocks", what);
     Maps maps;
     int rc = DBL_OK;
@@ -858,11 +858,7 @@ int launch_tiles(ScanArgs a, cudaStream_t st, const char* what)
         if (BWD && rc == DBL_OK) rc = encode<T>(&maps.dz, a.dgate, a, a.ld_x, 2 * LANES, St::ROWS, what);
         if (rc != DBL_OK) return rc;
     }
-    const size_t smem = smem_of(S);
-    rc = cuda_check(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem), what);
-    if (rc == DBL_OK && S > 8)
-        rc = cuda_check(cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1), what);
-    if (rc != DBL_OK) return rc;
+    if ((rc = allow_launch<kernel>(smem_of(kMaxCluster), true, what)) != DBL_OK) return rc;
     cudaLaunchConfig_t cfg = {};
     cudaLaunchAttribute at[1];
     at[0].id = cudaLaunchAttributeClusterDimension;
@@ -870,7 +866,7 @@ int launch_tiles(ScanArgs a, cudaStream_t st, const char* what)
     at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
     cfg.gridDim = dim3((unsigned)(cols * S));
     cfg.blockDim = dim3(subs * LANES);
-    cfg.dynamicSmemBytes = smem;
+    cfg.dynamicSmemBytes = smem_of(S);
     cfg.stream = st;
     cfg.attrs = at;
     cfg.numAttrs = 1;

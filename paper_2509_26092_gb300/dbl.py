@@ -197,10 +197,19 @@ def _ptr(t):
     return t.data_ptr()
 
 
+def _current_stream():
+    """The current stream's cudaStream_t: torch.cuda.current_stream() builds a Stream object for it, which takes
+    3 us of a call's 8; where this torch offers the handle itself, 0.4 us."""
+    import torch
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    if raw is None:
+        return torch.cuda.current_stream().cuda_stream
+    return raw(torch.cuda.current_device())
+
+
 def _stream(stream):
     if stream is None:
-        import torch
-        return torch.cuda.current_stream().cuda_stream
+        return _current_stream()
     if isinstance(stream, int):
         return stream
     return stream.cuda_stream
