@@ -117,58 +117,18 @@ class ParamEntry:
         self.numel = n
 
 
-class ResNet18Spec:
-    """Layer list and flat parameter layout of a ResNet-18 variant."""
+class FlatSpec:
+    """Parameter tensors laid out one after another in flat buffers (ALIGN elements apart at least)."""
 
-    def __init__(self, variant="cifar", classes=100, widths=WIDTHS):
-        if variant not in ("cifar", "imagenet"):
-            raise ValueError(variant)
-        self.variant, self.classes, self.widths = variant, classes, tuple(widths)
-        r, st, pad = (3, 1, 1) if variant == "cifar" else (7, 2, 3)
-        self.stem = ConvSpec("conv1", 64, 3, widths[0], r, st, pad)  # 64 = one unrolled row of 128 bytes
-        self.stem_layout = StemLayout.of(self.stem)
-        self.blocks = []
-        cin = widths[0]
-        for li, wd in enumerate(widths):
-            for bi in range(2):
-                stride = 2 if (li > 0 and bi == 0) else 1
-                self.blocks.append(BlockSpec(f"layer{li + 1}.{bi}", cin, wd, stride, stride != 1 or cin != wd))
-                cin = wd
-        self.entries = []
-        off = 0
+    def __init__(self):
+        self.entries, self.by_name, self.n_flat = [], {}, 0
 
-        def add(name, shape, logical, fan_in):
-            nonlocal off
-            e = ParamEntry(name, tuple(shape), tuple(logical), fan_in, off)
-            self.entries.append(e)
-            off += (e.numel + ALIGN - 1) // ALIGN * ALIGN
-
-        def conv(cs):
-            if cs is self.stem:  # stored [k][g*ceil(r/g)][8 columns][8/g channels], logical [k][r][r][3]
-                add(cs.name + ".w", self.stem_layout.stored_shape(cs), (cs.cout, cs.r, cs.r, cs.cin_logical),
-                    cs.r * cs.r * cs.cin_logical)
-                return
-            add(cs.name + ".w", (cs.cout, cs.r, cs.r, cs.cin), (cs.cout, cs.r, cs.r, cs.cin_logical),
-                cs.r * cs.r * cs.cin_logical)
-
-        def bn(name, c):
-            add(name + ".g", (c,), (c,), None)
-            add(name + ".b", (c,), (c,), None)
-
-        conv(self.stem)
-        bn("bn1", widths[0])
-        for b in self.blocks:
-            conv(ConvSpec(b.pre + ".conv1", b.cin, b.cin, b.cout, 3, b.stride, 1))
-            bn(b.pre + ".bn1", b.cout)
-            conv(ConvSpec(b.pre + ".conv2", b.cout, b.cout, b.cout, 3, 1, 1))
-            bn(b.pre + ".bn2", b.cout)
-            if b.proj:
-                conv(ConvSpec(b.pre + ".down", b.cin, b.cin, b.cout, 1, b.stride, 0))
-                bn(b.pre + ".downbn", b.cout)
-        add("fc.w", (classes, cin), (classes, cin), cin)
-        add("fc.b", (classes,), (classes,), None)
-        self.n_flat = off
-        self.by_name = {e.name: e for e in self.entries}
+    def add(self, name, shape, logical, fan_in):
+        """A tensor stored as ``shape``, of which the method defines the corner ``logical``."""
+        e = ParamEntry(name, tuple(shape), tuple(logical), fan_in, self.n_flat)
+        self.entries.append(e)
+        self.by_name[name] = e
+        self.n_flat += (e.numel + ALIGN - 1) // ALIGN * ALIGN
 
     def table(self):
         """(name, logical shape, fan_in) of every parameter tensor, for the input generator."""
@@ -215,6 +175,52 @@ class ResNet18Spec:
             v = self.view(flat, e.name)[tuple(slice(0, d) for d in e.logical)]
             out[e.name] = v.detach().double().cpu().numpy().copy()
         return out
+
+
+class ResNet18Spec(FlatSpec):
+    """Layer list and flat parameter layout of a ResNet-18 variant."""
+
+    def __init__(self, variant="cifar", classes=100, widths=WIDTHS):
+        super().__init__()
+        if variant not in ("cifar", "imagenet"):
+            raise ValueError(variant)
+        self.variant, self.classes, self.widths = variant, classes, tuple(widths)
+        r, st, pad = (3, 1, 1) if variant == "cifar" else (7, 2, 3)
+        self.stem = ConvSpec("conv1", 64, 3, widths[0], r, st, pad)  # 64 = one unrolled row of 128 bytes
+        self.stem_layout = StemLayout.of(self.stem)
+        self.blocks = []
+        cin = widths[0]
+        for li, wd in enumerate(widths):
+            for bi in range(2):
+                stride = 2 if (li > 0 and bi == 0) else 1
+                self.blocks.append(BlockSpec(f"layer{li + 1}.{bi}", cin, wd, stride, stride != 1 or cin != wd))
+                cin = wd
+        add = self.add
+
+        def conv(cs):
+            if cs is self.stem:  # stored [k][g*ceil(r/g)][8 columns][8/g channels], logical [k][r][r][3]
+                add(cs.name + ".w", self.stem_layout.stored_shape(cs), (cs.cout, cs.r, cs.r, cs.cin_logical),
+                    cs.r * cs.r * cs.cin_logical)
+                return
+            add(cs.name + ".w", (cs.cout, cs.r, cs.r, cs.cin), (cs.cout, cs.r, cs.r, cs.cin_logical),
+                cs.r * cs.r * cs.cin_logical)
+
+        def bn(name, c):
+            add(name + ".g", (c,), (c,), None)
+            add(name + ".b", (c,), (c,), None)
+
+        conv(self.stem)
+        bn("bn1", widths[0])
+        for b in self.blocks:
+            conv(ConvSpec(b.pre + ".conv1", b.cin, b.cin, b.cout, 3, b.stride, 1))
+            bn(b.pre + ".bn1", b.cout)
+            conv(ConvSpec(b.pre + ".conv2", b.cout, b.cout, b.cout, 3, 1, 1))
+            bn(b.pre + ".bn2", b.cout)
+            if b.proj:
+                conv(ConvSpec(b.pre + ".down", b.cin, b.cin, b.cout, 1, b.stride, 0))
+                bn(b.pre + ".downbn", b.cout)
+        add("fc.w", (classes, cin), (classes, cin), cin)
+        add("fc.b", (classes,), (classes,), None)
 
 
 def conv_out(n, r, st, pad):
