@@ -215,9 +215,9 @@ __global__ void __launch_bounds__(128) scan_bwd_short_kernel(ScanArgs a)
 // ---------------------------------------------------------------------------- staging
 // A warp's consecutive steps of its channels, copied ahead into shared memory of the warp's own, so that no other
 // warp is waited for.  ALIGNED, where every row starts at a multiple of 16 bytes: one tensor copy (TMA) of a box of
-// channels and steps, clipped at the tensor's ends, and the outputs go back the same way.  Otherwise each lane copies
-// a row, from the 16-byte boundary at or before its first element to the one at or after its last; a row for which
-// that would leave the tensor is copied by elements.  The lanes' own copies of 4 and 2 bytes took twice the time.
+// channels and steps, clipped at the tensor's ends, and the outputs go back the same way.  Otherwise the lanes copy the
+// rows in chunks of 16 bytes (a bulk copy for each row, which a lane at a time issues, took 2750 cycles of a warp for
+// 24 rows where these take 1600; words put together from two lanes' halves cost more than two stores of 16 bits).
 __device__ __forceinline__ void tma_store_3d(const void* tmap, const void* src, int32_t c0, int32_t c1, int32_t c2)
 {
     asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%2, %3, %4}], [%1];" ::"l"(
@@ -225,44 +225,41 @@ __device__ __forceinline__ void tma_store_3d(const void* tmap, const void* src, 
                  "r"(smem_u32(src)), "r"(c0), "r"(c1), "r"(c2)
                  : "memory");
 }
+__device__ __forceinline__ void cp_async16(uint32_t dst, uintptr_t src)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_all;" ::: "memory"); }
+
 constexpr int kBlock = 8;  // steps worked on at once
 
 template <class T, bool ALIGNED, int LANES, int R>
 struct Stage {
     typedef typename Pair<T>::raw raw;
     static constexpr int SUBS = 32 / LANES, ROWS = R * SUBS;  // threads one after another in a warp, steps of a warp
-    static_assert(ROWS <= 32, "a lane per row");
     static constexpr int ROW_BYTES = 2 * LANES * (int)sizeof(T), E = 16 / (int)sizeof(T);
     static constexpr int PITCH = ROW_BYTES + (ALIGNED ? 0 : 16);
     static constexpr int BYTES = (ROWS * PITCH + 127) / 128 * 128;  // one tensor, one warp
 
-    // Not ALIGNED: this lane's row of a tensor [lo, hi) of which the warp copies n rows, row 0 at g (its first channel),
-    // ch channels from there to the row's end.  from = 0: by elements.
-    struct Row {
-        uintptr_t from;
-        uint32_t bytes;
-    };
-    static __device__ __forceinline__ Row row_of(const T* g, int64_t ld, int n, int ch, uintptr_t lo, uintptr_t hi)
+    // Not ALIGNED: rows [0, n) of the warp, row 0 at g (its first channel), ch channels from there to the row's end, of a
+    // tensor [lo, hi): in chunks of 16 bytes, a row from the boundary at or before its first element to the one at or
+    // after its last.  By elements where that would leave the tensor, or pass 32 bits.
+    static __device__ __forceinline__ void load(char* dst, const T* g, int64_t ld, int n, int ch, uintptr_t lo, uintptr_t hi)
     {
-        const int lane = threadIdx.x & 31;
-        Row r = {0, 0};
-        if (lane < n) {
-            const uintptr_t p = reinterpret_cast<uintptr_t>(g + lane * ld), from = p & ~(uintptr_t)15;
-            const uintptr_t to = (p + min(ch, 2 * LANES) * sizeof(T) + 15) & ~(uintptr_t)15;
-            if (from >= lo && to <= hi) r = {from, (uint32_t)(to - from)};
-        }
-        return r;
-    }
-    static __device__ __forceinline__ void load(char* dst, Row r, const T* g, int64_t ld, int n, int ch, uint64_t* bar)
-    {
-        const int lane = threadIdx.x & 31;
-        if (r.from) bulk_load(smem_u32(dst + lane * PITCH), r.from, r.bytes, bar);
-        unsigned left = __ballot_sync(0xffffffffu, lane < n && !r.from);
-        for (; left; left &= left - 1) {
-            const int k = __ffs(left) - 1;
-            const T* p = g + k * ld;
-            T* s = reinterpret_cast<T*>(dst + k * PITCH) + offset(p);
-            for (int i = lane; i < min(ch, 2 * LANES); i += 32) s[i] = p[i];
+        constexpr int CHUNKS = PITCH / 16, COPIES = (ROWS * CHUNKS + 31) / 32;
+        const int lane = threadIdx.x & 31, seg = min(ch, 2 * LANES) * (int)sizeof(T);
+        const uintptr_t p = reinterpret_cast<uintptr_t>(g), base = p & ~(uintptr_t)15;
+        if (base >= lo && ((reinterpret_cast<uintptr_t>(g + (n - 1) * ld) + seg + 15) & ~(uintptr_t)15) <= hi && ld < (1 << 24)) {
+            const int b = (int)(p & 15), pitch = (int)ld * (int)sizeof(T);
+            const uint32_t to = smem_u32(dst);
+#pragma unroll
+            for (int j = 0; j < COPIES; ++j) {
+                const int q = lane + 32 * j, row = q / CHUNKS, at = q % CHUNKS * 16, off = b + row * pitch;
+                if (row < n && at < (off & 15) + seg) cp_async16(to + row * PITCH + at, base + (uint32_t)((off & ~15) + at));
+            }
+        } else {
+            for (int r = 0; r < n; ++r, g += ld, dst += PITCH)
+                for (int i = lane; i < min(ch, 2 * LANES); i += 32) reinterpret_cast<T*>(dst)[offset(g) + i] = g[i];
         }
     }
 
@@ -430,13 +427,8 @@ __global__ void __launch_bounds__(kThreads, BLOCKS) scan_fwd_kernel(ScanArgs a, 
                 tma_load_3d(stage[ring][1], &maps.z, &full[ring], w.ch0, row + ahead * step, (int)w.b);
             }
         } else {
-            const T *px = x + ahead * hop, *pz = z + ahead * hop;
-            const auto rx = St::row_of(px, a.ld_x, n, ch, x_lo, x_lo + x_size), rz = St::row_of(pz, a.ld_x, n, ch, z_lo, z_lo + x_size);
-            const uint32_t bytes = __reduce_add_sync(0xffffffffu, rx.bytes + rz.bytes);
-            if ((threadIdx.x & 31) == 0) mbar_arrive_expect_tx(&full[ring], bytes);
-            __syncwarp();
-            St::load(stage[ring][0], rx, px, a.ld_x, n, ch, &full[ring]);
-            St::load(stage[ring][1], rz, pz, a.ld_x, n, ch, &full[ring]);
+            St::load(stage[ring][0], x + ahead * hop, a.ld_x, n, ch, x_lo, x_lo + x_size);
+            St::load(stage[ring][1], z + ahead * hop, a.ld_x, n, ch, z_lo, z_lo + x_size);
         }
     };
     links_init(sm.links, w.S);
@@ -458,9 +450,13 @@ __global__ void __launch_bounds__(kThreads, BLOCKS) scan_fwd_kernel(ScanArgs a, 
         const int live = max(0, min(w.len - row, St::ROWS));
         char *sx = stage[par][0], *sz = stage[par][1];
         if (live > 0) {
-            link_wait(&full[par], phase >> par & 1, &sm.links.abort);
-            phase ^= 1 << par;
-            if (!ALIGNED) __syncwarp();
+            if constexpr (ALIGNED) {
+                link_wait(&full[par], phase >> par & 1, &sm.links.abort);
+                phase ^= 1 << par;
+            } else {
+                cp_wait();
+                __syncwarp();
+            }
         }
         if (live < St::ROWS) {
             __syncwarp();
@@ -534,16 +530,13 @@ __global__ void __launch_bounds__(kThreads, BLOCKS) scan_fwd_kernel(ScanArgs a, 
                 tma_store_3d(&maps.h, sx, w.ch0, row, (int)w.b);
                 bulk_commit();
             }
-        } else if (w.one) {
+        } else {
             T* g = out + o0 * a.ld_h + 2 * lane;
 #pragma unroll
             for (int i = 0; i < R; ++i, g += a.ld_h) {
                 const float2 v = __ffma2_rn(p[i], in, h[i]);
-                if (o0 + i < rows) st_any(g, o0 + i < live ? v : make_float2(0.f, 0.f), w.two, a.pairs);
+                if (w.one && o0 + i < rows) st_any(g, o0 + i < live ? v : make_float2(0.f, 0.f), w.two, a.pairs);
             }
-        }
-        if (!ALIGNED) {
-            fence_async_shared();
             __syncwarp();
         }
         row += step;
@@ -610,15 +603,9 @@ __global__ void __launch_bounds__(kThreads, BLOCKS) scan_bwd_kernel(ScanArgs a, 
                 tma_load_3d(stage[ring][2], &maps.dh, &full[ring], w.ch0, (int)from, (int)w.b);
             }
         } else {
-            const T *px = x - back * hop, *pz = z - back * hop, *pd = dh - back * hop_h;
-            const auto rx = St::row_of(px, a.ld_x, n, ch, x_lo, x_lo + x_size), rz = St::row_of(pz, a.ld_x, n, ch, z_lo, z_lo + x_size),
-                       rd = St::row_of(pd, a.ld_h, n, ch, d_lo, d_lo + d_size);
-            const uint32_t bytes = __reduce_add_sync(0xffffffffu, rx.bytes + rz.bytes + rd.bytes);
-            if ((threadIdx.x & 31) == 0) mbar_arrive_expect_tx(&full[ring], bytes);
-            __syncwarp();
-            St::load(stage[ring][0], rx, px, a.ld_x, n, ch, &full[ring]);
-            St::load(stage[ring][1], rz, pz, a.ld_x, n, ch, &full[ring]);
-            St::load(stage[ring][2], rd, pd, a.ld_h, n, ch, &full[ring]);
+            St::load(stage[ring][0], x - back * hop, a.ld_x, n, ch, x_lo, x_lo + x_size);
+            St::load(stage[ring][1], z - back * hop, a.ld_x, n, ch, z_lo, z_lo + x_size);
+            St::load(stage[ring][2], dh - back * hop_h, a.ld_h, n, ch, d_lo, d_lo + d_size);
         }
     };
     const float* kept = a.states + (w.b * w.chunks + (row + o0) / kChunk) * a.c + w.ch;
@@ -641,9 +628,13 @@ __global__ void __launch_bounds__(kThreads, BLOCKS) scan_bwd_kernel(ScanArgs a, 
         const int live = (int)max((int64_t)0, min(w.len - row, (int64_t)St::ROWS));
         char *sx = stage[par][0], *sz = stage[par][1], *sd = stage[par][2];
         if (live > 0) {
-            link_wait(&full[par], phase >> par & 1, &sm.links.abort);
-            phase ^= 1 << par;
-            if (!ALIGNED) __syncwarp();
+            if constexpr (ALIGNED) {
+                link_wait(&full[par], phase >> par & 1, &sm.links.abort);
+                phase ^= 1 << par;
+            } else {
+                cp_wait();
+                __syncwarp();
+            }
         }
         if (live < St::ROWS) {
             __syncwarp();
@@ -742,10 +733,12 @@ __global__ void __launch_bounds__(kThreads, BLOCKS) scan_bwd_kernel(ScanArgs a, 
                 if constexpr (ALIGNED) {
                     St::put(rx + o, lane, vx);
                     St::put(rz + o, lane, vz);
-                } else if (w.one && o0 + n < rows) {
+                } else {
                     if (o0 + n >= live) vx = vz = make_float2(0.f, 0.f);
-                    st_any(gx + n * a.ld_x, vx, w.two, a.pairs);
-                    st_any(gz + n * a.ld_x, vz, w.two, a.pairs);
+                    if (w.one && o0 + n < rows) {
+                        st_any(gx + n * a.ld_x, vx, w.two, a.pairs);
+                        st_any(gz + n * a.ld_x, vz, w.two, a.pairs);
+                    }
                 }
             }
         }
@@ -763,7 +756,6 @@ __global__ void __launch_bounds__(kThreads, BLOCKS) scan_bwd_kernel(ScanArgs a, 
                 bulk_commit();
             }
         } else {
-            fence_async_shared();
             __syncwarp();
             x -= hop, z -= hop, dh -= hop_h, dx -= hop, dz -= hop;
         }
