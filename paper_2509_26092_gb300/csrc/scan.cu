@@ -322,8 +322,10 @@ __device__ __forceinline__ float2 step2(float4 pair, float2 h) { return __ffma2_
 
 // Exchange between the blocks of a cluster.  Stores to another block's shared memory that count themselves on that
 // block's mbarrier, so that nobody waits but for the data: a barrier of the cluster would also wait for the blocks'
-// stores to global memory.  Two of each by turns: a block sends part n+2 only when it has the others' part n+1, which
-// they send when they have read part n.
+// stores to global memory.  Each block sends its pair to those that come after it in the scan's direction, and the last
+// one sends the state for the next part to all, which they wait for before they send a pair.  Two places of each by
+// turns: who has the state of part n knows that the last block has every block's pair of part n-1, which a block sends
+// when it has read what it was sent of part n-2.
 __device__ int g_scan_status;
 
 struct Links {
@@ -388,7 +390,7 @@ __device__ __forceinline__ void links_init(Links& l, int S)
 template <class T, bool ALIGNED, int LANES, int R>
 struct FwdSmem {
     typedef Stage<T, ALIGNED, LANES, R> St;
-    char stage[kThreads / 32][2][2][St::BYTES];
+    typedef char Stages[2][2][St::BYTES];  // of a warp: two parts of x and gate; before this struct
     float4 agg[2][kThreads / LANES][LANES];
     float2 carry[2][LANES];
     Links links;
@@ -401,7 +403,8 @@ __global__ void __launch_bounds__(kThreads, BLOCKS) scan_fwd_kernel(ScanArgs a, 
     typedef FwdSmem<T, ALIGNED, LANES, R> Smem;
     typedef typename Smem::St St;
     extern __shared__ __align__(128) char smem_raw[];
-    Smem& sm = *reinterpret_cast<Smem*>(smem_raw);
+    typename Smem::Stages* const stages = reinterpret_cast<typename Smem::Stages*>(smem_raw);
+    Smem& sm = *reinterpret_cast<Smem*>(stages + blockDim.x / 32);
     Place w;
     w.set<LANES>(a);
     const int tile = w.subs * R, step = tile * w.S, lane = w.lane, ch = a.c - w.ch0;
@@ -411,7 +414,7 @@ __global__ void __launch_bounds__(kThreads, BLOCKS) scan_fwd_kernel(ScanArgs a, 
     const T* z = static_cast<const T*>(a.gate) + row0 * a.ld_x + w.ch0;
     T* out = static_cast<T*>(a.h) + row0 * a.ld_h + w.ch0;
     const int64_t hop = step * a.ld_x, hop_h = step * a.ld_h;
-    char(*stage)[2][St::BYTES] = sm.stage[w.warp];
+    char(*stage)[2][St::BYTES] = stages[w.warp];
     uint64_t* full = sm.links.full[w.warp];
     const int mx = (int)(a.ld_x % St::E), o0 = w.wsub * R;
     const uintptr_t x_lo = reinterpret_cast<uintptr_t>(a.x), z_lo = reinterpret_cast<uintptr_t>(a.gate);
@@ -444,7 +447,7 @@ __global__ void __launch_bounds__(kThreads, BLOCKS) scan_fwd_kernel(ScanArgs a, 
     int par = 0, turn = 0, phase = 0;
     for (int at = 0; at < a.t; at += step, turn += par, par ^= 1) {
         if (w.S > 1 && threadIdx.x == 0) {
-            mbar_arrive_expect_tx(&sm.links.pairs[par], w.S * LANES * sizeof(float4));
+            mbar_arrive_expect_tx(&sm.links.pairs[par], w.rank * LANES * sizeof(float4));
             if (a.t - at > step) mbar_arrive_expect_tx(&sm.links.carry[par ^ 1], LANES * sizeof(float2));
         }
         const int live = max(0, min(w.len - row, St::ROWS));
@@ -480,26 +483,27 @@ __global__ void __launch_bounds__(kThreads, BLOCKS) scan_fwd_kernel(ScanArgs a, 
         __syncthreads();
         float2 in;
         if (w.S > 1) {
-            if (last) {  // the block's pair, to every block of the cluster
-#pragma unroll 4
-                for (int k = w.subs - 2; k >= 0; --k) {
+            if (at > 0) link_wait(&sm.links.carry[par], par ? turn & 1 : (turn & 1) ^ 1, &sm.links.abort);
+            if (w.rank + 1 + w.sub < w.S) {  // the block's pair, to the blocks after it
+                float2 ph = make_float2(0.f, 0.f), pb = make_float2(1.f, 1.f);
+#pragma unroll 8
+                for (int k = 0; k < w.subs; ++k) {
                     const float4 v = sm.agg[par][k][lane];
-                    hh = __ffma2_rn(pp, make_float2(v.z, v.w), hh);
-                    pp = __fmul2_rn(pp, make_float2(v.x, v.y));
+                    ph = step2(v, ph);
+                    pb = __fmul2_rn(pb, make_float2(v.x, v.y));
                 }
                 const uint32_t to = smem_u32(&sm.slot[(par * w.S + w.rank) * LANES + lane]), bar = smem_u32(&sm.links.pairs[par]);
-#pragma unroll 4
-                for (int k = 0; k < w.S; ++k) st_async4(mapa_shared(to, k), mapa_shared(bar, k), make_float4(pp.x, pp.y, hh.x, hh.y));
+                for (int k = w.rank + 1 + w.sub; k < w.S; k += w.subs)
+                    st_async4(mapa_shared(to, k), mapa_shared(bar, k), make_float4(pb.x, pb.y, ph.x, ph.y));
             }
-            if (at > 0) link_wait(&sm.links.carry[par], par ? turn & 1 : (turn & 1) ^ 1, &sm.links.abort);
             link_wait(&sm.links.pairs[par], turn & 1, &sm.links.abort);
             in = sm.carry[par][lane];
-#pragma unroll 4
+#pragma unroll 8
             for (int k = 0; k < w.rank; ++k) in = step2(sm.slot[(par * w.S + k) * LANES + lane], in);
         } else {
             in = sm.carry[par][lane];
         }
-#pragma unroll 4
+#pragma unroll 8
         for (int k = 0; k < w.sub; ++k) in = step2(sm.agg[par][k][lane], in);
         if (last) {
             end = __ffma2_rn(p[R - 1], in, h[R - 1]);
@@ -556,7 +560,7 @@ __global__ void __launch_bounds__(kThreads, BLOCKS) scan_fwd_kernel(ScanArgs a, 
 template <class T, bool ALIGNED, int LANES, int R>
 struct BwdSmem {
     typedef Stage<T, ALIGNED, LANES, R> St;
-    char stage[kThreads / 32][2][3][St::BYTES];
+    typedef char Stages[2][3][St::BYTES];  // of a warp: two parts of x, gate and dh; before this struct
     float4 agg[2][kThreads / LANES][LANES];
     float2 aggq[2][kThreads / LANES][LANES];
     float2 carry[2][LANES];
@@ -571,7 +575,8 @@ __global__ void __launch_bounds__(kThreads, BLOCKS) scan_bwd_kernel(ScanArgs a, 
     typedef typename Smem::St St;
     constexpr int SHARE = kChunk / R, NB = R / kBlock;
     extern __shared__ __align__(128) char smem_raw[];
-    Smem& sm = *reinterpret_cast<Smem*>(smem_raw);
+    typename Smem::Stages* const stages = reinterpret_cast<typename Smem::Stages*>(smem_raw);
+    Smem& sm = *reinterpret_cast<Smem*>(stages + blockDim.x / 32);
     Place w;
     w.set<LANES>(a);
     const int tile = w.subs * R, step = tile * w.S, lane = w.lane, ch = a.c - w.ch0;
@@ -584,7 +589,7 @@ __global__ void __launch_bounds__(kThreads, BLOCKS) scan_bwd_kernel(ScanArgs a, 
     T* dx = static_cast<T*>(a.h) + row0 * a.ld_x + w.ch0;
     T* dz = static_cast<T*>(a.dgate) + row0 * a.ld_x + w.ch0;
     const int64_t hop = step * a.ld_x, hop_h = step * a.ld_h;
-    char(*stage)[3][St::BYTES] = sm.stage[w.warp];
+    char(*stage)[3][St::BYTES] = stages[w.warp];
     uint64_t* full = sm.links.full[w.warp];
     const int mx = (int)(a.ld_x % St::E), mh = (int)(a.ld_h % St::E), o0 = w.wsub * R;
     const uintptr_t x_lo = reinterpret_cast<uintptr_t>(a.x), z_lo = reinterpret_cast<uintptr_t>(a.gate);
@@ -622,7 +627,7 @@ __global__ void __launch_bounds__(kThreads, BLOCKS) scan_bwd_kernel(ScanArgs a, 
     int par = 0, turn = 0, phase = 0;
     for (int at = top; at >= 0; at -= step, turn += par, par ^= 1) {
         if (w.S > 1 && threadIdx.x == 0) {
-            mbar_arrive_expect_tx(&sm.links.pairs[par], w.S * LANES * sizeof(float4));
+            mbar_arrive_expect_tx(&sm.links.pairs[par], (w.S - 1 - w.rank) * LANES * sizeof(float4));
             if (at > 0) mbar_arrive_expect_tx(&sm.links.carry[par ^ 1], LANES * sizeof(float2));
         }
         const int live = (int)max((int64_t)0, min(w.len - row, (int64_t)St::ROWS));
@@ -671,27 +676,27 @@ __global__ void __launch_bounds__(kThreads, BLOCKS) scan_bwd_kernel(ScanArgs a, 
         __syncthreads();
         float2 q;
         if (w.S > 1) {
-            if (last) {
-                float2 qb = qq, pb = pp;
-#pragma unroll 4
-                for (int k = 1; k < w.subs; ++k) {
+            if (at < top) link_wait(&sm.links.carry[par], par ? turn & 1 : (turn & 1) ^ 1, &sm.links.abort);
+            if (w.sub < w.rank) {  // the block's pair, to the blocks before it
+                float2 qb = make_float2(0.f, 0.f), pb = make_float2(1.f, 1.f);
+#pragma unroll 8
+                for (int k = w.subs - 1; k >= 0; --k) {
                     const float4 u = sm.agg[par][k][lane];
-                    qb = __ffma2_rn(pb, sm.aggq[par][k][lane], qb);
+                    qb = __ffma2_rn(make_float2(u.x, u.y), qb, sm.aggq[par][k][lane]);
                     pb = __fmul2_rn(pb, make_float2(u.x, u.y));
                 }
                 const uint32_t to = smem_u32(&sm.slot[(par * w.S + w.rank) * LANES + lane]), bar = smem_u32(&sm.links.pairs[par]);
-#pragma unroll 4
-                for (int k = 0; k < w.S; ++k) st_async4(mapa_shared(to, k), mapa_shared(bar, k), make_float4(pb.x, pb.y, qb.x, qb.y));
+                for (int k = w.sub; k < w.rank; k += w.subs)
+                    st_async4(mapa_shared(to, k), mapa_shared(bar, k), make_float4(pb.x, pb.y, qb.x, qb.y));
             }
-            if (at < top) link_wait(&sm.links.carry[par], par ? turn & 1 : (turn & 1) ^ 1, &sm.links.abort);
             link_wait(&sm.links.pairs[par], turn & 1, &sm.links.abort);
             q = sm.carry[par][lane];
-#pragma unroll 4
+#pragma unroll 8
             for (int k = w.S - 1; k > w.rank; --k) q = step2(sm.slot[(par * w.S + k) * LANES + lane], q);
         } else {
             q = sm.carry[par][lane];
         }
-#pragma unroll 4
+#pragma unroll 8
         for (int k = w.subs - 1; k > w.sub; --k) {
             const float4 u = sm.agg[par][k][lane];
             q = __ffma2_rn(make_float2(u.x, u.y), q, sm.aggq[par][k][lane]);
@@ -827,18 +832,23 @@ int launch_tiles(ScanArgs a, cudaStream_t st, const char* what)
 {
     constexpr auto kernel = kernel_of<T, ALIGNED, LANES, R, BLOCKS, BWD>();
     typedef Stage<T, ALIGNED, LANES, R> St;
-    const size_t fixed = BWD ? sizeof(BwdSmem<T, ALIGNED, LANES, R>) : sizeof(FwdSmem<T, ALIGNED, LANES, R>);
-    auto smem_of = [&](int S) { return fixed + (S > 1 ? sizeof(float4) * 2 * S * LANES : 0); };
+    typedef FwdSmem<T, ALIGNED, LANES, R> Fwd;
+    typedef BwdSmem<T, ALIGNED, LANES, R> Bwd;
+    auto smem_of = [&](int S, int warps) {
+        return (BWD ? sizeof(Bwd) + warps * sizeof(typename Bwd::Stages) : sizeof(Fwd) + warps * sizeof(typename Fwd::Stages)) +
+               (S > 1 ? sizeof(float4) * 2 * S * LANES : 0);
+    };
     a.groups = (a.c + 2 * LANES - 1) / (2 * LANES);
     const int64_t cols = (int64_t)a.n * a.groups;
-    const int unit = std::max(kChunk / R, 32 / LANES);  // threads of whole chunks, whole warps
+    // parts of whole chunks, where there are several; whole warps
     int subs = std::min(kThreads / LANES, (a.t + R - 1) / R);
+    const int unit = subs * R < a.t ? std::max(kChunk / R, 32 / LANES) : 32 / LANES;
     subs = (subs + unit - 1) / unit * unit;
     // As many blocks to a cluster as leave all of them resident, two on an SM: with fewer the SMs idle, with more the
     // clusters take turns (backward, 8 x 8192 x 1024: 1, 2 and 4 blocks 147, 132 and 136 us; forward, 4 x 8192 x 1024:
     // 2, 4 and 8 blocks 64, 48 and 54 us; 185 x 196 x 256: 1 and 2 blocks 24 and 30 us).
     int S = (int)std::max<int64_t>(1, std::min<int64_t>({kMaxCluster, 2 * sm_count() / cols, (a.t + subs * R - 1) / (subs * R)}));
-    while (S > 1 && !cluster_held<kernel>(S, kThreads, smem_of(kMaxCluster))) --S;
+    while (S > 1 && !cluster_held<kernel>(S, kThreads, smem_of(kMaxCluster, kThreads / 32))) --S;
     if (cols * S > 0x7fffffff) return set_error(DBL_ERR_UNSUPPORTED, "%s: more than 2^31 blocks", what);
     Maps maps;
     int rc = DBL_OK;
@@ -850,7 +860,7 @@ int launch_tiles(ScanArgs a, cudaStream_t st, const char* what)
         if (BWD && rc == DBL_OK) rc = encode<T>(&maps.dz, a.dgate, a, a.ld_x, 2 * LANES, St::ROWS, what);
         if (rc != DBL_OK) return rc;
     }
-    if ((rc = allow_launch<kernel>(smem_of(kMaxCluster), true, what)) != DBL_OK) return rc;
+    if ((rc = allow_launch<kernel>(smem_of(kMaxCluster, kThreads / 32), true, what)) != DBL_OK) return rc;
     cudaLaunchConfig_t cfg = {};
     cudaLaunchAttribute at[1];
     at[0].id = cudaLaunchAttributeClusterDimension;
@@ -858,7 +868,7 @@ int launch_tiles(ScanArgs a, cudaStream_t st, const char* what)
     at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
     cfg.gridDim = dim3((unsigned)(cols * S));
     cfg.blockDim = dim3(subs * LANES);
-    cfg.dynamicSmemBytes = smem_of(S);
+    cfg.dynamicSmemBytes = smem_of(S, subs * LANES / 32);
     cfg.stream = st;
     cfg.attrs = at;
     cfg.numAttrs = 1;
