@@ -63,6 +63,39 @@ struct Cols {
             f[0] = make_float2(i < c ? elem_f(p[0]) : 0.f, i + mate(G) < c ? elem_f(p[mate(G)]) : 0.f);
         }
     }
+    // all accesses; 16-bit pairs in one where the row begins at a word
+    static __device__ __forceinline__ void read_all(float2* f, const char* row, int off, int c, int g, int G)
+    {
+        if (!VEC && sizeof(T) == 2 && off % 2 == 0) {
+#pragma unroll
+            for (int j = 0; j < J; ++j) {
+                const int i = col(j, g, G);
+                uint32_t v = 0;
+                if (i < c) v = reinterpret_cast<const uint32_t*>(row)[(off + i) / 2];
+                f[j] = act::unpack2_u32(v);
+                if (i + 1 >= c) f[j].y = 0.f;  // another row's
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < J; ++j) read(f + j * P, row, off, c, g, G, j);
+        }
+    }
+    static __device__ __forceinline__ void write_all(T* row, const float2* f, int c, int g, int G)
+    {
+        if (!VEC && sizeof(T) == 2 && (reinterpret_cast<uintptr_t>(row) & 3) == 0) {
+#pragma unroll
+            for (int j = 0; j < J; ++j) {
+                const int i = col(j, g, G);
+                if (i + 1 < c)
+                    *reinterpret_cast<uint32_t*>(row + i) = act::pack2_u32(f[j].x, f[j].y);
+                else if (i < c)
+                    row[i] = elem_from<T>(f[j].x);
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < J; ++j) write(row, f + j * P, c, g, G, j);
+        }
+    }
     static __device__ __forceinline__ void write(T* row, const float2* f, int c, int g, int G, int j)
     {
         const int i = col(j, g, G);
@@ -250,21 +283,14 @@ __global__ void __launch_bounds__(THREADS, BLOCKS) ln_fwd_kernel(LnArgs a)
         float2 v[N / 2], s = both(0.f);
         w.wait(from, k, r);
         const int off = w.offset(from[0], r), off_r = w.offset(from[1], r);
-#pragma unroll
-        for (int j = 0; j < C::J; ++j) C::read(v + j * P, w.row(k, 0), off, a.c, g, G, j);
+        C::read_all(v, w.row(k, 0), off, a.c, g, G);
         if (a.res) {
+            float2 u[N / 2];
+            C::read_all(u, w.row(k, 1), off_r, a.c, g, G);
 #pragma unroll
-            for (int j = 0; j < C::J; ++j) {
-                float2 u[P];
-                C::read(u, w.row(k, 1), off_r, a.c, g, G, j);
-#pragma unroll
-                for (int i = 0; i < P; ++i) v[j * P + i] = __fadd2_rn(v[j * P + i], u[i]);
-            }
+            for (int i = 0; i < N / 2; ++i) v[i] = __fadd2_rn(v[i], u[i]);
         }
-        if (a.sum) {
-#pragma unroll
-            for (int j = 0; j < C::J; ++j) C::write(static_cast<T*>(a.sum) + r * a.ld_out, v + j * P, a.c, g, G, j);
-        }
+        if (a.sum) C::write_all(static_cast<T*>(a.sum) + r * a.ld_out, v, a.c, g, G);
 #pragma unroll
         for (int i = 0; i < N / 2; ++i) s = __fadd2_rn(s, v[i]);
         const float mean = w.total(s.x + s.y, 0) * inv_c;
@@ -296,8 +322,8 @@ __global__ void __launch_bounds__(THREADS, BLOCKS) ln_fwd_kernel(LnArgs a)
 #pragma unroll
             for (int i = 0; i < P; ++i)
                 f[i] = __ffma2_rn(__fmul2_rn(f[i], both(inv)), ga[(KEEP ? j * P : 0) + i], be[(KEEP ? j * P : 0) + i]);
-            C::write(static_cast<T*>(a.y) + r * a.ld_out, f, a.c, g, G, j);
         }
+        C::write_all(static_cast<T*>(a.y) + r * a.ld_out, v, a.c, g, G);
         if (g == 0 && a.mean) {
             a.mean[r] = mean;
             a.invstd[r] = inv;
@@ -335,24 +361,24 @@ __global__ void __launch_bounds__(THREADS, BLOCKS) ln_bwd_kernel(LnArgs a)
     bool first = true;
     int par = 0;
     for (int k = 0; r < a.rows; r += hop, k = k + 1 == w.depth ? 0 : k + 1, par ^= 1) {
-        float2 h[N / 2], d[N / 2], tx = both(0.f), ty = tx;
+        float2 h[N / 2], d[N / 2], ga[N / 2], tx = both(0.f), ty = tx;
+#pragma unroll
+        for (int j = 0; j < C::J; ++j) C::param(ga + j * P, a.gamma, 1.f, a.c, g, G, j);  // back before the row is
         w.wait(from, k, r);
         const int off_x = w.offset(from[0], r), off_d = w.offset(from[1], r);
         const float is = inv, mu = mean;
         if (r + hop < a.rows) mean = a.mean[r + hop], inv = a.invstd[r + hop];
 #pragma unroll
         for (int j = 0; j < C::J; ++j) {
-            float2 ga[P];
             C::read(h + j * P, w.row(k, 0), off_x, a.c, g, G, j);
             C::read(d + j * P, w.row(k, 1), off_d, a.c, g, G, j);
-            C::param(ga, a.gamma, 1.f, a.c, g, G, j);
 #pragma unroll
             for (int q = 0; q < P; ++q) {  // past the row's end d is 0
                 const int i = j * P + q;
                 h[i] = __fmul2_rn(__fadd2_rn(h[i], both(-mu)), both(is));
                 dg[i] = __ffma2_rn(d[i], h[i], dg[i]);
                 db[i] = __fadd2_rn(db[i], d[i]);
-                d[i] = __fmul2_rn(d[i], ga[q]);
+                d[i] = __fmul2_rn(d[i], ga[i]);
                 tx = __fadd2_rn(tx, d[i]);
                 ty = __ffma2_rn(d[i], h[i], ty);
             }
@@ -583,8 +609,8 @@ int run_fwd(LnArgs a, cudaStream_t st)
 {
     const char* what = "layer_norm_fwd";
     if (held(a, 2, sizeof(T))) {
-        if (a.c <= 256) return run_fwd_held<T, VEC, 8, kBlock, 4>(a, st, what);
-        if (a.c <= 16 * kBlock) return run_fwd_held<T, VEC, 16, kBlock, 3>(a, st, what);
+        if (a.c <= 256) return run_fwd_held<T, VEC, 8, kBlock, VEC ? 4 : 3>(a, st, what);
+        if (a.c <= 16 * kBlock) return run_fwd_held<T, VEC, 16, kBlock, VEC ? 3 : 2>(a, st, what);
         if (a.c <= 16 * kMaxGroup) return run_fwd_held<T, VEC, 16, kMaxGroup, 1>(a, st, what);
         return run_fwd_held<T, VEC, 32, kMaxGroup, 1>(a, st, what);
     }
