@@ -113,6 +113,28 @@ __device__ __forceinline__ void bounded_wait(uint64_t* bar, uint32_t parity, vol
     atomicExch(status, DBL_ERR_TIMEOUT);
 }
 
+// Stores to the shared memory of a block of the cluster, counted on a barrier of that block's.
+__device__ __forceinline__ void st_async4(uint32_t addr, uint32_t bar, float4 v)
+{
+    asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v4.b32 [%0], {%2, %3, %4, %5}, [%1];" ::"r"(addr),
+                 "r"(bar), "r"(__float_as_uint(v.x)), "r"(__float_as_uint(v.y)), "r"(__float_as_uint(v.z)),
+                 "r"(__float_as_uint(v.w))
+                 : "memory");
+}
+
+__device__ __forceinline__ void st_async2(uint32_t addr, uint32_t bar, float2 v)
+{
+    asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v2.b32 [%0], {%2, %3}, [%1];" ::"r"(addr), "r"(bar),
+                 "r"(__float_as_uint(v.x)), "r"(__float_as_uint(v.y))
+                 : "memory");
+}
+
+// A block stays until the others no longer write to its shared memory (also where one has given up).
+__device__ __forceinline__ void cluster_leave()
+{
+    asm volatile("barrier.cluster.arrive.relaxed.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory");
+}
+
 // Before a block's end: one that gave up leaves the copies that it started some time to land.
 __device__ __forceinline__ void linger(volatile int* abort)
 {

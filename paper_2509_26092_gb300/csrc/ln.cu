@@ -19,6 +19,7 @@ using namespace dbl::dev;
 
 constexpr int kMaxGroup = 512;     // threads of a row
 constexpr int kBlock = 256;        // threads of a block of several groups
+constexpr int kMaxSplit = 8;       // blocks of a row in the backward pass
 constexpr int kMaxDepth = 4;       // rows of a group on their way
 constexpr int kWide = 256;         // threads of the kernels for rows wider than a group
 constexpr int kSumThreads = 1024;
@@ -36,6 +37,7 @@ struct LnArgs {
     int c;
     float eps;
     int group, depth, slot;  // threads of a row, rows on their way, bytes of one in shared memory
+    int part;                // columns of a block, where a cluster takes a row
 };
 
 // This thread's columns of a row, in pairs: J accesses of 16 bytes where rows allow it (VEC; FULL: every thread has all
@@ -332,20 +334,60 @@ __global__ void __launch_bounds__(THREADS, BLOCKS) ln_fwd_kernel(LnArgs a)
     linger(w.abort);
 }
 
+// What the blocks of a cluster, each with its columns of a row, tell one another of it: a pair of sums, stored into every
+// block's slot of the sender, by turns in two places.  Who has all pairs of row n+1 knows that all blocks have read
+// those of row n: a block sends after its threads have met, and they have read by then.
+struct Exchange {
+    uint64_t bar[2];
+    float2 slot[2][kMaxSplit];
+
+    __device__ __forceinline__ void init()
+    {
+        if (threadIdx.x == 0) {
+            mbar_init(&bar[0], 1);
+            mbar_init(&bar[1], 1);
+            fence_mbar_init();
+        }
+        cluster_sync_all();
+    }
+    // v: the block's, the same in all its threads; returns the cluster's, the same bits in all its blocks
+    __device__ __forceinline__ float2 total(float2 v, int which, uint32_t parity, int S, int rank, int* abort)
+    {
+        if (threadIdx.x == 0) mbar_arrive_expect_tx(&bar[which], S * sizeof(float2));
+        if ((int)threadIdx.x < S)
+            st_async2(mapa_shared(smem_u32(&slot[which][rank]), threadIdx.x), mapa_shared(smem_u32(&bar[which]), threadIdx.x), v);
+        bounded_wait(&bar[which], parity, abort, &g_ln_status);
+        float2 t = slot[which][0];
+        for (int k = 1; k < S; ++k) t = __fadd2_rn(t, slot[which][k]);
+        return t;
+    }
+};
+
 // x: the normalised tensor, res: dskip, y: dx.  A thread also adds up dy*xhat and dy of its columns over the rows
 // that its group takes; a block leaves these sums in parts[block][2][c].
-template <class T, bool VEC, bool FULL, int N, int THREADS, int BLOCKS>
+template <class T, bool VEC, bool FULL, int N, int THREADS, int BLOCKS, bool SPLIT>
 __global__ void __launch_bounds__(THREADS, BLOCKS) ln_bwd_kernel(LnArgs a)
 {
     typedef Cols<T, VEC, FULL, N> C;
     constexpr int P = C::P;
     extern __shared__ __align__(128) char smem[];
+    __shared__ Exchange ex;
+    const int c = a.c, S = SPLIT ? (a.c + a.part - 1) / a.part : 1, rank = SPLIT ? (int)cluster_ctarank() : 0;
+    if (SPLIT) {  // of every row this block's columns
+        const int skip = rank * a.part;
+        a.c = min(a.part, c - skip);
+        a.x = static_cast<const T*>(a.x) + skip, a.dy = static_cast<const T*>(a.dy) + skip, a.y = static_cast<T*>(a.y) + skip;
+        if (a.res) a.res = static_cast<const T*>(a.res) + skip;
+        if (a.gamma) a.gamma += skip;
+        if (a.parts) a.parts += skip;
+        ex.init();
+    }
     Groups<T, VEC, 3> w;
     w.set(a, smem);
     const T* const from[3] = {static_cast<const T*>(a.x), static_cast<const T*>(a.dy), static_cast<const T*>(a.res)};
     const int g = w.g, G = w.G;
-    const int64_t hop = (int64_t)gridDim.x * w.n;
-    int64_t r = (int64_t)blockIdx.x * w.n + w.id;
+    const int64_t team = blockIdx.x / S, hop = (int64_t)gridDim.x / S * w.n;
+    int64_t r = team * w.n + w.id;
     float mean = 0.f, inv = 0.f;
     if (r < a.rows) {
         if (g == 0)
@@ -357,10 +399,11 @@ __global__ void __launch_bounds__(THREADS, BLOCKS) ln_bwd_kernel(LnArgs a)
     float2 dg[N / 2], db[N / 2];
 #pragma unroll
     for (int i = 0; i < N / 2; ++i) dg[i] = db[i] = both(0.f);
-    const float inv_c = 1.f / a.c;
+    const float inv_c = 1.f / c;
     bool first = true;
     int par = 0;
-    for (int k = 0; r < a.rows; r += hop, k = k + 1 == w.depth ? 0 : k + 1, par ^= 1) {
+    uint32_t turn = 0;  // of the exchange's two places
+    for (int k = 0; r < a.rows; r += hop, k = k + 1 == w.depth ? 0 : k + 1, turn ^= par, par ^= 1) {
         float2 h[N / 2], d[N / 2], ga[N / 2], tx = both(0.f), ty = tx;
 #pragma unroll
         for (int j = 0; j < C::J; ++j) C::param(ga + j * P, a.gamma, 1.f, a.c, g, G, j);  // back before the row is
@@ -383,7 +426,8 @@ __global__ void __launch_bounds__(THREADS, BLOCKS) ln_bwd_kernel(LnArgs a)
                 ty = __ffma2_rn(d[i], h[i], ty);
             }
         }
-        const float2 t = w.total(make_float2(tx.x + tx.y, ty.x + ty.y), par);
+        float2 t = w.total(make_float2(tx.x + tx.y, ty.x + ty.y), par);
+        if (SPLIT) t = ex.total(t, par, turn, S, rank, w.abort);
         if (w.warps == 1) __syncwarp();
         // the row before this one has been read by all of the group: its place is free
         if (g == 0 && !first && r + (w.depth - 1) * hop < a.rows) w.fetch(from, (k ? k : w.depth) - 1, r + (w.depth - 1) * hop);
@@ -404,9 +448,10 @@ __global__ void __launch_bounds__(THREADS, BLOCKS) ln_bwd_kernel(LnArgs a)
         }
     }
     linger(w.abort);
+    if (SPLIT) cluster_leave();
     if (!a.parts) return;
     // groups of one block: through shared memory, all rows being done
-    float* out = a.parts + (int64_t)blockIdx.x * 2 * a.c;
+    float* out = a.parts + team * 2 * c;
     float* sums = reinterpret_cast<float*>(w.ring - (size_t)w.id * w.depth * 3 * w.slot);
     if (w.n > 1) {
         __syncthreads();
@@ -417,8 +462,8 @@ __global__ void __launch_bounds__(THREADS, BLOCKS) ln_bwd_kernel(LnArgs a)
 #pragma unroll
         for (int q = 0; q < P; ++q) {
             const int i = C::col(j, g, G) + 2 * q, m = i + C::mate(G);
-            if (i < a.c) out[i] = dg[j * P + q].x, out[a.c + i] = db[j * P + q].x;
-            if (m < a.c) out[m] = dg[j * P + q].y, out[a.c + m] = db[j * P + q].y;
+            if (i < a.c) out[i] = dg[j * P + q].x, out[c + i] = db[j * P + q].x;
+            if (m < a.c) out[m] = dg[j * P + q].y, out[c + m] = db[j * P + q].y;
         }
     if (w.n == 1) return;
     __syncthreads();
@@ -551,40 +596,46 @@ bool vec_of(const LnArgs& a, size_t e)
            aligned16(a.dy) && aligned16(a.sum) && aligned16(a.y) && aligned16(a.gamma) && aligned16(a.beta);
 }
 
-// Groups, blocks and shared memory for n columns a thread and `tensors` rows to read, `resident` threads on an SM.
+// Groups, blocks and shared memory for c columns of a row, n to a thread, `tensors` rows to read, `resident` threads on
+// an SM and `split` blocks of them to a row.
 struct Plan {
-    int threads, blocks;
+    int threads, teams;  // of a block; blocks, or clusters of them
     size_t smem;
+    int split;           // blocks of a cluster
 };
-Plan plan_of(LnArgs& a, int n, int tensors, int resident, size_t least, size_t e)
+Plan plan_of(LnArgs& a, int n, int c, int tensors, int resident, int split, size_t e)
 {
     Plan p;
-    a.group = ((a.c + n - 1) / n + 31) / 32 * 32;
+    a.group = ((c + n - 1) / n + 31) / 32 * 32;
     const int groups = std::max(1, kBlock / a.group);
     p.threads = a.group * groups;
+    p.split = split;
     const int on_sm = std::max(1, resident / p.threads);
-    a.slot = (int)((a.c * e + 16 + 127) / 128 * 128);
-    a.depth = (int)std::min<size_t>(kMaxDepth, std::max<size_t>(least, kRingBytes / on_sm / ((size_t)groups * tensors * a.slot)));
+    a.slot = (int)((c * e + 16 + 127) / 128 * 128);
+    a.depth = (int)std::min<size_t>(kMaxDepth, std::max<size_t>(2, kRingBytes / on_sm / ((size_t)groups * tensors * a.slot)));
     p.smem = (Groups<float, true, 1>::head(p.threads / 32) + 127) / 128 * 128 +
-             std::max((size_t)groups * a.depth * tensors * a.slot, groups > 1 ? (size_t)groups * 2 * a.c * sizeof(float) : 0);
-    p.blocks = (int)std::max<int64_t>(1, std::min<int64_t>((a.rows + groups - 1) / groups, (int64_t)on_sm * sm_count()));
+             std::max((size_t)groups * a.depth * tensors * a.slot, groups > 1 ? (size_t)groups * 2 * c * sizeof(float) : 0);
+    p.teams = (int)std::max<int64_t>(1, std::min<int64_t>((a.rows + groups - 1) / groups, (int64_t)on_sm * sm_count() / split));
     return p;
 }
 
-// Whether rows of this width are held by a group, in two places of a ring at least.
-bool held(const LnArgs& a, int tensors, size_t e)
-{
-    return a.c <= 32 * kMaxGroup && 2 * tensors * (a.c * e + 144) <= kRingBytes;
-}
+// Whether rows of this width are held by a group of the forward pass, in two places of a ring at least.
+bool fwd_held(const LnArgs& a, size_t e) { return a.c <= 32 * kMaxGroup && 4 * (a.c * e + 144) <= kRingBytes; }
 
-// The backward pass's blocks, each of which leaves a row of partial column sums.  By the sizes alone, as the
+// The backward pass: rows of up to 16 columns for each of a group's threads, wider ones by clusters of such blocks.
+bool bwd_held(const LnArgs& a) { return a.c <= 16 * kMaxGroup * kMaxSplit; }
+
+// The backward pass's blocks or clusters, each of which leaves a row of partial column sums.  By the sizes alone, as the
 // workspace is.
 Plan bwd_plan(LnArgs& a, size_t e)
 {
-    if (!held(a, 3, e)) return {kWide, (int)std::max<int64_t>(1, std::min<int64_t>((a.rows + 15) / 16, 64)), 0};
-    if (a.c <= 256) return plan_of(a, 8, 3, 3 * kBlock, 2, e);
-    if (a.c <= 16 * kBlock) return plan_of(a, 16, 3, 2 * kBlock, 2, e);
-    return plan_of(a, a.c <= 16 * kMaxGroup ? 16 : 32, 3, kMaxGroup, 2, e);
+    a.part = a.c;
+    if (!bwd_held(a)) return {kWide, (int)std::max<int64_t>(1, std::min<int64_t>((a.rows + 15) / 16, 64)), 0, 1};
+    if (a.c <= 256) return plan_of(a, 8, a.c, 3, 3 * kBlock, 1, e);
+    if (a.c <= 16 * kBlock) return plan_of(a, 16, a.c, 3, 2 * kBlock, 1, e);
+    const int S = (a.c + 16 * kMaxGroup - 1) / (16 * kMaxGroup);
+    a.part = ((a.c + S - 1) / S + 15) / 16 * 16;  // whole 16-byte units; the last block's may be fewer
+    return plan_of(a, 16, std::min(a.part, a.c), 3, kMaxGroup, S, e);
 }
 
 template <auto KERNEL>
@@ -592,14 +643,26 @@ int launch(const LnArgs& a, const Plan& p, cudaStream_t st, const char* what)
 {
     const int rc = allow_launch<KERNEL>(kRingBytes + 16 * 1024, false, what);
     if (rc != DBL_OK) return rc;
-    KERNEL<<<p.blocks, p.threads, p.smem, st>>>(a);
-    return launch_check(what);
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = p.split;
+    at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+    cfg.gridDim = dim3((unsigned)(p.teams * p.split));
+    cfg.blockDim = dim3(p.threads);
+    cfg.dynamicSmemBytes = p.smem;
+    cfg.stream = st;
+    cfg.attrs = at;
+    cfg.numAttrs = p.split > 1;
+    const cudaError_t err = cudaLaunchKernelEx(&cfg, KERNEL, a);
+    const int ran = launch_check(what);
+    return err == cudaSuccess ? ran : cuda_check(err, what);
 }
 
 template <class T, bool VEC, int N, int THREADS, int BLOCKS>
 int run_fwd_held(LnArgs& a, cudaStream_t st, const char* what)
 {
-    const Plan p = plan_of(a, N, 2, THREADS * BLOCKS, 2, sizeof(T));
+    const Plan p = plan_of(a, N, a.c, 2, THREADS * BLOCKS, 1, sizeof(T));
     if (VEC && a.c == a.group * N) return launch<ln_fwd_kernel<T, VEC, VEC, N, THREADS, BLOCKS>>(a, p, st, what);
     return launch<ln_fwd_kernel<T, VEC, false, N, THREADS, BLOCKS>>(a, p, st, what);
 }
@@ -608,7 +671,7 @@ template <class T, bool VEC>
 int run_fwd(LnArgs a, cudaStream_t st)
 {
     const char* what = "layer_norm_fwd";
-    if (held(a, 2, sizeof(T))) {
+    if (fwd_held(a, sizeof(T))) {
         if (a.c <= 256) return run_fwd_held<T, VEC, 8, kBlock, VEC ? 4 : 3>(a, st, what);
         if (a.c <= 16 * kBlock) return run_fwd_held<T, VEC, 16, kBlock, VEC ? 3 : 2>(a, st, what);
         if (a.c <= 16 * kMaxGroup) return run_fwd_held<T, VEC, 16, kMaxGroup, 1>(a, st, what);
@@ -618,11 +681,11 @@ int run_fwd(LnArgs a, cudaStream_t st)
     return launch_check(what);
 }
 
-template <class T, bool VEC, int N, int THREADS, int BLOCKS>
+template <class T, bool VEC, int N, int THREADS, int BLOCKS, bool SPLIT>
 int run_bwd_held(const LnArgs& a, const Plan& p, cudaStream_t st, const char* what)
 {
-    if (VEC && a.c == a.group * N) return launch<ln_bwd_kernel<T, VEC, VEC, N, THREADS, BLOCKS>>(a, p, st, what);
-    return launch<ln_bwd_kernel<T, VEC, false, N, THREADS, BLOCKS>>(a, p, st, what);
+    if (VEC && a.c == a.group * N * p.split) return launch<ln_bwd_kernel<T, VEC, VEC, N, THREADS, BLOCKS, SPLIT>>(a, p, st, what);
+    return launch<ln_bwd_kernel<T, VEC, false, N, THREADS, BLOCKS, SPLIT>>(a, p, st, what);
 }
 
 template <class T, bool VEC>
@@ -630,16 +693,16 @@ int run_bwd(const LnArgs& a, const Plan& p, cudaStream_t st)
 {
     const char* what = "layer_norm_bwd";
     if (a.rows == 0) return DBL_OK;
-    if (held(a, 3, sizeof(T))) {
-        if (a.c <= 256) return run_bwd_held<T, VEC, 8, kBlock, 3>(a, p, st, what);
-        if (a.c <= 16 * kBlock) return run_bwd_held<T, VEC, 16, kBlock, 2>(a, p, st, what);
-        if (a.c <= 16 * kMaxGroup) return run_bwd_held<T, VEC, 16, kMaxGroup, 1>(a, p, st, what);
-        return run_bwd_held<T, VEC, 32, kMaxGroup, 1>(a, p, st, what);
+    if (bwd_held(a)) {
+        if (a.c <= 256) return run_bwd_held<T, VEC, 8, kBlock, 3, false>(a, p, st, what);
+        if (a.c <= 16 * kBlock) return run_bwd_held<T, VEC, 16, kBlock, 2, false>(a, p, st, what);
+        if (p.split == 1) return run_bwd_held<T, VEC, 16, kMaxGroup, 1, false>(a, p, st, what);
+        return run_bwd_held<T, VEC, 16, kMaxGroup, 1, true>(a, p, st, what);
     }
     ln_bwd_wide_kernel<T><<<(int)std::min<int64_t>(a.rows, 1 << 20), kWide, 0, st>>>(a);
     const int rc = launch_check(what);
     if (rc != DBL_OK || !a.parts) return rc;
-    ln_params_wide_kernel<T><<<dim3((a.c + kWide - 1) / kWide, p.blocks), kWide, 0, st>>>(a);
+    ln_params_wide_kernel<T><<<dim3((a.c + kWide - 1) / kWide, p.teams), kWide, 0, st>>>(a);
     return launch_check(what);
 }
 
@@ -676,7 +739,7 @@ size_t dbl_layer_norm_workspace_bytes(const dbl_ln_shape* s)
 {
     if (check(s, "layer_norm_workspace_bytes") != DBL_OK) return 0;
     LnArgs a = args(s);
-    return (size_t)bwd_plan(a, elem_bytes(s->dtype)).blocks * 2 * s->c * sizeof(float);
+    return (size_t)bwd_plan(a, elem_bytes(s->dtype)).teams * 2 * s->c * sizeof(float);
 }
 
 int dbl_layer_norm_bwd(const dbl_ln_shape* s, const void* dy, const void* dskip, const void* x, const float* gamma,
@@ -695,7 +758,7 @@ int dbl_layer_norm_bwd(const dbl_ln_shape* s, const void* dy, const void* dskip,
     LnArgs a = args(s);
     const Plan p = bwd_plan(a, e);
     if (dgamma) {
-        if (!ws || ws_bytes < (size_t)p.blocks * 2 * s->c * sizeof(float))
+        if (!ws || ws_bytes < (size_t)p.teams * 2 * s->c * sizeof(float))
             return set_error(DBL_ERR_WORKSPACE, "layer_norm_bwd: workspace too small");
         if (!aligned16(ws)) return set_error(DBL_ERR_INVALID, "layer_norm_bwd: workspace must be 16-byte aligned");
     }
@@ -717,7 +780,7 @@ int dbl_layer_norm_bwd(const dbl_ln_shape* s, const void* dy, const void* dskip,
     cfg.stream = st;
     cfg.attrs = at;
     cfg.numAttrs = 1;
-    const cudaError_t err = cudaLaunchKernelEx(&cfg, ln_params_sum_kernel, (const float*)a.parts, s->rows ? p.blocks : 0, s->c,
+    const cudaError_t err = cudaLaunchKernelEx(&cfg, ln_params_sum_kernel, (const float*)a.parts, s->rows ? p.teams : 0, s->c,
                                                dgamma, dbeta);
     rc = launch_check("layer_norm_bwd sums");
     return err == cudaSuccess ? rc : cuda_check(err, "layer_norm_bwd sums");

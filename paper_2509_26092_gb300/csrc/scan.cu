@@ -339,28 +339,7 @@ struct Maps {
     CUtensorMap x, z, dh, h, dz;  // h: dx in the backward pass
 };
 
-__device__ __forceinline__ void st_async4(uint32_t addr, uint32_t bar, float4 v)
-{
-    asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v4.b32 [%0], {%2, %3, %4, %5}, [%1];" ::"r"(addr),
-                 "r"(bar), "r"(__float_as_uint(v.x)), "r"(__float_as_uint(v.y)), "r"(__float_as_uint(v.z)),
-                 "r"(__float_as_uint(v.w))
-                 : "memory");
-}
-
-__device__ __forceinline__ void st_async2(uint32_t addr, uint32_t bar, float2 v)
-{
-    asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v2.b32 [%0], {%2, %3}, [%1];" ::"r"(addr), "r"(bar),
-                 "r"(__float_as_uint(v.x)), "r"(__float_as_uint(v.y))
-                 : "memory");
-}
-
 __device__ __forceinline__ void link_wait(uint64_t* bar, uint32_t parity, int* abort) { bounded_wait(bar, parity, abort, &g_scan_status); }
-
-// A block stays until the others no longer write to its shared memory (also where one has given up).
-__device__ __forceinline__ void cluster_leave()
-{
-    asm volatile("barrier.cluster.arrive.relaxed.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory");
-}
 
 // Barriers ready, and every block's shared memory there before it is written from afar.
 __device__ __forceinline__ void links_init(Links& l, int S)
