@@ -26,6 +26,7 @@ constexpr size_t kWarpBytes = 16384 + 16, kWarpBytesFew = 4096 + 16;  // this ma
 constexpr int kWarpK = 128;                  // and the teacher this many entries
 constexpr int kStream = 256;                 // threads of the kernel for rows that no cluster holds
 constexpr size_t kPartBytes = 68 * 1024;     // of a row, to a block: three blocks on an SM
+constexpr size_t kLargePartBytes = 106 * 1024;  // two
 constexpr size_t kMaxPartBytes = 200 * 1024;
 constexpr float kLog2e = 1.4426950408889634f;
 
@@ -529,9 +530,12 @@ int launch(const DistillArgs& a, cudaStream_t st, const char* what)
         kernel_w<<<(unsigned)grid, 32 * kWarpRows, group * kWarpRows, st>>>(a, (int)group);
         return launch_check(what);
     }
-    // as many blocks to a row as bring three on an SM, and for few rows, as fill the SMs with parts of 8 KB and more
+    // As many blocks to a row as bring two on an SM: a cluster's blocks wait for one another, and three smaller parts on
+    // an SM do not make up for that where there are many rows (4000 x 40000 in bf16: 196 us a block each, 224 us two;
+    // 600 x 50257 44 and 50 us; 200 x 50257 26 and 24 us).  For few rows, as fill the SMs, with parts of 8 KB and more.
     int S = 1;
-    while (S < kMaxCluster && part(S) > kPartBytes) S *= 2;
+    while (S < kMaxCluster && part(S) > kLargePartBytes) S *= 2;
+    while (S < kMaxCluster && part(S) > kPartBytes && a.rows * S * 2 <= 3 * sm_count()) S *= 2;
     while (S < kMaxCluster && a.rows * S * 2 <= sm_count() && part(2 * S) >= 8192) S *= 2;
     while (S > 1 && !cluster_held<kernel>(S, kMaxThreads + 32, kMaxPartBytes + head_bytes(kMaxK))) S /= 2;
     if (part(S) > kMaxPartBytes) {
@@ -540,8 +544,11 @@ int launch(const DistillArgs& a, cudaStream_t st, const char* what)
     }
     if (a.rows * S > 0x7fffffff) return set_error(DBL_ERR_UNSUPPORTED, "%s: more than 2^31 blocks", what);
     const size_t smem = head + part(S);
-    int threads = 64;  // four units of 16 bytes a thread and pass, or more
-    while (threads < kMaxThreads && (size_t)threads * 64 < part(S)) threads *= 2;
+    // 256 bytes of the part to a thread, so that registers allow more blocks on an SM (2673 x 15504 in bf16: 56 us, with
+    // 64 bytes 69 us); 64 where there are few rows
+    const size_t share = a.rows * S >= 2 * sm_count() ? 256 : 64;
+    int threads = 64;
+    while (threads < kMaxThreads && threads * share < part(S)) threads *= 2;
     int rc = allow_launch<kernel>(kMaxPartBytes + head_bytes(kMaxK), true, what);
     if (rc != DBL_OK) return rc;
     cudaLaunchConfig_t cfg = {};
