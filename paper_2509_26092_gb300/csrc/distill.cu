@@ -22,7 +22,7 @@ constexpr int kFewK = 64;                    // and up to this many, looks for c
 constexpr int kMaxK = DBL_DISTILL_MAX_K;
 constexpr int kMaxCluster = 16;
 constexpr int kWarpRows = 4;                 // rows of a block, a warp each, where they have
-constexpr size_t kWarpBytes = 16384 + 16, kWarpBytesFew = 4096 + 16;  // this many bytes at the most
+constexpr size_t kWarpBytes = 12288 + 16, kWarpBytesFew = 4096 + 16;  // this many bytes at the most
 constexpr int kWarpK = 128;                  // and the teacher this many entries
 constexpr int kStream = 256;                 // threads of the kernel for rows that no cluster holds
 constexpr size_t kPartBytes = 68 * 1024;     // of a row, to a block: three blocks on an SM
@@ -113,20 +113,40 @@ struct Entries {
     }
 };
 
-// Row r's entries and the student's logits z of their classes, by `threads` threads.
+// A lane's first entries of a row as they are in memory, asked for before anything else is known of the row.
+struct Ahead {
+    static constexpr int N = 2;
+    int c[N];
+    float t[N];
+    __device__ __forceinline__ void ask(const DistillArgs& a, int64_t r)
+    {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int j = i * 32 + (threadIdx.x & 31);
+            c[i] = j < a.k ? __ldg(a.cls + r * a.k + j) : -1;
+            t[i] = j < a.k ? __ldg(a.top + r * a.k + j) : 0.f;
+        }
+    }
+};
+
+// Row r's entries, by a warp; z: the student's logits where those of the entries' classes are to be kept too.
 template <class T>
-__device__ __forceinline__ void load_entries(const DistillArgs& a, int64_t r, const T* z, const Entries& en, int tid, int threads)
+__device__ __forceinline__ void load_entries(const DistillArgs& a, int64_t r, const T* z, const Entries& en, const Ahead& ahead)
 {
     const float inv_tau = 1.f / a.tau;
-#pragma unroll 4
-    for (int j = tid; j < (a.k + 3) / 4 * 4; j += threads) {
-        const int c = j < a.k ? __ldg(a.cls + r * a.k + j) : -1;
-        const float t = j < a.k ? __ldg(a.top + r * a.k + j) : 0.f;
+    auto keep = [&](int j, int c, float t) {
         const bool there = c >= 0 && c < a.v && t != -INFINITY && a.alpha > 0.f;  // a term of weight 0 is absent
         en.cls[j] = there ? c : -1;
         en.lt[j] = t * inv_tau;
-        en.zc[j] = there ? elem_f(z[c]) : 0.f;
-    }
+        if (z) en.zc[j] = there ? elem_f(z[c]) : 0.f;
+    };
+    const int lane = threadIdx.x & 31, end = (a.k + 3) / 4 * 4;
+#pragma unroll
+    for (int i = 0; i < Ahead::N; ++i)
+        if (i * 32 + lane < end) keep(i * 32 + lane, ahead.c[i], ahead.t[i]);
+#pragma unroll 4
+    for (int j = Ahead::N * 32 + lane; j < end; j += 32)
+        keep(j, j < a.k ? __ldg(a.cls + r * a.k + j) : -1, j < a.k ? __ldg(a.top + r * a.k + j) : 0.f);
 }
 
 // The teacher's distribution, by one warp.  log_t: log p = t/T less that.  False where there is no entry.
@@ -243,6 +263,13 @@ __global__ void __launch_bounds__(WARP ? 32 * kWarpRows : kMaxThreads + 32, WARP
     const int64_t r = WARP ? (int64_t)blockIdx.x * kWarpRows + (threadIdx.x >> 5) : S == 1 ? blockIdx.x : blockIdx.x / (unsigned)S;
     grid_dependency_trigger();
     if (r >= a.rows) return;
+    Ahead ahead;
+    if (WARP || side) ahead.ask(a, r);
+    if (tid == 0) {
+        mbar_init(&sm.full, 1);
+        sm.abort = 0;
+        fence_mbar_init();
+    }
     const T* z = static_cast<const T*>(a.z) + r * a.ld;
     T* dz = a.dz ? static_cast<T*>(a.dz) + r * a.ld_grad : nullptr;
     // the row in units of 16 bytes, from the boundary at or before its first element; this block's part of them
@@ -273,9 +300,6 @@ __global__ void __launch_bounds__(WARP ? 32 * kWarpRows : kMaxThreads + 32, WARP
     // whole units by one bulk copy, the row's ends by elements (nothing where they are another row's)
     const int c0 = u0 == 0 && lead ? 1 : 0, c1 = n - (u0 + n == all && (p1 & 15) && n > c0 ? 1 : 0);
     if (tid == 0) {
-        mbar_init(&sm.full, 1);
-        sm.abort = 0;
-        fence_mbar_init();
         const uint32_t bytes = (uint32_t)max(c1 - c0, 0) * 16;
         mbar_arrive_expect_tx(&sm.full, bytes);
         if (bytes) bulk_load(smem_u32(units + c0), (p0 & ~(uintptr_t)15) + (uintptr_t)(u0 + c0) * 16, bytes, &sm.full);
@@ -284,10 +308,10 @@ __global__ void __launch_bounds__(WARP ? 32 * kWarpRows : kMaxThreads + 32, WARP
         const int at = (tid < E ? 0 : c1 * E) + tid % E, el = first + at;
         elems[at] = el >= 0 && el < a.v ? z[el] : elem_from<T>(-INFINITY);
     }
-    const float zl = given ? elem_f(z[lab]) : 0.f;
+    float zl = given && !WARP ? elem_f(z[lab]) : 0.f;
     sync();
     if (WARP || side) {  // while the row is on its way
-        load_entries(a, r, z, en, tid & 31, 32);
+        load_entries(a, r, WARP ? nullptr : z, en, ahead);
         __syncwarp();
         float log_t;
         const bool some = teacher(a, en, log_t);
@@ -302,6 +326,10 @@ __global__ void __launch_bounds__(WARP ? 32 * kWarpRows : kMaxThreads + 32, WARP
     float4 t = make_float4(-INFINITY, 0.f, 0.f, 0.f);
     if (!side) {
         bounded_wait(&sm.full, 0, &sm.abort, &g_distill_status);
+        if (WARP) {  // the whole row is here
+            for (int j = tid; j < a.k; j += 32) en.zc[j] = en.cls[j] >= 0 ? elem_f(elems[en.cls[j] - first]) : 0.f;
+            if (given) zl = elem_f(elems[lab - first]);
+        }
         const uint32_t lowest = sizeof(T) == 4 ? 0xff800000u : act::kF16 ? 0xfc00fc00u : 0xff80ff80u;  // minus infinity
         uint4 mx = make_uint4(lowest, lowest, lowest, lowest);
 #pragma unroll 4
@@ -442,7 +470,9 @@ __global__ void __launch_bounds__(kStream) distill_stream_kernel(DistillArgs a)
         const bool given = lab >= 0 && lab < a.v;
         if (threadIdx.x < 32) {
             float log_t;
-            load_entries(a, r, z, en, threadIdx.x, 32);
+            Ahead ahead;
+            ahead.ask(a, r);
+            load_entries(a, r, z, en, ahead);
             __syncwarp();
             const bool some = teacher(a, en, log_t);
             if (threadIdx.x == 0) some_s = some, log_ts = log_t;
@@ -519,8 +549,8 @@ int launch(const DistillArgs& a, cudaStream_t st, const char* what)
     const size_t head = head_bytes(a.k);
     const size_t row = ((size_t)a.v * sizeof(T) + 15) / 16 * 16 + 16;
     auto part = [&](int S) { return (row / 16 + S - 1) / S * 16; };
-    // Many rows go by the rows in flight on an SM (8000 x 8000 in bf16: 85 us a warp each, 120 us a block each; 8000 x
-    // 4000 48 and 73 us), few by the threads of each.
+    // Many rows go by the rows in flight on an SM: of short ones a warp each leaves most room (8000 x 5000 in bf16: 59 us
+    // a warp each, 77 us a block each; 8000 x 8000 104 and 86 us).  Few go by the threads of each.
     if (row <= (a.rows >= 4 * sm_count() ? kWarpBytes : kWarpBytesFew) && a.k <= kWarpK) {
         const size_t group = (head + row + 127) / 128 * 128;
         const int64_t grid = (a.rows + kWarpRows - 1) / kWarpRows;
