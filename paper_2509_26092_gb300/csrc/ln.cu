@@ -256,32 +256,79 @@ struct Groups {
     }
 };
 
-template <class T, bool VEC, bool FULL, int N, int THREADS, int BLOCKS>
+// What the blocks of a cluster, each with its columns of a row, tell one another of it: a pair of sums, stored into every
+// block's slot of the sender, by turns in two places.  Who has all pairs of row n+1 knows that all blocks have read
+// those of row n: a block sends after its threads have met, and they have read by then.
+struct Exchange {
+    uint64_t bar[2];
+    float2 slot[2][kMaxSplit];
+
+    __device__ __forceinline__ void init()
+    {
+        if (threadIdx.x == 0) {
+            mbar_init(&bar[0], 1);
+            mbar_init(&bar[1], 1);
+            fence_mbar_init();
+        }
+        cluster_sync_all();
+    }
+    // v: the block's, the same in all its threads; returns the blocks' pairs in their order
+    __device__ __forceinline__ const float2* all(float2 v, int which, uint32_t parity, int S, int rank, int* abort)
+    {
+        if (threadIdx.x == 0) mbar_arrive_expect_tx(&bar[which], S * sizeof(float2));
+        if ((int)threadIdx.x < S)
+            st_async2(mapa_shared(smem_u32(&slot[which][rank]), threadIdx.x), mapa_shared(smem_u32(&bar[which]), threadIdx.x), v);
+        bounded_wait(&bar[which], parity, abort, &g_ln_status);
+        return slot[which];
+    }
+};
+
+// A cluster's columns of a row: the arguments with this block's part of every tensor.
+template <class T>
+__device__ __forceinline__ void take_part(LnArgs& a, int rank)
+{
+    const int skip = rank * a.part;
+    a.c = min(a.part, a.c - skip);
+    a.x = static_cast<const T*>(a.x) + skip, a.y = static_cast<T*>(a.y) + skip;
+    if (a.res) a.res = static_cast<const T*>(a.res) + skip;
+    if (a.dy) a.dy = static_cast<const T*>(a.dy) + skip;
+    if (a.sum) a.sum = static_cast<T*>(a.sum) + skip;
+    if (a.gamma) a.gamma += skip;
+    if (a.beta) a.beta += skip;
+    if (a.parts) a.parts += skip;
+}
+
+template <class T, bool VEC, bool FULL, int N, int THREADS, int BLOCKS, bool SPLIT>
 __global__ void __launch_bounds__(THREADS, BLOCKS) ln_fwd_kernel(LnArgs a)
 {
     typedef Cols<T, VEC, FULL, N> C;
     constexpr int P = C::P;
     extern __shared__ __align__(128) char smem[];
+    __shared__ Exchange ex;
+    const int c = a.c, S = SPLIT ? (a.c + a.part - 1) / a.part : 1, rank = SPLIT ? (int)cluster_ctarank() : 0;
+    if (SPLIT) {
+        take_part<T>(a, rank);
+        ex.init();
+    }
     Groups<T, VEC, 2> w;
     w.set(a, smem);
     const T* const from[2] = {static_cast<const T*>(a.x), static_cast<const T*>(a.res)};
     const int g = w.g, G = w.G;
-    const int64_t hop = (int64_t)gridDim.x * w.n;
-    int64_t r = (int64_t)blockIdx.x * w.n + w.id;
+    const int64_t hop = (int64_t)gridDim.x / S * w.n;
+    int64_t r = (int64_t)blockIdx.x / S * w.n + w.id;
     if (g == 0)
         for (int k = 0; k < w.depth; ++k)
             if (r + k * hop < a.rows) w.fetch(from, k, r + k * hop);
-    constexpr bool KEEP = N <= 16;  // the parameters, from row to row
-    float2 ga[KEEP ? N / 2 : P], be[KEEP ? N / 2 : P];
-    if (KEEP) {
+    float2 ga[N / 2], be[N / 2];  // from row to row
 #pragma unroll
-        for (int j = 0; j < C::J; ++j) {
-            C::param(ga + (KEEP ? j * P : 0), a.gamma, 1.f, a.c, g, G, j);
-            C::param(be + (KEEP ? j * P : 0), a.beta, 0.f, a.c, g, G, j);
-        }
+    for (int j = 0; j < C::J; ++j) {
+        C::param(ga + j * P, a.gamma, 1.f, a.c, g, G, j);
+        C::param(be + j * P, a.beta, 0.f, a.c, g, G, j);
     }
     const float inv_c = 1.f / a.c;
-    for (int k = 0; r < a.rows; r += hop, k = k + 1 == w.depth ? 0 : k + 1) {
+    int par = 0;
+    uint32_t turn = 0;  // of the exchange's two places
+    for (int k = 0; r < a.rows; r += hop, k = k + 1 == w.depth ? 0 : k + 1, turn ^= par, par ^= 1) {
         float2 v[N / 2], s = both(0.f);
         w.wait(from, k, r);
         const int off = w.offset(from[0], r), off_r = w.offset(from[1], r);
@@ -295,7 +342,7 @@ __global__ void __launch_bounds__(THREADS, BLOCKS) ln_fwd_kernel(LnArgs a)
         if (a.sum) C::write_all(static_cast<T*>(a.sum) + r * a.ld_out, v, a.c, g, G);
 #pragma unroll
         for (int i = 0; i < N / 2; ++i) s = __fadd2_rn(s, v[i]);
-        const float mean = w.total(s.x + s.y, 0) * inv_c;
+        float mean = w.total(s.x + s.y, 0) * inv_c;
         if (w.warps == 1) __syncwarp();
         if (g == 0 && r + w.depth * hop < a.rows) w.fetch(from, k, r + w.depth * hop);  // the group has read the place
         s = both(0.f);
@@ -313,55 +360,37 @@ __global__ void __launch_bounds__(THREADS, BLOCKS) ln_fwd_kernel(LnArgs a)
                 }
             }
         }
-        const float inv = 1.f / sqrtf(fmaf(w.total(s.x + s.y, 1), inv_c, a.eps));
+        float var = w.total(s.x + s.y, 1) * inv_c;
+        if (SPLIT) {  // the parts' means and variances as one: that of the means is added to those of the parts
+            const float2* p = ex.all(make_float2(mean, var), par, turn, S, rank, w.abort);
+            auto share = [&](int k) { return (float)min(a.part, c - k * a.part) / c; };
+            float whole = 0.f;
+            for (int k = 0; k < S; ++k) whole = fmaf(p[k].x, share(k), whole);
+            var = 0.f;
+            for (int k = 0; k < S; ++k) {
+                const float d = p[k].x - whole;
+                var = fmaf(fmaf(d, d, p[k].y), share(k), var);
+            }
+#pragma unroll
+            for (int i = 0; i < N / 2; ++i) v[i] = __fadd2_rn(v[i], both(mean - whole));
+            mean = whole;
+        }
+        const float inv = 1.f / sqrtf(var + a.eps);
 #pragma unroll
         for (int j = 0; j < C::J; ++j) {
             float2* f = v + j * P;
-            if (!KEEP) {
-                C::param(ga, a.gamma, 1.f, a.c, g, G, j);
-                C::param(be, a.beta, 0.f, a.c, g, G, j);
-            }
 #pragma unroll
-            for (int i = 0; i < P; ++i)
-                f[i] = __ffma2_rn(__fmul2_rn(f[i], both(inv)), ga[(KEEP ? j * P : 0) + i], be[(KEEP ? j * P : 0) + i]);
+            for (int i = 0; i < P; ++i) f[i] = __ffma2_rn(__fmul2_rn(f[i], both(inv)), ga[j * P + i], be[j * P + i]);
         }
         C::write_all(static_cast<T*>(a.y) + r * a.ld_out, v, a.c, g, G);
-        if (g == 0 && a.mean) {
+        if (g == 0 && rank == 0 && a.mean) {
             a.mean[r] = mean;
             a.invstd[r] = inv;
         }
     }
     linger(w.abort);
+    if (SPLIT) cluster_leave();
 }
-
-// What the blocks of a cluster, each with its columns of a row, tell one another of it: a pair of sums, stored into every
-// block's slot of the sender, by turns in two places.  Who has all pairs of row n+1 knows that all blocks have read
-// those of row n: a block sends after its threads have met, and they have read by then.
-struct Exchange {
-    uint64_t bar[2];
-    float2 slot[2][kMaxSplit];
-
-    __device__ __forceinline__ void init()
-    {
-        if (threadIdx.x == 0) {
-            mbar_init(&bar[0], 1);
-            mbar_init(&bar[1], 1);
-            fence_mbar_init();
-        }
-        cluster_sync_all();
-    }
-    // v: the block's, the same in all its threads; returns the cluster's, the same bits in all its blocks
-    __device__ __forceinline__ float2 total(float2 v, int which, uint32_t parity, int S, int rank, int* abort)
-    {
-        if (threadIdx.x == 0) mbar_arrive_expect_tx(&bar[which], S * sizeof(float2));
-        if ((int)threadIdx.x < S)
-            st_async2(mapa_shared(smem_u32(&slot[which][rank]), threadIdx.x), mapa_shared(smem_u32(&bar[which]), threadIdx.x), v);
-        bounded_wait(&bar[which], parity, abort, &g_ln_status);
-        float2 t = slot[which][0];
-        for (int k = 1; k < S; ++k) t = __fadd2_rn(t, slot[which][k]);
-        return t;
-    }
-};
 
 // x: the normalised tensor, res: dskip, y: dx.  A thread also adds up dy*xhat and dy of its columns over the rows
 // that its group takes; a block leaves these sums in parts[block][2][c].
@@ -373,13 +402,8 @@ __global__ void __launch_bounds__(THREADS, BLOCKS) ln_bwd_kernel(LnArgs a)
     extern __shared__ __align__(128) char smem[];
     __shared__ Exchange ex;
     const int c = a.c, S = SPLIT ? (a.c + a.part - 1) / a.part : 1, rank = SPLIT ? (int)cluster_ctarank() : 0;
-    if (SPLIT) {  // of every row this block's columns
-        const int skip = rank * a.part;
-        a.c = min(a.part, c - skip);
-        a.x = static_cast<const T*>(a.x) + skip, a.dy = static_cast<const T*>(a.dy) + skip, a.y = static_cast<T*>(a.y) + skip;
-        if (a.res) a.res = static_cast<const T*>(a.res) + skip;
-        if (a.gamma) a.gamma += skip;
-        if (a.parts) a.parts += skip;
+    if (SPLIT) {
+        take_part<T>(a, rank);
         ex.init();
     }
     Groups<T, VEC, 3> w;
@@ -427,7 +451,11 @@ __global__ void __launch_bounds__(THREADS, BLOCKS) ln_bwd_kernel(LnArgs a)
             }
         }
         float2 t = w.total(make_float2(tx.x + tx.y, ty.x + ty.y), par);
-        if (SPLIT) t = ex.total(t, par, turn, S, rank, w.abort);
+        if (SPLIT) {
+            const float2* p = ex.all(t, par, turn, S, rank, w.abort);
+            t = p[0];
+            for (int i = 1; i < S; ++i) t = __fadd2_rn(t, p[i]);
+        }
         if (w.warps == 1) __syncwarp();
         // the row before this one has been read by all of the group: its place is free
         if (g == 0 && !first && r + (w.depth - 1) * hop < a.rows) w.fetch(from, (k ? k : w.depth) - 1, r + (w.depth - 1) * hop);
@@ -619,23 +647,23 @@ Plan plan_of(LnArgs& a, int n, int c, int tensors, int resident, int split, size
     return p;
 }
 
-// Whether rows of this width are held by a group of the forward pass, in two places of a ring at least.
-bool fwd_held(const LnArgs& a, size_t e) { return a.c <= 32 * kMaxGroup && 4 * (a.c * e + 144) <= kRingBytes; }
-
-// The backward pass: rows of up to 16 columns for each of a group's threads, wider ones by clusters of such blocks.
-bool bwd_held(const LnArgs& a) { return a.c <= 16 * kMaxGroup * kMaxSplit; }
+// Rows of up to 16 columns for each of a group's threads, wider ones by clusters of such blocks.
+bool held(const LnArgs& a) { return a.c <= 16 * kMaxGroup * kMaxSplit; }
+Plan plan_wide(LnArgs& a, int tensors, size_t e)
+{
+    const int S = (a.c + 16 * kMaxGroup - 1) / (16 * kMaxGroup);
+    a.part = ((a.c + S - 1) / S + 15) / 16 * 16;  // whole 16-byte units; the last block's may be fewer
+    return plan_of(a, 16, std::min(a.part, a.c), tensors, kMaxGroup, S, e);
+}
 
 // The backward pass's blocks or clusters, each of which leaves a row of partial column sums.  By the sizes alone, as the
 // workspace is.
 Plan bwd_plan(LnArgs& a, size_t e)
 {
-    a.part = a.c;
-    if (!bwd_held(a)) return {kWide, (int)std::max<int64_t>(1, std::min<int64_t>((a.rows + 15) / 16, 64)), 0, 1};
+    if (!held(a)) return {kWide, (int)std::max<int64_t>(1, std::min<int64_t>((a.rows + 15) / 16, 64)), 0, 1};
     if (a.c <= 256) return plan_of(a, 8, a.c, 3, 3 * kBlock, 1, e);
     if (a.c <= 16 * kBlock) return plan_of(a, 16, a.c, 3, 2 * kBlock, 1, e);
-    const int S = (a.c + 16 * kMaxGroup - 1) / (16 * kMaxGroup);
-    a.part = ((a.c + S - 1) / S + 15) / 16 * 16;  // whole 16-byte units; the last block's may be fewer
-    return plan_of(a, 16, std::min(a.part, a.c), 3, kMaxGroup, S, e);
+    return plan_wide(a, 3, e);
 }
 
 template <auto KERNEL>
@@ -659,23 +687,31 @@ int launch(const LnArgs& a, const Plan& p, cudaStream_t st, const char* what)
     return err == cudaSuccess ? ran : cuda_check(err, what);
 }
 
-template <class T, bool VEC, int N, int THREADS, int BLOCKS>
-int run_fwd_held(LnArgs& a, cudaStream_t st, const char* what)
+template <class T, bool VEC, int N, int THREADS, int BLOCKS, bool SPLIT>
+int run_fwd_held(const LnArgs& a, const Plan& p, cudaStream_t st, const char* what)
 {
-    const Plan p = plan_of(a, N, a.c, 2, THREADS * BLOCKS, 1, sizeof(T));
-    if (VEC && a.c == a.group * N) return launch<ln_fwd_kernel<T, VEC, VEC, N, THREADS, BLOCKS>>(a, p, st, what);
-    return launch<ln_fwd_kernel<T, VEC, false, N, THREADS, BLOCKS>>(a, p, st, what);
+    if (VEC && a.c == a.group * N * p.split) return launch<ln_fwd_kernel<T, VEC, VEC, N, THREADS, BLOCKS, SPLIT>>(a, p, st, what);
+    return launch<ln_fwd_kernel<T, VEC, false, N, THREADS, BLOCKS, SPLIT>>(a, p, st, what);
 }
 
 template <class T, bool VEC>
 int run_fwd(LnArgs a, cudaStream_t st)
 {
     const char* what = "layer_norm_fwd";
-    if (fwd_held(a, sizeof(T))) {
-        if (a.c <= 256) return run_fwd_held<T, VEC, 8, kBlock, VEC ? 4 : 3>(a, st, what);
-        if (a.c <= 16 * kBlock) return run_fwd_held<T, VEC, 16, kBlock, VEC ? 3 : 2>(a, st, what);
-        if (a.c <= 16 * kMaxGroup) return run_fwd_held<T, VEC, 16, kMaxGroup, 1>(a, st, what);
-        return run_fwd_held<T, VEC, 32, kMaxGroup, 1>(a, st, what);
+    constexpr size_t e = sizeof(T);
+    if (held(a)) {
+        constexpr int B8 = VEC ? 4 : 3, B16 = VEC ? 3 : 2;
+        if (a.c <= 256) {
+            const Plan p = plan_of(a, 8, a.c, 2, kBlock * B8, 1, e);
+            return run_fwd_held<T, VEC, 8, kBlock, B8, false>(a, p, st, what);
+        }
+        if (a.c <= 16 * kBlock) {
+            const Plan p = plan_of(a, 16, a.c, 2, kBlock * B16, 1, e);
+            return run_fwd_held<T, VEC, 16, kBlock, B16, false>(a, p, st, what);
+        }
+        const Plan p = plan_wide(a, 2, e);
+        if (p.split == 1) return run_fwd_held<T, VEC, 16, kMaxGroup, 1, false>(a, p, st, what);
+        return run_fwd_held<T, VEC, 16, kMaxGroup, 1, true>(a, p, st, what);
     }
     ln_fwd_wide_kernel<T><<<(int)std::min<int64_t>(a.rows, 1 << 20), kWide, 0, st>>>(a);
     return launch_check(what);
@@ -693,7 +729,7 @@ int run_bwd(const LnArgs& a, const Plan& p, cudaStream_t st)
 {
     const char* what = "layer_norm_bwd";
     if (a.rows == 0) return DBL_OK;
-    if (bwd_held(a)) {
+    if (held(a)) {
         if (a.c <= 256) return run_bwd_held<T, VEC, 8, kBlock, 3, false>(a, p, st, what);
         if (a.c <= 16 * kBlock) return run_bwd_held<T, VEC, 16, kBlock, 2, false>(a, p, st, what);
         if (p.split == 1) return run_bwd_held<T, VEC, 16, kMaxGroup, 1, false>(a, p, st, what);
