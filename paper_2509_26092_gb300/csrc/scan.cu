@@ -878,7 +878,16 @@ int launch(ScanArgs a, cudaStream_t st, const char* what)
     // channels where there are no more: half the lanes would have nothing to do.
     constexpr int R = sizeof(T) == 2 ? 16 : 8, RU = BWD ? 8 : R;
     const bool aligned = rows_at(16);
-    if (a.c <= 32) return aligned ? launch_tiles<T, true, 16, R, 2, BWD>(a, st, what) : launch_tiles<T, false, 16, RU, 2, BWD>(a, st, what);
+    // Few sequences of few channels leave SMs idle even in the largest clusters: narrower blocks have more of them on
+    // the sequence at a time (1 x 65536 x 64, 8, 16 and 32 lanes: 30, 40 and 62 us, backward 40, 55 and 93; 1 x 65536 x
+    // 512, 16 and 32: 81 and 80, backward 154 and 181; 1 x 65536 x 256 in fp32: 83, 73 and 102, backward 127, 153 and 142).
+    auto narrow = [&](int lanes, int blocks) {  // up to so many blocks to an SM, and clusters that take turns on a sequence
+        return a.n * ((a.c + 2 * lanes - 1) / (2 * lanes)) * kMaxCluster <= blocks * sm_count() && a.t > kThreads / lanes * kMaxCluster * R;
+    };
+    if (narrow(8, BWD ? 2 : 1))
+        return aligned ? launch_tiles<T, true, 8, R, 2, BWD>(a, st, what) : launch_tiles<T, false, 8, RU, 2, BWD>(a, st, what);
+    if (a.c <= 32 || narrow(16, 2))
+        return aligned ? launch_tiles<T, true, 16, R, 2, BWD>(a, st, what) : launch_tiles<T, false, 16, RU, 2, BWD>(a, st, what);
     return aligned ? launch_tiles<T, true, 32, R, 2, BWD>(a, st, what) : launch_tiles<T, false, 32, RU, 2, BWD>(a, st, what);
 }
 
