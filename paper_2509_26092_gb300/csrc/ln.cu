@@ -47,31 +47,33 @@ struct Cols {
     static constexpr int A = VEC ? 16 / (int)sizeof(T) : 2, J = N / A, P = A / 2;  // columns, accesses, pairs of one
     // first column of access j, and how far the second of its (first) pair is: single fp32 columns lie side by side in
     // a warp, 16-bit ones in a thread, which can store them at once in rows that begin at a word
-    static __device__ __forceinline__ int col(int j, int g, int G) { return !VEC && sizeof(T) == 4 ? j * 2 * G + g : (j * G + g) * A; }
-    static __device__ __forceinline__ int mate(int G) { return !VEC && sizeof(T) == 4 ? G : 1; }
+    static constexpr bool ASIDE = !VEC && sizeof(T) == 4;
+    static constexpr int MATE = ASIDE ? 32 : 1;
+    static __device__ __forceinline__ int base(int g) { return (g >> 5) * 32 * N + (g & 31) * (ASIDE ? 1 : A); }
+    static __device__ __forceinline__ int col(int j, int g) { return base(g) + j * 32 * A; }
     static __device__ __forceinline__ float2 pair(const T* p) { return make_float2(elem_f(p[0]), elem_f(p[1])); }
     // access j of a row in shared memory that begins `off` elements after row; zeros past its end
-    static __device__ __forceinline__ void read(float2* f, const char* row, int off, int c, int g, int G, int j)
+    static __device__ __forceinline__ void read(float2* f, const char* row, int off, int c, int g, int j)
     {
-        const int i = col(j, g, G);
+        const int i = col(j, g);
         if constexpr (VEC) {
             uint4 r = make_uint4(0, 0, 0, 0);
-            if (FULL || i < c) r = reinterpret_cast<const uint4*>(row)[j * G + g];
+            if (FULL || i < c) r = *reinterpret_cast<const uint4*>(row + i * sizeof(T));
             const T* p = reinterpret_cast<const T*>(&r);
 #pragma unroll
             for (int k = 0; k < P; ++k) f[k] = pair(p + 2 * k);
         } else {
             const T* p = reinterpret_cast<const T*>(row) + off + i;
-            f[0] = make_float2(i < c ? elem_f(p[0]) : 0.f, i + mate(G) < c ? elem_f(p[mate(G)]) : 0.f);
+            f[0] = make_float2(i < c ? elem_f(p[0]) : 0.f, i + MATE < c ? elem_f(p[MATE]) : 0.f);
         }
     }
     // all accesses; 16-bit pairs in one where the row begins at a word
-    static __device__ __forceinline__ void read_all(float2* f, const char* row, int off, int c, int g, int G)
+    static __device__ __forceinline__ void read_all(float2* f, const char* row, int off, int c, int g)
     {
         if (!VEC && sizeof(T) == 2 && off % 2 == 0) {
 #pragma unroll
             for (int j = 0; j < J; ++j) {
-                const int i = col(j, g, G);
+                const int i = col(j, g);
                 uint32_t v = 0;
                 if (i < c) v = reinterpret_cast<const uint32_t*>(row)[(off + i) / 2];
                 f[j] = act::unpack2_u32(v);
@@ -79,15 +81,15 @@ struct Cols {
             }
         } else {
 #pragma unroll
-            for (int j = 0; j < J; ++j) read(f + j * P, row, off, c, g, G, j);
+            for (int j = 0; j < J; ++j) read(f + j * P, row, off, c, g, j);
         }
     }
-    static __device__ __forceinline__ void write_all(T* row, const float2* f, int c, int g, int G)
+    static __device__ __forceinline__ void write_all(T* row, const float2* f, int c, int g)
     {
         if (!VEC && sizeof(T) == 2 && (reinterpret_cast<uintptr_t>(row) & 3) == 0) {
 #pragma unroll
             for (int j = 0; j < J; ++j) {
-                const int i = col(j, g, G);
+                const int i = col(j, g);
                 if (i + 1 < c)
                     *reinterpret_cast<uint32_t*>(row + i) = act::pack2_u32(f[j].x, f[j].y);
                 else if (i < c)
@@ -95,12 +97,12 @@ struct Cols {
             }
         } else {
 #pragma unroll
-            for (int j = 0; j < J; ++j) write(row, f + j * P, c, g, G, j);
+            for (int j = 0; j < J; ++j) write(row, f + j * P, c, g, j);
         }
     }
-    static __device__ __forceinline__ void write(T* row, const float2* f, int c, int g, int G, int j)
+    static __device__ __forceinline__ void write(T* row, const float2* f, int c, int g, int j)
     {
-        const int i = col(j, g, G);
+        const int i = col(j, g);
         if constexpr (VEC) {
             uint4 o;
             T* p = reinterpret_cast<T*>(&o);
@@ -117,14 +119,14 @@ struct Cols {
                 *reinterpret_cast<uint32_t*>(row + i) = act::pack2_u32(f[0].x, f[0].y);
             } else {
                 if (i < c) row[i] = elem_from<T>(f[0].x);
-                if (i + mate(G) < c) row[i + mate(G)] = elem_from<T>(f[0].y);
+                if (i + MATE < c) row[i + MATE] = elem_from<T>(f[0].y);
             }
         }
     }
     // parameters of the same columns (`other` where there are none, and past the row's end)
-    static __device__ __forceinline__ void param(float2* f, const float* p, float other, int c, int g, int G, int j)
+    static __device__ __forceinline__ void param(float2* f, const float* p, float other, int c, int g, int j)
     {
-        const int i = col(j, g, G);
+        const int i = col(j, g);
 #pragma unroll
         for (int k = 0; k < P; ++k) {
             f[k] = make_float2(other, other);
@@ -135,7 +137,7 @@ struct Cols {
                 }
             } else if (p) {
                 if (i < c) f[k].x = __ldg(p + i);
-                if (i + mate(G) < c) f[k].y = __ldg(p + i + mate(G));
+                if (i + MATE < c) f[k].y = __ldg(p + i + MATE);
             }
         }
     }
@@ -313,7 +315,7 @@ __global__ void __launch_bounds__(THREADS, BLOCKS) ln_fwd_kernel(LnArgs a)
     Groups<T, VEC, 2> w;
     w.set(a, smem);
     const T* const from[2] = {static_cast<const T*>(a.x), static_cast<const T*>(a.res)};
-    const int g = w.g, G = w.G;
+    const int g = w.g;
     const int64_t hop = (int64_t)gridDim.x / S * w.n;
     int64_t r = (int64_t)blockIdx.x / S * w.n + w.id;
     if (g == 0)
@@ -322,8 +324,8 @@ __global__ void __launch_bounds__(THREADS, BLOCKS) ln_fwd_kernel(LnArgs a)
     float2 ga[N / 2], be[N / 2];  // from row to row
 #pragma unroll
     for (int j = 0; j < C::J; ++j) {
-        C::param(ga + j * P, a.gamma, 1.f, a.c, g, G, j);
-        C::param(be + j * P, a.beta, 0.f, a.c, g, G, j);
+        C::param(ga + j * P, a.gamma, 1.f, a.c, g, j);
+        C::param(be + j * P, a.beta, 0.f, a.c, g, j);
     }
     const float inv_c = 1.f / a.c;
     int par = 0;
@@ -332,14 +334,14 @@ __global__ void __launch_bounds__(THREADS, BLOCKS) ln_fwd_kernel(LnArgs a)
         float2 v[N / 2], s = both(0.f);
         w.wait(from, k, r);
         const int off = w.offset(from[0], r), off_r = w.offset(from[1], r);
-        C::read_all(v, w.row(k, 0), off, a.c, g, G);
+        C::read_all(v, w.row(k, 0), off, a.c, g);
         if (a.res) {
             float2 u[N / 2];
-            C::read_all(u, w.row(k, 1), off_r, a.c, g, G);
+            C::read_all(u, w.row(k, 1), off_r, a.c, g);
 #pragma unroll
             for (int i = 0; i < N / 2; ++i) v[i] = __fadd2_rn(v[i], u[i]);
         }
-        if (a.sum) C::write_all(static_cast<T*>(a.sum) + r * a.ld_out, v, a.c, g, G);
+        if (a.sum) C::write_all(static_cast<T*>(a.sum) + r * a.ld_out, v, a.c, g);
 #pragma unroll
         for (int i = 0; i < N / 2; ++i) s = __fadd2_rn(s, v[i]);
         float mean = w.total(s.x + s.y, 0) * inv_c;
@@ -348,7 +350,7 @@ __global__ void __launch_bounds__(THREADS, BLOCKS) ln_fwd_kernel(LnArgs a)
         s = both(0.f);
 #pragma unroll
         for (int j = 0; j < C::J; ++j) {
-            const int i0 = C::col(j, g, G);
+            const int i0 = C::col(j, g);
 #pragma unroll
             for (int i = j * P; i < (j + 1) * P; ++i) {
                 v[i] = __fadd2_rn(v[i], both(-mean));
@@ -356,7 +358,7 @@ __global__ void __launch_bounds__(THREADS, BLOCKS) ln_fwd_kernel(LnArgs a)
                     if (FULL || i0 < a.c) s = __ffma2_rn(v[i], v[i], s);
                 } else {
                     if (i0 < a.c) s.x = fmaf(v[i].x, v[i].x, s.x);
-                    if (i0 + C::mate(G) < a.c) s.y = fmaf(v[i].y, v[i].y, s.y);
+                    if (i0 + C::MATE < a.c) s.y = fmaf(v[i].y, v[i].y, s.y);
                 }
             }
         }
@@ -382,7 +384,7 @@ __global__ void __launch_bounds__(THREADS, BLOCKS) ln_fwd_kernel(LnArgs a)
 #pragma unroll
             for (int i = 0; i < P; ++i) f[i] = __ffma2_rn(__fmul2_rn(f[i], both(inv)), ga[j * P + i], be[j * P + i]);
         }
-        C::write_all(static_cast<T*>(a.y) + r * a.ld_out, v, a.c, g, G);
+        C::write_all(static_cast<T*>(a.y) + r * a.ld_out, v, a.c, g);
         if (g == 0 && rank == 0 && a.mean) {
             a.mean[r] = mean;
             a.invstd[r] = inv;
@@ -409,7 +411,7 @@ __global__ void __launch_bounds__(THREADS, BLOCKS) ln_bwd_kernel(LnArgs a)
     Groups<T, VEC, 3> w;
     w.set(a, smem);
     const T* const from[3] = {static_cast<const T*>(a.x), static_cast<const T*>(a.dy), static_cast<const T*>(a.res)};
-    const int g = w.g, G = w.G;
+    const int g = w.g;
     const int64_t team = blockIdx.x / S, hop = (int64_t)gridDim.x / S * w.n;
     int64_t r = team * w.n + w.id;
     float mean = 0.f, inv = 0.f;
@@ -430,15 +432,15 @@ __global__ void __launch_bounds__(THREADS, BLOCKS) ln_bwd_kernel(LnArgs a)
     for (int k = 0; r < a.rows; r += hop, k = k + 1 == w.depth ? 0 : k + 1, turn ^= par, par ^= 1) {
         float2 h[N / 2], d[N / 2], ga[N / 2], tx = both(0.f), ty = tx;
 #pragma unroll
-        for (int j = 0; j < C::J; ++j) C::param(ga + j * P, a.gamma, 1.f, a.c, g, G, j);  // back before the row is
+        for (int j = 0; j < C::J; ++j) C::param(ga + j * P, a.gamma, 1.f, a.c, g, j);  // back before the row is
         w.wait(from, k, r);
         const int off_x = w.offset(from[0], r), off_d = w.offset(from[1], r);
         const float is = inv, mu = mean;
         if (r + hop < a.rows) mean = a.mean[r + hop], inv = a.invstd[r + hop];
 #pragma unroll
         for (int j = 0; j < C::J; ++j) {
-            C::read(h + j * P, w.row(k, 0), off_x, a.c, g, G, j);
-            C::read(d + j * P, w.row(k, 1), off_d, a.c, g, G, j);
+            C::read(h + j * P, w.row(k, 0), off_x, a.c, g, j);
+            C::read(d + j * P, w.row(k, 1), off_d, a.c, g, j);
 #pragma unroll
             for (int q = 0; q < P; ++q) {  // past the row's end d is 0
                 const int i = j * P + q;
@@ -468,11 +470,11 @@ __global__ void __launch_bounds__(THREADS, BLOCKS) ln_bwd_kernel(LnArgs a)
         for (int j = 0; j < C::J; ++j) {
             if (a.res) {
                 float2 u[P];
-                C::read(u, w.row(k, 2), off_s, a.c, g, G, j);
+                C::read(u, w.row(k, 2), off_s, a.c, g, j);
 #pragma unroll
                 for (int q = 0; q < P; ++q) d[j * P + q] = __fadd2_rn(d[j * P + q], u[q]);
             }
-            C::write(static_cast<T*>(a.y) + r * a.ld_out, d + j * P, a.c, g, G, j);
+            C::write(static_cast<T*>(a.y) + r * a.ld_out, d + j * P, a.c, g, j);
         }
     }
     linger(w.abort);
@@ -489,7 +491,7 @@ __global__ void __launch_bounds__(THREADS, BLOCKS) ln_bwd_kernel(LnArgs a)
     for (int j = 0; j < C::J; ++j)
 #pragma unroll
         for (int q = 0; q < P; ++q) {
-            const int i = C::col(j, g, G) + 2 * q, m = i + C::mate(G);
+            const int i = C::col(j, g) + 2 * q, m = i + C::MATE;
             if (i < a.c) out[i] = dg[j * P + q].x, out[c + i] = db[j * P + q].x;
             if (m < a.c) out[m] = dg[j * P + q].y, out[c + m] = db[j * P + q].y;
         }
