@@ -199,20 +199,30 @@ struct Groups {
             mbar_arrive_expect_tx(&bars[k], sum);
 #pragma unroll
             for (int t = 0; t < TENSORS; ++t)
-                if (sp[t].bytes) bulk_load(smem_u32(to + t * slot), sp[t].lo, sp[t].bytes, &bars[k]);
+                if (sp[t].bytes) bulk_load(smem_u32(to + t * slot) + sp[t].skip, sp[t].lo, sp[t].bytes, &bars[k]);
         }
     }
     struct Span {
         uintptr_t lo;
-        uint32_t bytes;
+        uint32_t bytes, skip;  // skip: from the boundary at or before the row's first element
+        int head, tail;        // elements before the span, and the first one after it
     };
-    // A row from the 16-byte boundary at or before its first element to that at or after its last; nothing where that
-    // would leave the tensor.
+    // A row from the 16-byte boundary at or before its first element to that at or after its last; where that would leave
+    // the tensor, the 16-byte units within the row.
     __device__ __forceinline__ Span span(const T* from, int64_t r) const
     {
-        const uintptr_t p = reinterpret_cast<uintptr_t>(from + r * ld), e = (p + c * sizeof(T) + 15) & ~(uintptr_t)15, lo = p & ~(uintptr_t)15;
-        const bool whole = lo >= reinterpret_cast<uintptr_t>(from) && e <= reinterpret_cast<uintptr_t>(from + (rows - 1) * ld + c);
-        return {lo, from && whole ? (uint32_t)(e - lo) : 0u};
+        const uintptr_t p = reinterpret_cast<uintptr_t>(from + r * ld), end = p + c * sizeof(T);
+        uintptr_t lo = p & ~(uintptr_t)15, hi = (end + 15) & ~(uintptr_t)15;
+        Span s = {lo, 0, 0, 0, c};
+        if (!from) return s;
+        if (lo < reinterpret_cast<uintptr_t>(from) || hi > reinterpret_cast<uintptr_t>(from + (rows - 1) * ld + c)) {
+            lo = (p + 15) & ~(uintptr_t)15, hi = end & ~(uintptr_t)15;
+            if (hi < lo) hi = lo;
+            s.skip = (uint32_t)(lo - s.lo), s.lo = lo;
+            s.head = min(c, (int)((lo - p) / sizeof(T))), s.tail = max(s.head, (int)((hi - p) / sizeof(T)));
+        }
+        s.bytes = (uint32_t)(hi - lo);
+        return s;
     }
     // elements from the 16-byte boundary to a row's first one
     __device__ __forceinline__ int offset(const T* from, int64_t r) const
@@ -227,13 +237,19 @@ struct Groups {
         bounded_wait(&bars[k], phase >> k & 1, abort, &g_ln_status);
         phase ^= 1u << k;
         if (VEC || (r >= 16 && r < rows - 16)) return;  // of 16 rows the 16 bytes before or after are the tensor's
-        // rows at the tensor's ends, where no bulk copy has brought them
+        // rows at the tensor's ends: what the bulk copy has left out, fewer elements than a warp has lanes
+        T v[TENSORS];
+        int at[TENSORS];
 #pragma unroll
         for (int t = 0; t < TENSORS; ++t) {
-            if (!from[t] || span(from[t], r).bytes) continue;
-            T* to = reinterpret_cast<T*>(ring + ((size_t)k * TENSORS + t) * slot) + offset(from[t], r);
-            for (int i = g; i < c; i += G) to[i] = from[t][r * ld + i];
+            const Span s = span(from[t], r);
+            at[t] = !from[t] ? c : g < s.head ? g : s.tail + g - s.head;
+            if (at[t] < c) v[t] = from[t][r * ld + at[t]];
         }
+#pragma unroll
+        for (int t = 0; t < TENSORS; ++t)
+            if (at[t] < c) (reinterpret_cast<T*>(ring + ((size_t)k * TENSORS + t) * slot) + offset(from[t], r))[at[t]] = v[t];
+        fence_async_shared();  // before a later row's bulk copy to the same place
         sync();
     }
     // Sums over the group, the same bits in all its threads; which: 0 or 1, not the same twice in a row.
