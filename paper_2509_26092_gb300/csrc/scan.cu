@@ -424,7 +424,8 @@ __global__ void __launch_bounds__(kThreads, BLOCKS) scan_fwd_kernel(ScanArgs a, 
     float* keep = a.states ? a.states + (w.b * w.chunks + (row + o0) / kChunk) * a.c + w.ch : nullptr;
     const bool keeper = a.states && (row + o0) % kChunk == 0 && w.one;
     int par = 0, turn = 0, phase = 0;
-    for (int at = 0; at < a.t; at += step, turn += par, par ^= 1) {
+    const int parts_end = w.len > 0 ? (int)min((int64_t)a.t, ((int64_t)(w.len - 1) / step + 1) * step) : 0;
+    for (int at = 0; at < parts_end; at += step, turn += par, par ^= 1) {
         if (w.S > 1 && threadIdx.x == 0) {
             mbar_arrive_expect_tx(&sm.links.pairs[par], w.rank * LANES * sizeof(float4));
             if (a.t - at > step) mbar_arrive_expect_tx(&sm.links.carry[par ^ 1], LANES * sizeof(float2));
@@ -526,6 +527,17 @@ __global__ void __launch_bounds__(kThreads, BLOCKS) scan_fwd_kernel(ScanArgs a, 
         if (!ALIGNED) x += hop, z += hop, out += hop_h;
         if (a.states) keep += (int64_t)(step / kChunk) * a.c;
     }
+    if (parts_end < a.t) {  // parts after the sequence's end: its last state, and zeros
+        __syncthreads();
+        if (w.S > 1 && parts_end > 0) link_wait(&sm.links.carry[par], par ? turn & 1 : (turn & 1) ^ 1, &sm.links.abort);
+        const float2 in = sm.carry[par][lane];
+        if (a.states && w.one)
+            for (int j = parts_end / kChunk + w.rank * w.subs + w.sub; j < w.chunks; j += w.S * w.subs)
+                st_state(a.states + (w.b * w.chunks + j) * a.c + w.ch, in, w.two);
+        if (w.one)
+            for (int64_t i = (int64_t)parts_end + w.rank * w.subs + w.sub; i < a.t; i += w.S * w.subs)
+                st_any(static_cast<T*>(a.h) + (w.b * a.t + i) * a.ld_h + w.ch, make_float2(0.f, 0.f), w.two, a.pairs);
+    }
     if (ALIGNED) bulk_wait_read();
     linger(&sm.links.abort);
     if (w.S > 1) cluster_leave();
@@ -559,7 +571,7 @@ __global__ void __launch_bounds__(kThreads, BLOCKS) scan_bwd_kernel(ScanArgs a, 
     Place w;
     w.set<LANES>(a);
     const int tile = w.subs * R, step = tile * w.S, lane = w.lane, ch = a.c - w.ch0;
-    const int top = (a.t - 1) / step * step;
+    const int top = w.len > 0 ? (w.len - 1) / step * step : -step;  // the last part with a step of the sequence; -step: none
     int64_t row = (int64_t)top + w.rank * tile + w.warp * St::ROWS;
     const int64_t row0 = w.b * a.t + row;
     const T* x = static_cast<const T*>(a.x) + row0 * a.ld_x + w.ch0;
@@ -594,9 +606,15 @@ __global__ void __launch_bounds__(kThreads, BLOCKS) scan_bwd_kernel(ScanArgs a, 
     };
     const float* kept = a.states + (w.b * w.chunks + (row + o0) / kChunk) * a.c + w.ch;
     links_init(sm.links, w.S);
-    fetch(0, 0);
+    if (top >= 0) fetch(0, 0);
     float2 start = make_float2(0.f, 0.f);  // the state before this thread's chunk
-    if (w.one && row + o0 < a.t) start = ld_state(kept, w.two);
+    if (top >= 0 && w.one && row + o0 < a.t) start = ld_state(kept, w.two);
+    for (int64_t i = (int64_t)top + step + w.rank * w.subs + w.sub; i < a.t; i += w.S * w.subs)  // the parts after that one
+        if (w.one) {
+            const int64_t at = (w.b * a.t + i) * a.ld_x + w.ch;
+            st_any(static_cast<T*>(a.h) + at, make_float2(0.f, 0.f), w.two, a.pairs);
+            st_any(static_cast<T*>(a.dgate) + at, make_float2(0.f, 0.f), w.two, a.pairs);
+        }
     const bool last = w.sub == 0;
     float2 end = make_float2(0.f, 0.f);
     if (last) {

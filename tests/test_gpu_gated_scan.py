@@ -98,6 +98,9 @@ CASES = [
     dict(n=6, t=64, c=64, lengths=[-3, 0, 99, 63, 64, 1]), dict(n=3, t=1, c=24, lengths=[0, 1, 1]),
     dict(n=2, t=600, c=64, lengths=[0, 0]), dict(n=2, t=333, c=48, h0=False), dict(n=2, t=900, c=64, gate_mean=9.0),
     dict(n=2, t=300, c=64, gate_mean=-3.0),
+    # lengths that end whole parts of a block or a cluster before the tensor does
+    dict(n=3, t=9000, c=64, lengths=[100, 9000, 4500]), dict(n=2, t=9000, c=15, lengths=[0, 8193]),
+    dict(n=4, t=3001, c=101, lengths=[1024, 3000, 1, 2048], packed=True), dict(n=40, t=300, c=200, lengths=[7 * i for i in range(40)]),
 ]
 
 
