@@ -22,6 +22,8 @@ constexpr int kBlock = 256;        // threads of a block of several groups
 constexpr int kMaxSplit = 8;       // blocks of a row in the backward pass
 constexpr int kMaxDepth = 4;       // rows of a group on their way
 constexpr int kWide = 256;         // threads of the kernels for rows wider than a group
+constexpr int kShort = 256;        // columns of a short row, at the most
+constexpr int kShortFwd = 3, kShortBwd = 2;  // blocks on an SM for them
 constexpr int kSumThreads = 1024;
 constexpr size_t kRingBytes = 200 * 1024;  // shared memory for them on an SM
 
@@ -38,19 +40,20 @@ struct LnArgs {
     float eps;
     int group, depth, slot;  // threads of a row, rows on their way, bytes of one in shared memory
     int part;                // columns of a block, where a cluster takes a row
+    int batch;               // short rows at a time
 };
 
 // This thread's columns of a row, in pairs: J accesses of 16 bytes where rows allow it (VEC; FULL: every thread has all
 // of its columns), otherwise of 4 bytes.
-template <class T, bool VEC, bool FULL, int N>
+template <class T, bool VEC, bool FULL, int N, int W = 32>
 struct Cols {
     static constexpr int A = VEC ? 16 / (int)sizeof(T) : 2, J = N / A, P = A / 2;  // columns, accesses, pairs of one
     // first column of access j, and how far the second of its (first) pair is: single fp32 columns lie side by side in
     // a warp, 16-bit ones in a thread, which can store them at once in rows that begin at a word
     static constexpr bool ASIDE = !VEC && sizeof(T) == 4;
-    static constexpr int MATE = ASIDE ? 32 : 1;
-    static __device__ __forceinline__ int base(int g) { return (g >> 5) * 32 * N + (g & 31) * (ASIDE ? 1 : A); }
-    static __device__ __forceinline__ int col(int j, int g) { return base(g) + j * 32 * A; }
+    static constexpr int MATE = ASIDE ? W : 1;
+    static __device__ __forceinline__ int base(int g) { return g / W * W * N + g % W * (ASIDE ? 1 : A); }
+    static __device__ __forceinline__ int col(int j, int g) { return base(g) + j * W * A; }
     static __device__ __forceinline__ float2 pair(const T* p) { return make_float2(elem_f(p[0]), elem_f(p[1])); }
     // access j of a row in shared memory that begins `off` elements after row; zeros past its end
     static __device__ __forceinline__ void read(float2* f, const char* row, int off, int c, int g, int j)
@@ -145,6 +148,29 @@ struct Cols {
 
 __device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
 
+// What one bulk copy brings of `len` elements at p, of a tensor that goes from `first` to before `end`: all from the 16-byte
+// boundary at or before them to the one at or after them, or where that would leave the tensor, the 16-byte units within.
+struct Span {
+    uintptr_t lo;
+    uint32_t bytes, skip;  // skip: from the boundary at or before the first element
+    int head, tail;        // elements before the span, and the first one after it
+};
+template <class T>
+__device__ __forceinline__ Span span_of(const T* first, const T* end, const T* p, int len)
+{
+    const uintptr_t b = reinterpret_cast<uintptr_t>(p), e = b + len * sizeof(T);
+    uintptr_t lo = b & ~(uintptr_t)15, hi = (e + 15) & ~(uintptr_t)15;
+    Span s = {lo, 0, 0, 0, len};
+    if (lo < reinterpret_cast<uintptr_t>(first) || hi > reinterpret_cast<uintptr_t>(end)) {
+        lo = (b + 15) & ~(uintptr_t)15, hi = e & ~(uintptr_t)15;
+        if (hi < lo) hi = lo;
+        s.skip = (uint32_t)(lo - s.lo), s.lo = lo;
+        s.head = min(len, (int)((lo - b) / sizeof(T))), s.tail = max(s.head, (int)((hi - b) / sizeof(T)));
+    }
+    s.bytes = (uint32_t)(hi - lo);
+    return s;
+}
+
 // A block's groups: their places, barriers and rows in shared memory.
 template <class T, bool VEC, int TENSORS>
 struct Groups {
@@ -202,27 +228,10 @@ struct Groups {
                 if (sp[t].bytes) bulk_load(smem_u32(to + t * slot) + sp[t].skip, sp[t].lo, sp[t].bytes, &bars[k]);
         }
     }
-    struct Span {
-        uintptr_t lo;
-        uint32_t bytes, skip;  // skip: from the boundary at or before the row's first element
-        int head, tail;        // elements before the span, and the first one after it
-    };
-    // A row from the 16-byte boundary at or before its first element to that at or after its last; where that would leave
-    // the tensor, the 16-byte units within the row.
     __device__ __forceinline__ Span span(const T* from, int64_t r) const
     {
-        const uintptr_t p = reinterpret_cast<uintptr_t>(from + r * ld), end = p + c * sizeof(T);
-        uintptr_t lo = p & ~(uintptr_t)15, hi = (end + 15) & ~(uintptr_t)15;
-        Span s = {lo, 0, 0, 0, c};
-        if (!from) return s;
-        if (lo < reinterpret_cast<uintptr_t>(from) || hi > reinterpret_cast<uintptr_t>(from + (rows - 1) * ld + c)) {
-            lo = (p + 15) & ~(uintptr_t)15, hi = end & ~(uintptr_t)15;
-            if (hi < lo) hi = lo;
-            s.skip = (uint32_t)(lo - s.lo), s.lo = lo;
-            s.head = min(c, (int)((lo - p) / sizeof(T))), s.tail = max(s.head, (int)((hi - p) / sizeof(T)));
-        }
-        s.bytes = (uint32_t)(hi - lo);
-        return s;
+        if (!from) return {0, 0, 0, 0, c};
+        return span_of(from, from + (rows - 1) * ld + c, from + r * ld, c);
     }
     // elements from the 16-byte boundary to a row's first one
     __device__ __forceinline__ int offset(const T* from, int64_t r) const
@@ -520,6 +529,268 @@ __global__ void __launch_bounds__(THREADS, BLOCKS) ln_bwd_kernel(LnArgs a)
     }
 }
 
+// Short rows that lie one after another: W lanes take a row, a warp 32/W of them at a time; `batch` of them on their way in
+// one bulk copy, two such places to a warp.
+template <class T, bool VEC, int W, int TENSORS>
+struct Batches {
+    static constexpr int AT_ONCE = 32 / W;
+    int batch, slot, pitch, c;
+    int64_t rows;
+    uint64_t* bars;
+    char* ring;  // of this warp
+    int* abort;
+    unsigned phase;
+
+    static __host__ __device__ size_t head() { return 128 + kBlock / 32 * 2 * sizeof(uint64_t); }
+
+    __device__ __forceinline__ void set(const LnArgs& a, char* smem)
+    {
+        batch = a.batch, slot = a.slot, pitch = (a.res ? TENSORS : TENSORS - 1) * slot, c = a.c, rows = a.rows, phase = 0;
+        const int warp = threadIdx.x >> 5;
+        abort = reinterpret_cast<int*>(smem);
+        bars = reinterpret_cast<uint64_t*>(smem + 128) + warp * 2;
+        ring = smem + (head() + 127) / 128 * 128 + (size_t)warp * 2 * pitch;
+        if (threadIdx.x == 0) *abort = 0;
+        if ((threadIdx.x & 31) == 0) {
+            mbar_init(&bars[0], 1);
+            mbar_init(&bars[1], 1);
+            fence_mbar_init();
+        }
+        __syncthreads();
+    }
+    __device__ __forceinline__ int count(int64_t r) const { return (int)min((int64_t)batch, rows - r); }
+    __device__ __forceinline__ Span span(const T* from, int64_t r) const
+    {
+        if (!from) return {0, 0, 0, 0, 0};
+        return span_of(from, from + rows * c, from + r * c, count(r) * c);
+    }
+    // One lane's work: the rows from r into place k.
+    __device__ __forceinline__ void fetch(const T* const (&from)[TENSORS], int k, int64_t r) const
+    {
+        Span sp[TENSORS];
+        uint32_t sum = 0;
+#pragma unroll
+        for (int t = 0; t < TENSORS; ++t) sp[t] = span(from[t], r), sum += sp[t].bytes;
+        mbar_arrive_expect_tx(&bars[k], sum);
+#pragma unroll
+        for (int t = 0; t < TENSORS; ++t)
+            if (sp[t].bytes) bulk_load(smem_u32(ring + (size_t)k * pitch + t * slot) + sp[t].skip, sp[t].lo, sp[t].bytes, &bars[k]);
+    }
+    __device__ __forceinline__ const char* place(int k, int t) const { return ring + (size_t)k * pitch + t * slot; }
+    // elements from the 16-byte boundary to the first one of row r
+    __device__ __forceinline__ int offset(const T* from, int64_t r) const
+    {
+        return VEC ? 0 : (int)((reinterpret_cast<uintptr_t>(from + r * c) & 15) / sizeof(T));
+    }
+    __device__ __forceinline__ void wait(const T* const (&from)[TENSORS], int k, int64_t r)
+    {
+        bounded_wait(&bars[k], phase >> k & 1, abort, &g_ln_status);
+        phase ^= 1u << k;
+        if (VEC || (r > 16 && r + batch + 16 < rows)) return;
+        T v[TENSORS];
+        int at[TENSORS];
+        const int lane = threadIdx.x & 31, len = count(r) * c;
+#pragma unroll
+        for (int t = 0; t < TENSORS; ++t) {
+            const Span s = span(from[t], r);
+            at[t] = !from[t] ? len : lane < s.head ? lane : s.tail + lane - s.head;
+            if (at[t] < len) v[t] = from[t][r * c + at[t]];
+        }
+#pragma unroll
+        for (int t = 0; t < TENSORS; ++t)
+            if (at[t] < len) (reinterpret_cast<T*>(ring + (size_t)k * pitch + t * slot) + offset(from[t], r))[at[t]] = v[t];
+        fence_async_shared();
+        __syncwarp();
+    }
+    static __device__ __forceinline__ float total(float v)
+    {
+#pragma unroll
+        for (int o = W / 2; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+        return v;
+    }
+};
+
+template <class T, bool VEC, int W>
+__global__ void __launch_bounds__(kBlock, kShortFwd) ln_fwd_short_kernel(LnArgs a)
+{
+    typedef Cols<T, VEC, false, 8, W> C;
+    constexpr int P = C::P;
+    extern __shared__ __align__(128) char smem[];
+    Batches<T, VEC, W, 2> w;
+    w.set(a, smem);
+    const T* const from[2] = {static_cast<const T*>(a.x), static_cast<const T*>(a.res)};
+    const int lane = threadIdx.x & 31, g = lane % W, sub = lane / W;
+    const int64_t hop = (int64_t)gridDim.x * (kBlock / 32) * a.batch;
+    int64_t r = ((int64_t)blockIdx.x * (kBlock / 32) + (threadIdx.x >> 5)) * a.batch;
+    if (lane == 0)
+        for (int k = 0; k < 2; ++k)
+            if (r + k * hop < a.rows) w.fetch(from, k, r + k * hop);
+    float2 ga[4], be[4];
+#pragma unroll
+    for (int j = 0; j < C::J; ++j) {
+        C::param(ga + j * P, a.gamma, 1.f, a.c, g, j);
+        C::param(be + j * P, a.beta, 0.f, a.c, g, j);
+    }
+    const float inv_c = 1.f / a.c;
+    for (int k = 0; r < a.rows; r += hop, k ^= 1) {
+        const int n = w.count(r);
+        w.wait(from, k, r);
+        const int off = w.offset(from[0], r), off_r = w.offset(from[1], r);
+#pragma unroll 2
+        for (int i = sub; i < a.batch; i += w.AT_ONCE) {  // a whole number of times; rows past the last are not stored
+            if (i - sub >= n) break;
+            const int64_t row = r + i;
+            const int skip = i * a.c, bytes = VEC ? skip * (int)sizeof(T) : 0;
+            float2 v[4], s = both(0.f);
+#pragma unroll
+            for (int j = 0; j < C::J; ++j) {
+                C::read(v + j * P, w.place(k, 0) + bytes, off + skip, a.c, g, j);
+                if (a.res) {
+                    float2 u[P];
+                    C::read(u, w.place(k, 1) + bytes, off_r + skip, a.c, g, j);
+#pragma unroll
+                    for (int q = 0; q < P; ++q) v[j * P + q] = __fadd2_rn(v[j * P + q], u[q]);
+                }
+                if (a.sum && i < n) C::write(static_cast<T*>(a.sum) + row * a.ld_out, v + j * P, a.c, g, j);
+            }
+#pragma unroll
+            for (int q = 0; q < 4; ++q) s = __fadd2_rn(s, v[q]);
+            const float mean = w.total(s.x + s.y) * inv_c;
+            s = both(0.f);
+#pragma unroll
+            for (int j = 0; j < C::J; ++j) {
+                const int i0 = C::col(j, g);
+#pragma unroll
+                for (int q = j * P; q < (j + 1) * P; ++q) {
+                    v[q] = __fadd2_rn(v[q], both(-mean));
+                    if (VEC) {
+                        if (i0 < a.c) s = __ffma2_rn(v[q], v[q], s);
+                    } else {
+                        if (i0 < a.c) s.x = fmaf(v[q].x, v[q].x, s.x);
+                        if (i0 + C::MATE < a.c) s.y = fmaf(v[q].y, v[q].y, s.y);
+                    }
+                }
+            }
+            const float inv = 1.f / sqrtf(fmaf(w.total(s.x + s.y), inv_c, a.eps));
+#pragma unroll
+            for (int q = 0; q < 4; ++q) v[q] = __ffma2_rn(__fmul2_rn(v[q], both(inv)), ga[q], be[q]);
+            if (i < n) {
+#pragma unroll
+                for (int j = 0; j < C::J; ++j) C::write(static_cast<T*>(a.y) + row * a.ld_out, v + j * P, a.c, g, j);
+                if (g == 0 && a.mean) {
+                    a.mean[row] = mean;
+                    a.invstd[row] = inv;
+                }
+            }
+        }
+        __syncwarp();
+        if (lane == 0 && r + 2 * hop < a.rows) w.fetch(from, k, r + 2 * hop);
+    }
+    linger(w.abort);
+}
+
+template <class T, bool VEC, int W>
+__global__ void __launch_bounds__(kBlock, kShortBwd) ln_bwd_short_kernel(LnArgs a)
+{
+    typedef Cols<T, VEC, false, 8, W> C;
+    constexpr int P = C::P;
+    extern __shared__ __align__(128) char smem[];
+    Batches<T, VEC, W, 3> w;
+    w.set(a, smem);
+    const T* const from[3] = {static_cast<const T*>(a.x), static_cast<const T*>(a.dy), static_cast<const T*>(a.res)};
+    const int lane = threadIdx.x & 31, g = lane % W, sub = lane / W;
+    const int64_t hop = (int64_t)gridDim.x * (kBlock / 32) * a.batch;
+    int64_t r = ((int64_t)blockIdx.x * (kBlock / 32) + (threadIdx.x >> 5)) * a.batch;
+    if (lane == 0)
+        for (int k = 0; k < 2; ++k)
+            if (r + k * hop < a.rows) w.fetch(from, k, r + k * hop);
+    // a batch's statistics, a row's in its lane, asked for a batch ahead
+    float mean = 0.f, inv = 0.f;
+    auto ask = [&](int64_t r) {
+        const bool there = lane < a.batch && r + lane < a.rows;
+        mean = there ? a.mean[r + lane] : 0.f, inv = there ? a.invstd[r + lane] : 0.f;
+    };
+    ask(r);
+    grid_dependency_trigger();
+    float2 ga[4], dg[4], db[4];
+#pragma unroll
+    for (int j = 0; j < C::J; ++j) C::param(ga + j * P, a.gamma, 1.f, a.c, g, j);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) dg[q] = db[q] = both(0.f);
+    const float inv_c = 1.f / a.c;
+    for (int k = 0; r < a.rows; r += hop, k ^= 1) {
+        const int n = w.count(r);
+        w.wait(from, k, r);
+        const int off_x = w.offset(from[0], r), off_d = w.offset(from[1], r), off_s = w.offset(from[2], r);
+        const float mu_all = mean, is_all = inv;
+        ask(r + hop);
+#pragma unroll 2
+        for (int i = sub; i < a.batch; i += w.AT_ONCE) {
+            if (i - sub >= n) break;
+            const int skip = i * a.c, bytes = VEC ? skip * (int)sizeof(T) : 0;
+            const float mu = __shfl_sync(0xffffffffu, mu_all, i), is = __shfl_sync(0xffffffffu, is_all, i);
+            float2 h[4], d[4], tx = both(0.f), ty = tx;
+#pragma unroll
+            for (int j = 0; j < C::J; ++j) {
+                C::read(h + j * P, w.place(k, 0) + bytes, off_x + skip, a.c, g, j);
+                C::read(d + j * P, w.place(k, 1) + bytes, off_d + skip, a.c, g, j);
+            }
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {  // past the row's end d is 0
+                if (i >= n) h[q] = d[q] = both(0.f);
+                h[q] = __fmul2_rn(__fadd2_rn(h[q], both(-mu)), both(is));
+                dg[q] = __ffma2_rn(d[q], h[q], dg[q]);
+                db[q] = __fadd2_rn(db[q], d[q]);
+                d[q] = __fmul2_rn(d[q], ga[q]);
+                tx = __fadd2_rn(tx, d[q]);
+                ty = __ffma2_rn(d[q], h[q], ty);
+            }
+            tx = both(-w.total(tx.x + tx.y) * inv_c * is), ty = both(-w.total(ty.x + ty.y) * inv_c * is);
+#pragma unroll
+            for (int j = 0; j < C::J; ++j) {
+                float2 u[P];
+#pragma unroll
+                for (int q = 0; q < P; ++q) u[q] = __ffma2_rn(h[j * P + q], ty, __ffma2_rn(d[j * P + q], both(is), tx));
+                if (a.res) {
+                    float2 e[P];
+                    C::read(e, w.place(k, 2) + bytes, off_s + skip, a.c, g, j);
+#pragma unroll
+                    for (int q = 0; q < P; ++q) u[q] = __fadd2_rn(u[q], e[q]);
+                }
+                if (i < n) C::write(static_cast<T*>(a.y) + (r + i) * a.ld_out, u, a.c, g, j);
+            }
+        }
+        __syncwarp();
+        if (lane == 0 && r + 2 * hop < a.rows) w.fetch(from, k, r + 2 * hop);
+    }
+    linger(w.abort);
+    if (!a.parts) return;
+    // the sums of a warp's rows at a time, then of the block's warps
+    float* sums = reinterpret_cast<float*>(smem + (w.head() + 127) / 128 * 128);
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < C::J; ++j)
+#pragma unroll
+        for (int q = 0; q < P; ++q) {
+            float2 x = dg[j * P + q], y = db[j * P + q];
+#pragma unroll
+            for (int o = W; o < 32; o <<= 1) {
+                x.x += __shfl_xor_sync(0xffffffffu, x.x, o), x.y += __shfl_xor_sync(0xffffffffu, x.y, o);
+                y.x += __shfl_xor_sync(0xffffffffu, y.x, o), y.y += __shfl_xor_sync(0xffffffffu, y.y, o);
+            }
+            const int i = C::col(j, g) + 2 * q, m = i + C::MATE;
+            float* to = sums + (threadIdx.x >> 5) * 2 * a.c;
+            if (sub == 0 && i < a.c) to[i] = x.x, to[a.c + i] = y.x;
+            if (sub == 0 && m < a.c) to[m] = x.y, to[a.c + m] = y.y;
+        }
+    __syncthreads();
+    for (int i = threadIdx.x; i < 2 * a.c; i += kBlock) {
+        float t = 0.f;
+        for (int k = 0; k < kBlock / 32; ++k) t += sums[k * 2 * a.c + i];
+        a.parts[(int64_t)blockIdx.x * 2 * a.c + i] = t;
+    }
+}
+
 // Rows of more columns than a block holds: a block per row, which it reads once per step (from L2 but for the first).
 template <class T>
 __global__ void __launch_bounds__(kWide) ln_fwd_wide_kernel(LnArgs a)
@@ -665,6 +936,28 @@ Plan plan_of(LnArgs& a, int n, int c, int tensors, int resident, int split, size
     return p;
 }
 
+bool is_short(const LnArgs& a) { return a.c <= kShort && a.ld_in == a.c; }
+int lanes_of(const LnArgs& a) { return a.c <= 64 ? 8 : a.c <= 128 ? 16 : 32; }
+
+// Short rows: as many to a place as fill an SM's shared memory with what is on its way of `tensors`, but no more than leave
+// every warp some.
+Plan short_plan(LnArgs& a, int tensors, int there, int on_sm, size_t e)
+{
+    const int at_once = 32 / lanes_of(a), warps = kBlock / 32;
+    const size_t room = kRingBytes / on_sm / (warps * 2 * tensors) - 160;  // of a place, for one tensor
+    const int64_t even = (a.rows + (int64_t)on_sm * sm_count() * warps * at_once - 1) / ((int64_t)on_sm * sm_count() * warps * at_once);
+    const int64_t times = std::max<int64_t>(1, std::min<int64_t>({even, (int64_t)(room / (a.c * e * at_once)), 32 / at_once}));
+    a.batch = (int)times * at_once;
+    a.slot = (int)((a.batch * a.c * e + 32 + 127) / 128 * 128);
+    Plan p;
+    p.threads = kBlock;
+    p.split = 1;
+    p.smem = (Batches<float, true, 32, 1>::head() + 127) / 128 * 128 +
+             std::max((size_t)warps * 2 * there * a.slot, (size_t)warps * 2 * a.c * sizeof(float));
+    p.teams = (int)std::max<int64_t>(1, std::min<int64_t>((a.rows + (int64_t)a.batch * warps - 1) / ((int64_t)a.batch * warps), (int64_t)on_sm * sm_count()));
+    return p;
+}
+
 // Rows of up to 16 columns for each of a group's threads, wider ones by clusters of such blocks.
 bool held(const LnArgs& a) { return a.c <= 16 * kMaxGroup * kMaxSplit; }
 Plan plan_wide(LnArgs& a, int tensors, size_t e)
@@ -679,7 +972,7 @@ Plan plan_wide(LnArgs& a, int tensors, size_t e)
 Plan bwd_plan(LnArgs& a, size_t e)
 {
     if (!held(a)) return {kWide, (int)std::max<int64_t>(1, std::min<int64_t>((a.rows + 15) / 16, 64)), 0, 1};
-    if (a.c <= 256) return plan_of(a, 8, a.c, 3, 3 * kBlock, 1, e);
+    if (is_short(a)) return short_plan(a, 3, a.res ? 3 : 2, kShortBwd, e);
     if (a.c <= 16 * kBlock) return plan_of(a, 16, a.c, 3, 2 * kBlock, 1, e);
     return plan_wide(a, 3, e);
 }
@@ -718,10 +1011,12 @@ int run_fwd(LnArgs a, cudaStream_t st)
     const char* what = "layer_norm_fwd";
     constexpr size_t e = sizeof(T);
     if (held(a)) {
-        constexpr int B8 = VEC ? 4 : 3, B16 = VEC ? 3 : 2;
-        if (a.c <= 256) {
-            const Plan p = plan_of(a, 8, a.c, 2, kBlock * B8, 1, e);
-            return run_fwd_held<T, VEC, 8, kBlock, B8, false>(a, p, st, what);
+        constexpr int B16 = VEC ? 3 : 2;
+        if (is_short(a)) {
+            const Plan p = short_plan(a, a.res ? 2 : 1, a.res ? 2 : 1, kShortFwd, e);
+            if (a.c <= 64) return launch<ln_fwd_short_kernel<T, VEC, 8>>(a, p, st, what);
+            if (a.c <= 128) return launch<ln_fwd_short_kernel<T, VEC, 16>>(a, p, st, what);
+            return launch<ln_fwd_short_kernel<T, VEC, 32>>(a, p, st, what);
         }
         if (a.c <= 16 * kBlock) {
             const Plan p = plan_of(a, 16, a.c, 2, kBlock * B16, 1, e);
@@ -748,7 +1043,11 @@ int run_bwd(const LnArgs& a, const Plan& p, cudaStream_t st)
     const char* what = "layer_norm_bwd";
     if (a.rows == 0) return DBL_OK;
     if (held(a)) {
-        if (a.c <= 256) return run_bwd_held<T, VEC, 8, kBlock, 3, false>(a, p, st, what);
+        if (is_short(a)) {
+            if (a.c <= 64) return launch<ln_bwd_short_kernel<T, VEC, 8>>(a, p, st, what);
+            if (a.c <= 128) return launch<ln_bwd_short_kernel<T, VEC, 16>>(a, p, st, what);
+            return launch<ln_bwd_short_kernel<T, VEC, 32>>(a, p, st, what);
+        }
         if (a.c <= 16 * kBlock) return run_bwd_held<T, VEC, 16, kBlock, 2, false>(a, p, st, what);
         if (p.split == 1) return run_bwd_held<T, VEC, 16, kMaxGroup, 1, false>(a, p, st, what);
         return run_bwd_held<T, VEC, 16, kMaxGroup, 1, true>(a, p, st, what);
@@ -810,6 +1109,8 @@ int dbl_layer_norm_bwd(const dbl_ln_shape* s, const void* dy, const void* dskip,
         !aligned_to(save_mean, 4) || !aligned_to(save_invstd, 4) || !aligned_to(dgamma, 4) || !aligned_to(dbeta, 4))
         return set_error(DBL_ERR_INVALID, "layer_norm_bwd: a pointer is not aligned to its element type");
     LnArgs a = args(s);
+    a.x = x, a.res = dskip, a.dy = dy, a.gamma = gamma, a.y = dx, a.parts = dgamma ? static_cast<float*>(ws) : nullptr;
+    a.mean = const_cast<float*>(save_mean), a.invstd = const_cast<float*>(save_invstd);
     const Plan p = bwd_plan(a, e);
     if (dgamma) {
         if (!ws || ws_bytes < (size_t)p.teams * 2 * s->c * sizeof(float))
@@ -817,8 +1118,6 @@ int dbl_layer_norm_bwd(const dbl_ln_shape* s, const void* dy, const void* dskip,
         if (!aligned16(ws)) return set_error(DBL_ERR_INVALID, "layer_norm_bwd: workspace must be 16-byte aligned");
     }
     cudaStream_t st = as_stream(stream);
-    a.x = x, a.res = dskip, a.dy = dy, a.gamma = gamma, a.y = dx, a.parts = dgamma ? static_cast<float*>(ws) : nullptr;
-    a.mean = const_cast<float*>(save_mean), a.invstd = const_cast<float*>(save_invstd);
     if (s->dtype == DBL_F32)
         rc = vec_of(a, e) ? run_bwd<float, true>(a, p, st) : run_bwd<float, false>(a, p, st);
     else

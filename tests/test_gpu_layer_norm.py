@@ -38,7 +38,9 @@ SHAPES = [(1, 1, 0, 0, 0), (3, 7, 0, 0, 0), (5, 8, 0, 0, 0), (33, 100, 0, 0, 0),
           (6, 1023, 1, 1, 0), (130, 2048, 0, 0, 0), (11, 2050, 0, 0, 2), (3, 4097, 0, 0, 0), (40, 8192, 0, 0, 0),
           (2, 16384, 0, 0, 0), (2, 20000, 0, 0, 0), (2, 32768, 0, 0, 0), (2, 70001, 0, 0, 0), (3000, 24, 0, 0, 0),
           (10007, 3, 0, 0, 0), (2500, 256, 0, 0, 0), (1, 65536, 0, 0, 0), (300, 1002, 0, 0, 0), (40, 10447, 0, 0, 0),
-          (37, 9001, 3, 0, 1), (400, 8208, 0, 8, 0), (90, 16000, 0, 0, 0), (45, 33333, 0, 0, 0)]
+          (37, 9001, 3, 0, 1), (400, 8208, 0, 8, 0), (90, 16000, 0, 0, 0), (45, 33333, 0, 0, 0), (40000, 5, 0, 0, 0), (9000, 64, 0, 0, 0),
+          (9001, 33, 0, 2, 3), (20011, 101, 0, 0, 1), (6007, 128, 0, 0, 0), (5003, 200, 0, 8, 0), (5001, 255, 0, 0, 0),
+          (5001, 250, 6, 0, 0), (1, 3, 0, 0, 1)]
 
 
 @pytest.mark.parametrize("kind", ["bf16", "f16", "f32"])
