@@ -43,6 +43,21 @@ struct LnArgs {
     int batch;               // short rows at a time
 };
 
+// Loads that stay where they are written: the compiler moves others behind the wait for the row, where nothing hides them
+// (backward of 65536 x 2048: 173 and 204 us; of 40000 x 1001 95 and 101).  Not for single fp32 columns, which take the
+// registers for more addresses (10007 x 1537: 60 us, 54 where the compiler chooses).  v is left as it is where `there`
+// does not hold.
+__device__ __forceinline__ void ask(float4& v, const float* p, bool there)
+{
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.s32 p, %5, 0;\n\t@p ld.global.nc.v4.f32 {%0, %1, %2, %3}, [%4];\n\t}"
+                 : "+f"(v.x), "+f"(v.y), "+f"(v.z), "+f"(v.w)
+                 : "l"(p), "r"((int)there));
+}
+__device__ __forceinline__ void ask(float& v, const float* p, bool there)
+{
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.s32 p, %2, 0;\n\t@p ld.global.nc.f32 %0, [%1];\n\t}" : "+f"(v) : "l"(p), "r"((int)there));
+}
+
 // This thread's columns of a row, in pairs: J accesses of 16 bytes where rows allow it (VEC; FULL: every thread has all
 // of its columns), otherwise of 4 bytes.
 template <class T, bool VEC, bool FULL, int N, int W = 32>
@@ -52,7 +67,7 @@ struct Cols {
     // a warp, 16-bit ones in a thread, which can store them at once in rows that begin at a word
     static constexpr bool ASIDE = !VEC && sizeof(T) == 4;
     static constexpr int MATE = ASIDE ? W : 1;
-    static __device__ __forceinline__ int base(int g) { return g / W * W * N + g % W * (ASIDE ? 1 : A); }
+    static __device__ __forceinline__ int base(int g) { return (g & ~(W - 1)) * N + (g & (W - 1)) * (ASIDE ? 1 : A); }
     static __device__ __forceinline__ int col(int j, int g) { return base(g) + j * W * A; }
     static __device__ __forceinline__ float2 pair(const T* p) { return make_float2(elem_f(p[0]), elem_f(p[1])); }
     // access j of a row in shared memory that begins `off` elements after row; zeros past its end
@@ -132,15 +147,21 @@ struct Cols {
         const int i = col(j, g);
 #pragma unroll
         for (int k = 0; k < P; ++k) {
-            f[k] = make_float2(other, other);
             if constexpr (VEC) {
-                if (p && (FULL || i < c)) {
-                    const float4 q = __ldg(reinterpret_cast<const float4*>(p + i) + k / 2);
-                    f[k] = k & 1 ? make_float2(q.z, q.w) : make_float2(q.x, q.y);
+                if (k % 2 == 0) {
+                    float4 q = make_float4(other, other, other, other);
+                    ask(q, p + i + 2 * k, p && (FULL || i < c));
+                    f[k] = make_float2(q.x, q.y), f[k + 1] = make_float2(q.z, q.w);
                 }
-            } else if (p) {
-                if (i < c) f[k].x = __ldg(p + i);
-                if (i + MATE < c) f[k].y = __ldg(p + i + MATE);
+            } else {
+                f[k] = make_float2(other, other);
+                if constexpr (!ASIDE) {
+                    ask(f[k].x, p + i, p && i < c);
+                    ask(f[k].y, p + i + MATE, p && i + MATE < c);
+                } else if (p) {
+                    if (i < c) f[k].x = __ldg(p + i);
+                    if (i + MATE < c) f[k].y = __ldg(p + i + MATE);
+                }
             }
         }
     }
