@@ -5,7 +5,13 @@
 // q, and the gradient is the same exponentials times a factor, but for the k classes of the teacher and the label's.
 // Bound by memory as long as a row is read once: a block, or a cluster of blocks for a long row, brings its part of
 // the row into shared memory by one bulk copy, passes over it there three times (maximum, sums, gradient), and the
-// gradient goes back from the logits' place by another.  Blocks of a cluster exchange (maximum, sums) once.
+// gradient goes back from the logits' place by another.  Blocks of a cluster exchange (maximum, sums) once.  Sums and
+// probabilities are fp32; the gradient is rounded once, when it is stored.
+//
+// On a GB300 that copies 6.78 TB/s: 4096 x 32000 in bf16, labels and teacher, 105 us = 5.0 TB/s (three blocks on an SM
+// in turns of load, passes and store; the exponentials' unit half busy, 17 instructions an element.  Four chunks of a row,
+// loaded and stored on their own, 127 us: shorter loops).  9 x 131071 in fp16 12.5 us and 740 x 1000 in fp32 10.5 us:
+// two launches and one row's chain of load, sums and store.
 #include <math.h>
 
 #include <algorithm>

@@ -1,11 +1,20 @@
 // ln.cu -- layer norm over the last dimension, forward (with the residual addition before it) and backward (with
 // the skip path's gradient and the sums over rows for gamma and beta).
 //
-// Bound by memory.  A group of threads takes a row, 8 or 16 columns a thread, and goes on to another until there are
-// none; a group's next rows are on their way into shared memory meanwhile, each by one bulk copy, so that what is in
-// flight does not go by the registers (loads into registers a row ahead reached 0.4 of the copy rate).  A row is read
-// once and written once; the variance is taken of the deviations from the mean, so that an offset of the row costs no
-// digits.
+// With mu and s = 1/sqrt(variance + eps) of a row and h = (x - mu)*s: y = h*gamma + beta; for g = dy*gamma,
+// dx = s*(g - mean(g) - h*mean(g*h)) + dskip; dgamma = sum of dy*h over the rows, dbeta = sum of dy.  The variance is
+// taken of the deviations from the mean, so that an offset of the row costs no digits.  Rows, sums and statistics are
+// held in fp32; what is stored (the sum with the residual too) is rounded once, to the tensors' format.
+//
+// Bound by memory: a row is read once and written once.  A group of threads takes a row, 16 columns a thread, and goes
+// on to another until there are none; a group's next rows are on their way into shared memory meanwhile, each by one
+// bulk copy, so that what is in flight does not go by the registers (loads into registers a row ahead reached 0.4 of
+// the copy rate).  Rows of up to 256 columns: several to a warp.  Rows of more than 8192: a cluster of blocks each.
+//
+// On a GB300 that copies 6.78 TB/s, bf16 but where said: forward with the residual, 32768 x 1024 in fp16 52 us =
+// 5.1 TB/s (shared memory's latency between two sums over the row; 22 warps on an SM); 256 x 512 4.6 us, the launch.
+// Backward with the skip gradient, 65536 x 2048 174 us = 6.2 TB/s; 10007 x 1537 in fp32 54 us = 3.4 TB/s (rows that
+// begin at any word: 4-byte accesses, more than twice the instructions).  100000 x 64: 17.5 and 21 us.
 #include <math.h>
 
 #include <algorithm>
@@ -440,7 +449,7 @@ __global__ void __launch_bounds__(THREADS, BLOCKS) ln_fwd_kernel(LnArgs a)
     if (SPLIT) cluster_leave();
 }
 
-// x: the normalised tensor, res: dskip, y: dx.  A thread also adds up dy*xhat and dy of its columns over the rows
+// x: the normalised tensor, res: dskip, y: dx.  The row stays in registers between its two passes.  A thread also adds up dy*xhat and dy of its columns over the rows
 // that its group takes; a block leaves these sums in parts[block][2][c].
 template <class T, bool VEC, bool FULL, int N, int THREADS, int BLOCKS, bool SPLIT>
 __global__ void __launch_bounds__(THREADS, BLOCKS) ln_bwd_kernel(LnArgs a)
@@ -957,6 +966,7 @@ Plan plan_of(LnArgs& a, int n, int c, int tensors, int resident, int split, size
     return p;
 }
 
+// (100000 x 64 in bf16 with the residual: forward 17.5 us, backward 21; a row to a warp 36 and 46.)
 bool is_short(const LnArgs& a) { return a.c <= kShort && a.ld_in == a.c; }
 int lanes_of(const LnArgs& a) { return a.c <= 64 ? 8 : a.c <= 128 ? 16 : 32; }
 
@@ -979,7 +989,9 @@ Plan short_plan(LnArgs& a, int tensors, int there, int on_sm, size_t e)
     return p;
 }
 
-// Rows of up to 16 columns for each of a group's threads, wider ones by clusters of such blocks.
+// Rows of up to 16 columns for each of a group's threads, wider ones by clusters of such blocks (4000 x 16000 in bf16:
+// forward 110 us, 136 with 32 columns to a thread; backward 138, 192 with 32, which spill; clusters of four blocks of half
+// the columns 210 and 208: the exchange takes longer).
 bool held(const LnArgs& a) { return a.c <= 16 * kMaxGroup * kMaxSplit; }
 Plan plan_wide(LnArgs& a, int tensors, size_t e)
 {
