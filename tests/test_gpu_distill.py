@@ -80,7 +80,9 @@ def check(kind, seen, got, top, cls, labels, weight, tau, alpha, scale=1.0, grad
 
 SIZES = [(1, 1, 1), (3, 7, 2), (5, 10, 10), (64, 100, 5), (300, 100, 16), (33, 1000, 16), (9, 1003, 7), (4, 2048, 64),
          (7, 5000, 33), (3, 8192, 128), (2, 20001, 1), (2, 32000, 32), (3, 50008, 20), (2, 65537, 16), (1, 131071, 64),
-         (1, 260000, 8), (1, 700001, 4), (1, 2000003, 3)]
+         (1, 260000, 8), (1, 700001, 4), (1, 2000003, 3),
+         # many rows: a warp or few warps each, and parts of which two are held by an SM
+         (650, 701, 5), (700, 3000, 16), (620, 6001, 130), (700, 8001, 20), (310, 17000, 70), (240, 45001, 9)]
 
 
 @pytest.mark.parametrize("kind", ["bf16", "f16", "f32"])
@@ -202,3 +204,19 @@ def test_no_rows(D):
     loss = torch.ones(1, device="cuda")
     D.dbl_distill_fwd_bwd(D.distill_shape(0, 10, 2), 16, 16, 16, None, None, None, 16, loss, None)
     assert float(loss) == 0.0
+
+
+def test_gradient_is_the_slope_of_the_loss(D):
+    """Central differences of the call's own loss along a direction in the logits: a step of 2^-6 leaves an error of its
+    square times the third derivatives, 1e-3 of the terms at most for directions of a few units, and the loss's
+    rounding (at most 100 roundings of values up to 1 + the largest |log q|, 12 here) over the step."""
+    rows, v, k, tau, alpha = 5, 130, 9, 1.5, 0.6
+    z, top, cls, labels = problem("f32", rows, v, k, 2)
+    direction = np.random.default_rng(8).standard_normal((rows, v))
+    step = 2.0 ** -6
+    z = z.astype(np.float32).astype(np.float64)
+    ends = [call(D, "f32", z + s * direction, top, cls, labels, None, tau, alpha)[2] for s in (step, -step)]
+    slope = (float(ends[0]) - float(ends[1])) / (2 * step)
+    terms = call(D, "f32", z, top, cls, labels, None, tau, alpha)[3] * direction
+    bound = 1e-3 * np.abs(terms).sum() + 100 * EPS32 * 13 * (alpha * tau * tau + 1 - alpha) / step
+    assert abs(terms.sum() - slope) <= bound, (terms.sum(), slope, bound)

@@ -200,3 +200,35 @@ def test_on_another_stream_and_in_a_graph(D):
     torch.cuda.synchronize()
     for a, b, d in zip(want, side, graphed):
         assert torch.equal(a, b) and torch.equal(a, d)
+
+
+@pytest.mark.parametrize("rows,c", [(6, 65), (3, 700)])
+def test_gradient_is_the_slope_of_the_forward_pass(D, rows, c):
+    """Central differences of the kernel's own forward pass, along a direction in x, gamma and beta, in fp32: a step of
+    2^-7 leaves an error of its square times the third derivatives, below 16 of the terms for rows whose deviation and
+    direction are about 1, so 1e-3 of them at most; and y's rounding (64 roundings of values up to |y|) over the step."""
+    g = np.random.default_rng(rows * c)
+    x, dy, vx = g.standard_normal((rows, c)) + 0.5, g.standard_normal((rows, c)), g.standard_normal((rows, c))
+    gamma, beta, vg, vb = g.uniform(0.5, 1.5, c), g.standard_normal(c), g.standard_normal(c), g.standard_normal(c)
+    step = 2.0 ** -7
+    shape = D.ln_shape(rows, c, 1e-5, D.DBL_F32)
+    dev = lambda a: torch.from_numpy(np.ascontiguousarray(a, np.float32)).cuda()
+
+    def forward(s):
+        y, mean, inv = torch.empty(rows, c, device="cuda"), torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda")
+        tx = dev(x + s * vx)
+        D.dbl_layer_norm_fwd(shape, tx, None, dev(gamma + s * vg), dev(beta + s * vb), None, y, mean, inv)
+        torch.cuda.synchronize()
+        return y.double().cpu().numpy(), tx, mean, inv
+
+    up, down = forward(step)[0], forward(-step)[0]
+    slope = float(((up - down) / (2 * step) * dy.astype(np.float32)).sum())
+    y, tx, mean, inv = forward(0.0)
+    dx, dg, db = torch.empty(rows, c, device="cuda"), torch.empty(c, device="cuda"), torch.empty(c, device="cuda")
+    need = D.dbl_layer_norm_workspace_bytes(shape)
+    ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+    D.dbl_layer_norm_bwd(shape, dev(dy), None, tx, dev(gamma), mean, inv, dx, dg, db, ws, need)
+    check_status(D)
+    parts = [a.double().cpu().numpy() * v for a, v in ((dx, vx), (dg, vg), (db, vb))]
+    bound = 1e-3 * sum(np.abs(a).sum() for a in parts) + 64 * EPS32 * np.abs(y * dy).sum() / step
+    assert abs(sum(a.sum() for a in parts) - slope) <= bound, (sum(a.sum() for a in parts), slope, bound)
