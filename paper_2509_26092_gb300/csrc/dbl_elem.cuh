@@ -27,6 +27,35 @@ int allow_launch(size_t bytes, bool large_clusters, const char* what)
     return rc;
 }
 
+// Clusters of S blocks that the device holds at a time, 0 where none; KERNEL's launches of S blocks have the same threads and
+// shared memory, or these are their bounds.  Asked once per device, after allow_launch.
+template <auto KERNEL>
+int clusters_held(int dev, int S, int threads, size_t smem)
+{
+    static std::atomic<int> known[64][17] = {};
+    if (S > 1 && S > max_cluster()) return 0;
+    const bool keep = dev >= 0 && dev < 64 && S <= 16;
+    if (keep)
+        if (const int k = known[dev][S]) return k - 1;
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = S;
+    at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+    cfg.gridDim = dim3(S);
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    int n = 0;
+    if (cudaOccupancyMaxActiveClusters(&n, KERNEL, &cfg) != cudaSuccess) {
+        (void)cudaGetLastError();
+        n = 0;
+    }
+    if (keep) known[dev][S] = n + 1;
+    return n;
+}
+
 namespace dev {
 
 __device__ __forceinline__ float elem_f(float v) { return v; }

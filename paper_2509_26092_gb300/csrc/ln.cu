@@ -35,6 +35,7 @@ constexpr int kShort = 256;        // columns of a short row, at the most
 constexpr int kShortFwd = 3, kShortBwd = 2;  // blocks on an SM for them
 constexpr int kSumThreads = 1024;
 constexpr size_t kRingBytes = 200 * 1024;  // shared memory for them on an SM
+constexpr size_t kMaxSmem = kRingBytes + 16 * 1024;
 
 __device__ int g_ln_status;
 
@@ -992,12 +993,23 @@ Plan short_plan(LnArgs& a, int tensors, int there, int on_sm, size_t e)
 // Rows of up to 16 columns for each of a group's threads, wider ones by clusters of such blocks (4000 x 16000 in bf16:
 // forward 110 us, 136 with 32 columns to a thread; backward 138, 192 with 32, which spill; clusters of four blocks of half
 // the columns 210 and 208: the exchange takes longer).
-bool held(const LnArgs& a) { return a.c <= 16 * kMaxGroup * kMaxSplit; }
+bool held(const LnArgs& a) { return a.c <= 16 * kMaxGroup * std::min(kMaxSplit, std::max(1, max_cluster())); }
 Plan plan_wide(LnArgs& a, int tensors, size_t e)
 {
     const int S = (a.c + 16 * kMaxGroup - 1) / (16 * kMaxGroup);
     a.part = ((a.c + S - 1) / S + 15) / 16 * 16;  // whole 16-byte units; the last block's may be fewer
-    return plan_of(a, 16, std::min(a.part, a.c), tensors, kMaxGroup, S, e);
+    Plan p = plan_of(a, 16, std::min(a.part, a.c), tensors, kMaxGroup, S, e);
+    int dev = 0;
+    if (S > 1 && cudaGetDevice(&dev) == cudaSuccess) {
+        // no more clusters than the device holds (15 of seven blocks, not 21: backward of 700 x 50000 122 and 167 us), by
+        // one kernel for all, each of which takes an SM's registers
+        constexpr auto kernel = ln_bwd_kernel<act_t, true, false, 16, kMaxGroup, 1, true>;
+        const int fit = allow_launch<kernel>(kMaxSmem, false, "layer_norm") == DBL_OK ? clusters_held<kernel>(dev, S, kMaxGroup, kMaxSmem) : 0;
+        if (fit) p.teams = std::min(p.teams, fit);
+    } else if (S > 1) {
+        (void)cudaGetLastError();
+    }
+    return p;
 }
 
 // The backward pass's blocks or clusters, each of which leaves a row of partial column sums.  By the sizes alone, as the
@@ -1013,7 +1025,7 @@ Plan bwd_plan(LnArgs& a, size_t e)
 template <auto KERNEL>
 int launch(const LnArgs& a, const Plan& p, cudaStream_t st, const char* what)
 {
-    const int rc = allow_launch<KERNEL>(kRingBytes + 16 * 1024, false, what);
+    const int rc = allow_launch<KERNEL>(kMaxSmem, false, what);
     if (rc != DBL_OK) return rc;
     cudaLaunchConfig_t cfg = {};
     cudaLaunchAttribute at[1];

@@ -10,7 +10,7 @@
 //
 // Bound by memory where there are sequences enough, otherwise by the chain of parts: exchange of the pairs, state for
 // the next part.  On a GB300 that copies 6.78 TB/s, bf16 but where said: backward of 8 x 8192 x 1024 124 us = 5.4 TB/s;
-// forward of 1 x 65536 x 512 81 us = 2.5 TB/s, 16 parts of 4096 steps at 5 us each; of 185 x 196 x 256 in fp16 23 us =
+// forward of 1 x 65536 x 512 60 us = 3.4 TB/s, 22 parts of 3072 steps at 2.7 us each; of 185 x 196 x 256 in fp16 23 us =
 // 2.5 TB/s, 740 blocks in three rounds; one token of 64 x 512 4.5 us, the launch; backward of 12 x 3001 x 393 with
 // lengths 73 us = 1.4 TB/s (rows that begin anywhere: 190 instructions a step of 64 channels, 77 where TMA brings them).
 #include <math.h>
@@ -835,30 +835,57 @@ int encode(CUtensorMap* m, const void* p, const ScanArgs& a, int64_t ld, int col
     return r == CUDA_SUCCESS ? DBL_OK : set_error(DBL_ERR_CUDA, "%s: tensor map (%d)", what, (int)r);
 }
 
-template <class T, bool ALIGNED, int LANES, int R, int BLOCKS, bool BWD>
-int launch_tiles(ScanArgs a, cudaStream_t st, const char* what)
+template <class T, bool ALIGNED, int LANES, int R, bool BWD>
+size_t smem_of(int S, int warps)
 {
-    constexpr auto kernel = kernel_of<T, ALIGNED, LANES, R, BLOCKS, BWD>();
-    typedef Stage<T, ALIGNED, LANES, R> St;
     typedef FwdSmem<T, ALIGNED, LANES, R> Fwd;
     typedef BwdSmem<T, ALIGNED, LANES, R> Bwd;
-    auto smem_of = [&](int S, int warps) {
-        return (BWD ? sizeof(Bwd) + warps * sizeof(typename Bwd::Stages) : sizeof(Fwd) + warps * sizeof(typename Fwd::Stages)) +
-               (S > 1 ? sizeof(float4) * 2 * S * LANES : 0);
-    };
-    a.groups = (a.c + 2 * LANES - 1) / (2 * LANES);
-    const int64_t cols = (int64_t)a.n * a.groups;
+    return (BWD ? sizeof(Bwd) + warps * sizeof(typename Bwd::Stages) : sizeof(Fwd) + warps * sizeof(typename Fwd::Stages)) +
+           (S > 1 ? sizeof(float4) * 2 * S * LANES : 0);
+}
+
+// How a launch is split, and about how long it takes, in fourths of what a part takes without an exchange.
+struct Split {
+    int subs, S;
+    int64_t cols, cost;
+};
+
+// Blocks of a cluster: the fewest parts one after another.  How many clusters the device holds at a time depends on where
+// they fit, and one more waits until another is done (152 SMs hold 14 clusters of 16 blocks, 23 of 12, 36 of 8, 74 of 4 and
+// 152 of 2, two blocks on an SM: forward, 1 x 65536 x 512, 16 clusters of 16 blocks 83 us, of 12 60 us).  An exchange takes
+// a part a fourth longer (185 x 196 x 256: no exchange 24 us, clusters of two 30), a cluster's start takes about a part,
+// and rows of fewer channels are slower to bring (8 lanes and 32: forward, 4 x 8192 x 1024 54 and 46 us, backward 98 and
+// 69; 16 lanes and 32: backward, 15 x 1154 x 1660 87 and 82).
+template <class T, bool ALIGNED, int LANES, int R, int BLOCKS, bool BWD>
+int split_of(const ScanArgs& a, int dev, Split& best, const char* what)
+{
+    constexpr auto kernel = kernel_of<T, ALIGNED, LANES, R, BLOCKS, BWD>();
+    const int rc = allow_launch<kernel>(smem_of<T, ALIGNED, LANES, R, BWD>(kMaxCluster, kThreads / 32), true, what);
+    if (rc != DBL_OK) return rc;
     // parts of whole chunks, where there are several; whole warps
     int subs = std::min(kThreads / LANES, (a.t + R - 1) / R);
     const int unit = subs * R < a.t ? std::max(kChunk / R, 32 / LANES) : 32 / LANES;
     subs = (subs + unit - 1) / unit * unit;
-    // As many blocks to a cluster as leave all of them resident, two on an SM: with fewer the SMs idle, with more the
-    // clusters take turns (backward, 8 x 8192 x 1024: 1, 2 and 4 blocks 144, 124 and 130 us; forward, 4 x 8192 x 1024:
-    // 2, 4 and 9 blocks 60, 46 and 65 us; 185 x 196 x 256: 1 and 2 blocks 24 and 30 us).  The same where there are
-    // lengths (12 x 3001 x 392: 38 us, with half as many again 48).
-    int S = (int)std::max<int64_t>(1, std::min<int64_t>({kMaxCluster, 2 * sm_count() / cols, (a.t + subs * R - 1) / (subs * R)}));
-    while (S > 1 && !cluster_held<kernel>(S, kThreads, smem_of(kMaxCluster, kThreads / 32))) --S;
-    if (cols * S > 0x7fffffff) return set_error(DBL_ERR_UNSUPPORTED, "%s: more than 2^31 blocks", what);
+    best = {subs, 0, (int64_t)a.n * ((a.c + 2 * LANES - 1) / (2 * LANES)), 0};
+    for (int S = 1; S <= kMaxCluster; ++S) {
+        const int held = clusters_held<kernel>(dev, S, kThreads, smem_of<T, ALIGNED, LANES, R, BWD>(S, kThreads / 32));
+        if (held == 0) continue;
+        const int64_t parts = ((int64_t)a.t + (int64_t)subs * R * S - 1) / ((int64_t)subs * R * S);
+        const int64_t cost = (best.cols + held - 1) / held * (parts + 1) * (S > 1 ? 5 : 4) * (LANES == 32 ? 10 : LANES == 16 ? 13 : 18);
+        if (best.S == 0 || cost < best.cost) best.S = S, best.cost = cost;
+        if (parts == 1) break;
+    }
+    return best.S ? DBL_OK : set_error(DBL_ERR_UNSUPPORTED, "%s: no block fits the device", what);
+}
+
+template <class T, bool ALIGNED, int LANES, int R, int BLOCKS, bool BWD>
+int launch_tiles(ScanArgs a, const Split& sp, cudaStream_t st, const char* what)
+{
+    constexpr auto kernel = kernel_of<T, ALIGNED, LANES, R, BLOCKS, BWD>();
+    typedef Stage<T, ALIGNED, LANES, R> St;
+    a.groups = (a.c + 2 * LANES - 1) / (2 * LANES);
+    const int S = sp.S, subs = sp.subs;
+    if (sp.cols * S > 0x7fffffff) return set_error(DBL_ERR_UNSUPPORTED, "%s: more than 2^31 blocks", what);
     Maps maps;
     int rc = DBL_OK;
     if (ALIGNED) {
@@ -869,21 +896,37 @@ int launch_tiles(ScanArgs a, cudaStream_t st, const char* what)
         if (BWD && rc == DBL_OK) rc = encode<T>(&maps.dz, a.dgate, a, a.ld_x, 2 * LANES, St::ROWS, what);
         if (rc != DBL_OK) return rc;
     }
-    if ((rc = allow_launch<kernel>(smem_of(kMaxCluster, kThreads / 32), true, what)) != DBL_OK) return rc;
     cudaLaunchConfig_t cfg = {};
     cudaLaunchAttribute at[1];
     at[0].id = cudaLaunchAttributeClusterDimension;
     at[0].val.clusterDim.x = S;
     at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
-    cfg.gridDim = dim3((unsigned)(cols * S));
+    cfg.gridDim = dim3((unsigned)(sp.cols * S));
     cfg.blockDim = dim3(subs * LANES);
-    cfg.dynamicSmemBytes = smem_of(S, subs * LANES / 32);
+    cfg.dynamicSmemBytes = smem_of<T, ALIGNED, LANES, R, BWD>(S, subs * LANES / 32);
     cfg.stream = st;
     cfg.attrs = at;
     cfg.numAttrs = 1;
     const cudaError_t err = cudaLaunchKernelEx(&cfg, kernel, a, maps);
     rc = launch_check(what);
     return err == cudaSuccess ? rc : cuda_check(err, what);
+}
+
+// Narrower blocks have more of them on a sequence at a time (1 x 65536 x 64, 8, 16 and 32 lanes: 30, 40 and 62 us, backward
+// 40, 55 and 93); the widest that is as good.
+template <class T, bool ALIGNED, int R, bool BWD>
+int launch_lanes(const ScanArgs& a, cudaStream_t st, const char* what)
+{
+    Split s32, s16, s8;
+    int dev = 0;
+    int rc = cuda_check(cudaGetDevice(&dev), what);
+    if (rc == DBL_OK) rc = split_of<T, ALIGNED, 32, R, 2, BWD>(a, dev, s32, what);
+    if (rc == DBL_OK) rc = split_of<T, ALIGNED, 16, R, 2, BWD>(a, dev, s16, what);
+    if (rc == DBL_OK) rc = split_of<T, ALIGNED, 8, R, 2, BWD>(a, dev, s8, what);
+    if (rc != DBL_OK) return rc;
+    if (s32.cost <= s16.cost && s32.cost <= s8.cost) return launch_tiles<T, ALIGNED, 32, R, 2, BWD>(a, s32, st, what);
+    if (s16.cost <= s8.cost) return launch_tiles<T, ALIGNED, 16, R, 2, BWD>(a, s16, st, what);
+    return launch_tiles<T, ALIGNED, 8, R, 2, BWD>(a, s8, st, what);
 }
 
 template <class T, bool BWD>
@@ -904,21 +947,10 @@ int launch(ScanArgs a, cudaStream_t st, const char* what)
         return launch_check(what);
     }
     // 16 steps a thread halve the exchanges of 8 (forward, 1 x 65536 x 512: 83 and 122 us).  fp32 has room for 8, and so
-    // have the backward pass's unaligned rows (12 x 3001 x 393: 73 us; 75 with 16, one block on an SM).  Blocks of 32
-    // channels where there are no more: half the lanes would have nothing to do.
+    // have the backward pass's unaligned rows (12 x 3001 x 393: 73 us; 75 with 16, one block on an SM).
     constexpr int R = sizeof(T) == 2 ? 16 : 8, RU = BWD ? 8 : R;
     const bool aligned = rows_at(16);
-    // Few sequences of few channels leave SMs idle even in the largest clusters: narrower blocks have more of them on
-    // the sequence at a time (1 x 65536 x 64, 8, 16 and 32 lanes: 30, 40 and 62 us, backward 40, 55 and 93; 1 x 65536 x
-    // 512, 16 and 32: 81 and 80, backward 154 and 181; 1 x 65536 x 256 in fp32: 83, 73 and 102, backward 127, 153 and 142).
-    auto narrow = [&](int lanes, int blocks) {  // up to so many blocks to an SM, and clusters that take turns on a sequence
-        return a.n * ((a.c + 2 * lanes - 1) / (2 * lanes)) * kMaxCluster <= blocks * sm_count() && a.t > kThreads / lanes * kMaxCluster * R;
-    };
-    if (narrow(8, BWD ? 2 : 1))
-        return aligned ? launch_tiles<T, true, 8, R, 2, BWD>(a, st, what) : launch_tiles<T, false, 8, RU, 2, BWD>(a, st, what);
-    if (a.c <= 32 || narrow(16, 2))
-        return aligned ? launch_tiles<T, true, 16, R, 2, BWD>(a, st, what) : launch_tiles<T, false, 16, RU, 2, BWD>(a, st, what);
-    return aligned ? launch_tiles<T, true, 32, R, 2, BWD>(a, st, what) : launch_tiles<T, false, 32, RU, 2, BWD>(a, st, what);
+    return aligned ? launch_lanes<T, true, R, BWD>(a, st, what) : launch_lanes<T, false, RU, BWD>(a, st, what);
 }
 
 int pass_through(const dbl_scan_shape* s, const float* from, float* to, cudaStream_t st)
