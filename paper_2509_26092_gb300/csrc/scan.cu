@@ -10,7 +10,7 @@
 //
 // Bound by memory where there are sequences enough, otherwise by the chain of parts: exchange of the pairs, state for
 // the next part.  On a GB300 that copies 6.78 TB/s, bf16 but where said: backward of 8 x 8192 x 1024 124 us = 5.4 TB/s;
-// forward of 1 x 65536 x 512 60 us = 3.4 TB/s, 22 parts of 3072 steps at 2.7 us each; of 185 x 196 x 256 in fp16 23 us =
+// forward of 1 x 65536 x 512 60 us = 3.4 TB/s, 22 parts one after another at 2.7 us each; of 185 x 196 x 256 in fp16 23 us =
 // 2.5 TB/s, 740 blocks in three rounds; one token of 64 x 512 4.5 us, the launch; backward of 12 x 3001 x 393 with
 // lengths 73 us = 1.4 TB/s (rows that begin anywhere: 190 instructions a step of 64 channels, 77 where TMA brings them).
 #include <math.h>
