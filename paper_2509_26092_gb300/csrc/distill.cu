@@ -15,6 +15,7 @@
 #include <math.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "dbl_elem.cuh"
 
@@ -24,7 +25,9 @@ using namespace dbl;
 using namespace dbl::dev;
 
 constexpr int kMaxThreads = 256;             // that pass over the row; a warp more takes the teacher's entries
-constexpr int kFewK = 64;                    // and up to this many, looks for classes that are named twice
+constexpr int kFewK = 64;                    // and up to this many, looks for classes that are named twice; of more all
+                                             // threads do, and bring them (4096 x 32000 in bf16, 100 entries: 120 us,
+                                             // brought by the one warp 132; 1024: 245 us, all by the one warp 968)
 constexpr int kMaxK = DBL_DISTILL_MAX_K;
 constexpr int kMaxCluster = 16;
 constexpr int kWarpRows = 4;                 // rows of a block, a warp each, where they have
@@ -135,9 +138,11 @@ struct Ahead {
     }
 };
 
-// Row r's entries, by a warp; z: the student's logits where those of the entries' classes are to be kept too.
+// Row r's entries, by a warp of which each lane has its first ones, or by `threads` threads that have none; z: the student's
+// logits where those of the entries' classes are to be kept too.
 template <class T>
-__device__ __forceinline__ void load_entries(const DistillArgs& a, int64_t r, const T* z, const Entries& en, const Ahead& ahead)
+__device__ __forceinline__ void load_entries(const DistillArgs& a, int64_t r, const T* z, const Entries& en, const Ahead* ahead,
+                                             int tid, int threads)
 {
     const float inv_tau = 1.f / a.tau;
     auto keep = [&](int j, int c, float t) {
@@ -146,12 +151,14 @@ __device__ __forceinline__ void load_entries(const DistillArgs& a, int64_t r, co
         en.lt[j] = t * inv_tau;
         if (z) en.zc[j] = there ? elem_f(z[c]) : 0.f;
     };
-    const int lane = threadIdx.x & 31, end = (a.k + 3) / 4 * 4;
+    const int end = (a.k + 3) / 4 * 4;
+    if (ahead) {
 #pragma unroll
-    for (int i = 0; i < Ahead::N; ++i)
-        if (i * 32 + lane < end) keep(i * 32 + lane, ahead.c[i], ahead.t[i]);
+        for (int i = 0; i < Ahead::N; ++i)
+            if (i * 32 + tid < end) keep(i * 32 + tid, ahead->c[i], ahead->t[i]);
+    }
 #pragma unroll 4
-    for (int j = Ahead::N * 32 + lane; j < end; j += 32)
+    for (int j = (ahead ? Ahead::N * 32 : 0) + tid; j < end; j += threads)
         keep(j, j < a.k ? __ldg(a.cls + r * a.k + j) : -1, j < a.k ? __ldg(a.top + r * a.k + j) : 0.f);
 }
 
@@ -217,7 +224,7 @@ struct Smem {
     float4 part[kMaxCluster];            // (maximum, sum at T, sum at 1) of every block of the cluster
     float4 warp[kMaxThreads / 32];       // of every warp
     uint64_t full;
-    int abort, some;
+    int abort, some, named;  // named: an entry has the label's class
     float log_t;
 };
 
@@ -244,6 +251,7 @@ template <class T, bool WARP>
 __global__ void __launch_bounds__(WARP ? 32 * kWarpRows : kMaxThreads + 32, WARP ? 10 : 3) distill_kernel(DistillArgs a, int bytes_of_group)
 {
     typedef Unit<T> U;
+    typedef typename std::conditional<sizeof(T) == 2, uint16_t, uint32_t>::type Bits;
     constexpr int E = U::E, P = U::P;
     extern __shared__ __align__(128) char smem_raw[];
     char* const base = smem_raw + (WARP ? (threadIdx.x >> 5) * bytes_of_group : 0);
@@ -273,7 +281,7 @@ __global__ void __launch_bounds__(WARP ? 32 * kWarpRows : kMaxThreads + 32, WARP
     if (WARP || side) ahead.ask(a, r);
     if (tid == 0) {
         mbar_init(&sm.full, 1);
-        sm.abort = 0;
+        sm.abort = sm.named = 0;
         fence_mbar_init();
     }
     const T* z = static_cast<const T*>(a.z) + r * a.ld;
@@ -316,14 +324,19 @@ __global__ void __launch_bounds__(WARP ? 32 * kWarpRows : kMaxThreads + 32, WARP
     }
     float zl = given && !WARP ? elem_f(z[lab]) : 0.f;
     sync();
-    if (WARP || side) {  // while the row is on its way
-        load_entries(a, r, WARP ? nullptr : z, en, ahead);
+    // while the row is on its way
+    const bool many = a.k > kFewK;
+    if (many && !WARP) {
+        load_entries<T>(a, r, z, en, nullptr, tid, blockDim.x);
+        sync();
+    }
+    if (WARP || side) {
+        if (WARP || !many) load_entries<T>(a, r, WARP ? nullptr : z, en, &ahead, tid & 31, 32);
         __syncwarp();
         float log_t;
         const bool some = teacher(a, en, log_t);
         if ((tid & 31) == 0) sm.log_t = log_t, sm.some = some;
-        if (a.k <= kFewK)
-            for (int j = tid & 31; j < a.k; j += 32) en.fix[j] = again(a, en, j) ? 1.f : 0.f;
+        for (int j = tid & 31; j < a.k; j += 32) en.fix[j] = !many && again(a, en, j) ? 1.f : 0.f;
     }
     // Two kinds of exponential where there may be two terms and T is not 1.
     const bool kl = a.k > 0 && a.alpha > 0.f, two = kl && given && a.tau != 1.f;
@@ -404,17 +417,36 @@ __global__ void __launch_bounds__(WARP ? 32 * kWarpRows : kMaxThreads + 32, WARP
         const float2 g = __fmul2_rn(exp2_2(__fmul2_rn(d, both(cA))), both(fA));
         return two ? __ffma2_rn(exp2_2(__fmul2_rn(d, both(kLog2e))), both(fB), g) : g;
     };
+    // Many entries find those of the same class through the class's place in the row, whose logit is kept and whose gradient
+    // is written last: each leaves its number there, and who reads another's marks both.
+    auto place = [&](int j) { return elems + (en.cls[j] - first); };
+    auto here = [&](int j) { return en.cls[j] >= e0 && en.cls[j] < e1; };
+    if (many) {
+        if (!side)
+            for (int j = tid; j < a.k; j += threads)
+                if (here(j)) *reinterpret_cast<Bits*>(place(j)) = (Bits)j;
+        sync();
+        if (!side)
+            for (int j = tid; j < a.k; j += threads)
+                if (here(j)) {
+                    const int other = (int)*reinterpret_cast<const Bits*>(place(j));
+                    if (other != j) en.fix[other] = en.fix[j] = 1.f;
+                }
+        sync();
+    }
     // the classes of the teacher and the label, from their logits as they were
     const bool lab_here = given && lab >= e0 && lab < e1 && tid == threads - 1;
     float fix_lab = 0.f;
     if (!side) {
         for (int j = tid; j < a.k; j += threads) {
             const int c = en.cls[j];
-            if (c < e0 || c >= e1) continue;
-            const float pj = (a.k <= kFewK ? en.fix[j] != 0.f : again(a, en, j)) ? named(a, en, c) : en.p[j];
-            en.fix[j] = grad(both(en.zc[j])).x - gt * pj - (c == lab && given ? gl : 0.f);
+            if (!here(j)) continue;
+            const float pj = en.fix[j] != 0.f ? named(a, en, c) : en.p[j];
+            const bool label = given && c == lab;
+            en.fix[j] = grad(both(en.zc[j])).x - gt * pj - (label ? gl : 0.f);
+            if (label) sm.named = 1;
         }
-        if (lab_here) fix_lab = grad(both(zl)).x - gt * named(a, en, lab) - gl;
+        if (lab_here) fix_lab = grad(both(zl)).x - gl;
         if (two) {
 #pragma unroll 2
             for (int i = tid; i < n; i += threads) {
@@ -437,8 +469,8 @@ __global__ void __launch_bounds__(WARP ? 32 * kWarpRows : kMaxThreads + 32, WARP
     sync();
     if (!side) {
         for (int j = tid; j < a.k; j += threads)
-            if (en.cls[j] >= e0 && en.cls[j] < e1) elems[en.cls[j] - first] = elem_from<T>(en.fix[j]);
-        if (lab_here) elems[lab - first] = elem_from<T>(fix_lab);
+            if (here(j)) *place(j) = elem_from<T>(en.fix[j]);
+        if (lab_here && !sm.named) elems[lab - first] = elem_from<T>(fix_lab);
     }
     const bool same = ((reinterpret_cast<uintptr_t>(dz) ^ p0) & 15) == 0;  // rows begin at the same place of a unit
     if (same) fence_async_shared();
@@ -478,7 +510,7 @@ __global__ void __launch_bounds__(kStream) distill_stream_kernel(DistillArgs a)
             float log_t;
             Ahead ahead;
             ahead.ask(a, r);
-            load_entries(a, r, z, en, ahead);
+            load_entries(a, r, z, en, &ahead, threadIdx.x, 32);
             __syncwarp();
             const bool some = teacher(a, en, log_t);
             if (threadIdx.x == 0) some_s = some, log_ts = log_t;

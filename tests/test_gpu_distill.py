@@ -171,6 +171,24 @@ def test_labels_alone_and_large_k(D, kind, v):
     check(kind, got[0], got, top, cls, labels, None, 3.0, 0.25, 256.0)
 
 
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+@pytest.mark.parametrize("v", [40, 6000, 20001, 131071])
+def test_classes_named_again_among_many(D, kind, v):
+    """A hundred entries of 37 classes and absent ones; labels among them, beside them and not given."""
+    rows, k = 5, 100
+    z, top, cls, labels = problem(kind, rows, v, k, 6)
+    g = np.random.default_rng(v)
+    few = g.choice(v, 37, replace=False)
+    cls = few[g.integers(0, 37, (rows, k))].astype(np.int32)
+    cls[g.random((rows, k)) < 0.1] = -1
+    labels[0], labels[1] = few[0], next(c for c in range(v) if c not in few)
+    cls[0, 50:53] = few[0]
+    cls[2, 1:] = -1
+    labels[3] = -1
+    got = call(D, kind, z, top, cls, labels, None, 2.0, 0.4, 64.0)
+    check(kind, got[0], got, top, cls, labels, None, 2.0, 0.4, 64.0)
+
+
 def test_the_same_bits_again_on_another_stream_and_in_a_graph(D):
     rows, v, k = 50, 3001, 20
     gen = torch.Generator(device="cuda").manual_seed(0)
