@@ -158,10 +158,16 @@ __device__ __forceinline__ void st_async2(uint32_t addr, uint32_t bar, float2 v)
                  : "memory");
 }
 
+// The cluster's barrier in two steps, nothing written before it being read after it: who has waited knows that every block
+// of the cluster has arrived, so that its shared memory is there to be written to.
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.aligned;" ::: "memory"); }
+
 // A block stays until the others no longer write to its shared memory (also where one has given up).
 __device__ __forceinline__ void cluster_leave()
 {
-    asm volatile("barrier.cluster.arrive.relaxed.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory");
+    cluster_arrive();
+    cluster_wait();
 }
 
 // Before a block's end: one that gave up leaves the copies that it started some time to land.

@@ -324,6 +324,7 @@ __global__ void __launch_bounds__(WARP ? 32 * kWarpRows : kMaxThreads + 32, WARP
     }
     float zl = given && !WARP ? elem_f(z[lab]) : 0.f;
     sync();
+    if (!WARP && S > 1) cluster_arrive();  // here; w, and so the return above, is the same in all blocks of a row
     // while the row is on its way
     const bool many = a.k > kFewK;
     if (many && !WARP) {
@@ -386,6 +387,7 @@ __global__ void __launch_bounds__(WARP ? 32 * kWarpRows : kMaxThreads + 32, WARP
     if (!WARP) {
         t = join(sm.warp, threads >> 5, cA);
         if (S > 1) {
+            cluster_wait();  // a block's shared memory is stored to from afar once it has begun
             if (tid < S)
                 st_cluster_v4(mapa_shared(smem_u32(&sm.part[rank]), tid), __float_as_uint(t.x), __float_as_uint(t.y), __float_as_uint(t.z), 0);
             // also: no block writes a gradient to the logits' place before the others have read what they need there
