@@ -28,7 +28,7 @@ int allow_launch(size_t bytes, bool large_clusters, const char* what)
 }
 
 // Clusters of S blocks that the device holds at a time, 0 where none; KERNEL's launches of S blocks have the same threads and
-// shared memory, or these are their bounds.  Asked once per device, after allow_launch.
+// shared memory, or these are their bounds.  Asked until the device has answered, once per device, after allow_launch.
 template <auto KERNEL>
 int clusters_held(int dev, int S, int threads, size_t smem)
 {
@@ -48,11 +48,12 @@ int clusters_held(int dev, int S, int threads, size_t smem)
     cfg.attrs = at;
     cfg.numAttrs = 1;
     int n = 0;
-    if (cudaOccupancyMaxActiveClusters(&n, KERNEL, &cfg) != cudaSuccess) {
+    const cudaError_t e = cudaOccupancyMaxActiveClusters(&n, KERNEL, &cfg);
+    if (e != cudaSuccess) {
         (void)cudaGetLastError();
         n = 0;
     }
-    if (keep) known[dev][S] = n + 1;
+    if (keep && (e == cudaSuccess || e == cudaErrorInvalidClusterSize)) known[dev][S] = n + 1;  // its answer
     return n;
 }
 
