@@ -3899,22 +3899,17 @@ int dbl_conv_wgrad(const dbl_conv_shape* s, const void* x, const void* dy, float
     return launch_check("conv wgrad reduce");
 }
 
+static int read_word(int* status) { return dbl::status_read(g_conv_status, status); }
+static int clear_word() { return dbl::status_clear(g_conv_status); }
+
 int dbl_device_status(int32_t* status)
 {
     using namespace dbl;
     if (!status) return set_error(DBL_ERR_INVALID, "device_status: null");
     int rc = cuda_check(cudaDeviceSynchronize(), "device_status sync");
     if (rc) return rc;
-    int v = 0, zero = 0;
-    if ((rc = cuda_check(cudaMemcpyFromSymbol(&v, g_conv_status, sizeof(int)), "device_status read"))) return rc;
-    if ((rc = cuda_check(cudaMemcpyToSymbol(g_conv_status, &zero, sizeof(int)), "device_status clear"))) return rc;
-    for (auto take : {ln_device_status, scan_device_status, distill_device_status}) {
-        int other = 0;
-        if ((rc = take(&other))) return rc;
-        if (v == DBL_OK) v = other;
-    }
-    *status = v;
-    return DBL_OK;
+    const StatusWord words[] = {{read_word, clear_word}, ln_status_word(), scan_status_word(), distill_status_word()};
+    return take_status_words(words, 4, status);
 }
 
 }  // extern "C"

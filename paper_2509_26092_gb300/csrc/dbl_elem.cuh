@@ -181,15 +181,6 @@ __device__ __forceinline__ void linger(volatile int* abort)
 
 }  // namespace dev
 
-// Reads a device-side status word, and clears it if it is set (the device being idle).
-template <class S>
-int take_status(S& word, int* status)
-{
-    const int zero = 0;
-    int rc = cuda_check(cudaMemcpyFromSymbol(status, word, sizeof(int)), "device_status read");
-    if (rc == DBL_OK && *status != DBL_OK) rc = cuda_check(cudaMemcpyToSymbol(word, &zero, sizeof(int)), "device_status clear");
-    return rc;
-}
 #endif
 
 }  // namespace dbl

@@ -13,6 +13,7 @@
 
 #include "../../include/dbl.h"
 #include "dbl_act.cuh"
+#include "dbl_status.cuh"
 
 // ---------------------------------------------------------------------------- host-side errors
 namespace dbl {
@@ -104,10 +105,25 @@ int current_context_id(unsigned long long* id);
 int bn_fwd_finalize(int64_t count, int C, float eps, const float* sum, const float* sumsq, float* save_mean,
                     float* save_invstd, cudaStream_t st);
 
-// Read and clear the status words of these files' kernels (DBL_OK or DBL_ERR_TIMEOUT), the device being idle.
-int ln_device_status(int* status);
-int scan_device_status(int* status);
-int distill_device_status(int* status);
+// The status words of these files' kernels.
+StatusWord ln_status_word();
+StatusWord scan_status_word();
+StatusWord distill_status_word();
+
+#if defined(__CUDACC__)
+// Read and clear a status word, the device being idle.
+template <class S>
+int status_read(S& word, int* status)
+{
+    return cuda_check(cudaMemcpyFromSymbol(status, word, sizeof(int)), "device_status read");
+}
+template <class S>
+int status_clear(S& word)
+{
+    const int zero = DBL_OK;
+    return cuda_check(cudaMemcpyToSymbol(word, &zero, sizeof(int)), "device_status clear");
+}
+#endif
 
 }  // namespace dbl
 

@@ -641,7 +641,9 @@ int launch(const DistillArgs& a, cudaStream_t st, const char* what)
 
 namespace dbl {
 
-int distill_device_status(int* status) { return take_status(g_distill_status, status); }
+static int read_word(int* status) { return status_read(g_distill_status, status); }
+static int clear_word() { return status_clear(g_distill_status); }
+StatusWord distill_status_word() { return {read_word, clear_word}; }
 
 }  // namespace dbl
 

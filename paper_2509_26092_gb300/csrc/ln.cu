@@ -1108,7 +1108,9 @@ int run_bwd(const LnArgs& a, const Plan& p, cudaStream_t st)
 
 namespace dbl {
 
-int ln_device_status(int* status) { return take_status(g_ln_status, status); }
+static int read_word(int* status) { return status_read(g_ln_status, status); }
+static int clear_word() { return status_clear(g_ln_status); }
+StatusWord ln_status_word() { return {read_word, clear_word}; }
 
 }  // namespace dbl
 

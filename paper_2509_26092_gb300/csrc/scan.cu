@@ -967,7 +967,9 @@ int pass_through(const dbl_scan_shape* s, const float* from, float* to, cudaStre
 
 namespace dbl {
 
-int scan_device_status(int* status) { return take_status(g_scan_status, status); }
+static int read_word(int* status) { return status_read(g_scan_status, status); }
+static int clear_word() { return status_clear(g_scan_status); }
+StatusWord scan_status_word() { return {read_word, clear_word}; }
 
 }  // namespace dbl
 
