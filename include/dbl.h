@@ -523,7 +523,8 @@ DBL_API int dbl_resize_taps(int32_t in, int32_t out, int32_t* i0, int32_t* i1, f
  *  - dtype is DBL_BF16 (the library's 16-bit format) or DBL_F32, for every
  *    tensor given as void*; the arithmetic, statistics, states and sums are
  *    fp32 in both, and each output is rounded once.
- *  - Any channel count or class count is taken, odd ones included, and base
+ *  - Any channel count or class count below 2^30 is taken (above:
+ *    DBL_ERR_UNSUPPORTED), odd ones included, and at most 2^30 steps; base
  *    addresses need only the alignment of their element type.  Rows of a
  *    multiple of 16 bytes at 16-byte aligned addresses are the fastest.
  *  - ld_* are the elements from one row to the next (0: rows are dense).

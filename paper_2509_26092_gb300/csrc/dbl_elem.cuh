@@ -8,6 +8,7 @@ namespace dbl {
 
 inline bool elem_dtype_ok(int dtype) { return dtype == DBL_F32 || dtype == DBL_BF16; }
 inline size_t elem_bytes(int dtype) { return dtype == DBL_F32 ? sizeof(float) : sizeof(act_t); }
+constexpr int kMaxColumns = (1 << 30) - 1;  // of a row: the kernels' indexes and twice this are 32-bit
 inline bool aligned_to(const void* p, size_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
 
 #if defined(__CUDACC__)

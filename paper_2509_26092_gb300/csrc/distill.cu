@@ -654,6 +654,7 @@ extern "C" int dbl_distill_fwd_bwd(const dbl_distill_shape* s, const void* logit
     const char* w = "distill_fwd_bwd";
     if (!s || s->rows < 0 || s->classes <= 0 || s->k < 0)
         return set_error(DBL_ERR_INVALID, "%s: null shape, rows < 0, classes <= 0 or k < 0", w);
+    if (s->classes > kMaxColumns) return set_error(DBL_ERR_UNSUPPORTED, "%s: 2^30 classes or more", w);
     if (s->k > kMaxK) return set_error(DBL_ERR_UNSUPPORTED, "%s: k = %d, at most %d", w, s->k, kMaxK);
     if (!elem_dtype_ok(s->dtype)) return set_error(DBL_ERR_INVALID, "%s: dtype must be DBL_F32 or DBL_BF16", w);
     if (!(s->temperature > 0.f) || isinf(s->temperature) || !(s->alpha >= 0.f && s->alpha <= 1.f))

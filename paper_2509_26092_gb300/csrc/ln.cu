@@ -919,6 +919,7 @@ __global__ void __launch_bounds__(kSumThreads) ln_params_sum_kernel(const float*
 int check(const dbl_ln_shape* s, const char* what)
 {
     if (!s || s->rows < 0 || s->c <= 0) return set_error(DBL_ERR_INVALID, "%s: null shape, rows < 0 or c <= 0", what);
+    if (s->c > kMaxColumns) return set_error(DBL_ERR_UNSUPPORTED, "%s: 2^30 columns or more", what);
     if (!elem_dtype_ok(s->dtype)) return set_error(DBL_ERR_INVALID, "%s: dtype must be DBL_F32 or DBL_BF16", what);
     if ((s->ld_in && s->ld_in < s->c) || (s->ld_out && s->ld_out < s->c))
         return set_error(DBL_ERR_INVALID, "%s: a row stride is shorter than a row", what);

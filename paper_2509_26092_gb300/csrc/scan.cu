@@ -794,6 +794,7 @@ int check(const dbl_scan_shape* s, const char* what)
     if (!s || s->n < 0 || s->t < 0 || s->c <= 0)
         return set_error(DBL_ERR_INVALID, "%s: null shape, n < 0, t < 0 or c <= 0", what);
     if (s->t > (1 << 30)) return set_error(DBL_ERR_UNSUPPORTED, "%s: more than 2^30 steps", what);
+    if (s->c > kMaxColumns) return set_error(DBL_ERR_UNSUPPORTED, "%s: 2^30 channels or more", what);
     if (!elem_dtype_ok(s->dtype)) return set_error(DBL_ERR_INVALID, "%s: dtype must be DBL_F32 or DBL_BF16", what);
     if ((s->ld_x && s->ld_x < s->c) || (s->ld_h && s->ld_h < s->c))
         return set_error(DBL_ERR_INVALID, "%s: a row stride is shorter than a row", what);
