@@ -574,6 +574,12 @@ DBL_API int dbl_layer_norm_bwd(const dbl_ln_shape* shape, const void* dy, const 
  * the last step; h_last may be h0's buffer (a sequence continued call by call:
  * t = 1 is the form for single tokens).  The state is fp32 throughout; only
  * what is written to h is rounded.
+ * a_i is 2^-126 at the least (gates below -87, and -infinity, which so leaves
+ * an infinite state as it is), 1 - a_i is 0 for gates above 87.  An infinite
+ * state stays infinite, over any number of steps, until an infinity of the
+ * other sign or NaN joins it.  Where a gradient is infinite or NaN, or the
+ * state behind a dgate, that channel's gradients from there on back (that
+ * dgate) are infinite or NaN; which of the two is not said.
  * lengths (or NULL): [n] int32 on the device; sequence b has its first
  * lengths[b] steps only (taken as 0 below 0 and as t above t).  The steps
  * past it are neither read nor counted: h is 0 there, and h_last the state
