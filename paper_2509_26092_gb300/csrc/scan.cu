@@ -76,9 +76,11 @@ __device__ __forceinline__ float2 at_least(float2 p, float2 least)
 }
 __device__ __forceinline__ bool finite2(float2 v) { return fabsf(v.x) < INFINITY && fabsf(v.y) < INFINITY; }
 
-// a = sigma(z) and na = 1 - a of two channels, both to full relative precision (2^-21): a = 1/(1 + e), na = e*a with
-// e = exp(-z), held to 2^126 so that no product is infinity times 0 (a is 2^-126 at the least, for z < -87).  z = +inf
-// gives 1 and 0 exactly; e below 2^-126 counts as 0 (z > 87).
+// a = sigma(z) and na = 1 - a of two channels, neither by subtraction: a = 1/(1 + e), na = e*a with e = exp(-z), held to
+// 2^126 so that no product is infinity times 0 (a is 2^-126 at the least, for z < -87).  z = +inf gives 1 and 0 exactly;
+// e below 2^-126 counts as 0 (z > 87).  The exponent -z*log2(e) is one rounded product, so e is off by up to
+// (1.5*|z| + 4)*2^-24 of itself, and so is the smaller one of a and na; the larger one by a few units of 2^-24.  (The
+// product's remainder would cost two instructions and more a channel; what 16-bit outputs are rounded by is 2^-9.)
 __device__ __forceinline__ void gates2(float2 z, float2& a, float2& na)
 {
     const float2 t = __fmul2_rn(z, make_float2(-1.4426950408889634f, -1.4426950408889634f));

@@ -1,4 +1,5 @@
-"""The gated scan where states, inputs or gradients are infinite, against the recurrence step by step in 64 bits.
+"""The gated scan where states, inputs or gradients are infinite and where gates are large, against the recurrence step by
+step in 64 bits.
 
 Every finite gate a is above 0, so an infinite state stays infinite until something else joins it; products of gates
 over many steps round to 0 in fp32 (gates of 0.05 over 64 steps: 2^-276).  Finite values have the tolerance of
@@ -107,3 +108,63 @@ def test_an_infinite_gradient_is_not_lost(D, kind, case):
         finite = np.isfinite(want)
         assert not np.isfinite(got[~finite]).any(), what
         assert_within(np.where(finite, got, 0.0), np.where(finite, want, 0.0), np.where(finite, tol, 0.0), what)
+
+
+@pytest.mark.parametrize("t", [1, 70])
+def test_gates_of_any_size_keep_their_digits(D, t):
+    """One step that counts, from a zero state (h = (1 - a)*x) and from an input of zero (h = a*h0), in fp32: the exponential
+    of the gate is off by (1.5*|gate| + 4)*2^-24 of itself, quotient, products and the result's rounding by at most 12 more."""
+    c = 173
+    z = np.linspace(-86.0, 86.0, c).astype(np.float32)
+    a, na = T.gates(z)
+    tol = (1.5 * np.abs(z.astype(np.float64)) + 16) * EPS32
+    gate, zero = np.full((t, c), np.inf, np.float32), np.zeros((t, c), np.float32)
+    gate[0] = z  # open from there on
+    for value, x, h0 in ((na, zero + np.float32(1.5), None), (a, zero, np.full(c, 1.5, np.float32))):
+        rx, rz, h, last = Rows("f32", t, c, values=x), Rows("f32", t, c, values=gate), Rows("f32", t, c), Rows("f32", 1, c)
+        start = None if h0 is None else torch.from_numpy(h0).cuda()
+        D.dbl_gated_scan_fwd(D.scan_shape(1, t, c, D.DBL_F32), rx.ptr(), rz.ptr(), start, None, h.ptr(), last.ptr(), None)
+        check_status(D)
+        want = np.broadcast_to(1.5 * value, (t, c))
+        assert_within(h.values(), want, tol * want, "h")
+        assert_within(last.values()[0], want[0], tol * want[0], "h_last")
+
+
+@pytest.mark.parametrize("case", [dict(n=2, t=12, c=40), dict(n=2, t=300, c=64), dict(n=1, t=900, c=33)],
+                         ids=lambda c: "-".join(f"{k}{v}" for k, v in c.items()))
+def test_large_gates_forward_and_backward(D, case):
+    """Gates of -80 to 80 in fp32.  The bound of test_gpu_gated_scan.py with the exponential's error for |gate| = 80 in the
+    place of that for 14: K = 40 + 1.5*(80 - 14) + 1."""
+    big = 40 + 1.5 * 66 + 1
+    g = np.random.default_rng(1)
+    cs = Case("f32", **case)
+    n, t, c = cs.n, cs.t, cs.c
+    cs.rz.view().copy_(torch.from_numpy(g.uniform(-80, 80, (n * t, c))))
+    z, x = cs.rz.values().reshape(n, t, c), cs.x
+    wh, wl, _, prev = T.gated_scan_fwd(x, z, cs.h0)
+    a, na = T.gates(z)
+    size = T.gated_scan_fwd(np.abs(x), z, np.abs(cs.h0))[0]
+    scaled = lambda s, gates, live: carried(s * (big / K), gates, live, np.zeros((n, c)))
+    E, Elast = scaled(size, a, cs.live)
+    h, last, st = run(D, cs)
+    assert_within(h.values().reshape(n, t, c), wh, E + rounding("f32", np.abs(wh) + E), "h")
+    assert_within(last.values(), wl, Elast, "h_last")
+    DH = cs.dh.values().reshape(n, t, c)
+    wx, wz, w0, _ = T.gated_scan_bwd(DH, x, z, prev, cs.dlast)
+    G = T.gated_scan_bwd(np.abs(DH), x, z, prev, np.abs(cs.dlast))[3]
+    anext = np.concatenate([a[:, 1:], np.ones((n, 1, c))], 1)
+    EG = scaled(G[:, ::-1], anext[:, ::-1], cs.live[:, ::-1])[0][:, ::-1]
+    Eprev = np.concatenate([np.zeros((n, 1, c)), E[:, :-1]], 1)
+    pm = np.concatenate([np.abs(cs.h0)[:, None], size[:, :-1]], 1)
+    # a of 2^-126 at the least where the formula's is below it
+    floor = 2.0 ** -126 * (G + 1) * (pm + np.abs(x) + 1)
+    tolx = na * EG + big * EPS32 * na * G + floor
+    tolz = a * na * ((EG + big * EPS32 * G) * (pm + np.abs(x)) + G * Eprev) + floor
+    dx, dz, dh0 = Rows("f32", n * t, c), Rows("f32", n * t, c), Rows("f32", n, c)
+    D.dbl_gated_scan_bwd(cs.shape(D, D.DBL_F32), cs.dh.ptr(), torch.from_numpy(cs.dlast).cuda(), cs.px, cs.pz, st.ptr(), None,
+                         dx.ptr(), dz.ptr(), dh0.ptr())
+    check_status(D)
+    assert_within(dx.values().reshape(n, t, c), wx, tolx + rounding("f32", np.abs(wx) + tolx), "dx")
+    assert_within(dz.values().reshape(n, t, c), wz, tolz + rounding("f32", np.abs(wz) + tolz), "dgate")
+    first = a[:, 0] * (EG[:, 0] + big * EPS32 * G[:, 0]) + floor[:, 0]
+    assert_within(dh0.values(), w0, first + rounding("f32", np.abs(w0)), "dh0")
