@@ -48,7 +48,8 @@ class TokenSpec(FlatSpec):
 class TokenWorker:
     """Activations, gradients and scratch of one worker: ``n`` sequences of ``t`` tokens, a teacher of ``k``
     logits per token.  ``lengths`` ([n] int32, all t at first) ends sequences earlier; tokens past them count
-    neither in the loss nor in the states."""
+    neither in the loss nor in the states nor, whatever their features hold, in a gradient.  What a step reads
+    (teacher, lengths, labels) is set on the current stream, which the next iteration follows."""
 
     def __init__(self, spec, n, t, k, temperature=2.0, alpha=0.5, device="cuda", eps=1e-5, precision="bf16"):
         self.spec, self.batch, self.res, self.k, self.eps, self.precision = spec, n, t, k, eps, precision
@@ -82,6 +83,9 @@ class TokenWorker:
         self.labels = torch.full((rows,), -1, dtype=torch.int32, device=device)
         self.lengths = torch.full((n,), t, dtype=torch.int32, device=device)
         self.weight = torch.full((rows,), 1.0 / rows, device=device)
+        # the features that count: of the others a NaN would reach the weights' gradients as NaN times 0
+        self.live = torch.ones((n, t, 1), dtype=torch.bool, device=device)
+        self.features, self.none = act(w).view(n, t, w), torch.zeros((), dtype=dt, device=device)
         self.row_loss, self.loss = vec(rows), vec(1)
         self.grad = vec(spec.n_flat)
         self.scale_used = torch.ones(1, device=device)
@@ -101,7 +105,8 @@ class TokenWorker:
         """Tokens that count in each sequence ([n] int32); the loss is the mean over them all."""
         self.lengths.copy_(lengths)
         steps = torch.arange(self.res, device=self.lengths.device)
-        live = (steps[None, :] < self.lengths[:, None]).float().reshape(-1)
+        self.live.copy_((steps[None, :] < self.lengths[:, None])[..., None])
+        live = self.live.float().reshape(-1)
         self.weight.copy_(live / live.sum().clamp(min=1.0))
 
     def enqueue_step(self, server, features, native_len, stream):
@@ -114,11 +119,12 @@ class TokenWorker:
             raise ValueError(f"features must be contiguous [{self.batch}, {self.res}, {self.spec.width}] "
                              f"{ACT_DTYPE[self.precision]}")
         with D.precision(self.precision):
-            if server.scaled:
-                st = stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(stream)
-                with torch.cuda.stream(st):
+            st = stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(stream)
+            with torch.cuda.stream(st):
+                if server.scaled:
                     self.scale_used.copy_(server.scale_state[0:1].view(torch.float32))
-            self._enqueue_step(server, features, stream)
+                torch.where(self.live, features, self.none, out=self.features)
+            self._enqueue_step(server, self.features, stream)
 
     def _enqueue_step(self, server, features, stream):
         s = stream.cuda_stream if hasattr(stream, "cuda_stream") else stream
