@@ -71,9 +71,10 @@ DBL_API int dbl_version(void);
  * CUDA graph are not counted again.  Host; for instrumentation. */
 DBL_API int64_t dbl_kernel_launches(void);
 
-/* Synchronous: reads and clears the device-side status word of the current
+/* Synchronous: reads and clears the device-side status words of the current
  * device (DBL_OK or DBL_ERR_TIMEOUT), after synchronising the device.  For
- * tests and diagnostics only; never call it inside a captured graph. */
+ * tests and diagnostics only; never call it inside a captured graph.  A call
+ * that fails clears no word that it does not report. */
 DBL_API int dbl_device_status(int32_t* status);
 
 /* ========================================================================
@@ -596,7 +597,8 @@ typedef struct {
     int64_t ld_x, ld_h;
 } dbl_scan_shape;
 DBL_API size_t dbl_gated_scan_states_bytes(const dbl_scan_shape* shape);
-/* pass: DBL_PASS_FWD or DBL_PASS_DGRAD (0 for any other). */
+/* 0: neither pass needs scratch.  ws of the two calls may be NULL (with
+ * ws_bytes 0); it is not used.  The arguments are those of the other passes. */
 DBL_API size_t dbl_gated_scan_workspace_bytes(const dbl_scan_shape* shape, int pass);
 DBL_API int dbl_gated_scan_fwd(const dbl_scan_shape* shape, const void* x, const void* gate,
                                const float* h0 /* or NULL */, const int32_t* lengths /* or NULL */, void* h,

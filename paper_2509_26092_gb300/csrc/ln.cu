@@ -28,7 +28,7 @@ using namespace dbl::dev;
 
 constexpr int kMaxGroup = 512;     // threads of a row
 constexpr int kBlock = 256;        // threads of a block of several groups
-constexpr int kMaxSplit = 8;       // blocks of a row in the backward pass
+constexpr int kMaxSplit = 8;       // blocks of a row
 constexpr int kMaxDepth = 4;       // rows of a group on their way
 constexpr int kWide = 256;         // threads of the kernels for rows wider than a group
 constexpr int kShort = 256;        // columns of a short row, at the most
@@ -1013,8 +1013,8 @@ Plan plan_wide(LnArgs& a, int tensors, size_t e)
     return p;
 }
 
-// The backward pass's blocks or clusters, each of which leaves a row of partial column sums.  By the sizes alone, as the
-// workspace is.
+// The backward pass's blocks or clusters, each of which leaves a row of partial column sums.  By the sizes and by what the
+// device holds, which the workspace's size goes by too: the pointers' alignment and which are given have no part in it.
 Plan bwd_plan(LnArgs& a, size_t e)
 {
     if (!held(a)) return {kWide, (int)std::max<int64_t>(1, std::min<int64_t>((a.rows + 15) / 16, 64)), 0, 1};

@@ -10,8 +10,8 @@
 //
 // Bound by memory where there are sequences enough, otherwise by the chain of parts: exchange of the pairs, state for
 // the next part.  On a GB300 that copies 6.78 TB/s, bf16 but where said: backward of 8 x 8192 x 1024 124 us = 5.4 TB/s;
-// forward of 1 x 65536 x 512 60 us = 3.4 TB/s, 22 parts one after another at 2.7 us each; of 185 x 196 x 256 in fp16 23 us =
-// 2.5 TB/s, 740 blocks in three rounds; one token of 64 x 512 4.5 us, the launch; backward of 12 x 3001 x 393 with
+// forward of 1 x 65536 x 512 63 us = 3.2 TB/s, 22 parts one after another at 2.8 us each; of 185 x 196 x 256 in fp16 24 us =
+// 2.4 TB/s, 740 blocks in three rounds; one token of 64 x 512 4.5 us, the launch; backward of 12 x 3001 x 393 with
 // lengths 73 us = 1.4 TB/s (rows that begin anywhere: 190 instructions a step of 64 channels, 77 where TMA brings them).
 #include <math.h>
 
@@ -391,7 +391,8 @@ __device__ __forceinline__ void links_init(Links& l, int S)
 // channels.  A thread scans its steps from a zero state and keeps, for each, that state and the product of the gates
 // up to it: with the state h before them, the state after a step is state + product*h.  The threads' and the blocks'
 // last pairs (product, state) are combined through shared memory, the last thread's state goes on to the cluster's
-// next part.  So each element is read and written once, and the sums' order depends on the sizes alone.  Steps past
+// next part.  So each element is read and written once, and the sums' order depends on the sizes, the alignment and the
+// device (how many clusters it holds) alone.  Steps past
 // a length are given open gates, which leave the state as it is.
 template <class T, bool ALIGNED, int LANES, int R>
 struct FwdSmem {
@@ -884,7 +885,8 @@ struct Split {
 
 // Blocks of a cluster: the fewest parts one after another.  How many clusters the device holds at a time depends on where
 // they fit, and one more waits until another is done (152 SMs hold 14 clusters of 16 blocks, 23 of 12, 36 of 8, 74 of 4 and
-// 152 of 2, two blocks on an SM: forward, 1 x 65536 x 512, 16 clusters of 16 blocks 83 us, of 12 60 us).  An exchange takes
+// 152 of 2, two blocks on an SM: forward, 1 x 65536 x 512, 16 clusters of 16 blocks 83 us, of 12 63 us).  It is asked for
+// blocks of 256 threads, also where a short sequence's have fewer and more of them fit.  An exchange takes
 // a part a fourth longer (185 x 196 x 256: no exchange 24 us, clusters of two 30), a cluster's start takes about a part,
 // and rows of fewer channels are slower to bring (8 lanes and 32: forward, 4 x 8192 x 1024 54 and 46 us, backward 98 and
 // 69; 16 lanes and 32: backward, 15 x 1154 x 1660 87 and 82).
