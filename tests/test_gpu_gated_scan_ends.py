@@ -168,3 +168,23 @@ def test_large_gates_forward_and_backward(D, case):
     assert_within(dz.values().reshape(n, t, c), wz, tolz + rounding("f32", np.abs(wz) + tolz), "dgate")
     first = a[:, 0] * (EG[:, 0] + big * EPS32 * G[:, 0]) + floor[:, 0]
     assert_within(dh0.values(), w0, first + rounding("f32", np.abs(w0)), "dh0")
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+@pytest.mark.parametrize("t,c", [(16, 64), (200, 64), (200, 63), (3000, 16)])
+def test_a_closed_gate_ends_finite_states_only(D, kind, t, c):
+    """A gate of -infinity is 2^-126: it takes the input in the place of a finite state, and leaves an infinite state
+    infinite and NaN NaN, each in its channel alone."""
+    at = t // 2
+    cs = Case(kind, 1, t, c)
+    base = run(D, cs)[0].values()
+    cs.rz.view()[at] = -np.inf
+    cs.rx.view()[at - 1, 5] = float("nan")
+    cs.h0[0, 9] = np.inf
+    cs.th0.copy_(torch.from_numpy(cs.h0))
+    h = run(D, cs)[0].values()
+    rest = [i for i in range(c) if i not in (5, 9)]
+    assert np.array_equal(h[:at, rest], base[:at, rest])
+    assert np.array_equal(h[at, rest], cs.rx.values()[at, rest]) and np.isfinite(h[:, rest]).all()
+    assert np.isnan(h[at - 1:, 5]).all() and np.isfinite(h[:at - 1, 5]).all()
+    assert (h[:, 9] == np.inf).all()
