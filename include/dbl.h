@@ -652,6 +652,153 @@ DBL_API int dbl_distill_fwd_bwd(const dbl_distill_shape* shape, const void* logi
                                 float* row_loss, float* loss /* or NULL */, void* dlogits /* or NULL */,
                                 void* stream);
 
+/* ------------------------------------------------------------------------
+ * A layer of experts: the router names the experts of every token and groups
+ * the tokens by expert, the tokens go to their groups' rows, every group has
+ * products with weights of its own, and the tokens take back the weighted sum
+ * of what their experts gave.
+ *
+ * Entry (r, j), j = 0..k-1, is token r's j-th expert.  `chosen`, `weights` and
+ * `slots` are [rows, k], dense: the expert (-1: the entry is absent), its
+ * weight, and the row of the grouped tensors that is the entry's (-1: none).
+ * Grouped tensors have a row for each entry, group after group; `offsets`
+ * ([groups + 1] int32, on the device) says where: group e has the rows
+ * offsets[e] .. offsets[e+1] - 1.  Rows past the last group are in no group:
+ * they may be read but nothing of them is used, and they are not written.
+ * The numbers of rows are on the device alone, so that a captured graph
+ * serves every routing.  Indexes that do not fit the tensors do no harm to
+ * memory: a slot outside the grouped tensor is absent, offsets are taken as
+ * at least 0, at least the offset before and at most the tensor's rows.
+ * ------------------------------------------------------------------------ */
+
+/* The router.  With key_e = logits[r][e] + select_bias[e] (in fp32), the
+ * entries of row r are the k experts of the largest keys, largest first, the
+ * lowest expert first among equals.  Their weights are
+ *   exp(logits[r][e]) / sum over all experts   (normalise = 0), or
+ *   exp(logits[r][e]) / sum over the row's entries (normalise = 1).
+ * An expert whose key is -infinity or NaN is never chosen: where less than k
+ * are left, the last entries are absent, with weight 0.  A row with NaN or
+ * +infinity among its logits has no distribution: its entries are absent and
+ * their weights NaN.  row_weight (or NULL): [rows] fp32; a row of weight 0
+ * (padding) has no entries, and weights of 0, whatever it holds.
+ * select_bias (or NULL): [experts] fp32, added for the choice alone, to even
+ * out the experts' loads; it has no gradient.
+ * slots: the entries' places in the order of expert, then row, then j.
+ * offsets: [experts + 1]; the last is the number of entries that are there.
+ * At most DBL_ROUTE_MAX_EXPERTS experts, DBL_ROUTE_MAX_K of them (and at most
+ * all) in a row, and less than 2^31 entries.  ld: the logits' row stride. */
+#define DBL_ROUTE_MAX_EXPERTS 1024
+#define DBL_ROUTE_MAX_K 32
+typedef struct {
+    int64_t rows;
+    int32_t experts, k;
+    int32_t normalise;
+    int32_t dtype; /* of logits and dlogits */
+    int64_t ld, ld_grad;
+} dbl_route_shape;
+DBL_API size_t dbl_route_workspace_bytes(const dbl_route_shape* shape);
+DBL_API int dbl_route_fwd(const dbl_route_shape* shape, const void* logits, const float* select_bias /* or NULL */,
+                          const float* row_weight /* or NULL */, int32_t* chosen, float* weights, int32_t* slots,
+                          int32_t* offsets, void* ws, size_t ws_bytes, void* stream);
+
+/* Its backward pass, from the gradient of the weights ([rows, k] fp32; that
+ * of an absent entry is not used).  With d = sum_j weights_j*dweights_j,
+ *   normalise = 1: dlogits_e = w_j*(dweights_j - d) for the entry of expert e,
+ *   normalise = 0: dlogits_e = [w_j*dweights_j for the entry of e] - p_e*d,
+ *                  p = softmax(logits) over all experts,
+ * and 0 elsewhere.  A row without entries has gradient 0 and its logits are
+ * not used; one whose weights are NaN has gradient NaN.  logits may be NULL
+ * with normalise = 1.  dlogits: [rows, experts], row stride ld_grad. */
+DBL_API int dbl_route_bwd(const dbl_route_shape* shape, const void* logits, const int32_t* chosen,
+                          const float* weights, const float* dweights, void* dlogits, void* stream);
+
+/* Tokens to their groups and back.  dtype is that of every tensor of c
+ * columns; ld_rows is the row stride of the tokens' tensors (x, res, out,
+ * dout), ld_grouped that of the grouped ones, which have grouped_rows rows
+ * (0: rows*k).  Sums are fp32, over j in order.
+ *   scatter: xg[slots[r][j]] = x[r].
+ *   combine: out[r] = sum_j weights[r][j]*yg[slots[r][j]] [+ res[r]]; an absent
+ *     entry counts as a row of zeros (whose product with a weight of NaN is
+ *     NaN).  weights = NULL: 1, with which this is scatter's backward pass
+ *     (dx[r] = sum_j dxg[slots[r][j]] [+ dskip[r]]).
+ *   combine_bwd: dyg[slots[r][j]] = weights[r][j]*dout[r] (weights = NULL: 1),
+ *     dweights[r][j] = sum_c dout[r]*yg[slots[r][j]] (0 for an absent entry);
+ *     dweights may be NULL, yg too then.  dyg may be yg's own buffer.
+ * Two entries of the same slot: scatter and combine_bwd leave either's row. */
+typedef struct {
+    int64_t rows;
+    int32_t k, c;
+    int32_t dtype;
+    int64_t grouped_rows;
+    int64_t ld_rows, ld_grouped;
+} dbl_exchange_shape;
+DBL_API int dbl_expert_scatter(const dbl_exchange_shape* shape, const void* x, const int32_t* slots, void* xg,
+                               void* stream);
+DBL_API int dbl_expert_combine(const dbl_exchange_shape* shape, const void* yg, const int32_t* slots,
+                               const float* weights /* or NULL */, const void* res /* or NULL */, void* out,
+                               void* stream);
+DBL_API int dbl_expert_combine_bwd(const dbl_exchange_shape* shape, const void* dout, const void* yg /* or NULL */,
+                                   const int32_t* slots, const float* weights /* or NULL */, void* dyg,
+                                   float* dweights /* or NULL */, void* stream);
+
+/* Matrix products of each group's rows with its own weights, on the tensor
+ * cores.  w: [groups, n_out, n_in]; x: [rows, n_in]; y: [rows, n_out], all in
+ * the library's 16-bit format (as for the convolutions, there is no fp32
+ * form).  For row p of group e:
+ *   fwd:   y[p] = w_e x[p], with relu = 1 max(., 0) of it (NaN stays NaN);
+ *   dgrad: dx[p] = w_e^T dy[p], and 0 where mask is given and mask[p] is not
+ *          above 0: with the rows that a relu product left as the mask, the
+ *          gradient that passes its ReLU.  mask: [rows, n_in], dx's stride;
+ *   wgrad: dw_e = sum over the group's rows of dy[p] x[p]^T ([n_out, n_in]
+ *          fp32, dense), 0 for an empty group; added to dw with accumulate.
+ * Products are summed in fp32.  n_in and n_out are multiples of 8 below 2^24,
+ * addresses and rows (ld_in of x, dx and mask, ld_out of y and dy; 0: dense)
+ * multiples of 16 bytes.  rows: the tensors' rows, which the groups may leave
+ * a part of.  At most DBL_GROUPED_MAX_GROUPS groups and 2^30 rows. */
+#define DBL_GROUPED_MAX_GROUPS 1024
+typedef struct {
+    int64_t rows;
+    int32_t groups, n_in, n_out;
+    int32_t relu; /* fwd */
+    int64_t ld_in, ld_out;
+} dbl_grouped_shape;
+/* pass: DBL_PASS_FWD, _DGRAD or _WGRAD.  0: ws may be NULL. */
+DBL_API size_t dbl_grouped_workspace_bytes(const dbl_grouped_shape* shape, int pass);
+DBL_API int dbl_grouped_fwd(const dbl_grouped_shape* shape, const void* x, const void* w, const int32_t* offsets,
+                            void* y, void* ws, size_t ws_bytes, void* stream);
+DBL_API int dbl_grouped_dgrad(const dbl_grouped_shape* shape, const void* dy, const void* w, const int32_t* offsets,
+                              const void* mask /* or NULL */, void* dx, void* ws, size_t ws_bytes, void* stream);
+DBL_API int dbl_grouped_wgrad(const dbl_grouped_shape* shape, const void* x, const void* dy, const int32_t* offsets,
+                              float* dw, int accumulate, void* ws, size_t ws_bytes, void* stream);
+
+/* Dropout, with the residual addition (cyclic progressive learning raises its
+ * rate from sub-stage to sub-stage, Sec. 4.1):
+ *   y[r][c] = keep(r, c) * x[r][c]/(1 - rate) [+ res[r][c]].
+ * The mask is drawn, not stored: element (r, c) has word c mod 4 of the
+ * Philox4x32-10 block (Salmon et al., SC 2011) of counter (b low, b high,
+ * *step low, *step high), b = r*ceil(C/4) + floor(c/4), and key (seed low,
+ * seed high), each 32 bits; it is kept when the word is at least
+ * floor(rate*2^32).  What is dropped is 0, whatever it held.  The backward
+ * pass is the same call on the gradient (res then: the gradient past it), at
+ * the same step.  Every place of a model needs a seed of its own.  step: one
+ * uint64 on the device, not changed here: dbl_dropout_advance adds 1 to it,
+ * once a training step, so that a replayed graph draws new masks.  (The
+ * classifier's head has another generator, dbl_dropout_mask: Philox4x64 would
+ * take four times the multiplications here.)  rate in [0, 1); ld_in: the row
+ * stride of x and res, ld_out that of y, which may be x's or res's own buffer
+ * (with the same stride). */
+typedef struct {
+    int64_t rows;
+    int32_t c;
+    int32_t dtype;
+    int64_t ld_in, ld_out;
+    uint64_t seed;
+    float rate;
+} dbl_dropout_shape;
+DBL_API int dbl_dropout_residual(const dbl_dropout_shape* shape, const void* x, const void* res /* or NULL */,
+                                 const uint64_t* step, void* y, void* stream);
+DBL_API int dbl_dropout_advance(uint64_t* step, void* stream);
+
 /* ========================================================================
  * Host-side planner of dual-batch learning (Sec. 3.3-3.4).
  * ======================================================================== */

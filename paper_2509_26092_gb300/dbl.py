@@ -83,6 +83,35 @@ class DistillShape(ctypes.Structure):
 
 DBL_DISTILL_MAX_K = 1024
 
+
+class RouteShape(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("experts", ctypes.c_int32), ("k", ctypes.c_int32),
+                ("normalise", ctypes.c_int32), ("dtype", ctypes.c_int32), ("ld", ctypes.c_int64),
+                ("ld_grad", ctypes.c_int64)]
+
+
+DBL_ROUTE_MAX_EXPERTS, DBL_ROUTE_MAX_K = 1024, 32
+
+
+class ExchangeShape(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("k", ctypes.c_int32), ("c", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("grouped_rows", ctypes.c_int64), ("ld_rows", ctypes.c_int64), ("ld_grouped", ctypes.c_int64)]
+
+
+class GroupedShape(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("groups", ctypes.c_int32), ("n_in", ctypes.c_int32),
+                ("n_out", ctypes.c_int32), ("relu", ctypes.c_int32), ("ld_in", ctypes.c_int64),
+                ("ld_out", ctypes.c_int64)]
+
+
+DBL_GROUPED_MAX_GROUPS = 1024
+
+
+class DropoutShape(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("c", ctypes.c_int32), ("dtype", ctypes.c_int32), ("ld_in", ctypes.c_int64),
+                ("ld_out", ctypes.c_int64), ("seed", ctypes.c_uint64), ("rate", ctypes.c_float)]
+
+
 _libs = {}
 _precision = contextvars.ContextVar("dbl_precision", default="bf16")
 PRECISIONS = ("bf16", "f16")
@@ -178,6 +207,18 @@ def lib(p=None):
             "dbl_gated_scan_fwd": (ctypes.c_int, [ctypes.POINTER(ScanShape)] + [_V] * 8 + [_SZ, _V]),
             "dbl_gated_scan_bwd": (ctypes.c_int, [ctypes.POINTER(ScanShape)] + [_V] * 10 + [_SZ, _V]),
             "dbl_distill_fwd_bwd": (ctypes.c_int, [ctypes.POINTER(DistillShape)] + [_V] * 10),
+            "dbl_route_workspace_bytes": (_SZ, [ctypes.POINTER(RouteShape)]),
+            "dbl_route_fwd": (ctypes.c_int, [ctypes.POINTER(RouteShape)] + [_V] * 8 + [_SZ, _V]),
+            "dbl_route_bwd": (ctypes.c_int, [ctypes.POINTER(RouteShape)] + [_V] * 6),
+            "dbl_expert_scatter": (ctypes.c_int, [ctypes.POINTER(ExchangeShape)] + [_V] * 4),
+            "dbl_expert_combine": (ctypes.c_int, [ctypes.POINTER(ExchangeShape)] + [_V] * 6),
+            "dbl_expert_combine_bwd": (ctypes.c_int, [ctypes.POINTER(ExchangeShape)] + [_V] * 7),
+            "dbl_grouped_workspace_bytes": (_SZ, [ctypes.POINTER(GroupedShape), ctypes.c_int]),
+            "dbl_grouped_fwd": (ctypes.c_int, [ctypes.POINTER(GroupedShape)] + [_V] * 5 + [_SZ, _V]),
+            "dbl_grouped_dgrad": (ctypes.c_int, [ctypes.POINTER(GroupedShape)] + [_V] * 6 + [_SZ, _V]),
+            "dbl_grouped_wgrad": (ctypes.c_int, [ctypes.POINTER(GroupedShape)] + [_V] * 4 + [ctypes.c_int, _V, _SZ, _V]),
+            "dbl_dropout_residual": (ctypes.c_int, [ctypes.POINTER(DropoutShape)] + [_V] * 5),
+            "dbl_dropout_advance": (ctypes.c_int, [_V, _V]),
             "dbl_update_factor": (_D, [_D, _D, ctypes.c_int]),
             "dbl_plan": (ctypes.c_int, [_D, _D, _I32, _I32, _D, _D, _D, ctypes.c_int] + [ctypes.POINTER(_D)] * 4),
         }
@@ -534,6 +575,93 @@ def dbl_distill_fwd_bwd(shape, logits, teacher_logits, teacher_classes, labels, 
     _check(lib().dbl_distill_fwd_bwd(ctypes.byref(shape), _ptr(logits), _ptr(teacher_logits), _ptr(teacher_classes),
                                      _ptr(labels), _ptr(row_weight), _ptr(loss_scale), _ptr(row_loss), _ptr(loss),
                                      _ptr(dlogits), _stream(stream)))
+
+
+def route_shape(rows, experts, k, normalise=True, dtype=DBL_BF16, ld=0, ld_grad=0):
+    """dbl_route_shape; ld / ld_grad: row strides in elements of the logits / their gradient (0: dense)."""
+    return RouteShape(rows, experts, k, int(bool(normalise)), dtype, ld, ld_grad)
+
+
+def dbl_route_workspace_bytes(shape):
+    return lib().dbl_route_workspace_bytes(ctypes.byref(shape))
+
+
+def dbl_route_fwd(shape, logits, select_bias, row_weight, chosen, weights, slots, offsets, ws=None, ws_bytes=0,
+                  stream=None):
+    """chosen, slots [rows, k] int32, weights [rows, k] fp32, offsets [experts + 1] int32; select_bias and row_weight
+    may be None."""
+    _check(lib().dbl_route_fwd(ctypes.byref(shape), _ptr(logits), _ptr(select_bias), _ptr(row_weight), _ptr(chosen),
+                               _ptr(weights), _ptr(slots), _ptr(offsets), _ptr(ws), ws_bytes, _stream(stream)))
+
+
+def dbl_route_bwd(shape, logits, chosen, weights, dweights, dlogits, stream=None):
+    """logits may be None where the weights are normalised over the chosen experts."""
+    _check(lib().dbl_route_bwd(ctypes.byref(shape), _ptr(logits), _ptr(chosen), _ptr(weights), _ptr(dweights),
+                               _ptr(dlogits), _stream(stream)))
+
+
+def exchange_shape(rows, k, c, dtype=DBL_BF16, grouped_rows=0, ld_rows=0, ld_grouped=0):
+    """dbl_exchange_shape; grouped_rows: rows of the grouped tensors (0: rows*k); ld_*: row strides in elements."""
+    return ExchangeShape(rows, k, c, dtype, grouped_rows, ld_rows, ld_grouped)
+
+
+def dbl_expert_scatter(shape, x, slots, xg, stream=None):
+    _check(lib().dbl_expert_scatter(ctypes.byref(shape), _ptr(x), _ptr(slots), _ptr(xg), _stream(stream)))
+
+
+def dbl_expert_combine(shape, yg, slots, weights, res, out, stream=None):
+    """weights=None: 1, as in the backward pass of dbl_expert_scatter; res (or None) is added."""
+    _check(lib().dbl_expert_combine(ctypes.byref(shape), _ptr(yg), _ptr(slots), _ptr(weights), _ptr(res), _ptr(out),
+                                    _stream(stream)))
+
+
+def dbl_expert_combine_bwd(shape, dout, yg, slots, weights, dyg, dweights, stream=None):
+    """dweights=None: the grouped rows' gradient alone (yg may be None then)."""
+    _check(lib().dbl_expert_combine_bwd(ctypes.byref(shape), _ptr(dout), _ptr(yg), _ptr(slots), _ptr(weights), _ptr(dyg),
+                                        _ptr(dweights), _stream(stream)))
+
+
+def grouped_shape(rows, groups, n_in, n_out, relu=False, ld_in=0, ld_out=0):
+    """dbl_grouped_shape; ld_in / ld_out: row strides in elements of x, dx, mask / of y, dy (0: dense)."""
+    return GroupedShape(rows, groups, n_in, n_out, int(bool(relu)), ld_in, ld_out)
+
+
+def dbl_grouped_workspace_bytes(shape, pass_):
+    return lib().dbl_grouped_workspace_bytes(ctypes.byref(shape), pass_)
+
+
+def dbl_grouped_fwd(shape, x, w, offsets, y, ws=None, ws_bytes=0, stream=None):
+    """w [groups, n_out, n_in] in the 16-bit format, offsets [groups + 1] int32 on the device."""
+    _check(lib().dbl_grouped_fwd(ctypes.byref(shape), _ptr(x), _ptr(w), _ptr(offsets), _ptr(y), _ptr(ws), ws_bytes,
+                                 _stream(stream)))
+
+
+def dbl_grouped_dgrad(shape, dy, w, offsets, mask, dx, ws=None, ws_bytes=0, stream=None):
+    """mask (or None): the rows a ReLU left, where dx passes it."""
+    _check(lib().dbl_grouped_dgrad(ctypes.byref(shape), _ptr(dy), _ptr(w), _ptr(offsets), _ptr(mask), _ptr(dx), _ptr(ws),
+                                   ws_bytes, _stream(stream)))
+
+
+def dbl_grouped_wgrad(shape, x, dy, offsets, dw, accumulate=False, ws=None, ws_bytes=0, stream=None):
+    """dw [groups, n_out, n_in] fp32."""
+    _check(lib().dbl_grouped_wgrad(ctypes.byref(shape), _ptr(x), _ptr(dy), _ptr(offsets), _ptr(dw), int(bool(accumulate)),
+                                   _ptr(ws), ws_bytes, _stream(stream)))
+
+
+def dropout_shape(rows, c, rate, seed, dtype=DBL_BF16, ld_in=0, ld_out=0):
+    """dbl_dropout_shape; ld_in / ld_out: row strides in elements of x, res / of y (0: dense)."""
+    return DropoutShape(rows, c, dtype, ld_in, ld_out, int(seed) & (2**64 - 1), float(rate))
+
+
+def dbl_dropout_residual(shape, x, res, step, y, stream=None):
+    """y = dropout(x) [+ res]; step: device uint64 counter (an int64 tensor of one element).  Its backward pass is the
+    same call on the gradient."""
+    _check(lib().dbl_dropout_residual(ctypes.byref(shape), _ptr(x), _ptr(res), _ptr(step), _ptr(y), _stream(stream)))
+
+
+def dbl_dropout_advance(step, stream=None):
+    """Adds 1 to the step on the stream."""
+    _check(lib().dbl_dropout_advance(_ptr(step), _stream(stream)))
 
 
 def dbl_resize_taps(n_in, n_out):
