@@ -3908,8 +3908,9 @@ int dbl_device_status(int32_t* status)
     if (!status) return set_error(DBL_ERR_INVALID, "device_status: null");
     int rc = cuda_check(cudaDeviceSynchronize(), "device_status sync");
     if (rc) return rc;
-    const StatusWord words[] = {{read_word, clear_word}, ln_status_word(), scan_status_word(), distill_status_word()};
-    return take_status_words(words, 4, status);
+    const StatusWord words[] = {{read_word, clear_word}, ln_status_word(), scan_status_word(), distill_status_word(),
+                                grouped_status_word()};
+    return take_status_words(words, 5, status);
 }
 
 }  // extern "C"

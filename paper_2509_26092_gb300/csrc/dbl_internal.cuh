@@ -109,6 +109,7 @@ int bn_fwd_finalize(int64_t count, int C, float eps, const float* sum, const flo
 StatusWord ln_status_word();
 StatusWord scan_status_word();
 StatusWord distill_status_word();
+StatusWord grouped_status_word();
 
 #if defined(__CUDACC__)
 // Read and clear a status word, the device being idle.

@@ -9,16 +9,6 @@ using namespace dbl::dev;
 
 constexpr int kMaxGroups = DBL_GROUPED_MAX_GROUPS;
 
-struct GroupedArgs {
-    const act_t* a;     // x; dy; x
-    const act_t* b;     // w; w; dy
-    const act_t* mask;  // dgrad, or nullptr
-    void* out;          // y; dx; dw
-    const int32_t* offsets;
-    int64_t rows, ld_in, ld_out;
-    int groups, n_in, n_out, relu, accumulate;
-};
-
 // The groups' bounds into off[0..groups], in order and inside the tensors whatever the device memory holds.  By one warp.
 __device__ __forceinline__ void load_offsets(const int32_t* offsets, int groups, int64_t rows, int* off, int lane)
 {
@@ -37,82 +27,402 @@ __device__ __forceinline__ void load_offsets(const int32_t* offsets, int groups,
     }
 }
 
-constexpr int kTile = 64, kStep = 16;
+__device__ int g_grouped_status;  // DBL_OK or DBL_ERR_TIMEOUT, read by dbl_device_status()
 
-// 64 x 64 outputs to a block, 4 x 4 to a thread, on the CUDA cores.  PASS 0: rows of x and of w_e; 1: rows of dy, columns of
-// w_e; 2: columns of dy and of x, over the group's rows.
-template <int PASS>
-__global__ void __launch_bounds__(256) grouped_kernel(const GroupedArgs a)
+__device__ __forceinline__ void report_timeout(volatile int* abort)
 {
-    __shared__ int off[kMaxGroups + 1];
-    __shared__ float sa[kStep][kTile + 1], sb[kStep][kTile + 1];
-    if (threadIdx.x < 32) load_offsets(a.offsets, a.groups, a.rows, off, threadIdx.x);
-    __syncthreads();
-    int group = 0, row0 = 0, row1 = 0;
-    if (PASS == 2) {
-        group = blockIdx.z;
-        row0 = off[group], row1 = off[group + 1];
+    *abort = 1;
+    atomicExch(&g_grouped_status, DBL_ERR_TIMEOUT);
+}
+
+enum : int { kFwd = 0, kDgrad = 1, kWgrad = 2 };
+
+// A tile is 256 rows of the result by BN columns, one CTA pair's: each CTA stages its own 128 rows of A and half of the
+// BN columns of B, 64 elements of the reduction to a stage, and holds its 128 rows of the result in TMEM.
+template <int BN>
+struct Cfg {
+    static constexpr int BNC = BN / 2;
+    static constexpr int A_BYTES = 128 * 64 * 2, B_BYTES = BNC * 64 * 2;
+    static constexpr int STAGE_BYTES = A_BYTES + B_BYTES;
+    static constexpr int STAGES = 196608 / STAGE_BYTES;
+    static constexpr int SMEM = STAGES * STAGE_BYTES + 1024;
+    static constexpr int NB = 512 / BN;  // accumulators: all of TMEM
+    static constexpr int EPI = 8, PROD = 2, MMA_WARP = EPI + PROD;
+    static constexpr int THREADS = 32 * (EPI + PROD + 1);
+    static constexpr int CW = BN / 2;  // columns that one epilogue warp drains
+    static_assert(SMEM >= 117 * 1024, "one CTA on an SM: each takes all of TMEM before a cluster barrier");
+};
+
+// The weight gradient's reductions are cut into chains of this many stages, whose sums are added in registers: the tensor
+// cores cut the digits of a sum below those of its largest term at every step of 16.
+constexpr int kChain = 16;
+
+struct MmaArgs {
+    const act_t* mask;  // dgrad, or nullptr
+    void* out;
+    const int32_t* offsets;
+    int64_t rows, ld;   // ld: of out and mask
+    int groups, n_in, n_out, relu, accumulate;
+    int cols;           // of the result
+    int depth;          // of the reduction (fwd, dgrad)
+    int tiles_m, tiles_n;  // of a group (tiles_m: wgrad alone)
+};
+
+struct Tile {
+    int group, m0, n0, kb;  // kb: stages of the reduction
+    int row0, row1;         // of the group
+};
+
+// Tiles in the order of group, row block, column block: the column blocks of some rows run at the same time, so that x
+// is read once however long the group is.  Called with growing t.
+template <int PASS, int BN>
+__device__ __forceinline__ Tile tile_at(const MmaArgs& p, const int* off, const int* first, int64_t t, int& group)
+{
+    Tile c;
+    int local;
+    if (PASS == kWgrad) {
+        const int per = p.tiles_m * p.tiles_n;
+        group = (int)(t / per);
+        local = (int)(t - (int64_t)group * per);
     } else {
-        int tile = blockIdx.y;
-        for (; group < a.groups; ++group) {
-            const int n = (off[group + 1] - off[group] + kTile - 1) / kTile;
-            if (tile < n) break;
-            tile -= n;
-        }
-        if (group == a.groups) return;
-        row0 = off[group] + tile * kTile;
-        row1 = off[group + 1];
+        while ((int64_t)first[group + 1] * p.tiles_n <= t) ++group;
+        local = (int)(t - (int64_t)first[group] * p.tiles_n);
     }
-    const int col0 = blockIdx.x * kTile, out0 = blockIdx.y * kTile;  // out0: wgrad's rows
-    const int depth = PASS == 0 ? a.n_in : PASS == 1 ? a.n_out : row1 - row0;
-    const act_t* w = a.b + (PASS == 2 ? 0 : (int64_t)group * a.n_out * a.n_in);
-    const int tx = threadIdx.x % 16, ty = threadIdx.x / 16;
-    float acc[4][4] = {};
-    for (int k0 = 0; k0 < depth; k0 += kStep) {
-        for (int i = threadIdx.x; i < kTile * kStep; i += 256) {
-            const int m = PASS == 2 ? i % kTile : i / kStep, k = PASS == 2 ? i / kTile : i % kStep;
-            float v = 0.f;
-            if (k0 + k < depth) {
-                if (PASS == 0 && row0 + m < row1) v = elem_f(a.a[(int64_t)(row0 + m) * a.ld_in + k0 + k]);
-                if (PASS == 1 && row0 + m < row1) v = elem_f(a.a[(int64_t)(row0 + m) * a.ld_out + k0 + k]);
-                if (PASS == 2 && out0 + m < a.n_out) v = elem_f(a.b[(int64_t)(row0 + k0 + k) * a.ld_out + out0 + m]);
-            }
-            sa[k][m] = v;
-            const int n = PASS == 0 ? i / kStep : i % kTile, l = PASS == 0 ? i % kStep : i / kTile;
-            v = 0.f;
-            if (k0 + l < depth) {
-                if (PASS == 0 && col0 + n < a.n_out) v = elem_f(w[(int64_t)(col0 + n) * a.n_in + k0 + l]);
-                if (PASS == 1 && col0 + n < a.n_in) v = elem_f(w[(int64_t)(k0 + l) * a.n_in + col0 + n]);
-                if (PASS == 2 && col0 + n < a.n_in) v = elem_f(a.a[(int64_t)(row0 + k0 + l) * a.ld_in + col0 + n]);
-            }
-            sb[l][n] = v;
+    const int m = local / p.tiles_n;
+    c.group = group;
+    c.n0 = (local - m * p.tiles_n) * BN;
+    c.row0 = off[group];
+    c.row1 = off[group + 1];
+    c.m0 = m * 256 + (PASS == kWgrad ? 0 : c.row0);
+    c.kb = ((PASS == kWgrad ? c.row1 - c.row0 : p.depth) + 63) / 64;
+    return c;
+}
+
+// mbar_wait_warp, for what the other CTA of the pair wrote before its arrival too.
+__device__ __forceinline__ bool pair_try(uint64_t* bar, uint32_t parity) { return bounded_try(bar, parity); }
+__device__ __forceinline__ uint32_t pair_wait_warp(uint64_t* bar, uint32_t parity, volatile int* abort)
+{
+    const uint32_t ok = mbar_wait_warp(bar, parity, abort);
+    // the phase is over: this returns at once, and acquires at the cluster's scope
+    return ok ? (uint32_t)pair_try(bar, parity) : 0u;
+}
+
+template <int PASS, int BN>
+__global__ void __launch_bounds__(Cfg<BN>::THREADS, 1)
+    grouped_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const MmaArgs p)
+{
+    using C = Cfg<BN>;
+    constexpr int STAGES = C::STAGES;
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ __align__(8) uint64_t full_bar[STAGES], empty_bar[STAGES], accf_bar[C::NB], acce_bar[C::NB], tail_bar[C::PROD],
+        drain_bar;
+    __shared__ uint32_t tmem_slot;
+    __shared__ volatile int abort_flag;
+    __shared__ int off[kMaxGroups + 1], first[kMaxGroups + 1];  // first: row blocks of the groups before
+
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    const uint32_t sbase = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    uint8_t* sgen = smem_raw + (sbase - smem_u32(smem_raw));
+    const int rank = (int)cluster_ctarank();
+    const int unit0 = blockIdx.x / 2, nunits = gridDim.x / 2;
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < STAGES; ++s) {
+            mbar_init(&full_bar[s], PASS == kWgrad ? 2 : 1);  // wgrad: an arrival of each CTA's producer
+            mbar_init(&empty_bar[s], 1);
         }
-        __syncthreads();
-#pragma unroll
-        for (int k = 0; k < kStep; ++k)
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) acc[i][j] = fmaf(sa[k][ty + 16 * i], sb[k][tx + 16 * j], acc[i][j]);
-        __syncthreads();
+        for (int b = 0; b < C::NB; ++b) {
+            mbar_init(&accf_bar[b], 1);
+            mbar_init(&acce_bar[b], C::EPI * 2);
+        }
+        for (int b = 0; b < C::PROD; ++b) mbar_init(&tail_bar[b], 1);
+        mbar_init(&drain_bar, 1);
+        abort_flag = 0;
+        fence_mbar_init();
     }
-    for (int i = 0; i < 4; ++i)
-        for (int j = 0; j < 4; ++j) {
-            const int m = ty + 16 * i, n = col0 + tx + 16 * j;
-            float v = acc[i][j];
-            if (PASS == 2) {
-                if (out0 + m >= a.n_out || n >= a.n_in) continue;
-                float* o = static_cast<float*>(a.out) + ((int64_t)group * a.n_out + out0 + m) * a.n_in + n;
-                *o = a.accumulate ? *o + v : v;
-                continue;
+    if (warp >= C::EPI && warp < C::MMA_WARP && lane == 0) {
+        tma_prefetch_desc(&tmA);
+        tma_prefetch_desc(&tmB);
+    }
+    if (warp == C::MMA_WARP) {
+        tmem_alloc_cg<2>(&tmem_slot, C::NB * BN);
+        tmem_relinquish_cg<2>();
+    }
+    if (warp == 0) {
+        load_offsets(p.offsets, p.groups, p.rows, off, lane);
+        __syncwarp();
+        if (PASS != kWgrad) {
+            int before = 0;
+            for (int i0 = 0; i0 < p.groups; i0 += 32) {
+                const int i = i0 + lane;
+                int v = i < p.groups ? (off[i + 1] - off[i] + 255) / 256 : 0;
+                for (int o = 1; o < 32; o <<= 1) {
+                    const int u = __shfl_up_sync(0xffffffffu, v, o);
+                    if (lane >= o) v += u;
+                }
+                if (i < p.groups) first[i + 1] = before + v;
+                before += __shfl_sync(0xffffffffu, v, 31);
             }
-            if (row0 + m >= row1 || n >= (PASS == 0 ? a.n_out : a.n_in)) continue;
-            const int64_t ld = PASS == 0 ? a.ld_out : a.ld_in;
-            const int64_t at = (int64_t)(row0 + m) * ld + n;
-            if (PASS == 0 && a.relu && v < 0.f) v = 0.f;
-            if (PASS == 1 && a.mask && !(elem_f(a.mask[at]) > 0.f)) v = 0.f;
-            static_cast<act_t*>(a.out)[at] = elem_from<act_t>(v);
+            if (lane == 0) first[0] = 0;
         }
+    }
+    tc_fence_before();
+    __syncthreads();
+    cluster_sync_all();
+    tc_fence_after();
+    const uint32_t tmem = tmem_slot;
+    const int64_t total = PASS == kWgrad ? (int64_t)p.groups * p.tiles_m * p.tiles_n : (int64_t)first[p.groups] * p.tiles_n;
+
+    if (warp >= C::EPI && warp < C::MMA_WARP) {
+        // ------------------------------------------------------------------ TMA producers (whole warp, one lane issues)
+        const int prod = warp - C::EPI;
+        int it = 0, last_it = -1, group = 0, tails = 0;
+        bool failed = false;
+        for (int64_t t = unit0; t < total && !failed; t += nunits) {
+            const Tile tc = tile_at<PASS, BN>(p, off, first, t, group);
+            for (int k = 0; k < tc.kb; ++k, ++it) {
+                if (it % C::PROD != prod) continue;
+                const int s = it % STAGES;
+                const uint32_t ok = mbar_wait_warp(&empty_bar[s], ((it / STAGES) & 1) ^ 1, &abort_flag);
+                if (__any_sync(0xffffffffu, ok == 0u)) {
+                    failed = true;
+                    break;
+                }
+                uint8_t* sa = sgen + s * C::STAGE_BYTES;
+                uint8_t* sb = sa + C::A_BYTES;
+                const uint32_t fb0 = mapa_shared(smem_u32(&full_bar[s]), 0);
+                const int bcol = tc.n0 + rank * C::BNC;
+                if constexpr (PASS == kWgrad) {
+                    // the last rows of a group: what is behind them in the last 16 is of another group, or of none, and may be
+                    // NaN, so it is made 0 in both operands before the pair's MMAs may start
+                    const int row = tc.row0 + k * 64, valid = tc.row1 - row;
+                    const bool tail = valid < 64 && (valid & 15);
+                    const uint32_t bar = tail ? mapa_shared(smem_u32(&tail_bar[prod]), rank) : fb0;
+                    if (tail)
+                        mbar_arrive_expect_tx_elect(&tail_bar[prod], C::STAGE_BYTES);
+                    else if (rank == 0)
+                        mbar_arrive_expect_tx_elect(&full_bar[s], 2 * C::STAGE_BYTES);
+                    else if (lane == 0)
+                        mbar_arrive_cluster(fb0);
+                    __syncwarp();
+                    for (int j = 0; j < 2; ++j) tma_load_2d_cg<2>(sa + j * 8192, &tmA, bar, tc.m0 + rank * 128 + 64 * j, row);
+                    for (int j = 0; j < C::BNC / 64; ++j) tma_load_2d_cg<2>(sb + j * 8192, &tmB, bar, bcol + 64 * j, row);
+                    if (tail) {
+                        const uint32_t landed = mbar_wait_warp(&tail_bar[prod], tails & 1, &abort_flag);
+                        ++tails;
+                        if (__any_sync(0xffffffffu, landed == 0u)) {
+                            failed = true;
+                            break;
+                        }
+                        const int from = valid * 128, to = (valid + 15) / 16 * 2048;  // a row has 128 bytes of an atom of 64 columns
+                        for (int j = 0; j < C::STAGE_BYTES / 8192; ++j)
+                            for (int i = from + lane * 16; i < to; i += 512)
+                                *reinterpret_cast<uint4*>(sa + j * 8192 + i) = make_uint4(0, 0, 0, 0);
+                        fence_async_shared();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive_cluster(fb0);
+                        __syncwarp();
+                    }
+                } else {
+                    if (rank == 0) mbar_arrive_expect_tx_elect(&full_bar[s], 2 * C::STAGE_BYTES);
+                    tma_load_2d_cg<2>(sa, &tmA, fb0, k * 64, tc.m0 + rank * 128);
+                    if constexpr (PASS == kFwd)
+                        tma_load_3d_cg<2>(sb, &tmB, fb0, k * 64, bcol, tc.group);
+                    else
+                        for (int j = 0; j < C::BNC / 64; ++j)
+                            tma_load_3d_cg<2>(sb + j * 8192, &tmB, fb0, bcol + 64 * j, k * 64, tc.group);
+                }
+                last_it = it;
+            }
+        }
+        if (failed) {
+            if (lane == 0) report_timeout(&abort_flag);
+            if (rank == 0) {
+                // let copies this producer issued land before the CTA's shared memory goes away
+                for (int i = last_it; i >= 0 && i > last_it - STAGES * C::PROD; i -= C::PROD)
+                    (void)mbar_drain_warp(&full_bar[i % STAGES], (i / STAGES) & 1);
+            } else {
+                // rank 1's copies complete on rank 0's barriers: give them a fixed time instead
+                const uint64_t t0 = globaltimer();
+                while (globaltimer() - t0 < 1000000ull) {
+                }
+            }
+        }
+    } else if (warp == C::MMA_WARP) {
+        // ------------------------------------------------------------------ MMA issuer (rank 0: whole warp, one lane issues)
+        // K-major operands: rows of 128 bytes, 32 bytes a step of 16.  MN-major ones: atoms of 64 columns, 8 KB apart, 16
+        // rows of 128 bytes a step.
+        constexpr bool a_mn = PASS == kWgrad, b_mn = PASS != kFwd;
+        constexpr uint32_t idesc = idesc_act(256, BN, a_mn, b_mn);
+        const uint64_t dA = smem_desc(0, a_mn ? 8192 : 16, 1024, kSwizzle128B);
+        const uint64_t dB = smem_desc(0, b_mn ? 8192 : 16, 1024, kSwizzle128B);
+        constexpr uint64_t a_step = a_mn ? 2048 / 16 : 2, b_step = b_mn ? 2048 / 16 : 2;
+        bool failed = false;
+        auto wait_full = [&](int i) -> bool {
+            const uint32_t ok = PASS == kWgrad ? pair_wait_warp(&full_bar[i % STAGES], (i / STAGES) & 1, &abort_flag)
+                                               : mbar_wait_warp(&full_bar[i % STAGES], (i / STAGES) & 1, &abort_flag);
+            return !__any_sync(0xffffffffu, ok == 0u);
+        };
+        int it = 0, lt = 0, group = 0;
+        for (int64_t t = unit0; t < total && rank == 0 && !failed; t += nunits) {
+            const Tile tc = tile_at<PASS, BN>(p, off, first, t, group);
+            const int chain = PASS == kWgrad ? kChain : tc.kb;
+            for (int k0 = 0; k0 < tc.kb && !failed; k0 += chain, ++lt) {
+                const int buf = lt % C::NB, k1 = min(tc.kb, k0 + chain);
+                const uint32_t free = mbar_wait_warp(&acce_bar[buf], ((lt / C::NB) & 1) ^ 1, &abort_flag);
+                if (__any_sync(0xffffffffu, free == 0u) || !wait_full(it)) {
+                    failed = true;
+                    break;
+                }
+                const uint32_t d = tmem + (uint32_t)(buf * BN);
+                for (int k = k0; k < k1; ++k, ++it) {
+                    tc_fence_after();
+                    const int s = it % STAGES;
+                    const uint32_t sa = sbase + s * C::STAGE_BYTES;
+                    const uint64_t ad = dA | (uint64_t)((sa >> 4) & 0x3FFFu);
+                    const uint64_t bd = dB | (uint64_t)(((sa + C::A_BYTES) >> 4) & 0x3FFFu);
+                    // steps of 16 that hold something
+                    const int left = (PASS == kWgrad ? tc.row1 - tc.row0 : p.depth) - k * 64;
+                    const int steps = left >= 64 ? 4 : (left + 15) / 16;
+                    for (int j = 0; j < steps - 1; ++j)
+                        mma_act_elect_cg<2>(d, ad + j * a_step, bd + j * b_step, idesc, (k > k0 || j > 0) ? 1u : 0u);
+                    // the next stage is waited for while the tensor cores still have a step to do
+                    if (k + 1 < k1) failed = !wait_full(it + 1);
+                    mma_act_elect_cg<2>(d, ad + (steps - 1) * a_step, bd + (steps - 1) * b_step, idesc,
+                                        (k > k0 || steps > 1) ? 1u : 0u);
+                    mma_commit_elect_cg<2>(&empty_bar[s], 3);
+                    if (failed) break;
+                }
+                mma_commit_elect_cg<2>(&accf_bar[buf], 3);
+            }
+        }
+        if (failed && lane == 0) report_timeout(&abort_flag);
+        if (rank == 0) {
+            // every MMA issued above completes before the accumulators are freed
+            mma_commit_elect_cg<2>(&drain_bar, 1);
+            (void)mbar_drain_warp(&drain_bar, 0);
+        }
+    } else {
+        // ------------------------------------------------------------------ epilogue (warps 0 .. EPI-1)
+        constexpr int CW = C::CW, NCH = CW / 32;
+        const int quarter = warp & 3, cw0 = (warp >> 2) * CW;
+        int lt = 0, group = 0;
+        bool failed = false;
+        auto wait_acc = [&](int buf) -> bool {
+            const uint32_t ok = mbar_wait_warp(&accf_bar[buf], (lt / C::NB) & 1, &abort_flag);
+            if (__any_sync(0xffffffffu, ok == 0u)) {
+                if (lane == 0) report_timeout(&abort_flag);
+                failed = true;
+                return false;
+            }
+            tc_fence_after();
+            return true;
+        };
+        auto release = [&](int buf) {
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive_cluster(mapa_shared(smem_u32(&acce_bar[buf]), 0));
+        };
+        for (int64_t t = unit0; t < total && !failed; t += nunits) {
+            const Tile tc = tile_at<PASS, BN>(p, off, first, t, group);
+            const int m = tc.m0 + rank * 128 + quarter * 32 + lane;  // this thread's row of the result
+            if constexpr (PASS == kWgrad) {
+                float acc[CW];
+#pragma unroll
+                for (int i = 0; i < CW; ++i) acc[i] = 0.f;
+                for (int k0 = 0; k0 < tc.kb; k0 += kChain, ++lt) {
+                    const int buf = lt % C::NB;
+                    if (!wait_acc(buf)) break;
+                    const uint32_t taddr = tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(buf * BN + cw0);
+#pragma unroll
+                    for (int ch = 0; ch < NCH; ++ch) {
+                        uint32_t v[32];
+                        tmem_ld_32x32b_x32(taddr + ch * 32, v);
+                        tmem_ld_wait_regs(v);
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) acc[ch * 32 + i] += __uint_as_float(v[i]);
+                    }
+                    release(buf);
+                }
+                if (failed) break;
+                // consecutive lanes hold consecutive columns of dw: each store is a line of 128 bytes
+                if (m < p.n_in) {
+                    float* o = static_cast<float*>(p.out) + ((int64_t)tc.group * p.n_out + tc.n0 + cw0) * p.n_in + m;
+                    const int left = p.n_out - tc.n0 - cw0;
+#pragma unroll
+                    for (int i = 0; i < CW; ++i)
+                        if (i < left) {
+                            float* at = o + (int64_t)i * p.n_in;
+                            *at = p.accumulate ? *at + acc[i] : acc[i];
+                        }
+                }
+            } else {
+                const int buf = lt % C::NB;
+                const bool valid = m < tc.row1;
+                const int64_t at = (int64_t)m * p.ld + tc.n0 + cw0;
+                const int left = p.cols - tc.n0 - cw0;  // columns of this warp that there are, a multiple of 8
+                uint32_t pass[NCH];
+                if constexpr (PASS == kDgrad) {
+                    // which elements the gradient passes, read while the tensor cores are at work
+#pragma unroll
+                    for (int ch = 0; ch < NCH; ++ch) {
+                        pass[ch] = 0xffffffffu;
+                        if (p.mask && valid) {
+#pragma unroll
+                            for (int q = 0; q < 4; ++q)
+                                if (ch * 32 + q * 8 < left) {
+                                    const uint4 h = __ldg(reinterpret_cast<const uint4*>(p.mask + at + ch * 32 + q * 8));
+                                    const uint32_t w[4] = {h.x, h.y, h.z, h.w};
+                                    uint32_t bits = 0;
+#pragma unroll
+                                    for (int i = 0; i < 4; ++i) {
+                                        const float2 f = act::unpack2_u32(w[i]);
+                                        bits |= (f.x > 0.f ? 1u : 0u) << (2 * i) | (f.y > 0.f ? 2u : 0u) << (2 * i);
+                                    }
+                                    pass[ch] = (pass[ch] & ~(255u << (8 * q))) | bits << (8 * q);
+                                }
+                        }
+                    }
+                }
+                if (!wait_acc(buf)) break;
+                const uint32_t taddr = tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(buf * BN + cw0);
+                act_t* o = static_cast<act_t*>(p.out) + at;
+#pragma unroll
+                for (int ch = 0; ch < NCH; ++ch) {
+                    uint32_t v[32];
+                    tmem_ld_32x32b_x32(taddr + ch * 32, v);
+                    tmem_ld_wait_regs(v);
+                    uint4 pk[4];
+                    uint32_t* w32 = reinterpret_cast<uint32_t*>(pk);
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        float a = __uint_as_float(v[2 * i]), b = __uint_as_float(v[2 * i + 1]);
+                        if (PASS == kFwd && p.relu) a = a < 0.f ? 0.f : a, b = b < 0.f ? 0.f : b;  // NaN stays
+                        if (PASS == kDgrad) {
+                            a = pass[ch] >> (2 * i) & 1 ? a : 0.f;
+                            b = pass[ch] >> (2 * i + 1) & 1 ? b : 0.f;
+                        }
+                        w32[i] = act::pack2_u32(a, b);
+                    }
+                    if (valid) {
+#pragma unroll
+                        for (int q = 0; q < 4; ++q)
+                            if (ch * 32 + q * 8 < left) *reinterpret_cast<uint4*>(o + ch * 32 + q * 8) = pk[q];
+                    }
+                }
+                release(buf);
+                ++lt;
+            }
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    // neither CTA of a pair leaves while the other may still signal its barriers or read its TMEM
+    cluster_sync_all();
+    if (warp == C::MMA_WARP) {
+        tc_fence_after();
+        tmem_dealloc_cg<2>(tmem, C::NB * BN);
+    }
 }
 
 int check(const dbl_grouped_shape* s, const char* w)
@@ -129,22 +439,113 @@ int check(const dbl_grouped_shape* s, const char* w)
     return DBL_OK;
 }
 
+int encode(CUtensorMap* m, const void* base, int rank, const cuuint64_t* dims, const cuuint64_t* strides,
+           const cuuint32_t* box, const char* w)
+{
+    const auto fn = encode_tiled();
+    if (!fn) return set_error(DBL_ERR_CUDA, "%s: cuTensorMapEncodeTiled unavailable from the driver", w);
+    const cuuint32_t es[3] = {1, 1, 1};
+    const CUresult r = fn(m, act::kF16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, (cuuint32_t)rank,
+                          const_cast<void*>(base), dims, strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                          CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? DBL_OK : set_error(DBL_ERR_CUDA, "%s: tensor map encode failed (%d)", w, (int)r);
+}
+
+// Rows of c columns, in boxes of 64 columns.
+int encode_rows(CUtensorMap* m, const void* base, int64_t rows, int c, int64_t ld, int box_rows, const char* w)
+{
+    const cuuint64_t dims[2] = {(cuuint64_t)c, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)ld * sizeof(act_t)};
+    const cuuint32_t box[2] = {64, (cuuint32_t)box_rows};
+    return encode(m, base, 2, dims, strides, box, w);
+}
+
+int encode_weights(CUtensorMap* m, const void* base, const dbl_grouped_shape* s, int box_rows, const char* w)
+{
+    const cuuint64_t dims[3] = {(cuuint64_t)s->n_in, (cuuint64_t)s->n_out, (cuuint64_t)s->groups};
+    const cuuint64_t strides[2] = {dims[0] * sizeof(act_t), dims[0] * dims[1] * sizeof(act_t)};
+    const cuuint32_t box[3] = {64, (cuuint32_t)box_rows, 1};
+    return encode(m, base, 3, dims, strides, box, w);
+}
+
+template <int PASS, int BN>
+int launch(const CUtensorMap& ta, const CUtensorMap& tb, MmaArgs p, int64_t most_tiles, cudaStream_t st, const char* w)
+{
+    using C = Cfg<BN>;
+    int rc = allow_launch<grouped_kernel<PASS, BN>>(C::SMEM, false, w);
+    if (rc != DBL_OK) return rc;
+    int dev = 0;
+    if ((rc = cuda_check(cudaGetDevice(&dev), w)) != DBL_OK) return rc;
+    int pairs = clusters_held<grouped_kernel<PASS, BN>>(dev, 2, C::THREADS, C::SMEM);
+    if (pairs < 1) pairs = 1;  // as one pair after the other
+    if (pairs > most_tiles) pairs = (int)most_tiles;
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = 2;
+    at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+    cfg.gridDim = dim3(2 * pairs);
+    cfg.blockDim = dim3(C::THREADS);
+    cfg.dynamicSmemBytes = C::SMEM;
+    cfg.stream = st;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    const cudaError_t err = cudaLaunchKernelEx(&cfg, grouped_kernel<PASS, BN>, ta, tb, p);
+    rc = launch_check(w);
+    return err == cudaSuccess ? rc : cuda_check(err, w);
+}
+
+template <int PASS, int BN>
+int run_tiles(const dbl_grouped_shape* s, const void* a, const void* b, const int32_t* offsets, const void* mask, void* out,
+              int accumulate, cudaStream_t st, const char* w)
+{
+    const int64_t ld_in = s->ld_in ? s->ld_in : s->n_in, ld_out = s->ld_out ? s->ld_out : s->n_out;
+    CUtensorMap ta, tb;
+    int rc;
+    if (PASS == kFwd) {
+        if ((rc = encode_rows(&ta, a, s->rows, s->n_in, ld_in, 128, w)) != DBL_OK) return rc;
+        rc = encode_weights(&tb, b, s, BN / 2, w);
+    } else if (PASS == kDgrad) {
+        if ((rc = encode_rows(&ta, a, s->rows, s->n_out, ld_out, 128, w)) != DBL_OK) return rc;
+        rc = encode_weights(&tb, b, s, 64, w);
+    } else {
+        if ((rc = encode_rows(&ta, a, s->rows, s->n_in, ld_in, 64, w)) != DBL_OK) return rc;
+        rc = encode_rows(&tb, b, s->rows, s->n_out, ld_out, 64, w);
+    }
+    if (rc != DBL_OK) return rc;
+    MmaArgs p = {};
+    p.mask = static_cast<const act_t*>(mask);
+    p.out = out;
+    p.offsets = offsets;
+    p.rows = s->rows;
+    p.ld = PASS == kFwd ? ld_out : ld_in;
+    p.groups = s->groups, p.n_in = s->n_in, p.n_out = s->n_out;
+    p.relu = s->relu != 0, p.accumulate = accumulate;
+    p.cols = PASS == kDgrad ? s->n_in : s->n_out;
+    p.depth = PASS == kFwd ? s->n_in : s->n_out;
+    p.tiles_m = (s->n_in + 255) / 256;
+    p.tiles_n = (p.cols + BN - 1) / BN;
+    // the row blocks are the device's to count: a group's last one is partial
+    const int64_t blocks = PASS == kWgrad ? (int64_t)s->groups * p.tiles_m
+                                          : (s->rows < s->groups ? s->rows : s->rows / 256 + s->groups);
+    return launch<PASS, BN>(ta, tb, p, blocks * p.tiles_n, st, w);
+}
+
 template <int PASS>
 int run(const dbl_grouped_shape* s, const void* a, const void* b, const int32_t* offsets, const void* mask, void* out,
         int accumulate, void* stream, const char* w)
 {
-    const GroupedArgs g = {static_cast<const act_t*>(a), static_cast<const act_t*>(b), static_cast<const act_t*>(mask), out,
-                           offsets, s->rows, s->ld_in ? s->ld_in : s->n_in, s->ld_out ? s->ld_out : s->n_out, s->groups,
-                           s->n_in, s->n_out, s->relu != 0, accumulate};
-    const int cols = PASS == 0 ? s->n_out : s->n_in;
-    const dim3 grid((cols + kTile - 1) / kTile,
-                    PASS == 2 ? (s->n_out + kTile - 1) / kTile : (unsigned)(s->rows / kTile + s->groups),
-                    PASS == 2 ? s->groups : 1);
-    grouped_kernel<PASS><<<grid, 256, 0, as_stream(stream)>>>(g);
-    return launch_check(w);
+    return run_tiles<PASS, 256>(s, a, b, offsets, mask, out, accumulate, as_stream(stream), w);
 }
 
 }  // namespace
+
+namespace dbl {
+
+static int read_word(int* status) { return status_read(g_grouped_status, status); }
+static int clear_word() { return status_clear(g_grouped_status); }
+StatusWord grouped_status_word() { return {read_word, clear_word}; }
+
+}  // namespace dbl
 
 extern "C" size_t dbl_grouped_workspace_bytes(const dbl_grouped_shape* s, int pass)
 {
