@@ -98,15 +98,6 @@ __device__ __forceinline__ Tile tile_at(const MmaArgs& p, const int* off, const 
     return c;
 }
 
-// mbar_wait_warp, for what the other CTA of the pair wrote before its arrival too.
-__device__ __forceinline__ bool pair_try(uint64_t* bar, uint32_t parity) { return bounded_try(bar, parity); }
-__device__ __forceinline__ uint32_t pair_wait_warp(uint64_t* bar, uint32_t parity, volatile int* abort)
-{
-    const uint32_t ok = mbar_wait_warp(bar, parity, abort);
-    // the phase is over: this returns at once, and acquires at the cluster's scope
-    return ok ? (uint32_t)pair_try(bar, parity) : 0u;
-}
-
 template <int PASS, int BN>
 __global__ void __launch_bounds__(Cfg<BN>::THREADS, 1)
     grouped_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const MmaArgs p)
@@ -114,8 +105,8 @@ __global__ void __launch_bounds__(Cfg<BN>::THREADS, 1)
     using C = Cfg<BN>;
     constexpr int STAGES = C::STAGES;
     extern __shared__ uint8_t smem_raw[];
-    __shared__ __align__(8) uint64_t full_bar[STAGES], empty_bar[STAGES], accf_bar[C::NB], acce_bar[C::NB], tail_bar[C::PROD],
-        drain_bar;
+    __shared__ __align__(8) uint64_t full_bar[STAGES], empty_bar[STAGES], accf_bar[C::NB], acce_bar[C::NB], drain_bar;
+    __shared__ __align__(8) uint64_t tail_bar[C::PROD], peer_bar[STAGES];  // wgrad, the last rows of a group
     __shared__ uint32_t tmem_slot;
     __shared__ volatile int abort_flag;
     __shared__ int off[kMaxGroups + 1], first[kMaxGroups + 1];  // first: row blocks of the groups before
@@ -128,8 +119,9 @@ __global__ void __launch_bounds__(Cfg<BN>::THREADS, 1)
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < STAGES; ++s) {
-            mbar_init(&full_bar[s], PASS == kWgrad ? 2 : 1);  // wgrad: an arrival of each CTA's producer
+            mbar_init(&full_bar[s], 1);
             mbar_init(&empty_bar[s], 1);
+            mbar_init(&peer_bar[s], 1);
         }
         for (int b = 0; b < C::NB; ++b) {
             mbar_init(&accf_bar[b], 1);
@@ -202,9 +194,6 @@ __global__ void __launch_bounds__(Cfg<BN>::THREADS, 1)
                         mbar_arrive_expect_tx_elect(&tail_bar[prod], C::STAGE_BYTES);
                     else if (rank == 0)
                         mbar_arrive_expect_tx_elect(&full_bar[s], 2 * C::STAGE_BYTES);
-                    else if (lane == 0)
-                        mbar_arrive_cluster(fb0);
-                    __syncwarp();
                     for (int j = 0; j < 2; ++j) tma_load_2d_cg<2>(sa + j * 8192, &tmA, bar, tc.m0 + rank * 128 + 64 * j, row);
                     for (int j = 0; j < C::BNC / 64; ++j) tma_load_2d_cg<2>(sb + j * 8192, &tmB, bar, bcol + 64 * j, row);
                     if (tail) {
@@ -220,7 +209,7 @@ __global__ void __launch_bounds__(Cfg<BN>::THREADS, 1)
                                 *reinterpret_cast<uint4*>(sa + j * 8192 + i) = make_uint4(0, 0, 0, 0);
                         fence_async_shared();
                         __syncwarp();
-                        if (lane == 0) mbar_arrive_cluster(fb0);
+                        if (lane == 0) mbar_arrive_cluster(rank == 0 ? fb0 : mapa_shared(smem_u32(&peer_bar[s]), 0));
                         __syncwarp();
                     }
                 } else {
@@ -258,19 +247,26 @@ __global__ void __launch_bounds__(Cfg<BN>::THREADS, 1)
         const uint64_t dB = smem_desc(0, b_mn ? 8192 : 16, 1024, kSwizzle128B);
         constexpr uint64_t a_step = a_mn ? 2048 / 16 : 2, b_step = b_mn ? 2048 / 16 : 2;
         bool failed = false;
-        auto wait_full = [&](int i) -> bool {
-            const uint32_t ok = PASS == kWgrad ? pair_wait_warp(&full_bar[i % STAGES], (i / STAGES) & 1, &abort_flag)
-                                               : mbar_wait_warp(&full_bar[i % STAGES], (i / STAGES) & 1, &abort_flag);
+        uint32_t peers = 0;  // bit s: the phase of peer_bar[s]
+        auto wait_full = [&](int i, bool tail) -> bool {
+            const int s = i % STAGES;
+            uint32_t ok = mbar_wait_warp(&full_bar[s], (i / STAGES) & 1, &abort_flag);
+            if (tail) {
+                if (ok) ok = mbar_wait_warp(&peer_bar[s], peers >> s & 1, &abort_flag);
+                if (ok) ok = (uint32_t)bounded_try(&peer_bar[s], peers >> s & 1);  // at once: the peer's zeros acquired
+                peers ^= 1u << s;
+            }
             return !__any_sync(0xffffffffu, ok == 0u);
         };
         int it = 0, lt = 0, group = 0;
         for (int64_t t = unit0; t < total && rank == 0 && !failed; t += nunits) {
             const Tile tc = tile_at<PASS, BN>(p, off, first, t, group);
             const int chain = PASS == kWgrad ? kChain : tc.kb;
+            const bool tail = PASS == kWgrad && ((tc.row1 - tc.row0) & 15);
             for (int k0 = 0; k0 < tc.kb && !failed; k0 += chain, ++lt) {
                 const int buf = lt % C::NB, k1 = min(tc.kb, k0 + chain);
                 const uint32_t free = mbar_wait_warp(&acce_bar[buf], ((lt / C::NB) & 1) ^ 1, &abort_flag);
-                if (__any_sync(0xffffffffu, free == 0u) || !wait_full(it)) {
+                if (__any_sync(0xffffffffu, free == 0u) || !wait_full(it, k0 + 1 == tc.kb && tail)) {
                     failed = true;
                     break;
                 }
@@ -287,7 +283,7 @@ __global__ void __launch_bounds__(Cfg<BN>::THREADS, 1)
                     for (int j = 0; j < steps - 1; ++j)
                         mma_act_elect_cg<2>(d, ad + j * a_step, bd + j * b_step, idesc, (k > k0 || j > 0) ? 1u : 0u);
                     // the next stage is waited for while the tensor cores still have a step to do
-                    if (k + 1 < k1) failed = !wait_full(it + 1);
+                    if (k + 1 < k1) failed = !wait_full(it + 1, k + 2 == tc.kb && tail);
                     mma_act_elect_cg<2>(d, ad + (steps - 1) * a_step, bd + (steps - 1) * b_step, idesc,
                                         (k > k0 || steps > 1) ? 1u : 0u);
                     mma_commit_elect_cg<2>(&empty_bar[s], 3);
