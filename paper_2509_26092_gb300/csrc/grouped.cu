@@ -263,31 +263,32 @@ __global__ void __launch_bounds__(Cfg<BN>::THREADS, 1)
             const Tile tc = tile_at<PASS, BN>(p, off, first, t, group);
             const int chain = PASS == kWgrad ? kChain : tc.kb;
             const bool tail = PASS == kWgrad && ((tc.row1 - tc.row0) & 15);
+            const int length = PASS == kWgrad ? tc.row1 - tc.row0 : p.depth;
             for (int k0 = 0; k0 < tc.kb && !failed; k0 += chain, ++lt) {
                 const int buf = lt % C::NB, k1 = min(tc.kb, k0 + chain);
                 const uint32_t free = mbar_wait_warp(&acce_bar[buf], ((lt / C::NB) & 1) ^ 1, &abort_flag);
-                if (__any_sync(0xffffffffu, free == 0u) || !wait_full(it, k0 + 1 == tc.kb && tail)) {
+                if (__any_sync(0xffffffffu, free == 0u)) {
                     failed = true;
                     break;
                 }
                 const uint32_t d = tmem + (uint32_t)(buf * BN);
                 for (int k = k0; k < k1; ++k, ++it) {
+                    if (!wait_full(it, k + 1 == tc.kb && tail)) {
+                        failed = true;
+                        break;
+                    }
                     tc_fence_after();
                     const int s = it % STAGES;
                     const uint32_t sa = sbase + s * C::STAGE_BYTES;
                     const uint64_t ad = dA | (uint64_t)((sa >> 4) & 0x3FFFu);
                     const uint64_t bd = dB | (uint64_t)(((sa + C::A_BYTES) >> 4) & 0x3FFFu);
-                    // steps of 16 that hold something
-                    const int left = (PASS == kWgrad ? tc.row1 - tc.row0 : p.depth) - k * 64;
-                    const int steps = left >= 64 ? 4 : (left + 15) / 16;
-                    for (int j = 0; j < steps - 1; ++j)
-                        mma_act_elect_cg<2>(d, ad + j * a_step, bd + j * b_step, idesc, (k > k0 || j > 0) ? 1u : 0u);
-                    // the next stage is waited for while the tensor cores still have a step to do
-                    if (k + 1 < k1) failed = !wait_full(it + 1, k + 2 == tc.kb && tail);
-                    mma_act_elect_cg<2>(d, ad + (steps - 1) * a_step, bd + (steps - 1) * b_step, idesc,
-                                        (k > k0 || steps > 1) ? 1u : 0u);
+                    const int left = length - k * 64;
+                    if (left > 48)
+                        mma_act_x4_elect_cg<2>(d, ad, a_step, bd, b_step, idesc, k > k0 ? 1u : 0u);
+                    else  // the steps of 16 that hold something
+                        for (int j = 0; j < (left + 15) / 16; ++j)
+                            mma_act_elect_cg<2>(d, ad + j * a_step, bd + j * b_step, idesc, (k > k0 || j > 0) ? 1u : 0u);
                     mma_commit_elect_cg<2>(&empty_bar[s], 3);
-                    if (failed) break;
                 }
                 mma_commit_elect_cg<2>(&accf_bar[buf], 3);
             }
@@ -331,12 +332,12 @@ __global__ void __launch_bounds__(Cfg<BN>::THREADS, 1)
                     if (!wait_acc(buf)) break;
                     const uint32_t taddr = tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(buf * BN + cw0);
 #pragma unroll
-                    for (int ch = 0; ch < NCH; ++ch) {
-                        uint32_t v[32];
-                        tmem_ld_32x32b_x32(taddr + ch * 32, v);
+                    for (int ch = 0; ch < CW / 16; ++ch) {
+                        uint32_t v[16];
+                        tmem_ld_32x32b_x16(taddr + ch * 16, v);
                         tmem_ld_wait_regs(v);
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) acc[ch * 32 + i] += __uint_as_float(v[i]);
+                        for (int i = 0; i < 16; ++i) acc[ch * 16 + i] += __uint_as_float(v[i]);
                     }
                     release(buf);
                 }
