@@ -45,9 +45,9 @@ struct Cfg {
     static constexpr int A_BYTES = 128 * 64 * 2, B_BYTES = BNC * 64 * 2;
     static constexpr int STAGE_BYTES = A_BYTES + B_BYTES;
     static constexpr int STAGES = 196608 / STAGE_BYTES;
-    static constexpr int SMEM = STAGES * STAGE_BYTES + 1024;
-    static constexpr int NB = 512 / BN;  // accumulators: all of TMEM
     static constexpr int EPI = 8, PROD = 2, MMA_WARP = EPI + PROD;
+    static constexpr int SMEM = STAGES * STAGE_BYTES + EPI * 2048 + 1024;
+    static constexpr int NB = 512 / BN;  // accumulators: all of TMEM
     static constexpr int THREADS = 32 * (EPI + PROD + 1);
     static constexpr int CW = BN / 2;  // columns that one epilogue warp drains
     static_assert(SMEM >= 117 * 1024, "one CTA on an SM: each takes all of TMEM before a cluster barrier");
@@ -73,29 +73,58 @@ struct Tile {
     int row0, row1;         // of the group
 };
 
-// Tiles in the order of group, row block, column block: the column blocks of some rows run at the same time, so that x
-// is read once however long the group is.  Called with growing t.
+// The tiles of a CTA pair, every nunits-th in the order of group, row block, column block: the column blocks of some rows
+// run at the same time, so that x is read once however long the group is.  Counted on, as every role of the kernel would
+// divide for every tile.
 template <int PASS, int BN>
-__device__ __forceinline__ Tile tile_at(const MmaArgs& p, const int* off, const int* first, int64_t t, int& group)
-{
-    Tile c;
-    int local;
-    if (PASS == kWgrad) {
-        const int per = p.tiles_m * p.tiles_n;
-        group = (int)(t / per);
-        local = (int)(t - (int64_t)group * per);
-    } else {
-        while ((int64_t)first[group + 1] * p.tiles_n <= t) ++group;
-        local = (int)(t - (int64_t)first[group] * p.tiles_n);
+struct Walk {
+    int group, m, n, step_m, step_n;
+
+    __device__ __forceinline__ Walk(const MmaArgs& p, const int* first, int unit0, int nunits)
+        : group(0), m(unit0 / p.tiles_n), n(unit0 % p.tiles_n), step_m(nunits / p.tiles_n), step_n(nunits % p.tiles_n)
+    {
+        settle(p, first);
     }
-    const int m = local / p.tiles_n;
-    c.group = group;
-    c.n0 = (local - m * p.tiles_n) * BN;
-    c.row0 = off[group];
-    c.row1 = off[group + 1];
-    c.m0 = m * 256 + (PASS == kWgrad ? 0 : c.row0);
-    c.kb = ((PASS == kWgrad ? c.row1 - c.row0 : p.depth) + 63) / 64;
-    return c;
+    __device__ __forceinline__ void settle(const MmaArgs& p, const int* first)
+    {
+        for (; group < p.groups; ++group) {
+            const int blocks = PASS == kWgrad ? p.tiles_m : first[group + 1] - first[group];
+            if (m < blocks) return;
+            m -= blocks;
+        }
+    }
+    __device__ __forceinline__ void next(const MmaArgs& p, const int* first)
+    {
+        m += step_m;
+        if ((n += step_n) >= p.tiles_n) n -= p.tiles_n, ++m;
+        settle(p, first);
+    }
+    __device__ __forceinline__ bool there(const MmaArgs& p) const { return group < p.groups; }
+    __device__ __forceinline__ Tile tile(const MmaArgs& p, const int* off) const
+    {
+        Tile c;
+        c.group = group;
+        c.n0 = n * BN;
+        c.row0 = off[group];
+        c.row1 = off[group + 1];
+        c.m0 = m * 256 + (PASS == kWgrad ? 0 : c.row0);
+        c.kb = ((PASS == kWgrad ? c.row1 - c.row0 : p.depth) + 63) / 64;
+        return c;
+    }
+};
+
+// The larger of each half and 0; NaN stays.
+__device__ __forceinline__ uint32_t relu2(uint32_t v)
+{
+    uint32_t r;
+    asm("max.NaN." DBL_ACT_X2 " %0, %1, %2;" : "=r"(r) : "r"(v), "r"(0u));
+    return r;
+}
+
+// v where the half of h is above 0, else 0.
+__device__ __forceinline__ uint32_t pass2(uint32_t v, uint32_t h)
+{
+    return v & __hgt2_mask(*reinterpret_cast<const act2_t*>(&h), act::pack2(0.f, 0.f));
 }
 
 template <int PASS, int BN>
@@ -163,15 +192,15 @@ __global__ void __launch_bounds__(Cfg<BN>::THREADS, 1)
     cluster_sync_all();
     tc_fence_after();
     const uint32_t tmem = tmem_slot;
-    const int64_t total = PASS == kWgrad ? (int64_t)p.groups * p.tiles_m * p.tiles_n : (int64_t)first[p.groups] * p.tiles_n;
+    Walk<PASS, BN> walk(p, first, unit0, nunits);
 
     if (warp >= C::EPI && warp < C::MMA_WARP) {
         // ------------------------------------------------------------------ TMA producers (whole warp, one lane issues)
         const int prod = warp - C::EPI;
-        int it = 0, last_it = -1, group = 0, tails = 0;
+        int it = 0, last_it = -1, tails = 0;
         bool failed = false;
-        for (int64_t t = unit0; t < total && !failed; t += nunits) {
-            const Tile tc = tile_at<PASS, BN>(p, off, first, t, group);
+        for (; walk.there(p) && !failed; walk.next(p, first)) {
+            const Tile tc = walk.tile(p, off);
             for (int k = 0; k < tc.kb; ++k, ++it) {
                 if (it % C::PROD != prod) continue;
                 const int s = it % STAGES;
@@ -258,9 +287,9 @@ __global__ void __launch_bounds__(Cfg<BN>::THREADS, 1)
             }
             return !__any_sync(0xffffffffu, ok == 0u);
         };
-        int it = 0, lt = 0, group = 0;
-        for (int64_t t = unit0; t < total && rank == 0 && !failed; t += nunits) {
-            const Tile tc = tile_at<PASS, BN>(p, off, first, t, group);
+        int it = 0, lt = 0;
+        for (; walk.there(p) && rank == 0 && !failed; walk.next(p, first)) {
+            const Tile tc = walk.tile(p, off);
             const int chain = PASS == kWgrad ? kChain : tc.kb;
             const bool tail = PASS == kWgrad && ((tc.row1 - tc.row0) & 15);
             const int length = PASS == kWgrad ? tc.row1 - tc.row0 : p.depth;
@@ -301,9 +330,11 @@ __global__ void __launch_bounds__(Cfg<BN>::THREADS, 1)
         }
     } else {
         // ------------------------------------------------------------------ epilogue (warps 0 .. EPI-1)
-        constexpr int CW = C::CW, NCH = CW / 32;
+        constexpr int CW = C::CW;
+        [[maybe_unused]] constexpr int NCH = CW / 32;
         const int quarter = warp & 3, cw0 = (warp >> 2) * CW;
-        int lt = 0, group = 0;
+        [[maybe_unused]] uint4* stage = reinterpret_cast<uint4*>(sgen + STAGES * C::STAGE_BYTES) + warp * 128;  // 2 KB
+        int lt = 0;
         bool failed = false;
         auto wait_acc = [&](int buf) -> bool {
             const uint32_t ok = mbar_wait_warp(&accf_bar[buf], (lt / C::NB) & 1, &abort_flag);
@@ -320,10 +351,10 @@ __global__ void __launch_bounds__(Cfg<BN>::THREADS, 1)
             __syncwarp();
             if (lane == 0) mbar_arrive_cluster(mapa_shared(smem_u32(&acce_bar[buf]), 0));
         };
-        for (int64_t t = unit0; t < total && !failed; t += nunits) {
-            const Tile tc = tile_at<PASS, BN>(p, off, first, t, group);
-            const int m = tc.m0 + rank * 128 + quarter * 32 + lane;  // this thread's row of the result
+        for (; walk.there(p) && !failed; walk.next(p, first)) {
+            const Tile tc = walk.tile(p, off);
             if constexpr (PASS == kWgrad) {
+                const int m = tc.m0 + rank * 128 + quarter * 32 + lane;  // this thread's row of the result
                 float acc[CW];
 #pragma unroll
                 for (int i = 0; i < CW; ++i) acc[i] = 0.f;
@@ -345,40 +376,42 @@ __global__ void __launch_bounds__(Cfg<BN>::THREADS, 1)
                 // consecutive lanes hold consecutive columns of dw: each store is a line of 128 bytes
                 if (m < p.n_in) {
                     float* o = static_cast<float*>(p.out) + ((int64_t)tc.group * p.n_out + tc.n0 + cw0) * p.n_in + m;
-                    const int left = p.n_out - tc.n0 - cw0;
+                    const int left = p.n_out - tc.n0 - cw0;  // a multiple of 8
+                    if (p.accumulate) {
 #pragma unroll
-                    for (int i = 0; i < CW; ++i)
-                        if (i < left) {
-                            float* at = o + (int64_t)i * p.n_in;
-                            *at = p.accumulate ? *at + acc[i] : acc[i];
-                        }
+                        for (int i0 = 0; i0 < CW; i0 += 8)
+                            if (i0 < left) {
+                                float before[8];
+#pragma unroll
+                                for (int i = 0; i < 8; ++i) before[i] = o[(int64_t)i * p.n_in];
+#pragma unroll
+                                for (int i = 0; i < 8; ++i, o += p.n_in) *o = before[i] + acc[i0 + i];
+                            }
+                    } else {
+#pragma unroll
+                        for (int i0 = 0; i0 < CW; i0 += 8)
+                            if (i0 < left) {
+#pragma unroll
+                                for (int i = 0; i < 8; ++i, o += p.n_in) *o = acc[i0 + i];
+                            }
+                    }
                 }
             } else {
                 const int buf = lt % C::NB;
-                const bool valid = m < tc.row1;
-                const int64_t at = (int64_t)m * p.ld + tc.n0 + cw0;
-                const int left = p.cols - tc.n0 - cw0;  // columns of this warp that there are, a multiple of 8
-                uint32_t pass[NCH];
+                // A thread has 32 columns of a row, 64 bytes; through shared memory the warp's 32 rows become stores of four
+                // lanes to a row, so that a store meets 8 rows instead of 32.
+                const int r0 = tc.m0 + rank * 128 + quarter * 32 + lane / 4, q = lane % 4;
+                const int col = tc.n0 + cw0 + q * 8;
+                const int64_t at = (int64_t)r0 * p.ld + col, down = 8 * p.ld;
+                uint4 gate[NCH][4];  // dgrad: the mask, read while the tensor cores are at work
                 if constexpr (PASS == kDgrad) {
-                    // which elements the gradient passes, read while the tensor cores are at work
+                    if (p.mask) {
 #pragma unroll
-                    for (int ch = 0; ch < NCH; ++ch) {
-                        pass[ch] = 0xffffffffu;
-                        if (p.mask && valid) {
+                        for (int ch = 0; ch < NCH; ++ch)
 #pragma unroll
-                            for (int q = 0; q < 4; ++q)
-                                if (ch * 32 + q * 8 < left) {
-                                    const uint4 h = __ldg(reinterpret_cast<const uint4*>(p.mask + at + ch * 32 + q * 8));
-                                    const uint32_t w[4] = {h.x, h.y, h.z, h.w};
-                                    uint32_t bits = 0;
-#pragma unroll
-                                    for (int i = 0; i < 4; ++i) {
-                                        const float2 f = act::unpack2_u32(w[i]);
-                                        bits |= (f.x > 0.f ? 1u : 0u) << (2 * i) | (f.y > 0.f ? 2u : 0u) << (2 * i);
-                                    }
-                                    pass[ch] = (pass[ch] & ~(255u << (8 * q))) | bits << (8 * q);
-                                }
-                        }
+                            for (int i = 0; i < 4; ++i)
+                                if (r0 + 8 * i < tc.row1 && col + ch * 32 < p.cols)
+                                    gate[ch][i] = __ldg(reinterpret_cast<const uint4*>(p.mask + at + i * down + ch * 32));
                     }
                 }
                 if (!wait_acc(buf)) break;
@@ -389,25 +422,32 @@ __global__ void __launch_bounds__(Cfg<BN>::THREADS, 1)
                     uint32_t v[32];
                     tmem_ld_32x32b_x32(taddr + ch * 32, v);
                     tmem_ld_wait_regs(v);
-                    uint4 pk[4];
-                    uint32_t* w32 = reinterpret_cast<uint32_t*>(pk);
+                    if (ch == NCH - 1) release(buf);
+                    __syncwarp();  // the chunk before has been read
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        float a = __uint_as_float(v[2 * i]), b = __uint_as_float(v[2 * i + 1]);
-                        if (PASS == kFwd && p.relu) a = a < 0.f ? 0.f : a, b = b < 0.f ? 0.f : b;  // NaN stays
-                        if (PASS == kDgrad) {
-                            a = pass[ch] >> (2 * i) & 1 ? a : 0.f;
-                            b = pass[ch] >> (2 * i + 1) & 1 ? b : 0.f;
+                    for (int i = 0; i < 4; ++i) {
+                        uint4 pk;
+                        uint32_t* w32 = reinterpret_cast<uint32_t*>(&pk);
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            w32[j] = act::pack2_u32(__uint_as_float(v[8 * i + 2 * j]), __uint_as_float(v[8 * i + 2 * j + 1]));
+                            if (PASS == kFwd && p.relu) w32[j] = relu2(w32[j]);
                         }
-                        w32[i] = act::pack2_u32(a, b);
+                        stage[lane * 4 + (i ^ (lane >> 1 & 3))] = pk;  // in any eight lanes, eight different banks of 16 bytes
                     }
-                    if (valid) {
+                    __syncwarp();
 #pragma unroll
-                        for (int q = 0; q < 4; ++q)
-                            if (ch * 32 + q * 8 < left) *reinterpret_cast<uint4*>(o + ch * 32 + q * 8) = pk[q];
+                    for (int i = 0; i < 4; ++i) {
+                        const int r = 8 * i + lane / 4;
+                        uint4 pk = stage[r * 4 + (q ^ (r >> 1 & 3))];
+                        if (PASS == kDgrad && p.mask) {
+                            const uint4 h = gate[ch][i];
+                            pk = make_uint4(pass2(pk.x, h.x), pass2(pk.y, h.y), pass2(pk.z, h.z), pass2(pk.w, h.w));
+                        }
+                        if (r0 + 8 * i < tc.row1 && col + ch * 32 < p.cols)
+                            *reinterpret_cast<uint4*>(o + i * down + ch * 32) = pk;
                     }
                 }
-                release(buf);
                 ++lt;
             }
         }
