@@ -37,27 +37,75 @@ __device__ __forceinline__ void philox(uint64_t block, uint64_t step, uint32_t k
     w[0] = c0, w[1] = c1, w[2] = c2, w[3] = c3;
 }
 
-// One block of four channels to a thread, element by element.
 template <class T>
-__global__ void __launch_bounds__(256) dropout_kernel(const DropArgs a)
+__device__ __forceinline__ float dropped(const DropArgs& a, uint32_t word, float x, float res)
 {
-    const int per = (a.c + 3) / 4;
-    const int64_t total = a.rows * per;
+    return fmaf(word >= a.threshold ? x : 0.f, a.scale, res);
+}
+
+// Sixteen bytes of a row to a thread, two blocks of the generator (fp32: one), rows_per_block rows to a block.
+template <class T>
+__global__ void __launch_bounds__(256) dropout_kernel(const DropArgs a, int rows_per_block)
+{
+    constexpr int N = 16 / (int)sizeof(T);
+    const unsigned units = (unsigned)a.c / N;
+    const int64_t r0 = (int64_t)blockIdx.x * rows_per_block;
+    const unsigned n = (unsigned)min((int64_t)rows_per_block, a.rows - r0) * units;
     const uint64_t step = *a.step;
-    for (int64_t b = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; b < total; b += (int64_t)gridDim.x * blockDim.x) {
-        const int64_t row = b / per;
-        const int col = (int)(b - row * per) * 4;
-        uint32_t w[4];
-        philox((uint64_t)b, step, a.key0, a.key1, w);
-        const T* x = static_cast<const T*>(a.x) + row * a.ld_in + col;
-        const T* res = a.res ? static_cast<const T*>(a.res) + row * a.ld_in + col : nullptr;
-        T* y = static_cast<T*>(a.y) + row * a.ld_out + col;
+    for (unsigned i = threadIdx.x; i < n; i += 256) {
+        const unsigned l = i / units, u = i - l * units;
+        const int64_t r = r0 + l, in = r * a.ld_in + u * N, out = r * a.ld_out + u * N;
+        const uint4 xv = *reinterpret_cast<const uint4*>(static_cast<const T*>(a.x) + in);
+        uint4 rv = make_uint4(0, 0, 0, 0);
+        if (a.res) rv = *reinterpret_cast<const uint4*>(static_cast<const T*>(a.res) + in);
+        const uint32_t x[4] = {xv.x, xv.y, xv.z, xv.w}, res[4] = {rv.x, rv.y, rv.z, rv.w};
+        uint32_t y[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (col + i < a.c) {
-                const float v = w[i] >= a.threshold ? elem_f(x[i]) : 0.f;
-                y[i] = elem_from<T>(fmaf(v, a.scale, res ? elem_f(res[i]) : 0.f));
+        for (int b = 0; b < N / 4; ++b) {
+            uint32_t w[4];
+            philox((uint64_t)r * ((unsigned)a.c / 4) + (u * (N / 4) + b), step, a.key0, a.key1, w);
+            if constexpr (sizeof(T) == 4) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    y[e] = __float_as_uint(dropped<T>(a, w[e], __uint_as_float(x[e]), __uint_as_float(res[e])));
+            } else {
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const float2 f = act::unpack2_u32(x[2 * b + e]), g = act::unpack2_u32(res[2 * b + e]);
+                    y[2 * b + e] = act::pack2_u32(dropped<T>(a, w[2 * e], f.x, g.x), dropped<T>(a, w[2 * e + 1], f.y, g.y));
+                }
             }
+        }
+        *reinterpret_cast<uint4*>(static_cast<T*>(a.y) + out) = make_uint4(y[0], y[1], y[2], y[3]);
+    }
+}
+
+// Rows of any length and alignment: a block of the generator, four channels, to a thread.
+template <class T>
+__global__ void __launch_bounds__(256) dropout_any_kernel(const DropArgs a, int rows_per_block)
+{
+    const unsigned per = ((unsigned)a.c + 3) / 4;
+    const int64_t r0 = (int64_t)blockIdx.x * rows_per_block;
+    const unsigned n = (unsigned)min((int64_t)rows_per_block, a.rows - r0) * per;
+    const uint64_t step = *a.step;
+    for (unsigned i = threadIdx.x; i < n; i += 256) {
+        const unsigned l = i / per, col = (i - l * per) * 4;
+        const int64_t r = r0 + l;
+        const T* x = static_cast<const T*>(a.x) + r * a.ld_in + col;
+        const T* res = a.res ? static_cast<const T*>(a.res) + r * a.ld_in + col : nullptr;
+        T* y = static_cast<T*>(a.y) + r * a.ld_out + col;
+        float f[4], g[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const bool in = col + e < (unsigned)a.c;
+            f[e] = in ? elem_f(x[e]) : 0.f;
+            g[e] = in && res ? elem_f(res[e]) : 0.f;
+        }
+        uint32_t w[4];
+        philox((uint64_t)r * per + col / 4, step, a.key0, a.key1, w);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (col + e < (unsigned)a.c) y[e] = elem_from<T>(dropped<T>(a, w[e], f[e], g[e]));
     }
 }
 
@@ -66,10 +114,17 @@ __global__ void dropout_advance_kernel(unsigned long long* step) { *step += 1; }
 template <class T>
 int launch(const DropArgs& a, cudaStream_t st, const char* what)
 {
-    const int64_t total = a.rows * ((a.c + 3) / 4), cap = (int64_t)sm_count() * 8;
-    int64_t blocks = (total + 255) / 256;
-    if (blocks > cap) blocks = cap;
-    dropout_kernel<T><<<(unsigned)blocks, 256, 0, st>>>(a);
+    uintptr_t bits = reinterpret_cast<uintptr_t>(a.x) | reinterpret_cast<uintptr_t>(a.res) | reinterpret_cast<uintptr_t>(a.y);
+    bits |= (uintptr_t)(a.ld_in | a.ld_out | a.c) * sizeof(T);
+    const bool wide = (bits & 15) == 0;
+    const int64_t units = wide ? a.c / (16 / (int)sizeof(T)) : (a.c + 3) / 4;
+    const int per = a.rows * units >= (int64_t)sm_count() * 8 * 1024 ? 1024 : 256;  // four units to a thread, or one
+    const int rpb = units >= per ? 1 : (int)(per / units);
+    const unsigned blocks = (unsigned)((a.rows + rpb - 1) / rpb);
+    if (wide)
+        dropout_kernel<T><<<blocks, 256, 0, st>>>(a, rpb);
+    else
+        dropout_any_kernel<T><<<blocks, 256, 0, st>>>(a, rpb);
     return launch_check(what);
 }
 

@@ -1,5 +1,7 @@
 // exchange.cu -- tokens to their experts' groups and back: rows copied to the slots of their entries, the weighted sum
 // of the entries' rows, and the gradients of both.
+#include <type_traits>
+
 #include "dbl_elem.cuh"
 
 namespace {
@@ -24,62 +26,198 @@ __device__ __forceinline__ int64_t slot_of(const ExchangeArgs& a, int64_t entry)
     return s >= 0 && s < a.grouped_rows ? s : -1;
 }
 
-// A block to a token.
-template <class T>
-__global__ void __launch_bounds__(256) expert_scatter_kernel(const ExchangeArgs a)
+// VB bytes of a row, the most that all rows' addresses and lengths allow: 16, or 8, 4, 2.
+template <class T, int VB>
+struct Chunk {
+    static constexpr int N = VB / (int)sizeof(T);
+    static constexpr int W = VB < 4 ? 1 : VB / 4;
+    uint32_t w[W];
+
+    __device__ __forceinline__ void load(const T* p)
+    {
+        if constexpr (VB == 16) {
+            const uint4 v = *reinterpret_cast<const uint4*>(p);
+            w[0] = v.x, w[1] = v.y, w[2] = v.z, w[3] = v.w;
+        } else if constexpr (VB == 8) {
+            const uint2 v = *reinterpret_cast<const uint2*>(p);
+            w[0] = v.x, w[1] = v.y;
+        } else if constexpr (VB == 4) {
+            w[0] = *reinterpret_cast<const uint32_t*>(p);
+        } else {
+            w[0] = *reinterpret_cast<const uint16_t*>(p);
+        }
+    }
+    __device__ __forceinline__ void store(T* p) const
+    {
+        if constexpr (VB == 16)
+            *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+        else if constexpr (VB == 8)
+            *reinterpret_cast<uint2*>(p) = make_uint2(w[0], w[1]);
+        else if constexpr (VB == 4)
+            *reinterpret_cast<uint32_t*>(p) = w[0];
+        else
+            *reinterpret_cast<uint16_t*>(p) = (uint16_t)w[0];
+    }
+    __device__ __forceinline__ void get(float (&f)[N]) const
+    {
+        if constexpr (sizeof(T) == 4) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) f[i] = __uint_as_float(w[i]);
+        } else if constexpr (VB == 2) {
+            f[0] = act::unpack2_u32(w[0]).x;
+        } else {
+#pragma unroll
+            for (int i = 0; i < W; ++i) {
+                const float2 v = act::unpack2_u32(w[i]);
+                f[2 * i] = v.x, f[2 * i + 1] = v.y;
+            }
+        }
+    }
+    __device__ __forceinline__ void put(const float (&f)[N])
+    {
+        if constexpr (sizeof(T) == 4) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) w[i] = __float_as_uint(f[i]);
+        } else if constexpr (VB == 2) {
+            w[0] = act::pack2_u32(f[0], 0.f);
+        } else {
+#pragma unroll
+            for (int i = 0; i < W; ++i) w[i] = act::pack2_u32(f[2 * i], f[2 * i + 1]);
+        }
+    }
+};
+
+// A thread to a chunk of a row, rows_per_block rows to a block.
+template <class T, int VB>
+__global__ void __launch_bounds__(256) expert_scatter_kernel(const ExchangeArgs a, int rows_per_block)
 {
-    for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
-        const T* x = static_cast<const T*>(a.a) + r * a.ld_rows;
+    using V = Chunk<T, VB>;
+    const unsigned chunks = (unsigned)a.c / V::N;
+    const int64_t r0 = (int64_t)blockIdx.x * rows_per_block;
+    const unsigned n = (unsigned)min((int64_t)rows_per_block, a.rows - r0) * chunks;
+    for (unsigned i = threadIdx.x; i < n; i += 256) {
+        const unsigned l = i / chunks, u = (i - l * chunks) * V::N;
+        const int64_t r = r0 + l;
+        V v;
+        v.load(static_cast<const T*>(a.a) + r * a.ld_rows + u);
         for (int j = 0; j < a.k; ++j) {
             const int64_t s = slot_of(a, r * a.k + j);
-            if (s < 0) continue;
-            T* o = static_cast<T*>(a.out) + s * a.ld_grouped;
-            for (int i = threadIdx.x; i < a.c; i += blockDim.x) o[i] = x[i];
+            if (s >= 0) v.store(static_cast<T*>(a.out) + s * a.ld_grouped + u);
         }
     }
 }
 
-template <class T>
-__global__ void __launch_bounds__(256) expert_combine_kernel(const ExchangeArgs a)
+// The same; four entries' rows are asked for at a time.
+template <class T, int VB>
+__global__ void __launch_bounds__(256) expert_combine_kernel(const ExchangeArgs a, int rows_per_block)
 {
-    for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
-        T* o = static_cast<T*>(a.out) + r * a.ld_rows;
-        const T* res = a.b ? static_cast<const T*>(a.b) + r * a.ld_rows : nullptr;
-        for (int i = threadIdx.x; i < a.c; i += blockDim.x) {
-            float sum = 0.f;
-            for (int j = 0; j < a.k; ++j) {
-                const int64_t s = slot_of(a, r * a.k + j);
-                const float w = a.weights ? a.weights[r * a.k + j] : 1.f;
-                sum = fmaf(w, s < 0 ? 0.f : elem_f(static_cast<const T*>(a.a)[s * a.ld_grouped + i]), sum);
+    using V = Chunk<T, VB>;
+    const unsigned chunks = (unsigned)a.c / V::N;
+    const int64_t r0 = (int64_t)blockIdx.x * rows_per_block;
+    const unsigned n = (unsigned)min((int64_t)rows_per_block, a.rows - r0) * chunks;
+    for (unsigned i = threadIdx.x; i < n; i += 256) {
+        const unsigned l = i / chunks, u = (i - l * chunks) * V::N;
+        const int64_t r = r0 + l;
+        float sum[V::N] = {};
+        V res;
+        if (a.b) res.load(static_cast<const T*>(a.b) + r * a.ld_rows + u);
+        for (int j0 = 0; j0 < a.k; j0 += 4) {
+            V y[4] = {};
+            float w[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const bool in = j0 + j < a.k;
+                const int64_t s = in ? slot_of(a, r * a.k + j0 + j) : -1;
+                w[j] = in ? (a.weights ? a.weights[r * a.k + j0 + j] : 1.f) : 0.f;
+                if (s >= 0) y[j].load(static_cast<const T*>(a.a) + s * a.ld_grouped + u);
             }
-            o[i] = elem_from<T>(res ? sum + elem_f(res[i]) : sum);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                float f[V::N];
+                y[j].get(f);
+#pragma unroll
+                for (int e = 0; e < V::N; ++e) sum[e] = fmaf(w[j], f[e], sum[e]);
+            }
         }
+        if (a.b) {
+            float f[V::N];
+            res.get(f);
+#pragma unroll
+            for (int e = 0; e < V::N; ++e) sum[e] += f[e];
+        }
+        V o;
+        o.put(sum);
+        o.store(static_cast<T*>(a.out) + r * a.ld_rows + u);
     }
 }
 
-template <class T>
+// G threads to a row, NC chunks of it to a thread, kept while the entries pass (NC = 0: any number, read again for each).
+template <class T, int VB, int G, int NC>
 __global__ void __launch_bounds__(256) expert_combine_bwd_kernel(const ExchangeArgs a)
 {
+    using V = Chunk<T, VB>;
+    constexpr int HELD = NC ? NC : 1;
     __shared__ float red[32];
-    for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
-        const T* d = static_cast<const T*>(a.a) + r * a.ld_rows;
-        for (int j = 0; j < a.k; ++j) {
-            const int64_t s = slot_of(a, r * a.k + j);
+    const int chunks = a.c / V::N, g = threadIdx.x % G;
+    const int64_t r = (int64_t)blockIdx.x * (256 / G) + threadIdx.x / G;
+    if (G < 256 && (int64_t)blockIdx.x * (256 / G) + (threadIdx.x & ~31) / G >= a.rows) return;  // whole warps
+    const bool live = r < a.rows;
+    const T* d = static_cast<const T*>(a.a) + (live ? r : 0) * a.ld_rows;
+    V held[HELD];
+    if (NC && live) {
+#pragma unroll
+        for (int i = 0; i < NC; ++i)
+            if (g + i * G < chunks) held[i].load(d + (g + i * G) * V::N);
+    }
+    for (int j = 0; j < a.k; ++j) {
+        const int64_t s = live ? slot_of(a, r * a.k + j) : -1;
+        float dot = 0.f;
+        if (s >= 0) {
             const float w = a.weights ? a.weights[r * a.k + j] : 1.f;
-            float dot = 0.f;
-            if (s >= 0) {
-                T* o = static_cast<T*>(a.out) + s * a.ld_grouped;
-                const T* y = a.dweights ? static_cast<const T*>(a.b) + s * a.ld_grouped : nullptr;
-                for (int i = threadIdx.x; i < a.c; i += blockDim.x) {
-                    const float v = elem_f(d[i]);
-                    if (y) dot = fmaf(v, elem_f(y[i]), dot);
-                    o[i] = elem_from<T>(w * v);
+            T* o = static_cast<T*>(a.out) + s * a.ld_grouped;
+            const T* y = a.dweights ? static_cast<const T*>(a.b) + s * a.ld_grouped : nullptr;
+            auto one = [&](const V& dv, const V& yv, int u) {
+                float f[V::N];
+                dv.get(f);
+                if (y) {
+                    float h[V::N];
+                    yv.get(h);
+#pragma unroll
+                    for (int e = 0; e < V::N; ++e) dot = fmaf(f[e], h[e], dot);
+                }
+#pragma unroll
+                for (int e = 0; e < V::N; ++e) f[e] *= w;
+                V p;
+                p.put(f);
+                p.store(o + u);
+            };
+            if constexpr (NC > 0) {
+                V yv[NC];
+                if (y) {
+#pragma unroll
+                    for (int i = 0; i < NC; ++i)
+                        if (g + i * G < chunks) yv[i].load(y + (g + i * G) * V::N);
+                }
+#pragma unroll
+                for (int i = 0; i < NC; ++i)
+                    if (g + i * G < chunks) one(held[i], yv[i], (g + i * G) * V::N);
+            } else {
+                for (int i = g; i < chunks; i += G) {
+                    V dv, yv;
+                    dv.load(d + i * V::N);
+                    if (y) yv.load(y + i * V::N);
+                    one(dv, yv, i * V::N);
                 }
             }
-            if (!a.dweights) continue;
-            dot = block_sum(dot, red);
-            if (threadIdx.x == 0) a.dweights[r * a.k + j] = dot;
         }
+        if (!a.dweights) continue;
+        if constexpr (G == 256) {
+            dot = block_sum(dot, red);
+        } else {
+#pragma unroll
+            for (int o = G / 2; o; o >>= 1) dot += __shfl_xor_sync(0xffffffffu, dot, o);
+        }
+        if (live && g == 0) a.dweights[r * a.k + j] = dot;
     }
 }
 
@@ -103,10 +241,58 @@ ExchangeArgs args(const dbl_exchange_shape* s, const void* a, const void* b, con
             s->ld_rows ? s->ld_rows : s->c, s->ld_grouped ? s->ld_grouped : s->c, s->k, s->c};
 }
 
-unsigned grid_for(int64_t rows)
+// The bytes of a chunk: what the rows' addresses, strides and length have in common.
+int chunk_bytes(const ExchangeArgs& a, size_t e)
 {
-    const int64_t cap = (int64_t)sm_count() * 8;
-    return (unsigned)(rows < cap ? rows : cap);
+    uintptr_t bits = reinterpret_cast<uintptr_t>(a.a) | reinterpret_cast<uintptr_t>(a.b) | reinterpret_cast<uintptr_t>(a.out);
+    bits |= (uintptr_t)a.c * e | (uintptr_t)a.ld_rows * e | (uintptr_t)a.ld_grouped * e;
+    return bits & 1 ? 1 : bits & 2 ? 2 : bits & 4 ? 4 : bits & 8 ? 8 : 16;
+}
+
+// f(element type, chunk bytes), both as values of their types.
+template <class F>
+void with_chunks(int dtype, int bytes, F f)
+{
+    if (dtype == DBL_F32) {
+        if (bytes == 16) f(0.f, std::integral_constant<int, 16>());
+        else if (bytes == 8) f(0.f, std::integral_constant<int, 8>());
+        else f(0.f, std::integral_constant<int, 4>());
+    } else {
+        if (bytes == 16) f(act_t(), std::integral_constant<int, 16>());
+        else if (bytes == 8) f(act_t(), std::integral_constant<int, 8>());
+        else if (bytes == 4) f(act_t(), std::integral_constant<int, 4>());
+        else f(act_t(), std::integral_constant<int, 2>());
+    }
+}
+
+// Rows of a block of the kernels that have a thread for a chunk: four chunks to a thread where there are many rows, one where
+// there are few.
+int block_rows(const ExchangeArgs& a, int chunks)
+{
+    const int64_t all = a.rows * chunks;
+    const int per = all >= (int64_t)sm_count() * 8 * 1024 ? 1024 : 256;
+    return chunks >= per ? 1 : per / chunks;
+}
+
+template <class T, int VB>
+void launch_combine_bwd(const ExchangeArgs& a, cudaStream_t st)
+{
+    const int chunks = a.c / Chunk<T, VB>::N;
+    auto run = [&](auto g, auto nc) {
+        constexpr int G = decltype(g)::value, NC = decltype(nc)::value;
+        expert_combine_bwd_kernel<T, VB, G, NC><<<(unsigned)((a.rows + 256 / G - 1) / (256 / G)), 256, 0, st>>>(a);
+    };
+#define DBL_I(n) std::integral_constant<int, n>()
+    if (VB < 16 && chunks > 32) return chunks > 512 ? run(DBL_I(256), DBL_I(0)) : run(DBL_I(32), DBL_I(0));
+    if (chunks <= 8) return run(DBL_I(8), DBL_I(1));
+    if (chunks <= 16) return run(DBL_I(8), DBL_I(2));
+    if (chunks <= 32) return run(DBL_I(32), DBL_I(1));
+    if (chunks <= 64) return run(DBL_I(32), DBL_I(2));
+    if (chunks <= 128) return run(DBL_I(32), DBL_I(4));
+    if (chunks <= 512) return run(DBL_I(256), DBL_I(2));
+    if (chunks <= 1024) return run(DBL_I(256), DBL_I(4));
+    run(DBL_I(256), DBL_I(0));
+#undef DBL_I
 }
 
 }  // namespace
@@ -123,10 +309,11 @@ extern "C" int dbl_expert_scatter(const dbl_exchange_shape* s, const void* x, co
     if (!x || !slots || !xg) return set_error(DBL_ERR_INVALID, "%s: x, slots and xg must not be NULL", w);
     const ExchangeArgs a = args(s, x, nullptr, slots, nullptr, xg, nullptr);
     cudaStream_t st = as_stream(stream);
-    if (s->dtype == DBL_F32)
-        expert_scatter_kernel<float><<<grid_for(s->rows), 256, 0, st>>>(a);
-    else
-        expert_scatter_kernel<act_t><<<grid_for(s->rows), 256, 0, st>>>(a);
+    with_chunks(s->dtype, chunk_bytes(a, e), [&](auto type, auto bytes) {
+        using V = Chunk<decltype(type), decltype(bytes)::value>;
+        const int rpb = block_rows(a, a.c / V::N);
+        expert_scatter_kernel<decltype(type), decltype(bytes)::value><<<(unsigned)((a.rows + rpb - 1) / rpb), 256, 0, st>>>(a, rpb);
+    });
     return launch_check(w);
 }
 
@@ -143,10 +330,11 @@ extern "C" int dbl_expert_combine(const dbl_exchange_shape* s, const void* yg, c
     if (!yg || !slots || !out) return set_error(DBL_ERR_INVALID, "%s: yg, slots and out must not be NULL", w);
     const ExchangeArgs a = args(s, yg, res, slots, weights, out, nullptr);
     cudaStream_t st = as_stream(stream);
-    if (s->dtype == DBL_F32)
-        expert_combine_kernel<float><<<grid_for(s->rows), 256, 0, st>>>(a);
-    else
-        expert_combine_kernel<act_t><<<grid_for(s->rows), 256, 0, st>>>(a);
+    with_chunks(s->dtype, chunk_bytes(a, e), [&](auto type, auto bytes) {
+        using V = Chunk<decltype(type), decltype(bytes)::value>;
+        const int rpb = block_rows(a, a.c / V::N);
+        expert_combine_kernel<decltype(type), decltype(bytes)::value><<<(unsigned)((a.rows + rpb - 1) / rpb), 256, 0, st>>>(a, rpb);
+    });
     return launch_check(w);
 }
 
@@ -165,9 +353,6 @@ extern "C" int dbl_expert_combine_bwd(const dbl_exchange_shape* s, const void* d
         return set_error(DBL_ERR_INVALID, "%s: dout, slots and dyg must not be NULL, nor yg with dweights", w);
     const ExchangeArgs a = args(s, dout, yg, slots, weights, dyg, dweights);
     cudaStream_t st = as_stream(stream);
-    if (s->dtype == DBL_F32)
-        expert_combine_bwd_kernel<float><<<grid_for(s->rows), 256, 0, st>>>(a);
-    else
-        expert_combine_bwd_kernel<act_t><<<grid_for(s->rows), 256, 0, st>>>(a);
+    with_chunks(s->dtype, chunk_bytes(a, e), [&](auto type, auto bytes) { launch_combine_bwd<decltype(type), decltype(bytes)::value>(a, st); });
     return launch_check(w);
 }
