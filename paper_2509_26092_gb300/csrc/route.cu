@@ -2,6 +2,8 @@
 // grouped by expert, and the gradient of the logits.
 #include <math.h>
 
+#include <type_traits>
+
 #include "dbl_elem.cuh"
 
 namespace {
@@ -10,7 +12,9 @@ using namespace dbl;
 using namespace dbl::dev;
 
 constexpr int kMaxExperts = DBL_ROUTE_MAX_EXPERTS, kMaxK = DBL_ROUTE_MAX_K;
-constexpr int kMaxBlocks = 256;  // that count entries; the workspace holds one count for each block and expert
+constexpr int kMaxBlocks = 256;    // of the forward pass; the workspace holds one count for each block and expert
+constexpr int kOneBlockRows = 256;  // up to here one block chooses and places
+constexpr int kPlaceCounts = 8192;  // counts of a block's warps and experts in shared memory
 
 struct RouteArgs {
     const void* logits;
@@ -28,140 +32,249 @@ struct RouteArgs {
 // A number that orders keys as integers, 0 for those that are never chosen.
 __device__ __forceinline__ uint32_t rank_of(float key)
 {
-    if (!(key > -INFINITY)) return 0u;  // -infinity and NaN
     const uint32_t u = __float_as_uint(key + 0.f);  // -0 as 0
-    return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
+    const uint32_t r = u ^ ((uint32_t)((int)u >> 31) | 0x80000000u);
+    return key > -INFINITY ? r : 0u;  // not -infinity, not NaN
 }
 
-// A warp to a row; every lane has the experts lane, lane + 32, ...
-template <class T>
-__device__ __forceinline__ void choose_row(const RouteArgs& a, int64_t r, int lane, int32_t* chosen, float* weights)
+// A warp to a row, EPL experts to a lane, neighbours in a lane, so that the lowest lane has the lowest of equal experts.
+// Returns this lane's entry's expert (lane j < k: entry j) or -1, and its weight.
+template <class T, int EPL>
+__device__ __forceinline__ int choose_row(const RouteArgs& a, int64_t r, int lane, const float (&bias)[EPL], float& weight)
 {
     const T* z = static_cast<const T*>(a.logits) + r * a.ld;
-    const bool dead = a.row_weight && a.row_weight[r] == 0.f;
-    float peak = -INFINITY, sum = 0.f;
-    bool bad = false;
-    if (!dead) {
-        for (int e = lane; e < a.experts; e += 32) {
-            const float v = elem_f(z[e]);
-            bad |= !(v < INFINITY);
-            peak = fmaxf(peak, v);
-        }
-        peak = warp_max(peak);
-        bad = __any_sync(0xffffffffu, bad);
-        if (!a.normalise && !bad && peak > -INFINITY) {
-            for (int e = lane; e < a.experts; e += 32) sum += expf(elem_f(z[e]) - peak);
-            sum = warp_sum(sum);
-        }
-    }
-    if (dead || bad) {
-        for (int j = lane; j < a.k; j += 32) {
-            chosen[j] = -1;
-            weights[j] = dead ? 0.f : NAN;
-        }
-        return;
-    }
-    uint32_t last = 0xffffffffu;
-    int last_e = -1, mine = -1;
-    for (int j = 0; j < a.k; ++j) {
-        uint32_t best = 0;
-        int best_e = a.experts;
-        for (int e = lane; e < a.experts; e += 32) {
-            const uint32_t v = rank_of(elem_f(z[e]) + (a.bias ? a.bias[e] : 0.f));
-            const bool after = v < last || (v == last && e > last_e);  // what was chosen before comes before in this order
-            if (after && v > best) best = v, best_e = e;
-        }
-        const uint32_t top = __reduce_max_sync(0xffffffffu, best);
-        const int e = (int)__reduce_min_sync(0xffffffffu, best == top && top ? (unsigned)best_e : (unsigned)a.experts);
-        if (top == 0) break;
-        last = top;
-        last_e = e;
-        if (lane == j) mine = e;
-    }
-    const float v = mine >= 0 ? elem_f(z[mine]) : -INFINITY;
-    if (a.normalise) {
-        peak = warp_max(v);
-        sum = warp_sum(mine >= 0 ? expf(v - peak) : 0.f);
-    }
-    if (lane < a.k) {
-        chosen[lane] = mine;
-        weights[lane] = mine >= 0 ? expf(v - peak) / sum : 0.f;
-    }
-}
-
-// Counts the entries of each expert in the block's rows.
-template <class T>
-__global__ void __launch_bounds__(256) route_choose_kernel(const RouteArgs a)
-{
-    __shared__ int count[kMaxExperts];
-    for (int e = threadIdx.x; e < a.experts; e += blockDim.x) count[e] = 0;
-    __syncthreads();
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int64_t r0 = (int64_t)blockIdx.x * a.rows_per_block, r1 = min(a.rows, r0 + a.rows_per_block);
-    for (int64_t r = r0 + warp; r < r1; r += blockDim.x / 32) {
-        choose_row<T>(a, r, lane, a.chosen + r * a.k, a.weights + r * a.k);
-        __syncwarp();
-        const int e = lane < a.k ? a.chosen[r * a.k + lane] : -1;
-        if (e >= 0) atomicAdd(&count[e], 1);
-    }
-    __syncthreads();
-    for (int e = threadIdx.x; e < a.experts; e += blockDim.x) a.counts[blockIdx.x * a.experts + e] = count[e];
-}
-
-// Gives every entry its place: the entries of smaller experts, those of the same expert in the blocks before, and those
-// before it in this block.
-__global__ void __launch_bounds__(256) route_place_kernel(const RouteArgs a)
-{
-    __shared__ int at[kMaxExperts];          // the next place of an expert's entry
-    __shared__ int part[8];
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    int running = 0;
-    for (int e0 = 0; e0 < a.experts; e0 += 256) {
-        const int e = e0 + threadIdx.x;
-        int before = 0, all = 0;
-        if (e < a.experts)
-            for (int b = 0; b < (int)gridDim.x; ++b) {
-                const int n = a.counts[b * a.experts + e];
-                if (b < (int)blockIdx.x) before += n;
-                all += n;
+    const int e0 = lane * EPL;
+    weight = 0.f;
+    if (a.row_weight && a.row_weight[r] == 0.f) return -1;
+    float v[EPL];
+    if (sizeof(T) == 2 && EPL % 2 == 0 && (reinterpret_cast<uintptr_t>(z) & 3) == 0) {
+#pragma unroll
+        for (int i = 0; i < EPL; i += 2)
+            if (e0 + i + 1 < a.experts) {
+                const float2 f = act::unpack2_u32(*reinterpret_cast<const uint32_t*>(z + e0 + i));
+                v[i] = f.x, v[i + 1] = f.y;
+            } else {
+                v[i] = e0 + i < a.experts ? elem_f(z[e0 + i]) : -INFINITY;
+                v[i + 1] = -INFINITY;
             }
-        int sum = all;
+    } else {
+#pragma unroll
+        for (int i = 0; i < EPL; ++i) v[i] = e0 + i < a.experts ? elem_f(z[e0 + i]) : -INFINITY;
+    }
+    bool bad = false;  // NaN or +infinity in the row
+    uint32_t key[EPL], top = 0;
+#pragma unroll
+    for (int i = 0; i < EPL; ++i) {
+        bad |= !(v[i] < INFINITY);
+        top = max(top, rank_of(v[i]));
+        key[i] = rank_of(v[i] + bias[i]);
+    }
+    if (__any_sync(0xffffffffu, bad)) {
+        weight = NAN;
+        return -1;
+    }
+    top = __reduce_max_sync(0xffffffffu, top);
+    float peak = __uint_as_float(top ^ ((top & 0x80000000u) ? 0x80000000u : 0xffffffffu)), sum = 0.f;
+    if (!a.normalise && top) {
+#pragma unroll
+        for (int i = 0; i < EPL; ++i) sum += expf(v[i] - peak);
+        sum = warp_sum(sum);
+    }
+    // the lane's experts, largest first
+    uint32_t at = 0;  // EPL <= 4: where key[i] came from, four bits each
+    if constexpr (EPL <= 4) {
+        int from[EPL];
+#pragma unroll
+        for (int i = 0; i < EPL; ++i) from[i] = i;
+#pragma unroll
+        for (int pass = 0; pass < EPL - 1; ++pass)
+#pragma unroll
+            for (int i = 0; i + 1 < EPL - pass; ++i) {
+                const bool swap = key[i + 1] > key[i];
+                const uint32_t k0 = swap ? key[i + 1] : key[i], k1 = swap ? key[i] : key[i + 1];
+                const int f0 = swap ? from[i + 1] : from[i], f1 = swap ? from[i] : from[i + 1];
+                key[i] = k0, key[i + 1] = k1, from[i] = f0, from[i + 1] = f1;
+            }
+#pragma unroll
+        for (int i = 0; i < EPL; ++i) at |= (uint32_t)from[i] << (4 * i);
+    }
+    uint32_t best = 0;
+    int where = 0;
+    auto scan = [&]() {
+        best = 0;
+#pragma unroll
+        for (int i = 0; i < EPL; ++i)
+            if (key[i] > best) best = key[i], where = i;
+    };
+    if constexpr (EPL > 4) scan();
+    int mine = -1;
+    for (int j = 0; j < a.k; ++j) {
+        if constexpr (EPL <= 4) best = key[0], where = at & 15;
+        const uint32_t most = __reduce_max_sync(0xffffffffu, best);
+        if (most == 0) break;
+        const int from = __ffs(__ballot_sync(0xffffffffu, best == most)) - 1;
+        const int e = __shfl_sync(0xffffffffu, e0 + where, from);
+        if (lane == j) mine = e;
+        if (lane == from) {
+            if constexpr (EPL <= 4) {
+#pragma unroll
+                for (int i = 0; i + 1 < EPL; ++i) key[i] = key[i + 1];
+                key[EPL - 1] = 0;
+                at >>= 4;
+            } else {
+#pragma unroll
+                for (int i = 0; i < EPL; ++i)
+                    if (i == where) key[i] = 0;
+                scan();
+            }
+        }
+    }
+    const float logit = mine >= 0 ? elem_f(z[mine]) : -INFINITY;
+    if (a.normalise) {
+        peak = warp_max(logit);
+        sum = warp_sum(mine >= 0 ? expf(logit - peak) : 0.f);
+    }
+    if (mine >= 0) weight = expf(logit - peak) / sum;
+    return mine;
+}
+
+// Gives the entries of rows r0 .. r1 - 1 their places: after the entries of smaller experts, those of the same expert in
+// the blocks before (base[e] is both) and those before them in this block.  counts: [warps][experts] in shared memory; the
+// warps, which are so many that it fits, take parts of the entries in order.
+__device__ __forceinline__ void place(const RouteArgs& a, int64_t r0, int64_t r1, const int* base, int* counts, int warps)
+{
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int64_t n = (r1 - r0) * a.k, part = (n + warps * 32 - 1) / (warps * 32) * 32;
+    const int32_t* chosen = a.chosen + r0 * a.k;
+    int32_t* slots = a.slots + r0 * a.k;
+    const int64_t i0 = min(n, warp * part), i1 = min(n, i0 + part);
+    for (int i = threadIdx.x; i < warps * a.experts; i += blockDim.x) counts[i] = 0;
+    __syncthreads();
+    int* mine = counts + warp * a.experts;
+    if (warp < warps)
+        for (int64_t i = i0 + lane; i < i1; i += 32) {
+            const int e = chosen[i];
+            if (e >= 0) atomicAdd(&mine[e], 1);
+        }
+    __syncthreads();
+    for (int e = threadIdx.x; e < a.experts; e += blockDim.x) {
+        int at = base[e];
+        for (int w = 0; w < warps; ++w) {
+            const int c = counts[w * a.experts + e];
+            counts[w * a.experts + e] = at;
+            at += c;
+        }
+    }
+    __syncthreads();
+    if (warp < warps)
+        for (int64_t i = i0; i < i1; i += 32) {
+            const bool in = i + lane < i1;
+            const int e = in ? chosen[i + lane] : -1;
+            const uint32_t same = __match_any_sync(0xffffffffu, e);
+            const int rank = __popc(same & ((1u << lane) - 1));
+            const int at = e >= 0 ? mine[e] + rank : -1;
+            __syncwarp();
+            if (e >= 0 && rank == 0) mine[e] += __popc(same);
+            __syncwarp();
+            if (in) slots[i + lane] = at;
+        }
+}
+
+// Exclusive sums of total[0 .. experts) into base, added to what is there, and the groups' bounds; by all threads.
+__device__ __forceinline__ void bounds(const RouteArgs& a, const int* total, int* base, int* part, bool write)
+{
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
+    int running = 0;
+    for (int first = 0; first < a.experts; first += blockDim.x) {
+        const int e = first + threadIdx.x;
+        const int n = e < a.experts ? total[e] : 0;
+        int sum = n;
         for (int o = 1; o < 32; o <<= 1) {
             const int v = __shfl_up_sync(0xffffffffu, sum, o);
             if (lane >= o) sum += v;
         }
         if (lane == 31) part[warp] = sum;
         __syncthreads();
-        int base = running;
-        for (int w = 0; w < warp; ++w) base += part[w];
-        const int end = base + sum;
+        int before = running;
+        for (int w = 0; w < warps; ++w) {
+            if (w < warp) before += part[w];
+            running += part[w];
+        }
         if (e < a.experts) {
-            at[e] = end - all + before;
-            if (blockIdx.x == 0) {
+            base[e] += before + sum - n;
+            if (write) {
                 if (e == 0) a.offsets[0] = 0;
-                a.offsets[e + 1] = end;
+                a.offsets[e + 1] = before + sum;
             }
         }
-        for (int w = 0; w < 8; ++w) running += part[w];
         __syncthreads();
-    }
-    if (warp) return;
-    const int64_t r0 = (int64_t)blockIdx.x * a.rows_per_block, r1 = min(a.rows, r0 + a.rows_per_block);
-    for (int64_t i0 = r0 * a.k; i0 < r1 * a.k; i0 += 32) {
-        const bool in = i0 + lane < r1 * a.k;
-        const int e = in ? a.chosen[i0 + lane] : -1;
-        const uint32_t same = __match_any_sync(0xffffffffu, e);
-        const int rank = __popc(same & ((1u << lane) - 1));
-        const int place = e >= 0 ? at[e] + rank : -1;
-        __syncwarp();
-        if (e >= 0 && rank == 0) at[e] += __popc(same);
-        __syncwarp();
-        if (in) a.slots[i0 + lane] = place;
     }
 }
 
+template <int EPL>
+constexpr int choose_threads() { return EPL <= 8 ? 1024 : 512; }
+
+// Chooses the block's rows' experts and counts the entries of each; where there is one block, it places them too.
+template <class T, int EPL>
+__global__ void __launch_bounds__(choose_threads<EPL>()) route_choose_kernel(const RouteArgs a, int place_warps)
+{
+    extern __shared__ int counts[];  // one block: for place()
+    __shared__ int total[kMaxExperts], base[kMaxExperts], part[32];
+    for (int e = threadIdx.x; e < a.experts; e += blockDim.x) total[e] = base[e] = 0;
+    __syncthreads();
+    grid_dependency_trigger();
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int64_t r0 = (int64_t)blockIdx.x * a.rows_per_block, r1 = min(a.rows, r0 + a.rows_per_block);
+    float bias[EPL];
+#pragma unroll
+    for (int i = 0; i < EPL; ++i) bias[i] = a.bias && lane * EPL + i < a.experts ? a.bias[lane * EPL + i] : 0.f;
+    for (int64_t r = r0 + warp; r < r1; r += blockDim.x / 32) {
+        float weight;
+        const int e = choose_row<T, EPL>(a, r, lane, bias, weight);
+        if (lane < a.k) {
+            a.chosen[r * a.k + lane] = e;
+            a.weights[r * a.k + lane] = weight;
+            if (e >= 0) atomicAdd(&total[e], 1);
+        }
+    }
+    __syncthreads();
+    if (gridDim.x > 1) {
+        for (int e = threadIdx.x; e < a.experts; e += blockDim.x) a.counts[(int64_t)blockIdx.x * a.experts + e] = total[e];
+        return;
+    }
+    bounds(a, total, base, part, true);
+    place(a, r0, r1, base, counts, place_warps);
+}
+
+// Threads share an expert's counts where there are more threads than experts.
+__global__ void __launch_bounds__(1024) route_place_kernel(const RouteArgs a, int place_warps)
+{
+    extern __shared__ int counts[];
+    __shared__ int total[kMaxExperts], base[kMaxExperts], part[32];
+    for (int e = threadIdx.x; e < a.experts; e += 1024) total[e] = base[e] = 0;
+    __syncthreads();
+    grid_dependency_wait();
+    const int shares = max(1, 1024 / a.experts), blocks = (int)gridDim.x;
+    const int share = (int)threadIdx.x / a.experts, e = (int)threadIdx.x % a.experts;
+    if (share < shares) {
+        int before = 0, all = 0;
+#pragma unroll 8
+        for (int b = share; b < blocks; b += shares) {
+            const int n = a.counts[(int64_t)b * a.experts + e];
+            all += n;
+            if (b < (int)blockIdx.x) before += n;
+        }
+        atomicAdd(&total[e], all);
+        atomicAdd(&base[e], before);
+    }
+    __syncthreads();
+    bounds(a, total, base, part, blockIdx.x == 0);
+    const int64_t r0 = (int64_t)blockIdx.x * a.rows_per_block, r1 = min(a.rows, r0 + a.rows_per_block);
+    place(a, r0, r1, base, counts, place_warps);
+}
+
 // A warp to a row: first what every expert gets, then the entries' experts.
-template <class T>
+template <class T, int EPL>
 __global__ void __launch_bounds__(256) route_bwd_kernel(const void* logits, const int32_t* chosen, const float* weights,
                                                         const float* dweights, void* dlogits, int64_t rows, int experts,
                                                         int k, int normalise, int64_t ld, int64_t ld_grad)
@@ -173,27 +286,38 @@ __global__ void __launch_bounds__(256) route_bwd_kernel(const void* logits, cons
         int e = lane < k ? chosen[r * k + lane] : -1;
         if (e >= experts) e = -1;
         const float w = lane < k ? weights[r * k + lane] : 0.f;
+        const float dw = e >= 0 ? dweights[r * k + lane] : 0.f;
+        float v[EPL];
+        if (!normalise) {
+#pragma unroll
+            for (int i = 0; i < EPL; ++i) v[i] = lane + 32 * i < experts ? elem_f(z[lane + 32 * i]) : -INFINITY;
+        }
         const bool nan = __any_sync(0xffffffffu, isnan(w)), some = __any_sync(0xffffffffu, e >= 0);
-        const float wd = e >= 0 ? w * dweights[r * k + lane] : 0.f;
+        const float wd = e >= 0 ? w * dw : 0.f;
         const float d = warp_sum(wd);
+        float peak = -INFINITY, sum = 0.f;
         if (nan || !some || normalise) {
             const T fill = elem_from<T>(nan ? NAN : 0.f);
             for (int i = lane; i < experts; i += 32) dz[i] = fill;
             if (nan || !some) continue;
-        }
-        float peak = -INFINITY, sum = 0.f;
-        if (!normalise) {
-            for (int i = lane; i < experts; i += 32) peak = fmaxf(peak, elem_f(z[i]));
+        } else {
+#pragma unroll
+            for (int i = 0; i < EPL; ++i) peak = fmaxf(peak, v[i]);
             peak = warp_max(peak);
-            for (int i = lane; i < experts; i += 32) sum += expf(elem_f(z[i]) - peak);
+#pragma unroll
+            for (int i = 0; i < EPL; ++i) sum += v[i] = expf(v[i] - peak);
             sum = warp_sum(sum);
-            for (int i = lane; i < experts; i += 32) dz[i] = elem_from<T>(-d * (expf(elem_f(z[i]) - peak) / sum));
+            const float scale = -d / sum;
+#pragma unroll
+            for (int i = 0; i < EPL; ++i)
+                if (lane + 32 * i < experts) dz[lane + 32 * i] = elem_from<T>(v[i] * scale);
         }
         float total = 0.f;  // of the row's entries of this lane's expert
+        const float term = normalise ? wd - w * d : wd;
         for (int i = 0; i < k; ++i) {
             const int other = __shfl_sync(0xffffffffu, e, i);
-            const float v = __shfl_sync(0xffffffffu, normalise ? wd - w * d : wd, i);
-            if (other == e) total += v;
+            const float t = __shfl_sync(0xffffffffu, term, i);
+            if (other == e) total += t;
         }
         __syncwarp();
         if (e >= 0) dz[e] = elem_from<T>(normalise ? total : total - d * (expf(elem_f(z[e]) - peak) / sum));
@@ -217,10 +341,55 @@ int check(const dbl_route_shape* s, const char* w)
 // Rows of a block, and how many blocks there are.
 int plan_blocks(const dbl_route_shape* s, int* rows_per_block)
 {
-    int64_t per = (s->rows + kMaxBlocks - 1) / kMaxBlocks;
-    if (per < 16) per = 16;
+    if (s->rows <= kOneBlockRows) {
+        *rows_per_block = kOneBlockRows;
+        return 1;
+    }
+    const int most = sm_count() < kMaxBlocks ? sm_count() : kMaxBlocks;
+    int64_t per = (s->rows + most - 1) / most;
+    if (per < 32) per = 32;
     *rows_per_block = (int)per;
     return (int)((s->rows + per - 1) / per);
+}
+
+// f(experts to a lane, as a value of its type)
+template <class F>
+int with_lanes(int experts, F f)
+{
+    if (experts <= 32) return f(std::integral_constant<int, 1>());
+    if (experts <= 64) return f(std::integral_constant<int, 2>());
+    if (experts <= 128) return f(std::integral_constant<int, 4>());
+    if (experts <= 256) return f(std::integral_constant<int, 8>());
+    if (experts <= 512) return f(std::integral_constant<int, 16>());
+    return f(std::integral_constant<int, 32>());
+}
+
+template <class T>
+int launch_fwd(const RouteArgs& a, int blocks, cudaStream_t st, const char* what)
+{
+    int warps = kPlaceCounts / a.experts;
+    const auto choose = [&](auto epl) {
+        constexpr int EPL = decltype(epl)::value, threads = choose_threads<EPL>();
+        const int w = warps < threads / 32 ? warps : threads / 32;
+        route_choose_kernel<T, EPL><<<blocks, threads, blocks == 1 ? w * a.experts * sizeof(int) : 0, st>>>(a, w);
+        return launch_check(what);
+    };
+    const int rc = with_lanes(a.experts, choose);
+    if (rc != DBL_OK || blocks == 1) return rc;
+    if (warps > 32) warps = 32;
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.gridDim = dim3(blocks);
+    cfg.blockDim = dim3(1024);
+    cfg.dynamicSmemBytes = warps * a.experts * sizeof(int);
+    cfg.stream = st;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    const cudaError_t err = cudaLaunchKernelEx(&cfg, route_place_kernel, a, warps);
+    const int rc2 = launch_check("route_fwd place");
+    return err == cudaSuccess ? rc2 : cuda_check(err, "route_fwd place");
 }
 
 }  // namespace
@@ -229,7 +398,8 @@ extern "C" size_t dbl_route_workspace_bytes(const dbl_route_shape* s)
 {
     if (check(s, "route_workspace_bytes") != DBL_OK) return 0;
     int per;
-    return (size_t)plan_blocks(s, &per) * s->experts * sizeof(int32_t);
+    const int blocks = plan_blocks(s, &per);
+    return blocks > 1 ? (size_t)blocks * s->experts * sizeof(int32_t) : 0;
 }
 
 extern "C" int dbl_route_fwd(const dbl_route_shape* s, const void* logits, const float* select_bias, const float* row_weight,
@@ -247,19 +417,14 @@ extern "C" int dbl_route_fwd(const dbl_route_shape* s, const void* logits, const
     if (s->rows == 0) return cuda_check(cudaMemsetAsync(offsets, 0, (s->experts + 1) * sizeof(int32_t), st), w);
     if (!logits || !chosen || !weights || !slots)
         return set_error(DBL_ERR_INVALID, "%s: logits, chosen, weights and slots must not be NULL", w);
-    if (ws_bytes < dbl_route_workspace_bytes(s) || !ws) return set_error(DBL_ERR_WORKSPACE, "%s: workspace too small", w);
+    const size_t need = dbl_route_workspace_bytes(s);
+    if (need && (!ws || ws_bytes < need)) return set_error(DBL_ERR_WORKSPACE, "%s: workspace too small", w);
     if (!aligned16(ws)) return set_error(DBL_ERR_INVALID, "%s: the workspace is not 16-byte aligned", w);
     int per;
     const int blocks = plan_blocks(s, &per);
     const RouteArgs a = {logits, select_bias, row_weight, chosen, weights, slots, offsets, static_cast<int32_t*>(ws), s->rows,
                          s->ld ? s->ld : s->experts, s->experts, s->k, s->normalise != 0, per};
-    if (s->dtype == DBL_F32)
-        route_choose_kernel<float><<<blocks, 256, 0, st>>>(a);
-    else
-        route_choose_kernel<act_t><<<blocks, 256, 0, st>>>(a);
-    if ((rc = launch_check(w)) != DBL_OK) return rc;
-    route_place_kernel<<<blocks, 256, 0, st>>>(a);
-    return launch_check("route_fwd place");
+    return s->dtype == DBL_F32 ? launch_fwd<float>(a, blocks, st, w) : launch_fwd<act_t>(a, blocks, st, w);
 }
 
 extern "C" int dbl_route_bwd(const dbl_route_shape* s, const void* logits, const int32_t* chosen, const float* weights,
@@ -279,11 +444,14 @@ extern "C" int dbl_route_bwd(const dbl_route_shape* s, const void* logits, const
     const unsigned blocks = (unsigned)(need < cap ? need : cap);
     const int64_t ld = s->ld ? s->ld : s->experts, ld_grad = s->ld_grad ? s->ld_grad : s->experts;
     cudaStream_t st = as_stream(stream);
-    if (s->dtype == DBL_F32)
-        route_bwd_kernel<float><<<blocks, 256, 0, st>>>(logits, chosen, weights, dweights, dlogits, s->rows, s->experts, s->k,
-                                                        s->normalise != 0, ld, ld_grad);
-    else
-        route_bwd_kernel<act_t><<<blocks, 256, 0, st>>>(logits, chosen, weights, dweights, dlogits, s->rows, s->experts, s->k,
-                                                        s->normalise != 0, ld, ld_grad);
-    return launch_check(w);
+    return with_lanes(s->experts, [&](auto epl) {
+        constexpr int EPL = decltype(epl)::value;
+        if (s->dtype == DBL_F32)
+            route_bwd_kernel<float, EPL><<<blocks, 256, 0, st>>>(logits, chosen, weights, dweights, dlogits, s->rows, s->experts,
+                                                                 s->k, s->normalise != 0, ld, ld_grad);
+        else
+            route_bwd_kernel<act_t, EPL><<<blocks, 256, 0, st>>>(logits, chosen, weights, dweights, dlogits, s->rows, s->experts,
+                                                                 s->k, s->normalise != 0, ld, ld_grad);
+        return launch_check(w);
+    });
 }
