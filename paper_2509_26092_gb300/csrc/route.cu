@@ -1,7 +1,9 @@
 // route.cu -- the router of a layer of experts: the k experts of every token and their weights, the tokens' places
 // grouped by expert, and the gradient of the logits.
+#include <float.h>
 #include <math.h>
 
+#include <algorithm>
 #include <type_traits>
 
 #include "dbl_elem.cuh"
@@ -14,6 +16,7 @@ using namespace dbl::dev;
 constexpr int kMaxExperts = DBL_ROUTE_MAX_EXPERTS, kMaxK = DBL_ROUTE_MAX_K;
 constexpr int kMaxBlocks = 256;    // of the forward pass; the workspace holds one count for each block and expert
 constexpr int kOneBlockRows = 256;  // up to here one block chooses and places
+constexpr int kManyRows = 128;      // of a block: from here a thread takes a row
 constexpr int kPlaceCounts = 8192;  // counts of a block's warps and experts in shared memory
 
 struct RouteArgs {
@@ -138,9 +141,9 @@ __device__ __forceinline__ int choose_row(const RouteArgs& a, int64_t r, int lan
     return mine;
 }
 
-// Gives the entries of rows r0 .. r1 - 1 their places: after the entries of smaller experts, those of the same expert in
-// the blocks before (base[e] is both) and those before them in this block.  counts: [warps][experts] in shared memory; the
-// warps, which are so many that it fits, take parts of the entries in order.
+// Gives the entries of rows r0 .. r1 - 1 their places among the block's entries of the same expert, in order, counted from
+// base[e].  counts: [warps][experts] in shared memory; the warps, which are so many that it fits, take parts of the entries in
+// order.
 __device__ __forceinline__ void place(const RouteArgs& a, int64_t r0, int64_t r1, const int* base, int* counts, int warps)
 {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -151,14 +154,20 @@ __device__ __forceinline__ void place(const RouteArgs& a, int64_t r0, int64_t r1
     for (int i = threadIdx.x; i < warps * a.experts; i += blockDim.x) counts[i] = 0;
     __syncthreads();
     int* mine = counts + warp * a.experts;
+    constexpr int AHEAD = 4;  // entries that a lane asks for at a time
     if (warp < warps)
-        for (int64_t i = i0 + lane; i < i1; i += 32) {
-            const int e = chosen[i];
-            if (e >= 0) atomicAdd(&mine[e], 1);
+        for (int64_t i = i0 + lane; i < i1; i += 32 * AHEAD) {
+            int e[AHEAD];
+#pragma unroll
+            for (int q = 0; q < AHEAD; ++q) e[q] = i + 32 * q < i1 ? chosen[i + 32 * q] : -1;
+#pragma unroll
+            for (int q = 0; q < AHEAD; ++q)
+                if (e[q] >= 0) atomicAdd(&mine[e[q]], 1);
         }
     __syncthreads();
     for (int e = threadIdx.x; e < a.experts; e += blockDim.x) {
         int at = base[e];
+#pragma unroll 8
         for (int w = 0; w < warps; ++w) {
             const int c = counts[w * a.experts + e];
             counts[w * a.experts + e] = at;
@@ -167,16 +176,20 @@ __device__ __forceinline__ void place(const RouteArgs& a, int64_t r0, int64_t r1
     }
     __syncthreads();
     if (warp < warps)
-        for (int64_t i = i0; i < i1; i += 32) {
-            const bool in = i + lane < i1;
-            const int e = in ? chosen[i + lane] : -1;
-            const uint32_t same = __match_any_sync(0xffffffffu, e);
-            const int rank = __popc(same & ((1u << lane) - 1));
-            const int at = e >= 0 ? mine[e] + rank : -1;
-            __syncwarp();
-            if (e >= 0 && rank == 0) mine[e] += __popc(same);
-            __syncwarp();
-            if (in) slots[i + lane] = at;
+        for (int64_t i = i0 + lane; i - lane < i1; i += 32 * AHEAD) {
+            int e[AHEAD];
+#pragma unroll
+            for (int q = 0; q < AHEAD; ++q) e[q] = i + 32 * q < i1 ? chosen[i + 32 * q] : -1;
+#pragma unroll
+            for (int q = 0; q < AHEAD; ++q) {
+                const uint32_t same = __match_any_sync(0xffffffffu, e[q]);
+                const int rank = __popc(same & ((1u << lane) - 1));
+                const int at = e[q] >= 0 ? mine[e[q]] + rank : -1;
+                __syncwarp();
+                if (e[q] >= 0 && rank == 0) mine[e[q]] += __popc(same);
+                __syncwarp();
+                if (i + 32 * q < i1) slots[i + 32 * q] = at;
+            }
         }
 }
 
@@ -211,6 +224,17 @@ __device__ __forceinline__ void bounds(const RouteArgs& a, const int* total, int
     }
 }
 
+// After the block's rows are chosen and its entries counted: their places in the block, or, where it is the only one, among all.
+__device__ __forceinline__ void finish_block(const RouteArgs& a, int64_t r0, int64_t r1, const int* total, int* base, int* part,
+                                             int* counts, int place_warps)
+{
+    if (gridDim.x > 1)
+        for (int e = threadIdx.x; e < a.experts; e += blockDim.x) a.counts[(int64_t)blockIdx.x * a.experts + e] = total[e];
+    else
+        bounds(a, total, base, part, true);
+    place(a, r0, r1, base, counts, place_warps);
+}
+
 template <int EPL>
 constexpr int choose_threads() { return EPL <= 8 ? 1024 : 512; }
 
@@ -238,22 +262,225 @@ __global__ void __launch_bounds__(choose_threads<EPL>()) route_choose_kernel(con
         }
     }
     __syncthreads();
-    if (gridDim.x > 1) {
-        for (int e = threadIdx.x; e < a.experts; e += blockDim.x) a.counts[(int64_t)blockIdx.x * a.experts + e] = total[e];
-        return;
-    }
-    bounds(a, total, base, part, true);
-    place(a, r0, r1, base, counts, place_warps);
+    finish_block(a, r0, r1, total, base, part, counts, place_warps);
 }
 
-// Threads share an expert's counts where there are more threads than experts.
-__global__ void __launch_bounds__(1024) route_place_kernel(const RouteArgs a, int place_warps)
+// exp(x) for x <= 0, off by (1.5*|x| + 4)*2^-24 of it, and 0 below 2^-126: for sums that are divided by.
+__device__ __forceinline__ float exp_near(float x)
 {
-    extern __shared__ int counts[];
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x * 1.44269504f));
+    return r;
+}
+
+// The steps of a bitonic sort's runs of RUN, from STEP on: falling order where RUN is all.
+template <int RUN, int STEP>
+__device__ __forceinline__ void fall(float (&m)[16])
+{
+#pragma unroll
+    for (int j = 0; j < 16; ++j)
+        if ((j ^ STEP) > j) {
+            const float hi = fmaxf(m[j], m[j ^ STEP]), lo = fminf(m[j], m[j ^ STEP]);
+            m[j] = (j & RUN) ? lo : hi;
+            m[j ^ STEP] = (j & RUN) ? hi : lo;
+        }
+    if constexpr (STEP > 1) fall<RUN, STEP / 2>(m);
+}
+
+constexpr int kTileThreads = 512, kTileBytes = 160 * 1024;
+
+// The same where there are many rows: a thread to a row, its logits in shared memory.  The row's experts form 16 classes,
+// every 16th expert one; the k-th largest of the classes' maxima is a bound that at least k experts reach and few others
+// (about 11 of 128 for k = 8), so that few enter the sorted list of KT.  81 instructions of a warp to a row where a warp to
+// a row takes 400.  KT: k or more.  N: elements of 16 bytes.
+template <class T, int KT, bool BIAS>
+__global__ void __launch_bounds__(kTileThreads) route_choose_many_kernel(const RouteArgs a, int tile, int pitch, int place_warps)
+{
+    constexpr int N = 16 / (int)sizeof(T);
+    extern __shared__ __align__(16) uint8_t smem[];
+    __shared__ int total[kMaxExperts], base[kMaxExperts], part[32];
+    __shared__ float bias[BIAS ? 512 : 1];
+    for (int e = threadIdx.x; e < a.experts; e += blockDim.x) total[e] = base[e] = 0;
+    grid_dependency_trigger();
+    const int padded = (a.experts + 15) / 16 * 16;
+    if (BIAS)
+        for (int e = threadIdx.x; e < padded; e += blockDim.x) bias[e] = e < a.experts ? a.bias[e] : 0.f;
+    const int64_t r0 = (int64_t)blockIdx.x * a.rows_per_block, r1 = min(a.rows, r0 + a.rows_per_block);
+    const T* z0 = static_cast<const T*>(a.logits);
+    const bool quads = ((reinterpret_cast<uintptr_t>(a.chosen) | reinterpret_cast<uintptr_t>(a.weights)) & 15) == 0;
+    const bool wide = ((reinterpret_cast<uintptr_t>(z0) | (uintptr_t)a.ld * sizeof(T) | (uintptr_t)a.experts * sizeof(T)) & 15) == 0;
+    for (int64_t t0 = r0; t0 < r1; t0 += tile) {
+        const int n = (int)min((int64_t)tile, r1 - t0);
+        __syncthreads();
+        if (wide) {
+            const int per = a.experts / N;
+            for (int i = threadIdx.x; i < n * per; i += kTileThreads) {
+                const int l = i / per, u = i - l * per;
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(smem + l * pitch + u * 16)),
+                             "l"(z0 + (t0 + l) * a.ld + u * N)
+                             : "memory");
+            }
+        } else {
+            for (int i = threadIdx.x; i < n * a.experts; i += kTileThreads) {
+                const int l = i / a.experts, u = i - l * a.experts;
+                reinterpret_cast<T*>(smem + l * pitch)[u] = z0[(t0 + l) * a.ld + u];
+            }
+        }
+        const int64_t r = t0 + threadIdx.x;
+        const bool dead = (int)threadIdx.x < n && a.row_weight && a.row_weight[r] == 0.f;
+        const int tail = padded - a.experts;
+        for (int i = threadIdx.x; i < n * tail; i += kTileThreads)
+            reinterpret_cast<T*>(smem + i / tail * pitch)[a.experts + i % tail] = elem_from<T>(-INFINITY);
+        asm volatile("cp.async.wait_all;" ::: "memory");
+        __syncthreads();
+        if ((int)threadIdx.x >= n) continue;
+        const uint8_t* row = smem + threadIdx.x * pitch;
+        // sixteen logits from i on, and their keys
+        auto load16 = [&](int i, float (&v)[16], float (&key)[16]) {
+#pragma unroll
+            for (int q = 0; q < 16 / N; ++q) {
+                const uint4 u = *reinterpret_cast<const uint4*>(row + (i + q * N) * (int)sizeof(T));
+                const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    if constexpr (N == 8) {
+                        const float2 f = act::unpack2_u32(w[j]);
+                        v[q * 8 + 2 * j] = f.x, v[q * 8 + 2 * j + 1] = f.y;
+                    } else {
+                        v[q * 4 + j] = __uint_as_float(w[j]);
+                    }
+                }
+            }
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                float4 b = make_float4(0.f, 0.f, 0.f, 0.f);
+                if (BIAS) b = *reinterpret_cast<const float4*>(bias + i + 4 * q);
+                key[4 * q] = BIAS ? v[4 * q] + b.x : v[4 * q];
+                key[4 * q + 1] = BIAS ? v[4 * q + 1] + b.y : v[4 * q + 1];
+                key[4 * q + 2] = BIAS ? v[4 * q + 2] + b.z : v[4 * q + 2];
+                key[4 * q + 3] = BIAS ? v[4 * q + 3] + b.w : v[4 * q + 3];
+            }
+        };
+        float peak = -INFINITY, m[16];
+#pragma unroll
+        for (int j = 0; j < 16; ++j) m[j] = -INFINITY;
+        for (int i = 0; i < padded; i += 16) {
+            float v[16], key[16];
+            load16(i, v, key);
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+                asm("max.NaN.f32 %0, %0, %1;" : "+f"(peak) : "f"(v[j]));
+                m[j] = fmaxf(m[j], key[j]);
+            }
+        }
+        if (dead || !(peak < INFINITY)) {
+            for (int j = 0; j < a.k; ++j) {
+                a.chosen[r * a.k + j] = -1;
+                a.weights[r * a.k + j] = dead ? 0.f : NAN;
+            }
+            continue;
+        }
+        // the classes' maxima in falling order, then the bound
+        fall<2, 1>(m);
+        fall<4, 2>(m);
+        fall<8, 4>(m);
+        fall<16, 8>(m);
+#pragma unroll
+        for (int half = 8; half; half /= 2)
+#pragma unroll
+            for (int j = 0; j < half; ++j) m[j] = (a.k - 1 & half) ? m[j + half] : m[j];
+        const float bound = fmaxf(m[0], -FLT_MAX);  // the k-th; -infinity is never chosen
+        float top[KT];
+        int id[KT];
+#pragma unroll
+        for (int j = 0; j < KT; ++j) top[j] = -INFINITY, id[j] = -1;
+        float sum = 0.f;
+        for (int i0 = 0; i0 < padded; i0 += 64) {
+            uint64_t reach = 0;
+            for (int i = i0; i < min(padded, i0 + 64); i += 16) {
+                float v[16], key[16];
+                load16(i, v, key);
+                uint32_t bits = 0;
+                float s0 = 0.f, s1 = 0.f;
+#pragma unroll
+                for (int j = 0; j < 16; ++j)
+                    if (key[j] >= bound) bits |= 1u << j;
+                if (!a.normalise) {
+#pragma unroll
+                    for (int j = 0; j < 16; j += 2) s0 += exp_near(v[j] - peak), s1 += exp_near(v[j + 1] - peak);
+                    sum += s0 + s1;
+                }
+                reach |= (uint64_t)bits << (i - i0);
+            }
+            while (reach) {
+                const int e = i0 + __ffsll((long long)reach) - 1;
+                reach &= reach - 1;
+                const float key = elem_f(reinterpret_cast<const T*>(row)[e]) + (BIAS ? bias[e] : 0.f);
+                bool after[KT];  // what the list has there comes after this one: of equals the first stays before
+#pragma unroll
+                for (int j = 0; j < KT; ++j) after[j] = key > top[j];
+#pragma unroll
+                for (int j = KT - 1; j >= 0; --j) {
+                    const bool moves = j > 0 && after[j ? j - 1 : 0];
+                    top[j] = after[j] ? (moves ? top[j ? j - 1 : 0] : key) : top[j];
+                    id[j] = after[j] ? (moves ? id[j ? j - 1 : 0] : e) : id[j];
+                }
+            }
+        }
+        float over = peak;
+        if (a.normalise) {
+            over = -INFINITY;
+#pragma unroll
+            for (int j = 0; j < KT; ++j)
+                if (j < a.k && id[j] >= 0) over = fmaxf(over, elem_f(reinterpret_cast<const T*>(row)[id[j]]));
+        }
+        float weight[KT];
+#pragma unroll
+        for (int j = 0; j < KT; ++j) {
+            weight[j] = j < a.k && id[j] >= 0 ? expf(elem_f(reinterpret_cast<const T*>(row)[id[j]]) - over) : 0.f;
+            if (a.normalise) sum += weight[j];
+        }
+#pragma unroll
+        for (int j = 0; j < KT; ++j)
+            if (j < a.k) {
+                weight[j] = id[j] >= 0 ? weight[j] / sum : 0.f;
+                if (id[j] >= 0) atomicAdd(&total[id[j]], 1);
+            }
+        int32_t* c = a.chosen + r * a.k;
+        float* w = a.weights + r * a.k;
+        if (KT % 4 == 0 && a.k == KT && quads) {
+#pragma unroll
+            for (int j = 0; j + 3 < KT; j += 4) {
+                *reinterpret_cast<int4*>(c + j) = make_int4(id[j], id[j + 1], id[j + 2], id[j + 3]);
+                *reinterpret_cast<float4*>(w + j) = make_float4(weight[j], weight[j + 1], weight[j + 2], weight[j + 3]);
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < KT; ++j)
+                if (j < a.k) c[j] = id[j], w[j] = weight[j];
+        }
+    }
+    __syncthreads();
+    finish_block(a, r0, r1, total, base, part, reinterpret_cast<int*>(smem), place_warps);
+}
+
+// Places in the block become places among all: after the entries of smaller experts and those of the same expert in the blocks
+// before.  Threads share an expert's counts where there are more threads than experts.
+__global__ void __launch_bounds__(1024) route_place_kernel(const RouteArgs a)
+{
     __shared__ int total[kMaxExperts], base[kMaxExperts], part[32];
     for (int e = threadIdx.x; e < a.experts; e += 1024) total[e] = base[e] = 0;
     __syncthreads();
     grid_dependency_wait();
+    const int64_t r0 = (int64_t)blockIdx.x * a.rows_per_block, r1 = min(a.rows, r0 + a.rows_per_block);
+    const int64_t i0 = r0 * a.k + threadIdx.x, i1 = r1 * a.k;
+    constexpr int AHEAD = 4;  // entries of a thread that are asked for before the sums
+    int mine[AHEAD], at[AHEAD];
+#pragma unroll
+    for (int q = 0; q < AHEAD; ++q) {
+        mine[q] = i0 + 1024 * q < i1 ? a.chosen[i0 + 1024 * q] : -1;
+        at[q] = i0 + 1024 * q < i1 ? a.slots[i0 + 1024 * q] : 0;
+    }
     const int shares = max(1, 1024 / a.experts), blocks = (int)gridDim.x;
     const int share = (int)threadIdx.x / a.experts, e = (int)threadIdx.x % a.experts;
     if (share < shares) {
@@ -269,8 +496,14 @@ __global__ void __launch_bounds__(1024) route_place_kernel(const RouteArgs a, in
     }
     __syncthreads();
     bounds(a, total, base, part, blockIdx.x == 0);
-    const int64_t r0 = (int64_t)blockIdx.x * a.rows_per_block, r1 = min(a.rows, r0 + a.rows_per_block);
-    place(a, r0, r1, base, counts, place_warps);
+    __syncthreads();
+#pragma unroll
+    for (int q = 0; q < AHEAD; ++q)
+        if (mine[q] >= 0) a.slots[i0 + 1024 * q] = at[q] + base[mine[q]];
+    for (int64_t i = i0 + 1024 * AHEAD; i < i1; i += 1024) {
+        const int c = a.chosen[i];
+        if (c >= 0) a.slots[i] += base[c];
+    }
 }
 
 // A warp to a row: first what every expert gets, then the entries' experts.
@@ -364,32 +597,56 @@ int with_lanes(int experts, F f)
     return f(std::integral_constant<int, 32>());
 }
 
+template <class T, int KT, bool BIAS>
+int launch_many(const RouteArgs& a, int blocks, cudaStream_t st, const char* what)
+{
+    const int rc = allow_launch<route_choose_many_kernel<T, KT, BIAS>>(kTileBytes, false, what);
+    if (rc != DBL_OK) return rc;
+    const int pitch = (a.experts + 15) / 16 * 16 * (int)sizeof(T) + 16;  // an odd number of 16 bytes: rows in different banks
+    int tile = kTileBytes / pitch / 32 * 32;
+    if (tile > kTileThreads) tile = kTileThreads;
+    if (tile > a.rows_per_block) tile = a.rows_per_block;
+    int warps = kPlaceCounts / a.experts;
+    if (warps > kTileThreads / 32) warps = kTileThreads / 32;
+    const int places = warps * a.experts * (int)sizeof(int);
+    route_choose_many_kernel<T, KT, BIAS><<<blocks, kTileThreads, tile * pitch > places ? tile * pitch : places, st>>>(a, tile, pitch, warps);
+    return launch_check(what);
+}
+
 template <class T>
 int launch_fwd(const RouteArgs& a, int blocks, cudaStream_t st, const char* what)
 {
-    int warps = kPlaceCounts / a.experts;
-    const auto choose = [&](auto epl) {
-        constexpr int EPL = decltype(epl)::value, threads = choose_threads<EPL>();
-        const int w = warps < threads / 32 ? warps : threads / 32;
-        route_choose_kernel<T, EPL><<<blocks, threads, blocks == 1 ? w * a.experts * sizeof(int) : 0, st>>>(a, w);
-        return launch_check(what);
-    };
-    const int rc = with_lanes(a.experts, choose);
+    const bool many = std::min(a.rows, (int64_t)a.rows_per_block) >= kManyRows && a.experts > 16 && a.experts <= 512 && a.k <= 16;
+    int rc;
+    if (many) {
+        const auto go = [&](auto kt) {
+            constexpr int KT = decltype(kt)::value;
+            return a.bias ? launch_many<T, KT, true>(a, blocks, st, what) : launch_many<T, KT, false>(a, blocks, st, what);
+        };
+        rc = a.k <= 2 ? go(std::integral_constant<int, 2>()) : a.k <= 4 ? go(std::integral_constant<int, 4>())
+             : a.k <= 8 ? go(std::integral_constant<int, 8>()) : go(std::integral_constant<int, 16>());
+    } else {
+        rc = with_lanes(a.experts, [&](auto epl) {
+            constexpr int EPL = decltype(epl)::value, threads = choose_threads<EPL>();
+            int warps = kPlaceCounts / a.experts;
+            if (warps > threads / 32) warps = threads / 32;
+            route_choose_kernel<T, EPL><<<blocks, threads, warps * a.experts * sizeof(int), st>>>(a, warps);
+            return launch_check(what);
+        });
+    }
     if (rc != DBL_OK || blocks == 1) return rc;
-    if (warps > 32) warps = 32;
     cudaLaunchConfig_t cfg = {};
     cudaLaunchAttribute at[1];
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     at[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.gridDim = dim3(blocks);
     cfg.blockDim = dim3(1024);
-    cfg.dynamicSmemBytes = warps * a.experts * sizeof(int);
     cfg.stream = st;
     cfg.attrs = at;
     cfg.numAttrs = 1;
-    const cudaError_t err = cudaLaunchKernelEx(&cfg, route_place_kernel, a, warps);
-    const int rc2 = launch_check("route_fwd place");
-    return err == cudaSuccess ? rc2 : cuda_check(err, "route_fwd place");
+    const cudaError_t err = cudaLaunchKernelEx(&cfg, route_place_kernel, a);
+    rc = launch_check("route_fwd place");
+    return err == cudaSuccess ? rc : cuda_check(err, "route_fwd place");
 }
 
 }  // namespace
