@@ -3,7 +3,6 @@
 #include <float.h>
 #include <math.h>
 
-#include <algorithm>
 #include <type_traits>
 
 #include "dbl_elem.cuh"
@@ -209,7 +208,7 @@ __device__ __forceinline__ void bounds(const RouteArgs& a, const int* total, int
         if (lane == 31) part[warp] = sum;
         __syncthreads();
         int before = running;
-        for (int w = 0; w < warps; ++w) {
+        for (int w = 0; w < min(warps, (a.experts - first + 31) / 32); ++w) {
             if (w < warp) before += part[w];
             running += part[w];
         }
@@ -287,6 +286,7 @@ __device__ __forceinline__ void fall(float (&m)[16])
     if constexpr (STEP > 1) fall<RUN, STEP / 2>(m);
 }
 
+constexpr int kManyExperts = 512;
 constexpr int kTileThreads = 512, kTileBytes = 160 * 1024;
 
 // The same where there are many rows: a thread to a row, its logits in shared memory.  The row's experts form 16 classes,
@@ -294,20 +294,21 @@ constexpr int kTileThreads = 512, kTileBytes = 160 * 1024;
 // (about 11 of 128 for k = 8), so that few enter the sorted list of KT.  81 instructions of a warp to a row where a warp to
 // a row takes 400.  KT: k or more.  N: elements of 16 bytes.
 template <class T, int KT, bool BIAS>
-__global__ void __launch_bounds__(kTileThreads) route_choose_many_kernel(const RouteArgs a, int tile, int pitch, int place_warps)
+__global__ void __launch_bounds__(kTileThreads) route_choose_many_kernel(const RouteArgs a, int tile, int pitch)
 {
     constexpr int N = 16 / (int)sizeof(T);
     extern __shared__ __align__(16) uint8_t smem[];
-    __shared__ int total[kMaxExperts], base[kMaxExperts], part[32];
-    __shared__ float bias[BIAS ? 512 : 1];
-    for (int e = threadIdx.x; e < a.experts; e += blockDim.x) total[e] = base[e] = 0;
+    __shared__ int total[kManyExperts];
+    __shared__ float bias[BIAS ? kManyExperts : 1];
+    for (int e = threadIdx.x; e < a.experts; e += blockDim.x) total[e] = 0;
     grid_dependency_trigger();
     const int padded = (a.experts + 15) / 16 * 16;
     if (BIAS)
         for (int e = threadIdx.x; e < padded; e += blockDim.x) bias[e] = e < a.experts ? a.bias[e] : 0.f;
     const int64_t r0 = (int64_t)blockIdx.x * a.rows_per_block, r1 = min(a.rows, r0 + a.rows_per_block);
     const T* z0 = static_cast<const T*>(a.logits);
-    const bool quads = ((reinterpret_cast<uintptr_t>(a.chosen) | reinterpret_cast<uintptr_t>(a.weights)) & 15) == 0;
+    const bool quads = ((reinterpret_cast<uintptr_t>(a.chosen) | reinterpret_cast<uintptr_t>(a.weights) |
+                         reinterpret_cast<uintptr_t>(a.slots)) & 15) == 0;
     const bool wide = ((reinterpret_cast<uintptr_t>(z0) | (uintptr_t)a.ld * sizeof(T) | (uintptr_t)a.experts * sizeof(T)) & 15) == 0;
     for (int64_t t0 = r0; t0 < r1; t0 += tile) {
         const int n = (int)min((int64_t)tile, r1 - t0);
@@ -333,8 +334,7 @@ __global__ void __launch_bounds__(kTileThreads) route_choose_many_kernel(const R
             reinterpret_cast<T*>(smem + i / tail * pitch)[a.experts + i % tail] = elem_from<T>(-INFINITY);
         asm volatile("cp.async.wait_all;" ::: "memory");
         __syncthreads();
-        if ((int)threadIdx.x >= n) continue;
-        const uint8_t* row = smem + threadIdx.x * pitch;
+        const uint8_t* row = smem + min((int)threadIdx.x, n - 1) * pitch;
         // sixteen logits from i on, and their keys
         auto load16 = [&](int i, float (&v)[16], float (&key)[16]) {
 #pragma unroll
@@ -373,13 +373,7 @@ __global__ void __launch_bounds__(kTileThreads) route_choose_many_kernel(const R
                 m[j] = fmaxf(m[j], key[j]);
             }
         }
-        if (dead || !(peak < INFINITY)) {
-            for (int j = 0; j < a.k; ++j) {
-                a.chosen[r * a.k + j] = -1;
-                a.weights[r * a.k + j] = dead ? 0.f : NAN;
-            }
-            continue;
-        }
+        const bool none = dead || !(peak < INFINITY) || (int)threadIdx.x >= n;
         // the classes' maxima in falling order, then the bound
         fall<2, 1>(m);
         fall<4, 2>(m);
@@ -412,6 +406,7 @@ __global__ void __launch_bounds__(kTileThreads) route_choose_many_kernel(const R
                 }
                 reach |= (uint64_t)bits << (i - i0);
             }
+            if (none) reach = 0;
             while (reach) {
                 const int e = i0 + __ffsll((long long)reach) - 1;
                 reach &= reach - 1;
@@ -440,28 +435,57 @@ __global__ void __launch_bounds__(kTileThreads) route_choose_many_kernel(const R
             weight[j] = j < a.k && id[j] >= 0 ? expf(elem_f(reinterpret_cast<const T*>(row)[id[j]]) - over) : 0.f;
             if (a.normalise) sum += weight[j];
         }
+        const float empty = none && !dead ? NAN : 0.f;
+#pragma unroll
+        for (int j = 0; j < KT; ++j) {
+            weight[j] = id[j] >= 0 && j < a.k ? weight[j] / sum : empty;
+            if (j >= a.k) id[j] = -1;
+        }
+        // Places: a bit for each row in its expert's set; before a row are those of the tiles before, of the words before and
+        // the bits before.
+        __syncthreads();  // the logits are done with
+        const int words = (n + 31) / 32;
+        uint32_t* set = reinterpret_cast<uint32_t*>(smem);
+        int* before = reinterpret_cast<int*>(smem) + a.experts * words;
+        for (int i = threadIdx.x; i < a.experts * words; i += kTileThreads) set[i] = 0;
+        __syncthreads();
+        const int word = (int)threadIdx.x / 32;
+        const uint32_t bit = 1u << (threadIdx.x & 31);
 #pragma unroll
         for (int j = 0; j < KT; ++j)
-            if (j < a.k) {
-                weight[j] = id[j] >= 0 ? weight[j] / sum : 0.f;
-                if (id[j] >= 0) atomicAdd(&total[id[j]], 1);
+            if (id[j] >= 0) atomicOr(&set[id[j] * words + word], bit);
+        __syncthreads();
+        for (int e = threadIdx.x; e < a.experts; e += kTileThreads) {
+            int at = total[e];
+            for (int w = 0; w < words; ++w) {
+                before[e * words + w] = at;
+                at += __popc(set[e * words + w]);
             }
-        int32_t* c = a.chosen + r * a.k;
+            total[e] = at;
+        }
+        __syncthreads();
+        if ((int)threadIdx.x >= n) continue;
+        int slot[KT];
+#pragma unroll
+        for (int j = 0; j < KT; ++j)
+            slot[j] = id[j] >= 0 ? before[id[j] * words + word] + __popc(set[id[j] * words + word] & (bit - 1)) : -1;
+        int32_t *c = a.chosen + r * a.k, *s = a.slots + r * a.k;
         float* w = a.weights + r * a.k;
         if (KT % 4 == 0 && a.k == KT && quads) {
 #pragma unroll
             for (int j = 0; j + 3 < KT; j += 4) {
                 *reinterpret_cast<int4*>(c + j) = make_int4(id[j], id[j + 1], id[j + 2], id[j + 3]);
                 *reinterpret_cast<float4*>(w + j) = make_float4(weight[j], weight[j + 1], weight[j + 2], weight[j + 3]);
+                *reinterpret_cast<int4*>(s + j) = make_int4(slot[j], slot[j + 1], slot[j + 2], slot[j + 3]);
             }
         } else {
 #pragma unroll
             for (int j = 0; j < KT; ++j)
-                if (j < a.k) c[j] = id[j], w[j] = weight[j];
+                if (j < a.k) c[j] = id[j], w[j] = weight[j], s[j] = slot[j];
         }
     }
     __syncthreads();
-    finish_block(a, r0, r1, total, base, part, reinterpret_cast<int*>(smem), place_warps);
+    for (int e = threadIdx.x; e < a.experts; e += blockDim.x) a.counts[(int64_t)blockIdx.x * a.experts + e] = total[e];
 }
 
 // Places in the block become places among all: after the entries of smaller experts and those of the same expert in the blocks
@@ -485,11 +509,16 @@ __global__ void __launch_bounds__(1024) route_place_kernel(const RouteArgs a)
     const int share = (int)threadIdx.x / a.experts, e = (int)threadIdx.x % a.experts;
     if (share < shares) {
         int before = 0, all = 0;
-#pragma unroll 8
-        for (int b = share; b < blocks; b += shares) {
-            const int n = a.counts[(int64_t)b * a.experts + e];
-            all += n;
-            if (b < (int)blockIdx.x) before += n;
+        constexpr int LOADS = 20;  // asked for at a time: all of 152 blocks' for 128 experts
+        for (int b0 = share; b0 < blocks; b0 += LOADS * shares) {
+            int n[LOADS];
+#pragma unroll
+            for (int q = 0; q < LOADS; ++q) n[q] = b0 + q * shares < blocks ? a.counts[(int64_t)(b0 + q * shares) * a.experts + e] : 0;
+#pragma unroll
+            for (int q = 0; q < LOADS; ++q) {
+                all += n[q];
+                if (b0 + q * shares < (int)blockIdx.x) before += n[q];
+            }
         }
         atomicAdd(&total[e], all);
         atomicAdd(&base[e], before);
@@ -606,17 +635,15 @@ int launch_many(const RouteArgs& a, int blocks, cudaStream_t st, const char* wha
     int tile = kTileBytes / pitch / 32 * 32;
     if (tile > kTileThreads) tile = kTileThreads;
     if (tile > a.rows_per_block) tile = a.rows_per_block;
-    int warps = kPlaceCounts / a.experts;
-    if (warps > kTileThreads / 32) warps = kTileThreads / 32;
-    const int places = warps * a.experts * (int)sizeof(int);
-    route_choose_many_kernel<T, KT, BIAS><<<blocks, kTileThreads, tile * pitch > places ? tile * pitch : places, st>>>(a, tile, pitch, warps);
+    const int sets = a.experts * ((tile + 31) / 32) * 2 * (int)sizeof(int);
+    route_choose_many_kernel<T, KT, BIAS><<<blocks, kTileThreads, tile * pitch > sets ? tile * pitch : sets, st>>>(a, tile, pitch);
     return launch_check(what);
 }
 
 template <class T>
 int launch_fwd(const RouteArgs& a, int blocks, cudaStream_t st, const char* what)
 {
-    const bool many = std::min(a.rows, (int64_t)a.rows_per_block) >= kManyRows && a.experts > 16 && a.experts <= 512 && a.k <= 16;
+    const bool many = blocks > 1 && a.rows_per_block >= kManyRows && a.experts > 16 && a.experts <= kManyExperts && a.k <= 16;
     int rc;
     if (many) {
         const auto go = [&](auto kt) {
