@@ -37,19 +37,20 @@ __device__ __forceinline__ void report_timeout(volatile int* abort)
 
 enum : int { kFwd = 0, kDgrad = 1, kWgrad = 2 };
 
-// A tile is 256 rows of the result by BN columns, one CTA pair's: each CTA stages its own 128 rows of A and half of the
-// BN columns of B, 64 elements of the reduction to a stage, and holds its 128 rows of the result in TMEM.
-template <int BN>
+// A tile is a CTA pair's: 256 of the features that the weights have (fwd: n_out, dgrad: n_in) for up to 256 tokens of a group,
+// or 256 x 256 of a weight gradient.  The features are the MMA's M, 128 in each CTA, and the tokens its N, as many as there are
+// to the next multiple of 32: a group's last tokens cost what they are, and a group of a few costs the reading of its
+// weights.  (With the tokens as M, in blocks of 256: 122 rows over 8 groups of 512x2048 9.2 us, 65536 over 64 groups of
+// different lengths 352.)  64 elements of the reduction to a stage; each CTA stages its own features and half of the tokens,
+// and holds its features of the result in TMEM.
 struct Cfg {
-    static constexpr int BNC = BN / 2;
-    static constexpr int A_BYTES = 128 * 64 * 2, B_BYTES = BNC * 64 * 2;
+    static constexpr int A_BYTES = 128 * 64 * 2, B_BYTES = 128 * 64 * 2;
     static constexpr int STAGE_BYTES = A_BYTES + B_BYTES;
-    static constexpr int STAGES = 196608 / STAGE_BYTES;
+    static constexpr int STAGES = 6;
     static constexpr int EPI = 8, PROD = 2, MMA_WARP = EPI + PROD;
     static constexpr int SMEM = STAGES * STAGE_BYTES + EPI * 2048 + 1024;
-    static constexpr int NB = 512 / BN;  // accumulators: all of TMEM
+    static constexpr int NB = 2;  // accumulators of 256 columns: all of TMEM
     static constexpr int THREADS = 32 * (EPI + PROD + 1);
-    static constexpr int CW = BN / 2;  // columns that one epilogue warp drains
     static_assert(SMEM >= 117 * 1024, "one CTA on an SM: each takes all of TMEM before a cluster barrier");
 };
 
@@ -63,40 +64,44 @@ struct MmaArgs {
     const int32_t* offsets;
     int64_t rows, ld;   // ld: of out and mask
     int groups, n_in, n_out, relu, accumulate;
-    int cols;           // of the result
+    int features;       // of the result (fwd, dgrad)
     int depth;          // of the reduction (fwd, dgrad)
-    int tiles_m, tiles_n;  // of a group (tiles_m: wgrad alone)
+    int blocks_a, blocks_b;  // blocks of 256 features; wgrad: of n_in and n_out
 };
 
 struct Tile {
-    int group, m0, n0, kb;  // kb: stages of the reduction
-    int row0, row1;         // of the group
+    int group, a0, b0;  // a0: the first of 256 features (wgrad: of n_in); b0: the first row (wgrad: of 256 of n_out)
+    int n;              // the MMA's N
+    int kb;             // stages of the reduction
+    int row0, row1;     // of the group
 };
 
-// The tiles of a CTA pair, every nunits-th in the order of group, row block, column block: the column blocks of some rows
-// run at the same time, so that x is read once however long the group is.  Counted on, as every role of the kernel would
-// divide for every tile.
-template <int PASS, int BN>
+// The tiles of a CTA pair, every nunits-th in the order of group, block of rows (wgrad: of n_in), block of features (of
+// n_out): the features of some rows run at the same time, so that x is read once however long the group is.  Counted on, as
+// every role of the kernel would divide for every tile.
+template <int PASS>
 struct Walk {
-    int group, m, n, step_m, step_n;
+    int group, outer, inner, step_outer, step_inner;
 
+    __device__ __forceinline__ static int inners(const MmaArgs& p) { return PASS == kWgrad ? p.blocks_b : p.blocks_a; }
     __device__ __forceinline__ Walk(const MmaArgs& p, const int* first, int unit0, int nunits)
-        : group(0), m(unit0 / p.tiles_n), n(unit0 % p.tiles_n), step_m(nunits / p.tiles_n), step_n(nunits % p.tiles_n)
+        : group(0), outer(unit0 / inners(p)), inner(unit0 % inners(p)), step_outer(nunits / inners(p)),
+          step_inner(nunits % inners(p))
     {
         settle(p, first);
     }
     __device__ __forceinline__ void settle(const MmaArgs& p, const int* first)
     {
         for (; group < p.groups; ++group) {
-            const int blocks = PASS == kWgrad ? p.tiles_m : first[group + 1] - first[group];
-            if (m < blocks) return;
-            m -= blocks;
+            const int blocks = PASS == kWgrad ? p.blocks_a : first[group + 1] - first[group];
+            if (outer < blocks) return;
+            outer -= blocks;
         }
     }
     __device__ __forceinline__ void next(const MmaArgs& p, const int* first)
     {
-        m += step_m;
-        if ((n += step_n) >= p.tiles_n) n -= p.tiles_n, ++m;
+        outer += step_outer;
+        if ((inner += step_inner) >= inners(p)) inner -= inners(p), ++outer;
         settle(p, first);
     }
     __device__ __forceinline__ bool there(const MmaArgs& p) const { return group < p.groups; }
@@ -104,10 +109,11 @@ struct Walk {
     {
         Tile c;
         c.group = group;
-        c.n0 = n * BN;
         c.row0 = off[group];
         c.row1 = off[group + 1];
-        c.m0 = m * 256 + (PASS == kWgrad ? 0 : c.row0);
+        c.a0 = (PASS == kWgrad ? outer : inner) * 256;
+        c.b0 = PASS == kWgrad ? inner * 256 : c.row0 + outer * 256;
+        c.n = PASS == kWgrad ? 256 : min(256, (c.row1 - c.b0 + 31) / 32 * 32);
         c.kb = ((PASS == kWgrad ? c.row1 - c.row0 : p.depth) + 63) / 64;
         return c;
     }
@@ -127,11 +133,21 @@ __device__ __forceinline__ uint32_t pass2(uint32_t v, uint32_t h)
     return v & __hgt2_mask(*reinterpret_cast<const act2_t*>(&h), act::pack2(0.f, 0.f));
 }
 
-template <int PASS, int BN>
-__global__ void __launch_bounds__(Cfg<BN>::THREADS, 1)
-    grouped_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const MmaArgs p)
+// Four 8 x 8 matrices, each column of one to 16 bytes of shared memory: lane l gives column l % 8 of matrix l / 8 its address.
+__device__ __forceinline__ void store_columns(uint32_t addr, uint32_t m0, uint32_t m1, uint32_t m2, uint32_t m3)
 {
-    using C = Cfg<BN>;
+    asm volatile("stmatrix.sync.aligned.m8n8.x4.trans.shared.b16 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(m0), "r"(m1), "r"(m2),
+                 "r"(m3)
+                 : "memory");
+}
+
+// tmA: fwd, dgrad: the weights, wgrad: x; tmB: the tokens in boxes of 128, wgrad: dy; tmC: the tokens in boxes of 16.
+template <int PASS>
+__global__ void __launch_bounds__(Cfg::THREADS, 1)
+    grouped_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
+                   const __grid_constant__ CUtensorMap tmC, const MmaArgs p)
+{
+    using C = Cfg;
     constexpr int STAGES = C::STAGES;
     extern __shared__ uint8_t smem_raw[];
     __shared__ __align__(8) uint64_t full_bar[STAGES], empty_bar[STAGES], accf_bar[C::NB], acce_bar[C::NB], drain_bar;
@@ -166,7 +182,7 @@ __global__ void __launch_bounds__(Cfg<BN>::THREADS, 1)
         tma_prefetch_desc(&tmB);
     }
     if (warp == C::MMA_WARP) {
-        tmem_alloc_cg<2>(&tmem_slot, C::NB * BN);
+        tmem_alloc_cg<2>(&tmem_slot, C::NB * 256);
         tmem_relinquish_cg<2>();
     }
     if (warp == 0) {
@@ -192,7 +208,7 @@ __global__ void __launch_bounds__(Cfg<BN>::THREADS, 1)
     cluster_sync_all();
     tc_fence_after();
     const uint32_t tmem = tmem_slot;
-    Walk<PASS, BN> walk(p, first, unit0, nunits);
+    Walk<PASS> walk(p, first, unit0, nunits);
 
     if (warp >= C::EPI && warp < C::MMA_WARP) {
         // ------------------------------------------------------------------ TMA producers (whole warp, one lane issues)
@@ -212,7 +228,7 @@ __global__ void __launch_bounds__(Cfg<BN>::THREADS, 1)
                 uint8_t* sa = sgen + s * C::STAGE_BYTES;
                 uint8_t* sb = sa + C::A_BYTES;
                 const uint32_t fb0 = mapa_shared(smem_u32(&full_bar[s]), 0);
-                const int bcol = tc.n0 + rank * C::BNC;
+                const int acol = tc.a0 + rank * 128;
                 if constexpr (PASS == kWgrad) {
                     // the last rows of a group: what is behind them in the last 16 is of another group, or of none, and may be
                     // NaN, so it is made 0 in both operands before the pair's MMAs may start
@@ -223,8 +239,9 @@ __global__ void __launch_bounds__(Cfg<BN>::THREADS, 1)
                         mbar_arrive_expect_tx_elect(&tail_bar[prod], C::STAGE_BYTES);
                     else if (rank == 0)
                         mbar_arrive_expect_tx_elect(&full_bar[s], 2 * C::STAGE_BYTES);
-                    for (int j = 0; j < 2; ++j) tma_load_2d_cg<2>(sa + j * 8192, &tmA, bar, tc.m0 + rank * 128 + 64 * j, row);
-                    for (int j = 0; j < C::BNC / 64; ++j) tma_load_2d_cg<2>(sb + j * 8192, &tmB, bar, bcol + 64 * j, row);
+                    const int bcol = tc.b0 + rank * 128;
+                    for (int j = 0; j < 2; ++j) tma_load_2d_cg<2>(sa + j * 8192, &tmA, bar, acol + 64 * j, row);
+                    for (int j = 0; j < 2; ++j) tma_load_2d_cg<2>(sb + j * 8192, &tmB, bar, bcol + 64 * j, row);
                     if (tail) {
                         const uint32_t landed = mbar_wait_warp(&tail_bar[prod], tails & 1, &abort_flag);
                         ++tails;
@@ -242,13 +259,16 @@ __global__ void __launch_bounds__(Cfg<BN>::THREADS, 1)
                         __syncwarp();
                     }
                 } else {
-                    if (rank == 0) mbar_arrive_expect_tx_elect(&full_bar[s], 2 * C::STAGE_BYTES);
-                    tma_load_2d_cg<2>(sa, &tmA, fb0, k * 64, tc.m0 + rank * 128);
+                    const int half = tc.n / 2, row = tc.b0 + rank * half;  // this CTA's tokens
+                    if (rank == 0) mbar_arrive_expect_tx_elect(&full_bar[s], 2 * (C::A_BYTES + half * 128));
                     if constexpr (PASS == kFwd)
-                        tma_load_3d_cg<2>(sb, &tmB, fb0, k * 64, bcol, tc.group);
+                        tma_load_3d_cg<2>(sa, &tmA, fb0, k * 64, acol, tc.group);
                     else
-                        for (int j = 0; j < C::BNC / 64; ++j)
-                            tma_load_3d_cg<2>(sb + j * 8192, &tmB, fb0, bcol + 64 * j, k * 64, tc.group);
+                        for (int j = 0; j < 2; ++j) tma_load_3d_cg<2>(sa + j * 8192, &tmA, fb0, acol + 64 * j, k * 64, tc.group);
+                    if (half == 128)
+                        tma_load_2d_cg<2>(sb, &tmB, fb0, k * 64, row);
+                    else
+                        for (int j = 0; j < half; j += 16) tma_load_2d_cg<2>(sb + j * 128, &tmC, fb0, k * 64, row + j);
                 }
                 last_it = it;
             }
@@ -270,8 +290,7 @@ __global__ void __launch_bounds__(Cfg<BN>::THREADS, 1)
         // ------------------------------------------------------------------ MMA issuer (rank 0: whole warp, one lane issues)
         // K-major operands: rows of 128 bytes, 32 bytes a step of 16.  MN-major ones: atoms of 64 columns, 8 KB apart, 16
         // rows of 128 bytes a step.
-        constexpr bool a_mn = PASS == kWgrad, b_mn = PASS != kFwd;
-        constexpr uint32_t idesc = idesc_act(256, BN, a_mn, b_mn);
+        constexpr bool a_mn = PASS != kFwd, b_mn = PASS == kWgrad;
         const uint64_t dA = smem_desc(0, a_mn ? 8192 : 16, 1024, kSwizzle128B);
         const uint64_t dB = smem_desc(0, b_mn ? 8192 : 16, 1024, kSwizzle128B);
         constexpr uint64_t a_step = a_mn ? 2048 / 16 : 2, b_step = b_mn ? 2048 / 16 : 2;
@@ -293,6 +312,7 @@ __global__ void __launch_bounds__(Cfg<BN>::THREADS, 1)
             const int chain = PASS == kWgrad ? kChain : tc.kb;
             const bool tail = PASS == kWgrad && ((tc.row1 - tc.row0) & 15);
             const int length = PASS == kWgrad ? tc.row1 - tc.row0 : p.depth;
+            const uint32_t idesc = idesc_act(256, tc.n, a_mn, b_mn);
             for (int k0 = 0; k0 < tc.kb && !failed; k0 += chain, ++lt) {
                 const int buf = lt % C::NB, k1 = min(tc.kb, k0 + chain);
                 const uint32_t free = mbar_wait_warp(&acce_bar[buf], ((lt / C::NB) & 1) ^ 1, &abort_flag);
@@ -300,7 +320,7 @@ __global__ void __launch_bounds__(Cfg<BN>::THREADS, 1)
                     failed = true;
                     break;
                 }
-                const uint32_t d = tmem + (uint32_t)(buf * BN);
+                const uint32_t d = tmem + (uint32_t)(buf * 256);
                 for (int k = k0; k < k1; ++k, ++it) {
                     if (!wait_full(it, k + 1 == tc.kb && tail)) {
                         failed = true;
@@ -330,9 +350,9 @@ __global__ void __launch_bounds__(Cfg<BN>::THREADS, 1)
         }
     } else {
         // ------------------------------------------------------------------ epilogue (warps 0 .. EPI-1)
-        constexpr int CW = C::CW;
-        [[maybe_unused]] constexpr int NCH = CW / 32;
-        const int quarter = warp & 3, cw0 = (warp >> 2) * CW;
+        constexpr int CW = 128;  // wgrad: columns that one warp drains
+        const int quarter = warp & 3, part = warp >> 2;
+        const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16);
         [[maybe_unused]] uint4* stage = reinterpret_cast<uint4*>(sgen + STAGES * C::STAGE_BYTES) + warp * 128;  // 2 KB
         int lt = 0;
         bool failed = false;
@@ -354,14 +374,15 @@ __global__ void __launch_bounds__(Cfg<BN>::THREADS, 1)
         for (; walk.there(p) && !failed; walk.next(p, first)) {
             const Tile tc = walk.tile(p, off);
             if constexpr (PASS == kWgrad) {
-                const int m = tc.m0 + rank * 128 + quarter * 32 + lane;  // this thread's row of the result
+                const int m = tc.a0 + rank * 128 + quarter * 32 + lane;  // this thread's row of the result
+                const int n0 = tc.b0 + part * CW;
                 float acc[CW];
 #pragma unroll
                 for (int i = 0; i < CW; ++i) acc[i] = 0.f;
                 for (int k0 = 0; k0 < tc.kb; k0 += kChain, ++lt) {
                     const int buf = lt % C::NB;
                     if (!wait_acc(buf)) break;
-                    const uint32_t taddr = tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(buf * BN + cw0);
+                    const uint32_t taddr = lanes + (uint32_t)(buf * 256 + part * CW);
 #pragma unroll
                     for (int ch = 0; ch < CW / 16; ++ch) {
                         uint32_t v[16];
@@ -375,8 +396,8 @@ __global__ void __launch_bounds__(Cfg<BN>::THREADS, 1)
                 if (failed) break;
                 // consecutive lanes hold consecutive columns of dw: each store is a line of 128 bytes
                 if (m < p.n_in) {
-                    float* o = static_cast<float*>(p.out) + ((int64_t)tc.group * p.n_out + tc.n0 + cw0) * p.n_in + m;
-                    const int left = p.n_out - tc.n0 - cw0;  // a multiple of 8
+                    float* o = static_cast<float*>(p.out) + ((int64_t)tc.group * p.n_out + n0) * p.n_in + m;
+                    const int left = p.n_out - n0;  // a multiple of 8
                     if (p.accumulate) {
 #pragma unroll
                         for (int i0 = 0; i0 < CW; i0 += 8)
@@ -397,57 +418,70 @@ __global__ void __launch_bounds__(Cfg<BN>::THREADS, 1)
                     }
                 }
             } else {
-                const int buf = lt % C::NB;
-                // A thread has 32 columns of a row, 64 bytes; through shared memory the warp's 32 rows become stores of four
-                // lanes to a row, so that a store meets 8 rows instead of 32.
-                const int r0 = tc.m0 + rank * 128 + quarter * 32 + lane / 4, q = lane % 4;
-                const int col = tc.n0 + cw0 + q * 8;
+                // 32 features of 32 tokens at a time: pairs of tokens in a thread, turned through shared memory into 64 bytes of a
+                // token's row for four lanes, so that a store meets 8 rows.  The two warps of the same features take turns.
+                const int buf = lt % C::NB, chunks = tc.n / 32;
+                const int q = lane % 4, col = tc.a0 + rank * 128 + quarter * 32 + q * 8;
+                const int r0 = tc.b0 + lane / 4;
                 const int64_t at = (int64_t)r0 * p.ld + col, down = 8 * p.ld;
-                uint4 gate[NCH][4];  // dgrad: the mask, read while the tensor cores are at work
+                constexpr int MOST = PASS == kDgrad ? 4 : 1;
+                uint4 gate[MOST][4];  // dgrad: the mask, read while the tensor cores are at work
                 if constexpr (PASS == kDgrad) {
-                    if (p.mask) {
+                    if (p.mask && col < p.features) {
 #pragma unroll
-                        for (int ch = 0; ch < NCH; ++ch)
+                        for (int c = 0; c < 4; ++c)
 #pragma unroll
-                            for (int i = 0; i < 4; ++i)
-                                if (r0 + 8 * i < tc.row1 && col + ch * 32 < p.cols)
-                                    gate[ch][i] = __ldg(reinterpret_cast<const uint4*>(p.mask + at + i * down + ch * 32));
+                            for (int i = 0; i < 4; ++i) {
+                                const int row = (part + 2 * c) * 32 + 8 * i;
+                                if (r0 + row < tc.row1) gate[c][i] = __ldg(reinterpret_cast<const uint4*>(p.mask + at + row * p.ld));
+                            }
                     }
                 }
                 if (!wait_acc(buf)) break;
-                const uint32_t taddr = tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(buf * BN + cw0);
                 act_t* o = static_cast<act_t*>(p.out) + at;
-#pragma unroll
-                for (int ch = 0; ch < NCH; ++ch) {
-                    uint32_t v[32];
-                    tmem_ld_32x32b_x32(taddr + ch * 32, v);
-                    tmem_ld_wait_regs(v);
-                    if (ch == NCH - 1) release(buf);
+                const auto chunk = [&](int ch, const uint4 (&h)[4]) {
+                    const uint32_t taddr = lanes + (uint32_t)(buf * 256 + ch * 32);
+                    uint32_t lo[16], hi[16];
+                    tmem_ld_16x256b_x4(taddr, lo);
+                    tmem_ld_16x256b_x4(taddr + (16u << 16), hi);
+                    tmem_ld_wait_regs(lo);
+                    tmem_ld_wait_regs(hi);
                     __syncwarp();  // the chunk before has been read
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        uint4 pk;
-                        uint32_t* w32 = reinterpret_cast<uint32_t*>(&pk);
+                    for (int g = 0; g < 4; ++g) {
+                        uint32_t m[4];  // features 0-7, 8-15, 16-23, 24-31 of tokens 8g .. 8g + 7
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            w32[j] = act::pack2_u32(__uint_as_float(v[8 * i + 2 * j]), __uint_as_float(v[8 * i + 2 * j + 1]));
-                            if (PASS == kFwd && p.relu) w32[j] = relu2(w32[j]);
+                        for (int f = 0; f < 2; ++f) {
+                            m[f] = act::pack2_u32(__uint_as_float(lo[4 * g + 2 * f]), __uint_as_float(lo[4 * g + 2 * f + 1]));
+                            m[2 + f] = act::pack2_u32(__uint_as_float(hi[4 * g + 2 * f]), __uint_as_float(hi[4 * g + 2 * f + 1]));
                         }
-                        stage[lane * 4 + (i ^ (lane >> 1 & 3))] = pk;  // in any eight lanes, eight different banks of 16 bytes
+                        if (PASS == kFwd && p.relu) {
+#pragma unroll
+                            for (int f = 0; f < 4; ++f) m[f] = relu2(m[f]);
+                        }
+                        const int token = 8 * g + lane % 8;
+                        store_columns(smem_u32(stage + token * 4 + (lane / 8 ^ (token >> 1 & 3))), m[0], m[1], m[2], m[3]);
                     }
                     __syncwarp();
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        const int r = 8 * i + lane / 4;
-                        uint4 pk = stage[r * 4 + (q ^ (r >> 1 & 3))];
-                        if (PASS == kDgrad && p.mask) {
-                            const uint4 h = gate[ch][i];
-                            pk = make_uint4(pass2(pk.x, h.x), pass2(pk.y, h.y), pass2(pk.z, h.z), pass2(pk.w, h.w));
-                        }
-                        if (r0 + 8 * i < tc.row1 && col + ch * 32 < p.cols)
-                            *reinterpret_cast<uint4*>(o + i * down + ch * 32) = pk;
+                        const int token = 8 * i + lane / 4;
+                        uint4 pk = stage[token * 4 + (q ^ (token >> 1 & 3))];  // in any eight lanes, eight different 16 bytes
+                        if (PASS == kDgrad && p.mask)
+                            pk = make_uint4(pass2(pk.x, h[i].x), pass2(pk.y, h[i].y), pass2(pk.z, h[i].z), pass2(pk.w, h[i].w));
+                        if (r0 + ch * 32 + 8 * i < tc.row1 && col < p.features)
+                            *reinterpret_cast<uint4*>(o + ch * 32 * p.ld + i * down) = pk;
                     }
+                };
+                if constexpr (PASS == kDgrad) {
+#pragma unroll
+                    for (int c = 0; c < 4; ++c)
+                        if (part + 2 * c < chunks) chunk(part + 2 * c, gate[c]);
+                } else {
+#pragma unroll 1
+                    for (int ch = part; ch < chunks; ch += 2) chunk(ch, gate[0]);
                 }
+                release(buf);
                 ++lt;
             }
         }
@@ -458,7 +492,7 @@ __global__ void __launch_bounds__(Cfg<BN>::THREADS, 1)
     cluster_sync_all();
     if (warp == C::MMA_WARP) {
         tc_fence_after();
-        tmem_dealloc_cg<2>(tmem, C::NB * BN);
+        tmem_dealloc_cg<2>(tmem, C::NB * 256);
     }
 }
 
@@ -504,15 +538,15 @@ int encode_weights(CUtensorMap* m, const void* base, const dbl_grouped_shape* s,
     return encode(m, base, 3, dims, strides, box, w);
 }
 
-template <int PASS, int BN>
-int launch(const CUtensorMap& ta, const CUtensorMap& tb, MmaArgs p, int64_t most_tiles, cudaStream_t st, const char* w)
+template <int PASS>
+int launch(const CUtensorMap (&maps)[3], const MmaArgs& p, int64_t most_tiles, cudaStream_t st, const char* w)
 {
-    using C = Cfg<BN>;
-    int rc = allow_launch<grouped_kernel<PASS, BN>>(C::SMEM, false, w);
+    using C = Cfg;
+    int rc = allow_launch<grouped_kernel<PASS>>(C::SMEM, false, w);
     if (rc != DBL_OK) return rc;
     int dev = 0;
     if ((rc = cuda_check(cudaGetDevice(&dev), w)) != DBL_OK) return rc;
-    int pairs = clusters_held<grouped_kernel<PASS, BN>>(dev, 2, C::THREADS, C::SMEM);
+    int pairs = clusters_held<grouped_kernel<PASS>>(dev, 2, C::THREADS, C::SMEM);
     if (pairs < 1) pairs = 1;  // as one pair after the other
     if (pairs > most_tiles) pairs = (int)most_tiles;
     cudaLaunchConfig_t cfg = {};
@@ -526,29 +560,17 @@ int launch(const CUtensorMap& ta, const CUtensorMap& tb, MmaArgs p, int64_t most
     cfg.stream = st;
     cfg.attrs = at;
     cfg.numAttrs = 1;
-    const cudaError_t err = cudaLaunchKernelEx(&cfg, grouped_kernel<PASS, BN>, ta, tb, p);
+    const cudaError_t err = cudaLaunchKernelEx(&cfg, grouped_kernel<PASS>, maps[0], maps[1], maps[2], p);
     rc = launch_check(w);
     return err == cudaSuccess ? rc : cuda_check(err, w);
 }
 
-template <int PASS, int BN>
-int run_tiles(const dbl_grouped_shape* s, const void* a, const void* b, const int32_t* offsets, const void* mask, void* out,
-              int accumulate, cudaStream_t st, const char* w)
+// a: fwd, dgrad: the tokens' rows (x, dy), wgrad: x; b: the weights, wgrad: dy.
+template <int PASS>
+int run(const dbl_grouped_shape* s, const void* a, const void* b, const int32_t* offsets, const void* mask, void* out,
+        int accumulate, void* stream, const char* w)
 {
     const int64_t ld_in = s->ld_in ? s->ld_in : s->n_in, ld_out = s->ld_out ? s->ld_out : s->n_out;
-    CUtensorMap ta, tb;
-    int rc;
-    if (PASS == kFwd) {
-        if ((rc = encode_rows(&ta, a, s->rows, s->n_in, ld_in, 128, w)) != DBL_OK) return rc;
-        rc = encode_weights(&tb, b, s, BN / 2, w);
-    } else if (PASS == kDgrad) {
-        if ((rc = encode_rows(&ta, a, s->rows, s->n_out, ld_out, 128, w)) != DBL_OK) return rc;
-        rc = encode_weights(&tb, b, s, 64, w);
-    } else {
-        if ((rc = encode_rows(&ta, a, s->rows, s->n_in, ld_in, 64, w)) != DBL_OK) return rc;
-        rc = encode_rows(&tb, b, s->rows, s->n_out, ld_out, 64, w);
-    }
-    if (rc != DBL_OK) return rc;
     MmaArgs p = {};
     p.mask = static_cast<const act_t*>(mask);
     p.out = out;
@@ -557,21 +579,26 @@ int run_tiles(const dbl_grouped_shape* s, const void* a, const void* b, const in
     p.ld = PASS == kFwd ? ld_out : ld_in;
     p.groups = s->groups, p.n_in = s->n_in, p.n_out = s->n_out;
     p.relu = s->relu != 0, p.accumulate = accumulate;
-    p.cols = PASS == kDgrad ? s->n_in : s->n_out;
+    p.features = PASS == kDgrad ? s->n_in : s->n_out;
     p.depth = PASS == kFwd ? s->n_in : s->n_out;
-    p.tiles_m = (s->n_in + 255) / 256;
-    p.tiles_n = (p.cols + BN - 1) / BN;
-    // the row blocks are the device's to count: a group's last one is partial
-    const int64_t blocks = PASS == kWgrad ? (int64_t)s->groups * p.tiles_m
-                                          : (s->rows < s->groups ? s->rows : s->rows / 256 + s->groups);
-    return launch<PASS, BN>(ta, tb, p, blocks * p.tiles_n, st, w);
-}
-
-template <int PASS>
-int run(const dbl_grouped_shape* s, const void* a, const void* b, const int32_t* offsets, const void* mask, void* out,
-        int accumulate, void* stream, const char* w)
-{
-    return run_tiles<PASS, 256>(s, a, b, offsets, mask, out, accumulate, as_stream(stream), w);
+    p.blocks_a = ((PASS == kWgrad ? s->n_in : p.features) + 255) / 256;
+    p.blocks_b = (s->n_out + 255) / 256;
+    CUtensorMap maps[3];
+    int rc;
+    if (PASS == kWgrad) {
+        if ((rc = encode_rows(&maps[0], a, s->rows, s->n_in, ld_in, 64, w)) != DBL_OK) return rc;
+        if ((rc = encode_rows(&maps[1], b, s->rows, s->n_out, ld_out, 64, w)) != DBL_OK) return rc;
+        maps[2] = maps[1];
+    } else {
+        const int64_t ld = PASS == kFwd ? ld_in : ld_out;
+        if ((rc = encode_weights(&maps[0], b, s, PASS == kFwd ? 128 : 64, w)) != DBL_OK) return rc;
+        if ((rc = encode_rows(&maps[1], a, s->rows, p.depth, ld, 128, w)) != DBL_OK) return rc;
+        if ((rc = encode_rows(&maps[2], a, s->rows, p.depth, ld, 16, w)) != DBL_OK) return rc;
+    }
+    // the blocks of rows are the device's to count: a group's last one is partial
+    const int64_t tiles = PASS == kWgrad ? (int64_t)s->groups * p.blocks_a * p.blocks_b
+                                         : (s->rows < s->groups ? s->rows : s->rows / 256 + s->groups) * p.blocks_a;
+    return launch<PASS>(maps, p, tiles, as_stream(stream), w);
 }
 
 }  // namespace
