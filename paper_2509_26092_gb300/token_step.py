@@ -10,13 +10,20 @@ The model takes features [n, t, width] (the positions of a feature map, or embed
 one of ``classes`` at every token:
 
     s = features
-    for each layer:  s = s + out.w * scan( in.w * norm(s) )      (x and gate: the halves of in.w's output)
+    for each layer:  s = s + drop( out.w * scan( in.w * norm(s) ) )   (x and gate: the halves of in.w's output)
+        with experts:  s = s + drop( sum_j weight_j * down.w[e_j] * relu( up.w[e_j] * norm(s) ) )
     logits = vocab.w * norm(s)
 
 with layer norm, the gated scan and the distillation loss against a teacher's stored top logits
 (``dbl_layer_norm_*``, ``dbl_gated_scan_*``, ``dbl_distill_fwd_bwd``) and the products as 1x1
-convolutions.  The residual additions run inside the norms, forward and backward.
+convolutions.  A layer of experts (``experts`` of them, ``chosen`` for a token, of ``hidden`` channels) takes
+the largest of router.w * norm(s) with their softmax as weights (``dbl_route_*``), the tokens to their experts'
+rows and back (``dbl_expert_*``) and the products of each expert's rows (``dbl_grouped_*``).  drop is dropout
+(``dbl_dropout_residual``), whose rate cyclic progressive learning raises with the sub-stage; without it the
+residual additions run inside the norms, forward and backward.
 """
+import argparse
+
 import torch
 
 from . import dbl as D
@@ -25,18 +32,31 @@ from .resnet18 import ACT_DTYPE, DualBatchIteration, FlatSpec, ServerState
 
 class TokenSpec(FlatSpec):
     """Parameters of the model: ``width`` channels (a multiple of 64), ``layers``, ``classes`` (any number;
-    stored in rows padded to a multiple of 64, the padding staying zero)."""
+    stored in rows padded to a multiple of 64, the padding staying zero).  ``experts`` > 0: a layer of experts
+    behind each mixing layer, of ``hidden`` channels (a multiple of 8; 0: 4 * width), ``chosen`` for each token."""
 
-    def __init__(self, width=512, layers=2, classes=1000):
+    def __init__(self, width=512, layers=2, classes=1000, experts=0, hidden=0, chosen=2):
         super().__init__()
         if width % 64:
             raise ValueError("width must be a multiple of 64")
+        hidden = hidden or 4 * width
+        if experts and (hidden % 8 or not 1 <= chosen <= min(experts, D.DBL_ROUTE_MAX_K)
+                        or experts > D.DBL_ROUTE_MAX_EXPERTS):
+            raise ValueError(f"a layer of experts has 1 to {D.DBL_ROUTE_MAX_EXPERTS} experts, 1 to "
+                             f"{D.DBL_ROUTE_MAX_K} of them for a token, and a multiple of 8 hidden channels")
         self.width, self.layers, self.classes = width, layers, classes
+        self.experts, self.hidden, self.chosen = experts, hidden, chosen
         self.padded = -(-classes // 64) * 64
+        self.routed = -(-experts // 64) * 64  # the router's output, padded likewise
         for i in range(layers):
             self._norm(f"layer{i}.norm")
             self.add(f"layer{i}.in.w", (2 * width, width), (2 * width, width), width)
             self.add(f"layer{i}.out.w", (width, width), (width, width), width)
+            if experts:
+                self._norm(f"layer{i}.experts.norm")
+                self.add(f"layer{i}.router.w", (self.routed, width), (experts, width), width)
+                self.add(f"layer{i}.up.w", (experts, hidden, width), (experts, hidden, width), width)
+                self.add(f"layer{i}.down.w", (experts, width, hidden), (experts, width, hidden), hidden)
         self._norm("norm")
         self.add("vocab.w", (self.padded, width), (classes, width), width)
 
@@ -48,10 +68,13 @@ class TokenSpec(FlatSpec):
 class TokenWorker:
     """Activations, gradients and scratch of one worker: ``n`` sequences of ``t`` tokens, a teacher of ``k``
     logits per token.  ``lengths`` ([n] int32, all t at first) ends sequences earlier; tokens past them count
-    neither in the loss nor in the states nor, whatever their features hold, in a gradient.  What a step reads
-    (teacher, lengths, labels) is set on the current stream, which the next iteration follows."""
+    neither in the loss nor in the states nor, whatever their features hold, in a gradient, and go to no expert.
+    ``dropout``: the rate of what each layer adds to the stream, its masks drawn from ``seed`` and ``step``, the
+    worker's count of its iterations on the device.  What a step reads (teacher, lengths, labels) is set on the
+    current stream, which the next iteration follows."""
 
-    def __init__(self, spec, n, t, k, temperature=2.0, alpha=0.5, device="cuda", eps=1e-5, precision="bf16"):
+    def __init__(self, spec, n, t, k, temperature=2.0, alpha=0.5, device="cuda", eps=1e-5, precision="bf16",
+                 dropout=0.0, seed=0):
         self.spec, self.batch, self.res, self.k, self.eps, self.precision = spec, n, t, k, eps, precision
         rows, w = n * t, spec.width
         self.rows = rows
@@ -63,6 +86,9 @@ class TokenWorker:
         def vec(m, dtype=torch.float32):
             return torch.zeros(m, dtype=dtype, device=device)
 
+        def entries(c):
+            return torch.zeros((rows * spec.chosen, c), dtype=dt, device=device)
+
         self.norm_shape = D.ln_shape(rows, w, eps)
         self.scan_shape = D.scan_shape(n, t, w, ld_x=2 * w)  # x and gate are the halves of one projection
         self.loss_shape = D.distill_shape(rows, spec.classes, k, temperature, alpha, ld=spec.padded, ld_grad=spec.padded)
@@ -70,11 +96,34 @@ class TokenWorker:
         self.out_shape = D.conv_shape(n, t, 1, w, w, 1, 1, 0)
         self.vocab_shape = D.conv_shape(n, t, 1, w, spec.padded, 1, 1, 0)
         chunks = D.dbl_gated_scan_states_bytes(self.scan_shape) // 4
-        # per layer: the norm's output, the projection, the scan's output, the layer's; s (but the first) and the
-        # norm's statistics; the last entry is the norm before the vocabulary
-        self.layers = [dict(a=act(w), u=act(2 * w), h=act(w), v=act(w), states=vec(chunks), mean=vec(rows),
-                            istd=vec(rows), s=act(w) if i else None) for i in range(spec.layers)]
-        self.last = dict(a=act(w), mean=vec(rows), istd=vec(rows), s=act(w))
+        # what reads the stream, in order; each has the norm's output, s (but the first) and the norm's statistics,
+        # and what it adds to the stream (v); the last is the norm before the vocabulary
+        def block(kind, pre, norm, **more):
+            return dict(kind=kind, pre=pre, norm=norm, a=act(w), v=act(w) if kind else None, mean=vec(rows), istd=vec(rows),
+                        s=act(w) if self.blocks else None, **more)
+
+        self.blocks = []
+        for i in range(spec.layers):
+            self.blocks.append(block("mix", f"layer{i}", f"layer{i}.norm", u=act(2 * w), h=act(w), states=vec(chunks),
+                                     layer=i))
+            if spec.experts:
+                self.blocks.append(block("experts", f"layer{i}", f"layer{i}.experts.norm", r=act(spec.routed),
+                                         chosen=vec(rows * spec.chosen, torch.int32), slots=vec(rows * spec.chosen, torch.int32),
+                                         weights=vec(rows * spec.chosen), offsets=vec(spec.experts + 1, torch.int32),
+                                         xg=entries(w), hg=entries(spec.hidden), yg=entries(w)))
+        self.blocks.append(block(None, None, "norm"))
+        self.last = self.blocks[-1]
+        if spec.experts:
+            self.router_shape = D.conv_shape(n, t, 1, w, spec.routed, 1, 1, 0)
+            self.route_shape = D.route_shape(rows, spec.experts, spec.chosen, True, ld=spec.routed, ld_grad=spec.routed)
+            self.exchange_shape = D.exchange_shape(rows, spec.chosen, w)
+            self.up_shape = D.grouped_shape(rows * spec.chosen, spec.experts, w, spec.hidden, relu=True)
+            self.down_shape = D.grouped_shape(rows * spec.chosen, spec.experts, spec.hidden, w)
+            self.dhg, self.dr, self.dweights = entries(spec.hidden), act(spec.routed), vec(rows * spec.chosen)
+        self.dropout, self.step = float(dropout), torch.zeros(1, dtype=torch.int64, device=device)
+        self.drops = [D.dropout_shape(rows, w, dropout, seed ^ (0x9E3779B97F4A7C15 * (i + 1)))
+                      for i in range(len(self.blocks) - 1)]
+        self.dv = act(w) if self.dropout else None
         self.h_last = torch.zeros((spec.layers, n, w), device=device)
         self.logits = act(spec.padded)  # its gradient takes its place; the padding stays zero
         self.da, self.dh, self.du, self.ds = act(w), act(w), act(2 * w), [act(w), act(w)]
@@ -92,8 +141,12 @@ class TokenWorker:
         need = [D.dbl_layer_norm_workspace_bytes(self.norm_shape),
                 D.dbl_gated_scan_workspace_bytes(self.scan_shape, D.DBL_PASS_FWD),
                 D.dbl_gated_scan_workspace_bytes(self.scan_shape, D.DBL_PASS_DGRAD)]
-        need += [D.dbl_conv_workspace_bytes(s, p) for s in (self.in_shape, self.out_shape, self.vocab_shape)
-                 for p in (D.DBL_PASS_FWD, D.DBL_PASS_DGRAD, D.DBL_PASS_WGRAD)]
+        passes, convs = (D.DBL_PASS_FWD, D.DBL_PASS_DGRAD, D.DBL_PASS_WGRAD), [self.in_shape, self.out_shape, self.vocab_shape]
+        if spec.experts:
+            convs.append(self.router_shape)
+            need.append(D.dbl_route_workspace_bytes(self.route_shape))
+            need += [D.dbl_grouped_workspace_bytes(s, p) for s in (self.up_shape, self.down_shape) for p in passes]
+        need += [D.dbl_conv_workspace_bytes(s, p) for s in convs for p in passes]
         self.ws = torch.empty(int(max(need)) + 256, dtype=torch.uint8, device=device)
 
     def set_teacher(self, logits, classes):
@@ -133,21 +186,30 @@ class TokenWorker:
         gate = lambda u: u.data_ptr() + w * u.element_size()  # the projection's second half
         # ---- forward
         x, v = features, None
-        for i, d in enumerate(self.layers + [self.last]):
-            pre = f"layer{i}.norm" if d is not self.last else "norm"
+        for j, d in enumerate(self.blocks):
+            pre = d["norm"]
+            if v is not None and self.dropout:
+                D.dbl_dropout_residual(self.drops[j - 1], v, x, self.step, d["s"], s)
+                x, v = d["s"], None
             # the stream takes up the layer before (x + v) as the norm reads it
             D.dbl_layer_norm_fwd(norm, x if v is None else v, None if v is None else x, pv(pre + ".g"), pv(pre + ".b"),
                                  None if v is None else d["s"], d["a"], d["mean"], d["istd"], s)
             if v is not None:
                 x = d["s"]
-            d["x"] = x
-            if d is self.last:
-                break
-            D.dbl_conv_fwd(self.in_shape, d["a"], wv(f"layer{i}.in.w"), d["u"], None, None, ws, wsb, s)
-            D.dbl_gated_scan_fwd(self.scan_shape, d["u"], gate(d["u"]), None, self.lengths, d["h"], self.h_last[i],
-                                 d["states"], ws, wsb, s)
-            D.dbl_conv_fwd(self.out_shape, d["h"], wv(f"layer{i}.out.w"), d["v"], None, None, ws, wsb, s)
-            v = d["v"]
+            d["x"], v = x, d["v"]
+            if d["kind"] == "mix":
+                D.dbl_conv_fwd(self.in_shape, d["a"], wv(d["pre"] + ".in.w"), d["u"], None, None, ws, wsb, s)
+                D.dbl_gated_scan_fwd(self.scan_shape, d["u"], gate(d["u"]), None, self.lengths, d["h"],
+                                     self.h_last[d["layer"]], d["states"], ws, wsb, s)
+                D.dbl_conv_fwd(self.out_shape, d["h"], wv(d["pre"] + ".out.w"), v, None, None, ws, wsb, s)
+            elif d["kind"] == "experts":
+                D.dbl_conv_fwd(self.router_shape, d["a"], wv(d["pre"] + ".router.w"), d["r"], None, None, ws, wsb, s)
+                D.dbl_route_fwd(self.route_shape, d["r"], None, self.weight, d["chosen"], d["weights"], d["slots"],
+                                d["offsets"], ws, wsb, s)
+                D.dbl_expert_scatter(self.exchange_shape, d["a"], d["slots"], d["xg"], s)
+                D.dbl_grouped_fwd(self.up_shape, d["xg"], wv(d["pre"] + ".up.w"), d["offsets"], d["hg"], ws, wsb, s)
+                D.dbl_grouped_fwd(self.down_shape, d["hg"], wv(d["pre"] + ".down.w"), d["offsets"], d["yg"], ws, wsb, s)
+                D.dbl_expert_combine(self.exchange_shape, d["yg"], d["slots"], d["weights"], None, v, s)
         D.dbl_conv_fwd(self.vocab_shape, self.last["a"], wv("vocab.w"), self.logits, None, None, ws, wsb, s)
         # ---- loss; the logits' gradient in their place
         D.dbl_distill_fwd_bwd(self.loss_shape, self.logits, self.teacher_logits, self.teacher_classes, self.labels,
@@ -159,27 +221,47 @@ class TokenWorker:
         D.dbl_conv_dgrad(self.vocab_shape, self.logits, wv("vocab.w"), self.da, ws, wsb, s)
         D.dbl_layer_norm_bwd(norm, self.da, None, d["x"], pv("norm.g"), d["mean"], d["istd"], ds, gv("norm.g"),
                              gv("norm.b"), ws, wsb, s)
-        for i in reversed(range(spec.layers)):
-            d, pre, du = self.layers[i], f"layer{i}", self.du
-            D.dbl_conv_wgrad(self.out_shape, d["h"], ds, gv(pre + ".out.w"), False, ws, wsb, s)
-            D.dbl_conv_dgrad(self.out_shape, ds, wv(pre + ".out.w"), self.dh, ws, wsb, s)
-            D.dbl_gated_scan_bwd(self.scan_shape, self.dh, None, d["u"], gate(d["u"]), d["states"], self.lengths, du,
-                                 gate(du), None, ws, wsb, s)
-            D.dbl_conv_wgrad(self.in_shape, d["a"], du, gv(pre + ".in.w"), False, ws, wsb, s)
-            D.dbl_conv_dgrad(self.in_shape, du, wv(pre + ".in.w"), self.da, ws, wsb, s)
+        for j in reversed(range(len(self.blocks) - 1)):
+            d, dv = self.blocks[j], ds
+            pre, du = d["pre"], self.du
+            if self.dropout:
+                dv = self.dv
+                D.dbl_dropout_residual(self.drops[j], ds, None, self.step, dv, s)
+            if d["kind"] == "mix":
+                D.dbl_conv_wgrad(self.out_shape, d["h"], dv, gv(pre + ".out.w"), False, ws, wsb, s)
+                D.dbl_conv_dgrad(self.out_shape, dv, wv(pre + ".out.w"), self.dh, ws, wsb, s)
+                D.dbl_gated_scan_bwd(self.scan_shape, self.dh, None, d["u"], gate(d["u"]), d["states"], self.lengths, du,
+                                     gate(du), None, ws, wsb, s)
+                D.dbl_conv_wgrad(self.in_shape, d["a"], du, gv(pre + ".in.w"), False, ws, wsb, s)
+                D.dbl_conv_dgrad(self.in_shape, du, wv(pre + ".in.w"), self.da, ws, wsb, s)
+            else:
+                # the grouped rows' gradients take the rows' places, but for hg's, which the weights' gradient reads
+                D.dbl_expert_combine_bwd(self.exchange_shape, dv, d["yg"], d["slots"], d["weights"], d["yg"], self.dweights, s)
+                D.dbl_grouped_wgrad(self.down_shape, d["hg"], d["yg"], d["offsets"], gv(pre + ".down.w"), False, ws, wsb, s)
+                D.dbl_grouped_dgrad(self.down_shape, d["yg"], wv(pre + ".down.w"), d["offsets"], d["hg"], self.dhg, ws, wsb, s)
+                D.dbl_grouped_wgrad(self.up_shape, d["xg"], self.dhg, d["offsets"], gv(pre + ".up.w"), False, ws, wsb, s)
+                D.dbl_grouped_dgrad(self.up_shape, self.dhg, wv(pre + ".up.w"), d["offsets"], None, d["xg"], ws, wsb, s)
+                # the router's part of the norm's gradient, then the experts' added to it
+                D.dbl_route_bwd(self.route_shape, d["r"], d["chosen"], d["weights"], self.dweights, self.dr, s)
+                D.dbl_conv_wgrad(self.router_shape, d["a"], self.dr, gv(pre + ".router.w"), False, ws, wsb, s)
+                D.dbl_conv_dgrad(self.router_shape, self.dr, wv(pre + ".router.w"), self.dh, ws, wsb, s)
+                D.dbl_expert_combine(self.exchange_shape, d["xg"], d["slots"], None, self.dh, self.da, s)
             # the gradient of the stream past the norm joins the one through it
             out = self.ds[1] if ds is self.ds[0] else self.ds[0]
-            D.dbl_layer_norm_bwd(norm, self.da, ds, d["x"], pv(pre + ".norm.g"), d["mean"], d["istd"], out,
-                                 gv(pre + ".norm.g"), gv(pre + ".norm.b"), ws, wsb, s)
+            D.dbl_layer_norm_bwd(norm, self.da, ds, d["x"], pv(d["norm"] + ".g"), d["mean"], d["istd"], out,
+                                 gv(d["norm"] + ".g"), gv(d["norm"] + ".b"), ws, wsb, s)
             ds = out
+        if self.dropout:
+            D.dbl_dropout_advance(self.step, s)
         self.dfeatures = ds
 
 
-def demo(iterations=30, precision="bf16", device="cuda"):
+def demo(iterations=30, precision="bf16", device="cuda", experts=0, dropout=0.0):
     """Dual-batch training of a student on a fixed random teacher over three lengths, shortest first: returns
-    the losses (large worker, small worker) of every iteration."""
+    the losses (large worker, small worker) of every iteration.  dropout: the rate at the last length, raised
+    to in three equal steps."""
     gen = torch.Generator(device=device).manual_seed(0)
-    spec, k = TokenSpec(256, 2, 500), 8
+    spec, k = TokenSpec(256, 2, 500, experts, 512), 8
     normal = lambda *shape: torch.randn(shape, device=device, generator=gen)
     params = {e.name: (normal(*e.logical) / e.fan_in ** 0.5 if e.fan_in else
                        torch.ones(e.logical, device=device) if e.name.endswith(".g") else
@@ -187,8 +269,9 @@ def demo(iterations=30, precision="bf16", device="cuda"):
     server = ServerState(spec, params, precision=precision, device=device)
     mix = normal(spec.width, spec.classes) / 4.0
     losses = []
-    for t in (64, 96, 128):
-        workers = [TokenWorker(spec, n, t, k, precision=precision, device=device) for n in (16, 4)]
+    for stage, t in enumerate((64, 96, 128)):
+        workers = [TokenWorker(spec, n, t, k, precision=precision, device=device, dropout=dropout * (stage + 1) / 3,
+                               seed=2 * stage + i) for i, n in enumerate((16, 4))]
         it = DualBatchIteration(server, *workers, t, lr=0.5, f_small=19.0 / 21.0)
         for _ in range(iterations // 3):
             data = []
@@ -204,5 +287,9 @@ def demo(iterations=30, precision="bf16", device="cuda"):
 
 
 if __name__ == "__main__":
-    for i, (large, small) in enumerate(demo()):
+    parser = argparse.ArgumentParser(description="Trains a small model over tokens by two workers.")
+    parser.add_argument("--experts", type=int, default=0, help="experts of the layer behind each mixing layer (0: none)")
+    parser.add_argument("--dropout", type=float, default=0.0, help="rate at the last length")
+    args = parser.parse_args()
+    for i, (large, small) in enumerate(demo(experts=args.experts, dropout=args.dropout)):
         print(f"iteration {i}: loss {large:.4f} (large worker), {small:.4f} (small)")
