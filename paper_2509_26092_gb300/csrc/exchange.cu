@@ -107,47 +107,62 @@ __global__ void __launch_bounds__(256) expert_scatter_kernel(const ExchangeArgs 
     }
 }
 
-// The same; four entries' rows are asked for at a time.
-template <class T, int VB>
-__global__ void __launch_bounds__(256) expert_combine_kernel(const ExchangeArgs a, int rows_per_block)
+// G threads to a row, NC chunks of it to a thread at a time, two entries' rows and the residual's asked for together.
+template <class T, int VB, int G, int NC>
+__global__ void __launch_bounds__(256) expert_combine_kernel(const ExchangeArgs a)
 {
     using V = Chunk<T, VB>;
-    const unsigned chunks = (unsigned)a.c / V::N;
-    const int64_t r0 = (int64_t)blockIdx.x * rows_per_block;
-    const unsigned n = (unsigned)min((int64_t)rows_per_block, a.rows - r0) * chunks;
-    for (unsigned i = threadIdx.x; i < n; i += 256) {
-        const unsigned l = i / chunks, u = (i - l * chunks) * V::N;
-        const int64_t r = r0 + l;
-        float sum[V::N] = {};
-        V res;
-        if (a.b) res.load(static_cast<const T*>(a.b) + r * a.ld_rows + u);
-        for (int j0 = 0; j0 < a.k; j0 += 4) {
-            V y[4] = {};
-            float w[4];
+    const int chunks = a.c / V::N, g = threadIdx.x % G;
+    const int64_t r = (int64_t)blockIdx.x * (256 / G) + threadIdx.x / G;
+    if (r >= a.rows) return;
+    const T* res = a.b ? static_cast<const T*>(a.b) + r * a.ld_rows : nullptr;
+    T* out = static_cast<T*>(a.out) + r * a.ld_rows;
+    for (int c0 = g; c0 < chunks; c0 += G * NC) {
+        V rv[NC];
+        if (res) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
+            for (int i = 0; i < NC; ++i)
+                if (c0 + i * G < chunks) rv[i].load(res + (c0 + i * G) * V::N);
+        }
+        float sum[NC][V::N] = {};
+        for (int j0 = 0; j0 < a.k; j0 += 2) {
+            V y[2][NC] = {};
+            float w[2];
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
                 const bool in = j0 + j < a.k;
                 const int64_t s = in ? slot_of(a, r * a.k + j0 + j) : -1;
                 w[j] = in ? (a.weights ? a.weights[r * a.k + j0 + j] : 1.f) : 0.f;
-                if (s >= 0) y[j].load(static_cast<const T*>(a.a) + s * a.ld_grouped + u);
+                if (s >= 0) {
+                    const T* row = static_cast<const T*>(a.a) + s * a.ld_grouped;
+#pragma unroll
+                    for (int i = 0; i < NC; ++i)
+                        if (c0 + i * G < chunks) y[j][i].load(row + (c0 + i * G) * V::N);
+                }
             }
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                float f[V::N];
-                y[j].get(f);
+            for (int j = 0; j < 2; ++j)
 #pragma unroll
-                for (int e = 0; e < V::N; ++e) sum[e] = fmaf(w[j], f[e], sum[e]);
+                for (int i = 0; i < NC; ++i) {
+                    float f[V::N];
+                    y[j][i].get(f);
+#pragma unroll
+                    for (int e = 0; e < V::N; ++e) sum[i][e] = fmaf(w[j], f[e], sum[i][e]);
+                }
+        }
+#pragma unroll
+        for (int i = 0; i < NC; ++i)
+            if (c0 + i * G < chunks) {
+                if (res) {
+                    float f[V::N];
+                    rv[i].get(f);
+#pragma unroll
+                    for (int e = 0; e < V::N; ++e) sum[i][e] += f[e];
+                }
+                V o;
+                o.put(sum[i]);
+                o.store(out + (c0 + i * G) * V::N);
             }
-        }
-        if (a.b) {
-            float f[V::N];
-            res.get(f);
-#pragma unroll
-            for (int e = 0; e < V::N; ++e) sum[e] += f[e];
-        }
-        V o;
-        o.put(sum);
-        o.store(static_cast<T*>(a.out) + r * a.ld_rows + u);
     }
 }
 
@@ -274,6 +289,24 @@ int block_rows(const ExchangeArgs& a, int chunks)
     return chunks >= per ? 1 : per / chunks;
 }
 
+// Threads to a row and chunks to a thread of the forward pass: rows of up to 8, 32, 64, 128 chunks are held at once.
+template <class T, int VB>
+void launch_combine(const ExchangeArgs& a, cudaStream_t st)
+{
+    const int chunks = a.c / Chunk<T, VB>::N;
+    auto run = [&](auto g, auto nc) {
+        constexpr int G = decltype(g)::value, NC = decltype(nc)::value;
+        expert_combine_kernel<T, VB, G, NC><<<(unsigned)((a.rows + 256 / G - 1) / (256 / G)), 256, 0, st>>>(a);
+    };
+#define DBL_I(n) std::integral_constant<int, n>()
+    if (chunks <= 8) return run(DBL_I(8), DBL_I(1));
+    if (chunks <= 32) return run(DBL_I(32), DBL_I(1));
+    if (chunks <= 64) return run(DBL_I(32), DBL_I(2));
+    if (chunks <= 256) return run(DBL_I(32), DBL_I(4));
+    run(DBL_I(256), DBL_I(2));
+#undef DBL_I
+}
+
 template <class T, int VB>
 void launch_combine_bwd(const ExchangeArgs& a, cudaStream_t st)
 {
@@ -330,11 +363,7 @@ extern "C" int dbl_expert_combine(const dbl_exchange_shape* s, const void* yg, c
     if (!yg || !slots || !out) return set_error(DBL_ERR_INVALID, "%s: yg, slots and out must not be NULL", w);
     const ExchangeArgs a = args(s, yg, res, slots, weights, out, nullptr);
     cudaStream_t st = as_stream(stream);
-    with_chunks(s->dtype, chunk_bytes(a, e), [&](auto type, auto bytes) {
-        using V = Chunk<decltype(type), decltype(bytes)::value>;
-        const int rpb = block_rows(a, a.c / V::N);
-        expert_combine_kernel<decltype(type), decltype(bytes)::value><<<(unsigned)((a.rows + rpb - 1) / rpb), 256, 0, st>>>(a, rpb);
-    });
+    with_chunks(s->dtype, chunk_bytes(a, e), [&](auto type, auto bytes) { launch_combine<decltype(type), decltype(bytes)::value>(a, st); });
     return launch_check(w);
 }
 

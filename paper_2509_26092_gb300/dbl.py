@@ -126,16 +126,19 @@ def lib_path(p=None):
     return build_lib.library_path(p or _precision.get())
 
 
-@contextlib.contextmanager
-def precision(p):
+class precision(contextlib.ContextDecorator):
     """Route the calls made inside the block to the library of storage format p ("bf16" or "f16")."""
-    if p not in PRECISIONS:
-        raise ValueError(f"precision must be one of {PRECISIONS}, not {p!r}")
-    tok = _precision.set(p)
-    try:
-        yield
-    finally:
-        _precision.reset(tok)
+
+    def __init__(self, p):
+        if p not in PRECISIONS:
+            raise ValueError(f"precision must be one of {PRECISIONS}, not {p!r}")
+        self._p, self._tokens = p, []
+
+    def __enter__(self):
+        self._tokens.append(_precision.set(self._p))
+
+    def __exit__(self, *exc):
+        _precision.reset(self._tokens.pop())
 
 
 def current_precision():
