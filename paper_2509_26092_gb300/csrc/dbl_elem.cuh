@@ -108,6 +108,98 @@ __device__ __forceinline__ float block_max(float v, float* red)
     return s;
 }
 
+// Rows that begin at any element, in units of 16 bytes.  A unit that is stored lies on a 16-byte boundary and holds the
+// row's elements from e on (N = 16 / sizeof(T) of them; e may be below 0 in the row's first unit, and the last may reach
+// past its end); a unit that is read for it lies anywhere, put together from the two on boundaries that it covers, of which
+// a lane loads one and takes the other from its neighbour.
+template <class T>
+struct RowOf {
+    const T* row;
+    uintptr_t begin, end, low, high;  // bytes of the row, and of the tensor that it belongs to
+
+    // row r of [rows, c] at stride ld
+    __device__ __forceinline__ RowOf(const void* tensor, int64_t r, int64_t rows, int c, int64_t ld)
+        : row(static_cast<const T*>(tensor) + r * ld), begin(reinterpret_cast<uintptr_t>(row)), end(begin + (size_t)c * sizeof(T)),
+          low(reinterpret_cast<uintptr_t>(tensor)), high(low + ((size_t)(rows - 1) * ld + c) * sizeof(T))
+    {
+    }
+    // The 16 bytes at a boundary: 0 where nothing of the row is in them, by elements where the tensor begins or ends in them.
+    __device__ __forceinline__ uint4 on_boundary(uintptr_t at) const
+    {
+        uint4 v = make_uint4(0, 0, 0, 0);
+        if (at + 16 <= begin || at >= end) return v;
+        if (at >= low && at + 16 <= high) return *reinterpret_cast<const uint4*>(at);
+        uint32_t w[4] = {0, 0, 0, 0};
+#pragma unroll
+        for (int i = 0; i < 16; i += (int)sizeof(T)) {
+            if (at + i < begin || at + i >= end) continue;
+            if constexpr (sizeof(T) == 2)
+                w[i / 4] |= (uint32_t)*reinterpret_cast<const uint16_t*>(at + i) << (8 * (i & 3));
+            else
+                w[i / 4] = *reinterpret_cast<const uint32_t*>(at + i);
+        }
+        return make_uint4(w[0], w[1], w[2], w[3]);
+    }
+    // All lanes of a warp, with e growing by N from lane to lane.
+    __device__ __forceinline__ uint4 from(int e) const
+    {
+        const uintptr_t a = begin + (intptr_t)e * (intptr_t)sizeof(T), at = a & ~(uintptr_t)15;
+        const uint32_t d = (uint32_t)a & 15u;  // the same in all lanes
+        const uint4 v = on_boundary(at);
+        if (d == 0) return v;
+        uint4 n;
+        n.x = __shfl_down_sync(0xffffffffu, v.x, 1);
+        n.y = __shfl_down_sync(0xffffffffu, v.y, 1);
+        n.z = __shfl_down_sync(0xffffffffu, v.z, 1);
+        n.w = __shfl_down_sync(0xffffffffu, v.w, 1);
+        if ((threadIdx.x & 31) == 31) n = on_boundary(at + 16);
+        uint32_t w[8] = {v.x, v.y, v.z, v.w, n.x, n.y, n.z, n.w};
+        if (d & 8) {
+#pragma unroll
+            for (int i = 0; i < 6; ++i) w[i] = w[i + 2];
+        }
+        if (d & 4) {
+#pragma unroll
+            for (int i = 0; i < 5; ++i) w[i] = w[i + 1];
+        }
+        if (sizeof(T) == 2) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) w[i] = __funnelshift_r(w[i], w[i + 1], (d & 2) * 8);
+        }
+        return make_uint4(w[0], w[1], w[2], w[3]);
+    }
+};
+
+// Elements `first` to last - 1 of a unit to the row's from e + first on, those that the row has, one by one.
+template <class T>
+__device__ __forceinline__ void store_part(T* row, int c, int e, uint4 v, int first, int last)
+{
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 16 / (int)sizeof(T); ++i) {
+        if (i < first || i >= last || e + i < 0 || e + i >= c) continue;
+        if constexpr (sizeof(T) == 2)
+            reinterpret_cast<uint16_t*>(row)[e + i] = (uint16_t)(w[i / 2] >> (16 * (i & 1)));
+        else
+            reinterpret_cast<uint32_t*>(row)[e + i] = w[i];
+    }
+}
+
+// A unit to the row's elements from e on, row + e being on a boundary.
+template <class T>
+__device__ __forceinline__ void store_unit(T* row, int c, int e, uint4 v)
+{
+    constexpr int N = 16 / (int)sizeof(T);
+    if (e >= 0 && e + N <= c)
+        *reinterpret_cast<uint4*>(row + e) = v;
+    else
+        store_part(row, c, e, v, 0, N);
+}
+
+// Elements of the unit on a boundary in which a row begins that come before it.
+template <class T>
+__device__ __forceinline__ int unit_lead(const T* row) { return (int)((reinterpret_cast<uintptr_t>(row) & 15u) / sizeof(T)); }
+
 // From a 16-byte boundary to one, a multiple of 16 bytes; counted on the barrier.
 __device__ __forceinline__ void bulk_load(uint32_t dst, uintptr_t src, uint32_t bytes, uint64_t* bar)
 {

@@ -43,7 +43,34 @@ __device__ __forceinline__ float dropped(const DropArgs& a, uint32_t word, float
     return fmaf(word >= a.threshold ? x : 0.f, a.scale, res);
 }
 
-// Sixteen bytes of a row to a thread, two blocks of the generator (fp32: one), rows_per_block rows to a block.
+// Sixteen bytes of row r from channel `col` on, a multiple of four: two blocks of the generator, fp32 one.
+template <class T>
+__device__ __forceinline__ uint4 unit(const DropArgs& a, uint64_t step, int64_t r, unsigned col, uint4 xv, uint4 rv)
+{
+    constexpr int N = 16 / (int)sizeof(T);
+    const uint32_t x[4] = {xv.x, xv.y, xv.z, xv.w}, res[4] = {rv.x, rv.y, rv.z, rv.w};
+    const uint64_t first = (uint64_t)r * (((unsigned)a.c + 3) / 4) + col / 4;
+    uint32_t y[4];
+#pragma unroll
+    for (int b = 0; b < N / 4; ++b) {
+        uint32_t w[4];
+        philox(first + b, step, a.key0, a.key1, w);
+        if constexpr (sizeof(T) == 4) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                y[e] = __float_as_uint(dropped<T>(a, w[e], __uint_as_float(x[e]), __uint_as_float(res[e])));
+        } else {
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const float2 f = act::unpack2_u32(x[2 * b + e]), g = act::unpack2_u32(res[2 * b + e]);
+                y[2 * b + e] = act::pack2_u32(dropped<T>(a, w[2 * e], f.x, g.x), dropped<T>(a, w[2 * e + 1], f.y, g.y));
+            }
+        }
+    }
+    return make_uint4(y[0], y[1], y[2], y[3]);
+}
+
+// Rows of a multiple of 16 bytes at 16-byte addresses: a unit to a thread, rows_per_block rows to a block.
 template <class T>
 __global__ void __launch_bounds__(256) dropout_kernel(const DropArgs a, int rows_per_block)
 {
@@ -53,35 +80,34 @@ __global__ void __launch_bounds__(256) dropout_kernel(const DropArgs a, int rows
     const unsigned n = (unsigned)min((int64_t)rows_per_block, a.rows - r0) * units;
     const uint64_t step = *a.step;
     for (unsigned i = threadIdx.x; i < n; i += 256) {
-        const unsigned l = i / units, u = i - l * units;
-        const int64_t r = r0 + l, in = r * a.ld_in + u * N, out = r * a.ld_out + u * N;
-        const uint4 xv = *reinterpret_cast<const uint4*>(static_cast<const T*>(a.x) + in);
-        uint4 rv = make_uint4(0, 0, 0, 0);
-        if (a.res) rv = *reinterpret_cast<const uint4*>(static_cast<const T*>(a.res) + in);
-        const uint32_t x[4] = {xv.x, xv.y, xv.z, xv.w}, res[4] = {rv.x, rv.y, rv.z, rv.w};
-        uint32_t y[4];
-#pragma unroll
-        for (int b = 0; b < N / 4; ++b) {
-            uint32_t w[4];
-            philox((uint64_t)r * ((unsigned)a.c / 4) + (u * (N / 4) + b), step, a.key0, a.key1, w);
-            if constexpr (sizeof(T) == 4) {
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    y[e] = __float_as_uint(dropped<T>(a, w[e], __uint_as_float(x[e]), __uint_as_float(res[e])));
-            } else {
-#pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    const float2 f = act::unpack2_u32(x[2 * b + e]), g = act::unpack2_u32(res[2 * b + e]);
-                    y[2 * b + e] = act::pack2_u32(dropped<T>(a, w[2 * e], f.x, g.x), dropped<T>(a, w[2 * e + 1], f.y, g.y));
-                }
-            }
-        }
-        *reinterpret_cast<uint4*>(static_cast<T*>(a.y) + out) = make_uint4(y[0], y[1], y[2], y[3]);
+        const unsigned l = i / units, col = (i - l * units) * N;
+        const int64_t r = r0 + l, in = r * a.ld_in + col;
+        const uint4 x = *reinterpret_cast<const uint4*>(static_cast<const T*>(a.x) + in);
+        uint4 res = make_uint4(0, 0, 0, 0);
+        if (a.res) res = *reinterpret_cast<const uint4*>(static_cast<const T*>(a.res) + in);
+        *reinterpret_cast<uint4*>(static_cast<T*>(a.y) + r * a.ld_out + col) = unit<T>(a, step, r, col, x, res);
     }
 }
 
-// Rows of any length and alignment: a block of the generator, four channels, to a thread.
-template <class T>
+// Eight bytes in accesses of W.
+template <int W>
+__device__ __forceinline__ uint2 load8(const void* p)
+{
+    if (W == 8) return *static_cast<const uint2*>(p);
+    return make_uint2(static_cast<const uint32_t*>(p)[0], static_cast<const uint32_t*>(p)[1]);
+}
+template <int W>
+__device__ __forceinline__ void store8(void* p, uint2 v)
+{
+    if (W == 8)
+        *static_cast<uint2*>(p) = v;
+    else
+        static_cast<uint32_t*>(p)[0] = v.x, static_cast<uint32_t*>(p)[1] = v.y;
+}
+
+// Rows of any length and alignment: a block of the generator, four channels, to a thread.  60000 rows of 1001 with the residual
+// 89 us; units on boundaries put together by shuffles 145, a choice of accesses for each row 107.
+template <class T, int W>
 __global__ void __launch_bounds__(256) dropout_any_kernel(const DropArgs a, int rows_per_block)
 {
     const unsigned per = ((unsigned)a.c + 3) / 4;
@@ -89,23 +115,30 @@ __global__ void __launch_bounds__(256) dropout_any_kernel(const DropArgs a, int 
     const unsigned n = (unsigned)min((int64_t)rows_per_block, a.rows - r0) * per;
     const uint64_t step = *a.step;
     for (unsigned i = threadIdx.x; i < n; i += 256) {
-        const unsigned l = i / per, col = (i - l * per) * 4;
-        const int64_t r = r0 + l;
-        const T* x = static_cast<const T*>(a.x) + r * a.ld_in + col;
-        const T* res = a.res ? static_cast<const T*>(a.res) + r * a.ld_in + col : nullptr;
+        const unsigned l = i / per, col = (i - l * per) * 4, left = (unsigned)a.c - col;
+        const int64_t r = r0 + l, in = r * a.ld_in + col;
+        const T *x = static_cast<const T*>(a.x) + in, *res = static_cast<const T*>(a.res) + in;
         T* y = static_cast<T*>(a.y) + r * a.ld_out + col;
+        uint32_t w[4];
+        if (W > (int)sizeof(T) && left >= 4) {
+            const uint2 xv = load8<W>(x), rv = a.res ? load8<W>(res) : make_uint2(0, 0);
+            philox((uint64_t)r * per + col / 4, step, a.key0, a.key1, w);
+            const float2 x0 = act::unpack2_u32(xv.x), x1 = act::unpack2_u32(xv.y);
+            const float2 g0 = act::unpack2_u32(rv.x), g1 = act::unpack2_u32(rv.y);
+            store8<W>(y, make_uint2(act::pack2_u32(dropped<T>(a, w[0], x0.x, g0.x), dropped<T>(a, w[1], x0.y, g0.y)),
+                                    act::pack2_u32(dropped<T>(a, w[2], x1.x, g1.x), dropped<T>(a, w[3], x1.y, g1.y))));
+            continue;
+        }
         float f[4], g[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const bool in = col + e < (unsigned)a.c;
-            f[e] = in ? elem_f(x[e]) : 0.f;
-            g[e] = in && res ? elem_f(res[e]) : 0.f;
+        for (unsigned e = 0; e < 4; ++e) {
+            f[e] = e < left ? elem_f(x[e]) : 0.f;
+            g[e] = e < left && a.res ? elem_f(res[e]) : 0.f;
         }
-        uint32_t w[4];
         philox((uint64_t)r * per + col / 4, step, a.key0, a.key1, w);
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (col + e < (unsigned)a.c) y[e] = elem_from<T>(dropped<T>(a, w[e], f[e], g[e]));
+        for (unsigned e = 0; e < 4; ++e)
+            if (e < left) y[e] = elem_from<T>(dropped<T>(a, w[e], f[e], g[e]));
     }
 }
 
@@ -123,8 +156,12 @@ int launch(const DropArgs& a, cudaStream_t st, const char* what)
     const unsigned blocks = (unsigned)((a.rows + rpb - 1) / rpb);
     if (wide)
         dropout_kernel<T><<<blocks, 256, 0, st>>>(a, rpb);
+    else if (sizeof(T) == 4 || (bits & 3))
+        dropout_any_kernel<T, (int)sizeof(T)><<<blocks, 256, 0, st>>>(a, rpb);
+    else if (bits & 7)
+        dropout_any_kernel<T, 4><<<blocks, 256, 0, st>>>(a, rpb);
     else
-        dropout_any_kernel<T><<<blocks, 256, 0, st>>>(a, rpb);
+        dropout_any_kernel<T, 8><<<blocks, 256, 0, st>>>(a, rpb);
     return launch_check(what);
 }
 

@@ -26,72 +26,55 @@ __device__ __forceinline__ int64_t slot_of(const ExchangeArgs& a, int64_t entry)
     return s >= 0 && s < a.grouped_rows ? s : -1;
 }
 
-// VB bytes of a row, the most that all rows' addresses and lengths allow: 16, or 8, 4, 2.
-template <class T, int VB>
+// Sixteen bytes of a row, or one element.
+template <class T, bool WIDE = true>
 struct Chunk {
-    static constexpr int N = VB / (int)sizeof(T);
-    static constexpr int W = VB < 4 ? 1 : VB / 4;
-    uint32_t w[W];
+    static constexpr int N = 16 / (int)sizeof(T);
+    uint4 v;
 
-    __device__ __forceinline__ void load(const T* p)
-    {
-        if constexpr (VB == 16) {
-            const uint4 v = *reinterpret_cast<const uint4*>(p);
-            w[0] = v.x, w[1] = v.y, w[2] = v.z, w[3] = v.w;
-        } else if constexpr (VB == 8) {
-            const uint2 v = *reinterpret_cast<const uint2*>(p);
-            w[0] = v.x, w[1] = v.y;
-        } else if constexpr (VB == 4) {
-            w[0] = *reinterpret_cast<const uint32_t*>(p);
-        } else {
-            w[0] = *reinterpret_cast<const uint16_t*>(p);
-        }
-    }
-    __device__ __forceinline__ void store(T* p) const
-    {
-        if constexpr (VB == 16)
-            *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
-        else if constexpr (VB == 8)
-            *reinterpret_cast<uint2*>(p) = make_uint2(w[0], w[1]);
-        else if constexpr (VB == 4)
-            *reinterpret_cast<uint32_t*>(p) = w[0];
-        else
-            *reinterpret_cast<uint16_t*>(p) = (uint16_t)w[0];
-    }
+    __device__ __forceinline__ void load(const T* p) { v = *reinterpret_cast<const uint4*>(p); }
+    __device__ __forceinline__ void store(T* p) const { *reinterpret_cast<uint4*>(p) = v; }
     __device__ __forceinline__ void get(float (&f)[N]) const
     {
-        if constexpr (sizeof(T) == 4) {
+        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-            for (int i = 0; i < N; ++i) f[i] = __uint_as_float(w[i]);
-        } else if constexpr (VB == 2) {
-            f[0] = act::unpack2_u32(w[0]).x;
-        } else {
-#pragma unroll
-            for (int i = 0; i < W; ++i) {
-                const float2 v = act::unpack2_u32(w[i]);
-                f[2 * i] = v.x, f[2 * i + 1] = v.y;
+        for (int i = 0; i < 4; ++i)
+            if constexpr (sizeof(T) == 4) {
+                f[i] = __uint_as_float(w[i]);
+            } else {
+                const float2 t = act::unpack2_u32(w[i]);
+                f[2 * i] = t.x, f[2 * i + 1] = t.y;
             }
-        }
     }
     __device__ __forceinline__ void put(const float (&f)[N])
     {
-        if constexpr (sizeof(T) == 4) {
+        uint32_t w[4];
 #pragma unroll
-            for (int i = 0; i < N; ++i) w[i] = __float_as_uint(f[i]);
-        } else if constexpr (VB == 2) {
-            w[0] = act::pack2_u32(f[0], 0.f);
-        } else {
-#pragma unroll
-            for (int i = 0; i < W; ++i) w[i] = act::pack2_u32(f[2 * i], f[2 * i + 1]);
-        }
+        for (int i = 0; i < 4; ++i)
+            if constexpr (sizeof(T) == 4)
+                w[i] = __float_as_uint(f[i]);
+            else
+                w[i] = act::pack2_u32(f[2 * i], f[2 * i + 1]);
+        v = make_uint4(w[0], w[1], w[2], w[3]);
     }
 };
 
+template <class T>
+struct Chunk<T, false> {
+    static constexpr int N = 1;
+    T v = elem_from<T>(0.f);
+
+    __device__ __forceinline__ void load(const T* p) { v = *p; }
+    __device__ __forceinline__ void store(T* p) const { *p = v; }
+    __device__ __forceinline__ void get(float (&f)[1]) const { f[0] = elem_f(v); }
+    __device__ __forceinline__ void put(const float (&f)[1]) { v = elem_from<T>(f[0]); }
+};
+
 // A thread to a chunk of a row, rows_per_block rows to a block.
-template <class T, int VB>
+template <class T, bool WIDE>
 __global__ void __launch_bounds__(256) expert_scatter_kernel(const ExchangeArgs a, int rows_per_block)
 {
-    using V = Chunk<T, VB>;
+    using V = Chunk<T, WIDE>;
     const unsigned chunks = (unsigned)a.c / V::N;
     const int64_t r0 = (int64_t)blockIdx.x * rows_per_block;
     const unsigned n = (unsigned)min((int64_t)rows_per_block, a.rows - r0) * chunks;
@@ -108,10 +91,10 @@ __global__ void __launch_bounds__(256) expert_scatter_kernel(const ExchangeArgs 
 }
 
 // G threads to a row, NC chunks of it to a thread at a time, two entries' rows and the residual's asked for together.
-template <class T, int VB, int G, int NC>
+template <class T, bool WIDE, int G, int NC>
 __global__ void __launch_bounds__(256) expert_combine_kernel(const ExchangeArgs a)
 {
-    using V = Chunk<T, VB>;
+    using V = Chunk<T, WIDE>;
     const int chunks = a.c / V::N, g = threadIdx.x % G;
     const int64_t r = (int64_t)blockIdx.x * (256 / G) + threadIdx.x / G;
     if (r >= a.rows) return;
@@ -126,7 +109,7 @@ __global__ void __launch_bounds__(256) expert_combine_kernel(const ExchangeArgs 
         }
         float sum[NC][V::N] = {};
         for (int j0 = 0; j0 < a.k; j0 += 2) {
-            V y[2][NC] = {};
+            V y[2][NC] = {};  // zeros where an entry is absent
             float w[2];
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
@@ -167,10 +150,10 @@ __global__ void __launch_bounds__(256) expert_combine_kernel(const ExchangeArgs 
 }
 
 // G threads to a row, NC chunks of it to a thread, kept while the entries pass (NC = 0: any number, read again for each).
-template <class T, int VB, int G, int NC>
+template <class T, bool WIDE, int G, int NC>
 __global__ void __launch_bounds__(256) expert_combine_bwd_kernel(const ExchangeArgs a)
 {
-    using V = Chunk<T, VB>;
+    using V = Chunk<T, WIDE>;
     constexpr int HELD = NC ? NC : 1;
     __shared__ float red[32];
     const int chunks = a.c / V::N, g = threadIdx.x % G;
@@ -236,6 +219,114 @@ __global__ void __launch_bounds__(256) expert_combine_bwd_kernel(const ExchangeA
     }
 }
 
+// The same for long rows that begin anywhere: a warp to a part of a row, kPart units of it.
+constexpr int kPart = 128;
+
+template <class T>
+__device__ __forceinline__ RowOf<T> token_row(const ExchangeArgs& a, const void* p, int64_t r) { return {p, r, a.rows, a.c, a.ld_rows}; }
+template <class T>
+__device__ __forceinline__ RowOf<T> grouped_row(const ExchangeArgs& a, const void* p, int64_t s) { return {p, s, a.grouped_rows, a.c, a.ld_grouped}; }
+
+template <class T>
+__global__ void __launch_bounds__(256) expert_scatter_any_kernel(const ExchangeArgs a, int parts)
+{
+    constexpr int N = Chunk<T>::N;
+    const int lane = threadIdx.x & 31;
+    const int64_t item = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5), r = item / parts;
+    const int part = (int)(item - r * parts);
+    if (r >= a.rows) return;
+    const RowOf<T> x = token_row<T>(a, a.a, r);
+    for (int j = 0; j < a.k; ++j) {
+        const int64_t s = slot_of(a, r * a.k + j);
+        if (s < 0) continue;
+        T* o = static_cast<T*>(a.out) + s * a.ld_grouped;
+        const int lead = unit_lead(o), units = (a.c + lead + N - 1) / N, end = min(units, (part + 1) * kPart);
+        for (int u0 = part * kPart; u0 < end; u0 += 32) {
+            const int e = (u0 + lane) * N - lead;
+            const uint4 v = x.from(e);
+            if (u0 + lane < end) store_unit(o, a.c, e, v);
+        }
+    }
+}
+
+template <class T>
+__global__ void __launch_bounds__(256) expert_combine_any_kernel(const ExchangeArgs a, int parts)
+{
+    constexpr int N = Chunk<T>::N;
+    const int lane = threadIdx.x & 31;
+    const int64_t item = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5), r = item / parts;
+    const int part = (int)(item - r * parts);
+    if (r >= a.rows) return;
+    T* o = static_cast<T*>(a.out) + r * a.ld_rows;
+    const int lead = unit_lead(o), units = (a.c + lead + N - 1) / N, end = min(units, (part + 1) * kPart);
+    for (int u0 = part * kPart; u0 < end; u0 += 32) {
+        const int e = (u0 + lane) * N - lead;
+        float sum[N] = {}, f[N];
+        for (int j = 0; j < a.k; ++j) {
+            const int64_t s = slot_of(a, r * a.k + j);
+            const float w = a.weights ? a.weights[r * a.k + j] : 1.f;
+            Chunk<T> y = {};
+            if (s >= 0) y.v = grouped_row<T>(a, a.a, s).from(e);
+            y.get(f);
+#pragma unroll
+            for (int i = 0; i < N; ++i) sum[i] = fmaf(w, f[i], sum[i]);
+        }
+        Chunk<T> t;
+        if (a.b) {
+            t.v = token_row<T>(a, a.b, r).from(e);
+            t.get(f);
+#pragma unroll
+            for (int i = 0; i < N; ++i) sum[i] += f[i];
+        }
+        t.put(sum);
+        if (u0 + lane < end) store_unit(o, a.c, e, t.v);
+    }
+}
+
+// G threads to a row.
+template <class T, int G>
+__global__ void __launch_bounds__(256) expert_combine_bwd_any_kernel(const ExchangeArgs a)
+{
+    constexpr int N = Chunk<T>::N;
+    __shared__ float red[32];
+    const int lane = threadIdx.x & 31, warp = (threadIdx.x % G) >> 5;
+    const int64_t r = (int64_t)blockIdx.x * (256 / G) + threadIdx.x / G;
+    if (r >= a.rows) return;
+    const RowOf<T> d = token_row<T>(a, a.a, r);
+    for (int j = 0; j < a.k; ++j) {
+        const int64_t s = slot_of(a, r * a.k + j);
+        float dot = 0.f;
+        if (s >= 0) {
+            const float w = a.weights ? a.weights[r * a.k + j] : 1.f;
+            T* o = static_cast<T*>(a.out) + s * a.ld_grouped;
+            const RowOf<T> y = grouped_row<T>(a, a.dweights ? a.b : a.out, s);
+            const int lead = unit_lead(o), units = (a.c + lead + N - 1) / N;
+            for (int u0 = warp * 32; u0 < units; u0 += G) {
+                const int e = (u0 + lane) * N - lead;
+                Chunk<T> dv, yv;
+                float f[N], h[N];
+                dv.v = d.from(e);
+                dv.get(f);
+                if (a.dweights) {
+                    yv.v = y.from(e);
+                    yv.get(h);
+                    // a row's first and last unit hold what is outside it
+#pragma unroll
+                    for (int i = 0; i < N; ++i)
+                        if (e + i >= 0 && e + i < a.c) dot = fmaf(f[i], h[i], dot);
+                }
+#pragma unroll
+                for (int i = 0; i < N; ++i) f[i] *= w;
+                dv.put(f);
+                if (u0 + lane < units) store_unit(o, a.c, e, dv.v);
+            }
+        }
+        if (!a.dweights) continue;
+        dot = G == 256 ? block_sum(dot, red) : warp_sum(dot);
+        if (threadIdx.x % G == 0) a.dweights[r * a.k + j] = dot;
+    }
+}
+
 int check(const dbl_exchange_shape* s, const char* w)
 {
     if (!s || s->rows < 0 || s->k <= 0 || s->c <= 0 || s->grouped_rows < 0)
@@ -256,31 +347,23 @@ ExchangeArgs args(const dbl_exchange_shape* s, const void* a, const void* b, con
             s->ld_rows ? s->ld_rows : s->c, s->ld_grouped ? s->ld_grouped : s->c, s->k, s->c};
 }
 
-// The bytes of a chunk: what the rows' addresses, strides and length have in common.
-int chunk_bytes(const ExchangeArgs& a, size_t e)
+// How the rows are taken: in chunks of 16 bytes where all are of a multiple of them at 16-byte addresses; else element by
+// element where they are short (30000 rows of 70 elements, two entries: combine 17 us by units, as a warp has a row, 7 so),
+// or in units put together (8000 rows of 1001, four entries: scatter 32 us by elements, 21 so, the gradients 68 and 52).
+enum Way { kChunks, kElements, kUnits };
+Way way_of(const ExchangeArgs& a, size_t e)
 {
     uintptr_t bits = reinterpret_cast<uintptr_t>(a.a) | reinterpret_cast<uintptr_t>(a.b) | reinterpret_cast<uintptr_t>(a.out);
     bits |= (uintptr_t)a.c * e | (uintptr_t)a.ld_rows * e | (uintptr_t)a.ld_grouped * e;
-    return bits & 1 ? 1 : bits & 2 ? 2 : bits & 4 ? 4 : bits & 8 ? 8 : 16;
+    return (bits & 15) == 0 ? kChunks : a.c * e < 512 ? kElements : kUnits;
 }
 
-// f(element type, chunk bytes), both as values of their types.
-template <class F>
-void with_chunks(int dtype, int bytes, F f)
-{
-    if (dtype == DBL_F32) {
-        if (bytes == 16) f(0.f, std::integral_constant<int, 16>());
-        else if (bytes == 8) f(0.f, std::integral_constant<int, 8>());
-        else f(0.f, std::integral_constant<int, 4>());
-    } else {
-        if (bytes == 16) f(act_t(), std::integral_constant<int, 16>());
-        else if (bytes == 8) f(act_t(), std::integral_constant<int, 8>());
-        else if (bytes == 4) f(act_t(), std::integral_constant<int, 4>());
-        else f(act_t(), std::integral_constant<int, 2>());
-    }
-}
+// Parts of a row that begins anywhere, and the blocks of eight warps that take them.
+template <class T>
+int row_parts(const ExchangeArgs& a) { return ((a.c + 2 * (Chunk<T>::N - 1)) / Chunk<T>::N + kPart - 1) / kPart; }
+unsigned part_blocks(const ExchangeArgs& a, int parts) { return (unsigned)((a.rows * parts + 7) / 8); }
 
-// Rows of a block of the kernels that have a thread for a chunk: four chunks to a thread where there are many rows, one where
+// Rows of a block of the kernel that has a thread for a chunk: four chunks to a thread where there are many rows, one where
 // there are few.
 int block_rows(const ExchangeArgs& a, int chunks)
 {
@@ -289,42 +372,80 @@ int block_rows(const ExchangeArgs& a, int chunks)
     return chunks >= per ? 1 : per / chunks;
 }
 
+template <class T>
+void launch_scatter(const ExchangeArgs& a, cudaStream_t st)
+{
+    const Way way = way_of(a, sizeof(T));
+    if (way == kUnits) {
+        const int parts = row_parts<T>(a);
+        expert_scatter_any_kernel<T><<<part_blocks(a, parts), 256, 0, st>>>(a, parts);
+        return;
+    }
+    const int rpb = block_rows(a, way == kChunks ? a.c / Chunk<T>::N : a.c);
+    const unsigned blocks = (unsigned)((a.rows + rpb - 1) / rpb);
+    if (way == kChunks)
+        expert_scatter_kernel<T, true><<<blocks, 256, 0, st>>>(a, rpb);
+    else
+        expert_scatter_kernel<T, false><<<blocks, 256, 0, st>>>(a, rpb);
+}
+
 // Threads to a row and chunks to a thread of the forward pass: rows of up to 8, 32, 64, 128 chunks are held at once.
-template <class T, int VB>
+template <class T>
 void launch_combine(const ExchangeArgs& a, cudaStream_t st)
 {
-    const int chunks = a.c / Chunk<T, VB>::N;
-    auto run = [&](auto g, auto nc) {
+    const Way way = way_of(a, sizeof(T));
+    if (way == kUnits) {
+        const int parts = row_parts<T>(a);
+        expert_combine_any_kernel<T><<<part_blocks(a, parts), 256, 0, st>>>(a, parts);
+        return;
+    }
+    auto run = [&](auto wide, auto g, auto nc) {
+        constexpr bool WIDE = decltype(wide)::value;
         constexpr int G = decltype(g)::value, NC = decltype(nc)::value;
-        expert_combine_kernel<T, VB, G, NC><<<(unsigned)((a.rows + 256 / G - 1) / (256 / G)), 256, 0, st>>>(a);
+        expert_combine_kernel<T, WIDE, G, NC><<<(unsigned)((a.rows + 256 / G - 1) / (256 / G)), 256, 0, st>>>(a);
     };
 #define DBL_I(n) std::integral_constant<int, n>()
-    if (chunks <= 8) return run(DBL_I(8), DBL_I(1));
-    if (chunks <= 32) return run(DBL_I(32), DBL_I(1));
-    if (chunks <= 64) return run(DBL_I(32), DBL_I(2));
-    if (chunks <= 256) return run(DBL_I(32), DBL_I(4));
-    run(DBL_I(256), DBL_I(2));
+    if (way == kElements)
+        return a.c <= 16 ? run(std::false_type(), DBL_I(8), DBL_I(2)) : run(std::false_type(), DBL_I(32), DBL_I(4));
+    const std::true_type wide;
+    const int chunks = a.c / Chunk<T>::N;
+    if (chunks <= 8) return run(wide, DBL_I(8), DBL_I(1));
+    if (chunks <= 32) return run(wide, DBL_I(32), DBL_I(1));
+    if (chunks <= 64) return run(wide, DBL_I(32), DBL_I(2));
+    if (chunks <= 256) return run(wide, DBL_I(32), DBL_I(4));
+    run(wide, DBL_I(256), DBL_I(2));
 #undef DBL_I
 }
 
-template <class T, int VB>
+template <class T>
 void launch_combine_bwd(const ExchangeArgs& a, cudaStream_t st)
 {
-    const int chunks = a.c / Chunk<T, VB>::N;
-    auto run = [&](auto g, auto nc) {
+    const Way way = way_of(a, sizeof(T));
+    if (way == kUnits) {
+        if (a.c / Chunk<T>::N > 512)
+            expert_combine_bwd_any_kernel<T, 256><<<(unsigned)a.rows, 256, 0, st>>>(a);
+        else
+            expert_combine_bwd_any_kernel<T, 32><<<(unsigned)((a.rows + 7) / 8), 256, 0, st>>>(a);
+        return;
+    }
+    auto run = [&](auto wide, auto g, auto nc) {
+        constexpr bool WIDE = decltype(wide)::value;
         constexpr int G = decltype(g)::value, NC = decltype(nc)::value;
-        expert_combine_bwd_kernel<T, VB, G, NC><<<(unsigned)((a.rows + 256 / G - 1) / (256 / G)), 256, 0, st>>>(a);
+        expert_combine_bwd_kernel<T, WIDE, G, NC><<<(unsigned)((a.rows + 256 / G - 1) / (256 / G)), 256, 0, st>>>(a);
     };
 #define DBL_I(n) std::integral_constant<int, n>()
-    if (VB < 16 && chunks > 32) return chunks > 512 ? run(DBL_I(256), DBL_I(0)) : run(DBL_I(32), DBL_I(0));
-    if (chunks <= 8) return run(DBL_I(8), DBL_I(1));
-    if (chunks <= 16) return run(DBL_I(8), DBL_I(2));
-    if (chunks <= 32) return run(DBL_I(32), DBL_I(1));
-    if (chunks <= 64) return run(DBL_I(32), DBL_I(2));
-    if (chunks <= 128) return run(DBL_I(32), DBL_I(4));
-    if (chunks <= 512) return run(DBL_I(256), DBL_I(2));
-    if (chunks <= 1024) return run(DBL_I(256), DBL_I(4));
-    run(DBL_I(256), DBL_I(0));
+    if (way == kElements)
+        return a.c <= 16 ? run(std::false_type(), DBL_I(8), DBL_I(2)) : run(std::false_type(), DBL_I(32), DBL_I(8));
+    const std::true_type wide;
+    const int chunks = a.c / Chunk<T>::N;
+    if (chunks <= 8) return run(wide, DBL_I(8), DBL_I(1));
+    if (chunks <= 16) return run(wide, DBL_I(8), DBL_I(2));
+    if (chunks <= 32) return run(wide, DBL_I(32), DBL_I(1));
+    if (chunks <= 64) return run(wide, DBL_I(32), DBL_I(2));
+    if (chunks <= 128) return run(wide, DBL_I(32), DBL_I(4));
+    if (chunks <= 512) return run(wide, DBL_I(256), DBL_I(2));
+    if (chunks <= 1024) return run(wide, DBL_I(256), DBL_I(4));
+    run(wide, DBL_I(256), DBL_I(0));
 #undef DBL_I
 }
 
@@ -342,11 +463,7 @@ extern "C" int dbl_expert_scatter(const dbl_exchange_shape* s, const void* x, co
     if (!x || !slots || !xg) return set_error(DBL_ERR_INVALID, "%s: x, slots and xg must not be NULL", w);
     const ExchangeArgs a = args(s, x, nullptr, slots, nullptr, xg, nullptr);
     cudaStream_t st = as_stream(stream);
-    with_chunks(s->dtype, chunk_bytes(a, e), [&](auto type, auto bytes) {
-        using V = Chunk<decltype(type), decltype(bytes)::value>;
-        const int rpb = block_rows(a, a.c / V::N);
-        expert_scatter_kernel<decltype(type), decltype(bytes)::value><<<(unsigned)((a.rows + rpb - 1) / rpb), 256, 0, st>>>(a, rpb);
-    });
+    s->dtype == DBL_F32 ? launch_scatter<float>(a, st) : launch_scatter<act_t>(a, st);
     return launch_check(w);
 }
 
@@ -363,7 +480,7 @@ extern "C" int dbl_expert_combine(const dbl_exchange_shape* s, const void* yg, c
     if (!yg || !slots || !out) return set_error(DBL_ERR_INVALID, "%s: yg, slots and out must not be NULL", w);
     const ExchangeArgs a = args(s, yg, res, slots, weights, out, nullptr);
     cudaStream_t st = as_stream(stream);
-    with_chunks(s->dtype, chunk_bytes(a, e), [&](auto type, auto bytes) { launch_combine<decltype(type), decltype(bytes)::value>(a, st); });
+    s->dtype == DBL_F32 ? launch_combine<float>(a, st) : launch_combine<act_t>(a, st);
     return launch_check(w);
 }
 
@@ -382,6 +499,6 @@ extern "C" int dbl_expert_combine_bwd(const dbl_exchange_shape* s, const void* d
         return set_error(DBL_ERR_INVALID, "%s: dout, slots and dyg must not be NULL, nor yg with dweights", w);
     const ExchangeArgs a = args(s, dout, yg, slots, weights, dyg, dweights);
     cudaStream_t st = as_stream(stream);
-    with_chunks(s->dtype, chunk_bytes(a, e), [&](auto type, auto bytes) { launch_combine_bwd<decltype(type), decltype(bytes)::value>(a, st); });
+    s->dtype == DBL_F32 ? launch_combine_bwd<float>(a, st) : launch_combine_bwd<act_t>(a, st);
     return launch_check(w);
 }
