@@ -26,19 +26,39 @@ __device__ __forceinline__ int64_t slot_of(const ExchangeArgs& a, int64_t entry)
     return s >= 0 && s < a.grouped_rows ? s : -1;
 }
 
-// Sixteen bytes of a row, or one element.
-template <class T, bool WIDE = true>
+// W bytes of a row: 16, 8 or 4, or one element.
+template <class T, int W = 16>
 struct Chunk {
-    static constexpr int N = 16 / (int)sizeof(T);
-    uint4 v;
+    static constexpr int N = W / (int)sizeof(T), WORDS = W / 4;
+    uint32_t w[WORDS];
 
-    __device__ __forceinline__ void load(const T* p) { v = *reinterpret_cast<const uint4*>(p); }
-    __device__ __forceinline__ void store(T* p) const { *reinterpret_cast<uint4*>(p) = v; }
+    __device__ __forceinline__ void load(const T* p)
+    {
+        if constexpr (W == 16) {
+            const uint4 v = *reinterpret_cast<const uint4*>(p);
+            w[0] = v.x, w[1] = v.y, w[2] = v.z, w[3] = v.w;
+        } else if constexpr (W == 8) {
+            const uint2 v = *reinterpret_cast<const uint2*>(p);
+            w[0] = v.x, w[1] = v.y;
+        } else {
+            w[0] = *reinterpret_cast<const uint32_t*>(p);
+        }
+    }
+    __device__ __forceinline__ void store(T* p) const
+    {
+        if constexpr (W == 16)
+            *reinterpret_cast<uint4*>(p) = vec();
+        else if constexpr (W == 8)
+            *reinterpret_cast<uint2*>(p) = make_uint2(w[0], w[1]);
+        else
+            *reinterpret_cast<uint32_t*>(p) = w[0];
+    }
+    __device__ __forceinline__ uint4 vec() const { return make_uint4(w[0], w[1 % WORDS], w[2 % WORDS], w[3 % WORDS]); }
+    __device__ __forceinline__ void set(uint4 v) { w[0] = v.x, w[1 % WORDS] = v.y, w[2 % WORDS] = v.z, w[3 % WORDS] = v.w; }
     __device__ __forceinline__ void get(float (&f)[N]) const
     {
-        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+        for (int i = 0; i < WORDS; ++i)
             if constexpr (sizeof(T) == 4) {
                 f[i] = __uint_as_float(w[i]);
             } else {
@@ -48,33 +68,31 @@ struct Chunk {
     }
     __device__ __forceinline__ void put(const float (&f)[N])
     {
-        uint32_t w[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+        for (int i = 0; i < WORDS; ++i)
             if constexpr (sizeof(T) == 4)
                 w[i] = __float_as_uint(f[i]);
             else
                 w[i] = act::pack2_u32(f[2 * i], f[2 * i + 1]);
-        v = make_uint4(w[0], w[1], w[2], w[3]);
     }
 };
 
-template <class T>
-struct Chunk<T, false> {
+template <>
+struct Chunk<act_t, 2> {
     static constexpr int N = 1;
-    T v = elem_from<T>(0.f);
+    act_t v = elem_from<act_t>(0.f);
 
-    __device__ __forceinline__ void load(const T* p) { v = *p; }
-    __device__ __forceinline__ void store(T* p) const { *p = v; }
+    __device__ __forceinline__ void load(const act_t* p) { v = *p; }
+    __device__ __forceinline__ void store(act_t* p) const { *p = v; }
     __device__ __forceinline__ void get(float (&f)[1]) const { f[0] = elem_f(v); }
-    __device__ __forceinline__ void put(const float (&f)[1]) { v = elem_from<T>(f[0]); }
+    __device__ __forceinline__ void put(const float (&f)[1]) { v = elem_from<act_t>(f[0]); }
 };
 
 // A thread to a chunk of a row, rows_per_block rows to a block.
-template <class T, bool WIDE>
+template <class T, int W>
 __global__ void __launch_bounds__(256) expert_scatter_kernel(const ExchangeArgs a, int rows_per_block)
 {
-    using V = Chunk<T, WIDE>;
+    using V = Chunk<T, W>;
     const unsigned chunks = (unsigned)a.c / V::N;
     const int64_t r0 = (int64_t)blockIdx.x * rows_per_block;
     const unsigned n = (unsigned)min((int64_t)rows_per_block, a.rows - r0) * chunks;
@@ -91,10 +109,10 @@ __global__ void __launch_bounds__(256) expert_scatter_kernel(const ExchangeArgs 
 }
 
 // G threads to a row, NC chunks of it to a thread at a time, two entries' rows and the residual's asked for together.
-template <class T, bool WIDE, int G, int NC>
+template <class T, int W, int G, int NC>
 __global__ void __launch_bounds__(256) expert_combine_kernel(const ExchangeArgs a)
 {
-    using V = Chunk<T, WIDE>;
+    using V = Chunk<T, W>;
     const int chunks = a.c / V::N, g = threadIdx.x % G;
     const int64_t r = (int64_t)blockIdx.x * (256 / G) + threadIdx.x / G;
     if (r >= a.rows) return;
@@ -150,10 +168,10 @@ __global__ void __launch_bounds__(256) expert_combine_kernel(const ExchangeArgs 
 }
 
 // G threads to a row, NC chunks of it to a thread, kept while the entries pass (NC = 0: any number, read again for each).
-template <class T, bool WIDE, int G, int NC>
+template <class T, int W, int G, int NC>
 __global__ void __launch_bounds__(256) expert_combine_bwd_kernel(const ExchangeArgs a)
 {
-    using V = Chunk<T, WIDE>;
+    using V = Chunk<T, W>;
     constexpr int HELD = NC ? NC : 1;
     __shared__ float red[32];
     const int chunks = a.c / V::N, g = threadIdx.x % G;
@@ -266,20 +284,20 @@ __global__ void __launch_bounds__(256) expert_combine_any_kernel(const ExchangeA
             const int64_t s = slot_of(a, r * a.k + j);
             const float w = a.weights ? a.weights[r * a.k + j] : 1.f;
             Chunk<T> y = {};
-            if (s >= 0) y.v = grouped_row<T>(a, a.a, s).from(e);
+            if (s >= 0) y.set(grouped_row<T>(a, a.a, s).from(e));
             y.get(f);
 #pragma unroll
             for (int i = 0; i < N; ++i) sum[i] = fmaf(w, f[i], sum[i]);
         }
         Chunk<T> t;
         if (a.b) {
-            t.v = token_row<T>(a, a.b, r).from(e);
+            t.set(token_row<T>(a, a.b, r).from(e));
             t.get(f);
 #pragma unroll
             for (int i = 0; i < N; ++i) sum[i] += f[i];
         }
         t.put(sum);
-        if (u0 + lane < end) store_unit(o, a.c, e, t.v);
+        if (u0 + lane < end) store_unit(o, a.c, e, t.vec());
     }
 }
 
@@ -305,10 +323,10 @@ __global__ void __launch_bounds__(256) expert_combine_bwd_any_kernel(const Excha
                 const int e = (u0 + lane) * N - lead;
                 Chunk<T> dv, yv;
                 float f[N], h[N];
-                dv.v = d.from(e);
+                dv.set(d.from(e));
                 dv.get(f);
                 if (a.dweights) {
-                    yv.v = y.from(e);
+                    yv.set(y.from(e));
                     yv.get(h);
                     // a row's first and last unit hold what is outside it
 #pragma unroll
@@ -318,7 +336,7 @@ __global__ void __launch_bounds__(256) expert_combine_bwd_any_kernel(const Excha
 #pragma unroll
                 for (int i = 0; i < N; ++i) f[i] *= w;
                 dv.put(f);
-                if (u0 + lane < units) store_unit(o, a.c, e, dv.v);
+                if (u0 + lane < units) store_unit(o, a.c, e, dv.vec());
             }
         }
         if (!a.dweights) continue;
@@ -347,15 +365,29 @@ ExchangeArgs args(const dbl_exchange_shape* s, const void* a, const void* b, con
             s->ld_rows ? s->ld_rows : s->c, s->ld_grouped ? s->ld_grouped : s->c, s->k, s->c};
 }
 
-// How the rows are taken: in chunks of 16 bytes where all are of a multiple of them at 16-byte addresses; else element by
-// element where they are short (30000 rows of 70 elements, two entries: combine 17 us by units, as a warp has a row, 7 so),
-// or in units put together (8000 rows of 1001, four entries: scatter 32 us by elements, 21 so, the gradients 68 and 52).
-enum Way { kChunks, kElements, kUnits };
-Way way_of(const ExchangeArgs& a, size_t e)
+// The bytes of a chunk: what the rows' addresses, strides and length have in common, 16 at most, an element at least; 0: long
+// rows that begin at any element, in units put together.  (30000 rows of 70 elements, two entries: combine 17 us by units, as a
+// warp has a row, 7 so; 8000 rows of 1001, four entries: scatter 32 us by elements, 21 by units, the gradients 68 and 52.)
+int chunk_bytes(const ExchangeArgs& a, size_t e)
 {
     uintptr_t bits = reinterpret_cast<uintptr_t>(a.a) | reinterpret_cast<uintptr_t>(a.b) | reinterpret_cast<uintptr_t>(a.out);
     bits |= (uintptr_t)a.c * e | (uintptr_t)a.ld_rows * e | (uintptr_t)a.ld_grouped * e;
-    return (bits & 15) == 0 ? kChunks : a.c * e < 512 ? kElements : kUnits;
+    if (bits & 3) return a.c < 256 ? 2 : 0;
+    return bits & 4 ? 4 : bits & 8 ? 8 : 16;
+}
+
+// f(bytes, as a value of their type)
+template <class T, class F>
+void with_bytes(int bytes, F f)
+{
+    if (bytes == 16)
+        f(std::integral_constant<int, 16>());
+    else if (bytes == 8)
+        f(std::integral_constant<int, 8>());
+    else if (bytes == 4)
+        f(std::integral_constant<int, 4>());
+    else if constexpr (sizeof(T) == 2)
+        f(std::integral_constant<int, 2>());
 }
 
 // Parts of a row that begins anywhere, and the blocks of eight warps that take them.
@@ -375,78 +407,77 @@ int block_rows(const ExchangeArgs& a, int chunks)
 template <class T>
 void launch_scatter(const ExchangeArgs& a, cudaStream_t st)
 {
-    const Way way = way_of(a, sizeof(T));
-    if (way == kUnits) {
+    const int bytes = chunk_bytes(a, sizeof(T));
+    if (bytes == 0) {
         const int parts = row_parts<T>(a);
         expert_scatter_any_kernel<T><<<part_blocks(a, parts), 256, 0, st>>>(a, parts);
         return;
     }
-    const int rpb = block_rows(a, way == kChunks ? a.c / Chunk<T>::N : a.c);
-    const unsigned blocks = (unsigned)((a.rows + rpb - 1) / rpb);
-    if (way == kChunks)
-        expert_scatter_kernel<T, true><<<blocks, 256, 0, st>>>(a, rpb);
-    else
-        expert_scatter_kernel<T, false><<<blocks, 256, 0, st>>>(a, rpb);
+    with_bytes<T>(bytes, [&](auto w) {
+        constexpr int W = decltype(w)::value;
+        const int rpb = block_rows(a, a.c / Chunk<T, W>::N);
+        expert_scatter_kernel<T, W><<<(unsigned)((a.rows + rpb - 1) / rpb), 256, 0, st>>>(a, rpb);
+    });
 }
 
 // Threads to a row and chunks to a thread of the forward pass: rows of up to 8, 32, 64, 128 chunks are held at once.
 template <class T>
 void launch_combine(const ExchangeArgs& a, cudaStream_t st)
 {
-    const Way way = way_of(a, sizeof(T));
-    if (way == kUnits) {
+    const int bytes = chunk_bytes(a, sizeof(T));
+    if (bytes == 0) {
         const int parts = row_parts<T>(a);
         expert_combine_any_kernel<T><<<part_blocks(a, parts), 256, 0, st>>>(a, parts);
         return;
     }
-    auto run = [&](auto wide, auto g, auto nc) {
-        constexpr bool WIDE = decltype(wide)::value;
-        constexpr int G = decltype(g)::value, NC = decltype(nc)::value;
-        expert_combine_kernel<T, WIDE, G, NC><<<(unsigned)((a.rows + 256 / G - 1) / (256 / G)), 256, 0, st>>>(a);
-    };
+    with_bytes<T>(bytes, [&](auto w) {
+        constexpr int W = decltype(w)::value;
+        const int chunks = a.c / Chunk<T, W>::N;
+        auto run = [&](auto g, auto nc) {
+            constexpr int G = decltype(g)::value, NC = decltype(nc)::value;
+            expert_combine_kernel<T, W, G, NC><<<(unsigned)((a.rows + 256 / G - 1) / (256 / G)), 256, 0, st>>>(a);
+        };
 #define DBL_I(n) std::integral_constant<int, n>()
-    if (way == kElements)
-        return a.c <= 16 ? run(std::false_type(), DBL_I(8), DBL_I(2)) : run(std::false_type(), DBL_I(32), DBL_I(4));
-    const std::true_type wide;
-    const int chunks = a.c / Chunk<T>::N;
-    if (chunks <= 8) return run(wide, DBL_I(8), DBL_I(1));
-    if (chunks <= 32) return run(wide, DBL_I(32), DBL_I(1));
-    if (chunks <= 64) return run(wide, DBL_I(32), DBL_I(2));
-    if (chunks <= 256) return run(wide, DBL_I(32), DBL_I(4));
-    run(wide, DBL_I(256), DBL_I(2));
+        if (chunks <= 8) return run(DBL_I(8), DBL_I(1));
+        if (chunks <= 32) return run(DBL_I(32), DBL_I(1));
+        if (chunks <= 64) return run(DBL_I(32), DBL_I(2));
+        if (chunks <= 256) return run(DBL_I(32), DBL_I(4));
+        run(DBL_I(256), DBL_I(2));
 #undef DBL_I
+    });
 }
 
 template <class T>
 void launch_combine_bwd(const ExchangeArgs& a, cudaStream_t st)
 {
-    const Way way = way_of(a, sizeof(T));
-    if (way == kUnits) {
+    const int bytes = chunk_bytes(a, sizeof(T));
+    if (bytes == 0) {
         if (a.c / Chunk<T>::N > 512)
             expert_combine_bwd_any_kernel<T, 256><<<(unsigned)a.rows, 256, 0, st>>>(a);
         else
             expert_combine_bwd_any_kernel<T, 32><<<(unsigned)((a.rows + 7) / 8), 256, 0, st>>>(a);
         return;
     }
-    auto run = [&](auto wide, auto g, auto nc) {
-        constexpr bool WIDE = decltype(wide)::value;
-        constexpr int G = decltype(g)::value, NC = decltype(nc)::value;
-        expert_combine_bwd_kernel<T, WIDE, G, NC><<<(unsigned)((a.rows + 256 / G - 1) / (256 / G)), 256, 0, st>>>(a);
-    };
+    with_bytes<T>(bytes, [&](auto w) {
+        constexpr int W = decltype(w)::value;
+        const int chunks = a.c / Chunk<T, W>::N;
+        auto run = [&](auto g, auto nc) {
+            constexpr int G = decltype(g)::value, NC = decltype(nc)::value;
+            expert_combine_bwd_kernel<T, W, G, NC><<<(unsigned)((a.rows + 256 / G - 1) / (256 / G)), 256, 0, st>>>(a);
+        };
 #define DBL_I(n) std::integral_constant<int, n>()
-    if (way == kElements)
-        return a.c <= 16 ? run(std::false_type(), DBL_I(8), DBL_I(2)) : run(std::false_type(), DBL_I(32), DBL_I(8));
-    const std::true_type wide;
-    const int chunks = a.c / Chunk<T>::N;
-    if (chunks <= 8) return run(wide, DBL_I(8), DBL_I(1));
-    if (chunks <= 16) return run(wide, DBL_I(8), DBL_I(2));
-    if (chunks <= 32) return run(wide, DBL_I(32), DBL_I(1));
-    if (chunks <= 64) return run(wide, DBL_I(32), DBL_I(2));
-    if (chunks <= 128) return run(wide, DBL_I(32), DBL_I(4));
-    if (chunks <= 512) return run(wide, DBL_I(256), DBL_I(2));
-    if (chunks <= 1024) return run(wide, DBL_I(256), DBL_I(4));
-    run(wide, DBL_I(256), DBL_I(0));
+        if (chunks <= 8) return run(DBL_I(8), DBL_I(1));
+        if (chunks <= 16) return run(DBL_I(8), DBL_I(2));
+        if (chunks <= 32) return run(DBL_I(32), DBL_I(1));
+        if (chunks <= 64) return run(DBL_I(32), DBL_I(2));
+        if (chunks <= 128) return run(DBL_I(32), DBL_I(4));
+        if (chunks <= 256) return run(DBL_I(32), DBL_I(8));
+        if (W < 16 && chunks <= 512) return run(DBL_I(32), DBL_I(16));
+        if (chunks <= 512) return run(DBL_I(256), DBL_I(2));
+        if (chunks <= 1024) return run(DBL_I(256), DBL_I(4));
+        run(DBL_I(256), DBL_I(0));
 #undef DBL_I
+    });
 }
 
 }  // namespace
