@@ -70,12 +70,14 @@ struct MmaArgs {
     int features;       // of the result (fwd, dgrad)
     int depth;          // of the reduction (fwd, dgrad)
     int blocks_a, blocks_b;  // blocks of 256 features; wgrad: of n_in and n_out
+    int parts;          // of a tile's reduction; more than 1: out holds fp32 sums [parts][rows][features], [parts][dw]
 };
 
 struct Tile {
     int group, a0, b0;  // a0: the first of 256 features (wgrad: of n_in); b0: the first row (wgrad: of 256 of n_out)
     int n;              // the MMA's N
-    int kb;             // stages of the reduction
+    int k0, k1;         // stages of the reduction
+    int part;
     int row0, row1;     // of the group
 };
 
@@ -86,7 +88,8 @@ template <int PASS>
 struct Walk {
     int group, outer, inner, step_outer, step_inner;
 
-    __device__ __forceinline__ static int inners(const MmaArgs& p) { return PASS == kWgrad ? p.blocks_b : p.blocks_a; }
+    // a tile's parts are neighbours
+    __device__ __forceinline__ static int inners(const MmaArgs& p) { return (PASS == kWgrad ? p.blocks_b : p.blocks_a) * p.parts; }
     __device__ __forceinline__ Walk(const MmaArgs& p, const int* first, int unit0, int nunits)
         : group(0), outer(unit0 / inners(p)), inner(unit0 % inners(p)), step_outer(nunits / inners(p)),
           step_inner(nunits % inners(p))
@@ -114,10 +117,14 @@ struct Walk {
         c.group = group;
         c.row0 = off[group];
         c.row1 = off[group + 1];
-        c.a0 = (PASS == kWgrad ? outer : inner) * 256;
-        c.b0 = PASS == kWgrad ? inner * 256 : c.row0 + outer * 256;
+        const int block = p.parts > 1 ? inner / p.parts : inner;
+        c.part = inner - block * p.parts;
+        c.a0 = (PASS == kWgrad ? outer : block) * 256;
+        c.b0 = PASS == kWgrad ? block * 256 : c.row0 + outer * 256;
         c.n = PASS == kWgrad ? 256 : min(256, (c.row1 - c.b0 + 31) / 32 * 32);
-        c.kb = ((PASS == kWgrad ? c.row1 - c.row0 : p.depth) + 63) / 64;
+        const int kb = ((PASS == kWgrad ? c.row1 - c.row0 : p.depth) + 63) / 64;
+        c.k0 = p.parts > 1 ? (int)((int64_t)kb * c.part / p.parts) : 0;
+        c.k1 = p.parts > 1 ? (int)((int64_t)kb * (c.part + 1) / p.parts) : kb;
         return c;
     }
 };
@@ -220,7 +227,7 @@ __global__ void __launch_bounds__(Cfg::THREADS, 1)
         bool failed = false;
         for (; walk.there(p) && !failed; walk.next(p, first)) {
             const Tile tc = walk.tile(p, off);
-            for (int k = 0; k < tc.kb; ++k, ++it) {
+            for (int k = tc.k0; k < tc.k1; ++k, ++it) {
                 if (it % C::PROD != prod) continue;
                 const int s = it % STAGES;
                 const uint32_t ok = mbar_wait_warp(&empty_bar[s], ((it / STAGES) & 1) ^ 1, &abort_flag);
@@ -312,12 +319,12 @@ __global__ void __launch_bounds__(Cfg::THREADS, 1)
         int it = 0, lt = 0;
         for (; walk.there(p) && rank == 0 && !failed; walk.next(p, first)) {
             const Tile tc = walk.tile(p, off);
-            const int chain = PASS == kWgrad ? kChain : tc.kb;
+            const int chain = PASS == kWgrad ? kChain : tc.k1 - tc.k0;
             const bool tail = PASS == kWgrad && ((tc.row1 - tc.row0) & 15);
             const int length = PASS == kWgrad ? tc.row1 - tc.row0 : p.depth;
             const uint32_t idesc = idesc_act(256, tc.n, a_mn, b_mn);
-            for (int k0 = 0; k0 < tc.kb && !failed; k0 += chain, ++lt) {
-                const int buf = lt % C::NB, k1 = min(tc.kb, k0 + chain);
+            for (int k0 = tc.k0; k0 < tc.k1 && !failed; k0 += chain, ++lt) {
+                const int buf = lt % C::NB, k1 = min(tc.k1, k0 + chain);
                 const uint32_t free = mbar_wait_warp(&acce_bar[buf], ((lt / C::NB) & 1) ^ 1, &abort_flag);
                 if (__any_sync(0xffffffffu, free == 0u)) {
                     failed = true;
@@ -325,7 +332,7 @@ __global__ void __launch_bounds__(Cfg::THREADS, 1)
                 }
                 const uint32_t d = tmem + (uint32_t)(buf * 256);
                 for (int k = k0; k < k1; ++k, ++it) {
-                    if (!wait_full(it, k + 1 == tc.kb && tail)) {
+                    if (!wait_full(it, tail && length - k * 64 < 64)) {
                         failed = true;
                         break;
                     }
@@ -382,7 +389,7 @@ __global__ void __launch_bounds__(Cfg::THREADS, 1)
                 float acc[CW];
 #pragma unroll
                 for (int i = 0; i < CW; ++i) acc[i] = 0.f;
-                for (int k0 = 0; k0 < tc.kb; k0 += kChain, ++lt) {
+                for (int k0 = tc.k0; k0 < tc.k1; k0 += kChain, ++lt) {
                     const int buf = lt % C::NB;
                     if (!wait_acc(buf)) break;
                     const uint32_t taddr = lanes + (uint32_t)(buf * 256 + part * CW);
@@ -399,7 +406,7 @@ __global__ void __launch_bounds__(Cfg::THREADS, 1)
                 if (failed) break;
                 // consecutive lanes hold consecutive columns of dw: each store is a line of 128 bytes
                 if (m < p.n_in) {
-                    float* o = static_cast<float*>(p.out) + ((int64_t)tc.group * p.n_out + n0) * p.n_in + m;
+                    float* o = static_cast<float*>(p.out) + (((int64_t)tc.part * p.groups + tc.group) * p.n_out + n0) * p.n_in + m;
                     const int left = p.n_out - n0;  // a multiple of 8
                     if (p.accumulate) {
 #pragma unroll
@@ -421,6 +428,25 @@ __global__ void __launch_bounds__(Cfg::THREADS, 1)
                     }
                 }
             } else {
+                if (p.parts > 1) {
+                    // fp32 sums of this part: consecutive lanes hold consecutive features
+                    const int buf = lt % C::NB, f = tc.a0 + rank * 128 + quarter * 32 + lane;
+                    if (!wait_acc(buf)) break;
+                    float* o = static_cast<float*>(p.out) + ((int64_t)tc.part * p.rows + tc.b0) * p.features + f;
+#pragma unroll 1
+                    for (int ch = part; ch < tc.n / 32; ch += 2) {
+                        uint32_t v[32];
+                        tmem_ld_32x32b_x32(lanes + (uint32_t)(buf * 256 + ch * 32), v);
+                        tmem_ld_wait_regs(v);
+#pragma unroll
+                        for (int i = 0; i < 32; ++i)
+                            if (f < p.features && tc.b0 + ch * 32 + i < tc.row1)
+                                o[(int64_t)(ch * 32 + i) * p.features] = __uint_as_float(v[i]);
+                    }
+                    release(buf);
+                    ++lt;
+                    continue;
+                }
                 // 32 features of 32 tokens at a time: pairs of tokens in a thread, turned through shared memory into 64 bytes of a
                 // token's row for four lanes, so that a store meets 8 rows.  The two warps of the same features take turns.
                 const int buf = lt % C::NB, chunks = tc.n / 32;
@@ -499,6 +525,64 @@ __global__ void __launch_bounds__(Cfg::THREADS, 1)
     }
 }
 
+// The sum of a result's parts, in their order.  fwd, dgrad: eight features of a row to a thread, the rows of all groups.
+template <int PASS>
+__global__ void __launch_bounds__(256) grouped_sum_kernel(const float* parts, const MmaArgs p)
+{
+    grid_dependency_wait();
+    const int per = p.features / 8;
+    // the groups are neighbours: from the first one's first row to the last one's end, clamped as load_offsets does
+    int first = 0, last = 0;
+    if (threadIdx.x < 32) {
+        first = min((int64_t)max(p.offsets[0], 0), p.rows);
+        for (int i = threadIdx.x; i <= p.groups; i += 32) last = max(last, (int)min((int64_t)max(p.offsets[i], 0), p.rows));
+        last = __reduce_max_sync(0xffffffffu, last);
+    }
+    __shared__ int range[2];
+    if (threadIdx.x == 0) range[0] = first, range[1] = last;
+    __syncthreads();
+    const int64_t total = (int64_t)(range[1] - range[0]) * per, slice = p.rows * p.features;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
+        const int64_t row = range[0] + i / per;
+        const int col = (int)(i % per) * 8;
+        float f[8] = {};
+        const float* src = parts + row * p.features + col;
+#pragma unroll 4
+        for (int k = 0; k < p.parts; ++k) {
+            const float4 a = *reinterpret_cast<const float4*>(src + k * slice), b = *reinterpret_cast<const float4*>(src + k * slice + 4);
+            f[0] += a.x, f[1] += a.y, f[2] += a.z, f[3] += a.w;
+            f[4] += b.x, f[5] += b.y, f[6] += b.z, f[7] += b.w;
+        }
+        uint32_t w[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            w[j] = act::pack2_u32(f[2 * j], f[2 * j + 1]);
+            if (PASS == kFwd && p.relu) w[j] = relu2(w[j]);
+        }
+        const int64_t at = row * p.ld + col;
+        if (PASS == kDgrad && p.mask) {
+            const uint4 h = *reinterpret_cast<const uint4*>(p.mask + at);
+            w[0] = pass2(w[0], h.x), w[1] = pass2(w[1], h.y), w[2] = pass2(w[2], h.z), w[3] = pass2(w[3], h.w);
+        }
+        *reinterpret_cast<uint4*>(static_cast<act_t*>(p.out) + at) = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+}
+
+// wgrad: four elements to a thread.
+__global__ void __launch_bounds__(256) grouped_sum_dw_kernel(const float* parts, float* dw, int64_t n, int count, int accumulate)
+{
+    grid_dependency_wait();
+    for (int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4; i < n; i += (int64_t)gridDim.x * 1024) {
+        float4 f = accumulate ? *reinterpret_cast<const float4*>(dw + i) : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+        for (int k = 0; k < count; ++k) {
+            const float4 a = *reinterpret_cast<const float4*>(parts + k * n + i);
+            f.x += a.x, f.y += a.y, f.z += a.z, f.w += a.w;
+        }
+        *reinterpret_cast<float4*>(dw + i) = f;
+    }
+}
+
 int check(const dbl_grouped_shape* s, const char* w)
 {
     if (!s || s->rows < 0 || s->groups <= 0 || s->n_in <= 0 || s->n_out <= 0)
@@ -568,20 +652,64 @@ int launch(const CUtensorMap (&maps)[3], const MmaArgs& p, int64_t most_tiles, c
     return err == cudaSuccess ? rc : cuda_check(err, w);
 }
 
+// Tiles of a pass, an upper bound for the forward pass and the data gradient: the blocks of rows are the device's to count.
+int64_t tiles_of(const dbl_grouped_shape* s, int pass)
+{
+    const int64_t in = (s->n_in + 255) / 256, out = (s->n_out + 255) / 256;
+    if (pass == kWgrad) return s->groups * in * out;
+    return (s->rows < s->groups ? s->rows : s->rows / 256 + s->groups) * (pass == kFwd ? out : in);
+}
+
+// Elements of the result that a part has.
+int64_t part_elements(const dbl_grouped_shape* s, int pass)
+{
+    return pass == kWgrad ? (int64_t)s->groups * s->n_out * s->n_in : s->rows * (pass == kFwd ? s->n_out : s->n_in);
+}
+
+// Parts of a tile's reduction, which a second launch adds, where there are few tiles.  fwd, dgrad: as many as fill the pairs, with
+// eight stages each at least: 8 rows of one group of 4096x4096 24.8 -> 14.7 us.  wgrad: the least modelled time in us, a stage
+// taking 0.3, an item's end 2, the second launch 3 and what it reads and the parts are written at 5 TB/s; the groups are taken as
+// of the same length.  65000 rows of one group of 512x512 312 -> 41 us, 40000 of two of 2048x256 105 -> 47, 48000 rows of
+// one of 664x3424 (42 tiles for 76 pairs) 238 -> 208.
+int parts_of(const dbl_grouped_shape* s, int pass)
+{
+    const int64_t tiles = tiles_of(s, pass), pairs = sm_count() / 2;
+    if (tiles == 0) return 1;
+    const int64_t depth = pass == kFwd ? s->n_in : pass == kDgrad ? s->n_out : s->rows / s->groups, stages = depth / 64;
+    if (pass != kWgrad) {
+        const int64_t most = pairs / tiles, parts = most < stages / 8 ? most : stages / 8;
+        return parts > 1 ? (int)parts : 1;
+    }
+    const double bytes = 4.0 * (double)part_elements(s, pass);
+    int best = 1;
+    double least = 0.0;
+    for (int n = 1; n <= 76 && (n == 1 || stages / n >= 8); ++n) {
+        const double rounds = (double)((tiles * n + pairs - 1) / pairs);
+        const double us = rounds * (0.3 * (double)stages / n + 2.0) + (n > 1 ? 3.0 + 2 * n * bytes / 5e6 : 0.0);
+        if (n == 1 || us < least) least = us, best = n;
+    }
+    return best;
+}
+
 // a: fwd, dgrad: the tokens' rows (x, dy), wgrad: x; b: the weights, wgrad: dy.
 template <int PASS>
 int run(const dbl_grouped_shape* s, const void* a, const void* b, const int32_t* offsets, const void* mask, void* out,
-        int accumulate, void* stream, const char* w)
+        int accumulate, void* ws, size_t ws_bytes, void* stream, const char* w)
 {
+    const int parts = parts_of(s, PASS);
+    const size_t need = dbl_grouped_workspace_bytes(s, PASS);
+    if (need && (!ws || ws_bytes < need)) return set_error(DBL_ERR_WORKSPACE, "%s: workspace too small", w);
+    if (!aligned16(ws)) return set_error(DBL_ERR_INVALID, "%s: the workspace is not 16-byte aligned", w);
     const int64_t ld_in = s->ld_in ? s->ld_in : s->n_in, ld_out = s->ld_out ? s->ld_out : s->n_out;
     MmaArgs p = {};
     p.mask = static_cast<const act_t*>(mask);
-    p.out = out;
+    p.out = parts > 1 ? ws : out;
     p.offsets = offsets;
     p.rows = s->rows;
+    p.parts = parts;
     p.ld = PASS == kFwd ? ld_out : ld_in;
     p.groups = s->groups, p.n_in = s->n_in, p.n_out = s->n_out;
-    p.relu = s->relu != 0, p.accumulate = accumulate;
+    p.relu = s->relu != 0, p.accumulate = accumulate && parts == 1;
     p.features = PASS == kDgrad ? s->n_in : s->n_out;
     p.depth = PASS == kFwd ? s->n_in : s->n_out;
     p.blocks_a = ((PASS == kWgrad ? s->n_in : p.features) + 255) / 256;
@@ -598,10 +726,28 @@ int run(const dbl_grouped_shape* s, const void* a, const void* b, const int32_t*
         if ((rc = encode_rows(&maps[1], a, s->rows, p.depth, ld, 128, w)) != DBL_OK) return rc;
         if ((rc = encode_rows(&maps[2], a, s->rows, p.depth, ld, 16, w)) != DBL_OK) return rc;
     }
-    // the blocks of rows are the device's to count: a group's last one is partial
-    const int64_t tiles = PASS == kWgrad ? (int64_t)s->groups * p.blocks_a * p.blocks_b
-                                         : (s->rows < s->groups ? s->rows : s->rows / 256 + s->groups) * p.blocks_a;
-    return launch<PASS>(maps, p, tiles, as_stream(stream), w);
+    cudaStream_t st = as_stream(stream);
+    rc = launch<PASS>(maps, p, tiles_of(s, PASS) * parts, st, w);
+    if (rc != DBL_OK || parts == 1) return rc;
+    p.out = out;
+    const int64_t items = part_elements(s, PASS) / (PASS == kWgrad ? 4 : 8), blocks = (items + 255) / 256, cap = (int64_t)sm_count() * 8;
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.gridDim = dim3((unsigned)(blocks < cap ? blocks : cap));
+    cfg.blockDim = dim3(256);
+    cfg.stream = st;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    const float* sums = static_cast<const float*>(ws);
+    cudaError_t err;
+    if constexpr (PASS == kWgrad)
+        err = cudaLaunchKernelEx(&cfg, grouped_sum_dw_kernel, sums, static_cast<float*>(out), part_elements(s, PASS), parts, accumulate);
+    else
+        err = cudaLaunchKernelEx(&cfg, grouped_sum_kernel<PASS>, sums, p);
+    rc = launch_check("grouped sum");
+    return err == cudaSuccess ? rc : cuda_check(err, "grouped sum");
 }
 
 }  // namespace
@@ -616,44 +762,41 @@ StatusWord grouped_status_word() { return {read_word, clear_word}; }
 
 extern "C" size_t dbl_grouped_workspace_bytes(const dbl_grouped_shape* s, int pass)
 {
-    (void)pass;
-    (void)check(s, "grouped_workspace_bytes");
-    return 0;
+    if (check(s, "grouped_workspace_bytes") != DBL_OK || pass < kFwd || pass > kWgrad || s->rows == 0) return 0;
+    const int parts = parts_of(s, pass);
+    return parts > 1 ? (size_t)parts * part_elements(s, pass) * sizeof(float) : 0;
 }
 
 extern "C" int dbl_grouped_fwd(const dbl_grouped_shape* s, const void* x, const void* wt, const int32_t* offsets, void* y,
                                void* ws, size_t ws_bytes, void* stream)
 {
     const char* w = "grouped_fwd";
-    (void)ws, (void)ws_bytes;
     int rc = check(s, w);
     if (rc != DBL_OK) return rc;
     if (!aligned16(x) || !aligned16(wt) || !aligned16(y) || !aligned_to(offsets, 4))
         return set_error(DBL_ERR_INVALID, "%s: a tensor is not 16-byte aligned, or offsets not to 4 bytes", w);
     if (s->rows == 0) return DBL_OK;
     if (!x || !wt || !offsets || !y) return set_error(DBL_ERR_INVALID, "%s: a tensor is NULL", w);
-    return run<0>(s, x, wt, offsets, nullptr, y, 0, stream, w);
+    return run<kFwd>(s, x, wt, offsets, nullptr, y, 0, ws, ws_bytes, stream, w);
 }
 
 extern "C" int dbl_grouped_dgrad(const dbl_grouped_shape* s, const void* dy, const void* wt, const int32_t* offsets,
                                  const void* mask, void* dx, void* ws, size_t ws_bytes, void* stream)
 {
     const char* w = "grouped_dgrad";
-    (void)ws, (void)ws_bytes;
     int rc = check(s, w);
     if (rc != DBL_OK) return rc;
     if (!aligned16(dy) || !aligned16(wt) || !aligned16(mask) || !aligned16(dx) || !aligned_to(offsets, 4))
         return set_error(DBL_ERR_INVALID, "%s: a tensor is not 16-byte aligned, or offsets not to 4 bytes", w);
     if (s->rows == 0) return DBL_OK;
     if (!dy || !wt || !offsets || !dx) return set_error(DBL_ERR_INVALID, "%s: a tensor is NULL", w);
-    return run<1>(s, dy, wt, offsets, mask, dx, 0, stream, w);
+    return run<kDgrad>(s, dy, wt, offsets, mask, dx, 0, ws, ws_bytes, stream, w);
 }
 
 extern "C" int dbl_grouped_wgrad(const dbl_grouped_shape* s, const void* x, const void* dy, const int32_t* offsets, float* dw,
                                  int accumulate, void* ws, size_t ws_bytes, void* stream)
 {
     const char* w = "grouped_wgrad";
-    (void)ws, (void)ws_bytes;
     int rc = check(s, w);
     if (rc != DBL_OK) return rc;
     if (!aligned16(x) || !aligned16(dy) || !aligned16(dw) || !aligned_to(offsets, 4))
@@ -664,5 +807,5 @@ extern "C" int dbl_grouped_wgrad(const dbl_grouped_shape* s, const void* x, cons
         return cuda_check(cudaMemsetAsync(dw, 0, (size_t)s->groups * s->n_in * s->n_out * sizeof(float), as_stream(stream)), w);
     }
     if (!x || !dy || !offsets) return set_error(DBL_ERR_INVALID, "%s: a tensor is NULL", w);
-    return run<2>(s, x, dy, offsets, nullptr, dw, accumulate != 0, stream, w);
+    return run<kWgrad>(s, x, dy, offsets, nullptr, dw, accumulate != 0, ws, ws_bytes, stream, w);
 }

@@ -100,6 +100,14 @@ def test_grouped_refusals(D, prec):
                        dict(o=P + 2)):
                 refused(D, INV, f, *a(**kw))
         refused(D, INV, D.dbl_grouped_dgrad, *calls[D.dbl_grouped_dgrad][1](m=P + 8))
+        for f, s in ((D.dbl_grouped_fwd, D.grouped_shape(8, 1, 4096, 256)), (D.dbl_grouped_dgrad, D.grouped_shape(8, 1, 256, 4096)),
+                     (D.dbl_grouped_wgrad, D.grouped_shape(9000, 1, 256, 256))):
+            which, a = calls[f]
+            need = D.dbl_grouped_workspace_bytes(s, which)
+            assert need > 0 and D.dbl_grouped_workspace_bytes(s, 3) == D.dbl_grouped_workspace_bytes(s, -1) == 0
+            refused(D, D.DBL_ERR_WORKSPACE, f, *a(s, n=need - 1))
+            refused(D, D.DBL_ERR_WORKSPACE, f, *a(s, ws=None))
+            refused(D, INV, f, *a(s, ws=P + 8))
     assert D.lib().dbl_grouped_fwd(None, P, P, P, P, None, 0, None) == INV
     assert D.lib().dbl_grouped_workspace_bytes(None, 0) == 0
 

@@ -14,7 +14,11 @@ CASES = [  # lengths of the groups, rows past the last, n_in, n_out, strides bey
     ([130, 1, 0, 7], 3, 72, 136, 0), ([256, 256], 0, 128, 256, 0), ([257, 255, 31], 1, 512, 520, 16),
     ([5, 9, 0, 1, 33, 127, 128, 129], 50, 200, 1000, 24), ([700], 0, 1000, 72, 0), ([40] * 20, 0, 256, 512, 0),
     ([0, 0, 1500, 0], 9, 264, 248, 8), ([16, 17, 15, 1, 2, 300], 0, 1032, 264, 0), ([2] * 70, 1, 64, 72, 0),
-    ([600, 20, 1], 0, 2048, 96, 0), ([90, 70], 0, 96, 2056, 8)]
+    ([600, 20, 1], 0, 2048, 96, 0), ([90, 70], 0, 96, 2056, 8),
+    # few tiles and long reductions, which are split: in the groups' rows (the last with parts that get none of a group), in
+    # n_in, in n_out
+    ([5003], 2, 72, 64, 0), ([1500, 0, 2600], 3, 264, 136, 8), ([5000, 1, 40, 700], 0, 64, 200, 0), ([9], 1, 4104, 72, 0),
+    ([33, 2], 0, 72, 3080, 0)]
 
 
 def setup(kind, case):
