@@ -634,7 +634,7 @@ int launch(const CUtensorMap (&maps)[3], const MmaArgs& p, int64_t most_tiles, c
     int dev = 0;
     if ((rc = cuda_check(cudaGetDevice(&dev), w)) != DBL_OK) return rc;
     int pairs = clusters_held<grouped_kernel<PASS>>(dev, 2, C::THREADS, C::SMEM);
-    if (pairs < 1) pairs = 1;  // as one pair after the other
+    if (pairs < 1) pairs = sm_count() / 2;  // the device has not answered, or DBL_MAX_CLUSTER is 1: there is no other form
     if (pairs > most_tiles) pairs = (int)most_tiles;
     cudaLaunchConfig_t cfg = {};
     cudaLaunchAttribute at[1];

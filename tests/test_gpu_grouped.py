@@ -18,7 +18,7 @@ CASES = [  # lengths of the groups, rows past the last, n_in, n_out, strides bey
     # few tiles and long reductions, which are split: in the groups' rows (the last with parts that get none of a group), in
     # n_in, in n_out
     ([5003], 2, 72, 64, 0), ([1500, 0, 2600], 3, 264, 136, 8), ([5000, 1, 40, 700], 0, 64, 200, 0), ([9], 1, 4104, 72, 0),
-    ([33, 2], 0, 72, 3080, 0)]
+    ([33, 2], 0, 72, 3080, 0), ([i % 3 if i % 7 else 40 for i in range(1024)], 5, 64, 72, 0)]
 
 
 def setup(kind, case):
@@ -50,7 +50,7 @@ def sum_error(terms, size):
 
 @pytest.mark.parametrize("kind", ["bf16", "f16"])
 @pytest.mark.parametrize("relu", [False, True])
-@pytest.mark.parametrize("case", CASES, ids=str)
+@pytest.mark.parametrize("case", CASES, ids=lambda c: f"{len(c[0])}x{sum(c[0])}-{c[2]}x{c[3]}")
 def test_fwd(kind, relu, case):
     D = load_dbl()
     lengths, _, n_in, n_out, _ = case
@@ -77,7 +77,7 @@ def test_fwd(kind, relu, case):
 
 @pytest.mark.parametrize("kind", ["bf16", "f16"])
 @pytest.mark.parametrize("masked", [False, True])
-@pytest.mark.parametrize("case", CASES, ids=str)
+@pytest.mark.parametrize("case", CASES, ids=lambda c: f"{len(c[0])}x{sum(c[0])}-{c[2]}x{c[3]}")
 def test_dgrad(kind, masked, case):
     D = load_dbl()
     lengths, _, n_in, n_out, _ = case
@@ -105,7 +105,7 @@ def test_dgrad(kind, masked, case):
 
 @pytest.mark.parametrize("kind", ["bf16", "f16"])
 @pytest.mark.parametrize("accumulate", [False, True])
-@pytest.mark.parametrize("case", CASES, ids=str)
+@pytest.mark.parametrize("case", CASES, ids=lambda c: f"{len(c[0])}x{sum(c[0])}-{c[2]}x{c[3]}")
 def test_wgrad(kind, accumulate, case):
     D = load_dbl()
     lengths, _, n_in, n_out, _ = case

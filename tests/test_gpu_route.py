@@ -43,7 +43,9 @@ CASES = [  # rows, experts, k, stride, offset
     (1, 1, 1, 0, 0), (1, 8, 2, 0, 0), (5, 3, 3, 0, 0), (64, 8, 2, 0, 0), (130, 60, 4, 0, 0), (33, 64, 8, 72, 1),
     (1000, 128, 8, 0, 0), (257, 33, 32, 0, 0), (70, 1024, 6, 0, 0), (4099, 16, 1, 0, 0), (12, 257, 32, 264, 3),
     (9000, 7, 2, 0, 0), (3, 500, 1, 0, 0), (600, 256, 8, 0, 0), (301, 160, 12, 0, 0), (20000, 32, 4, 0, 0),
-    (2500, 512, 3, 0, 0), (777, 100, 9, 0, 0)]
+    (2500, 512, 3, 0, 0), (777, 100, 9, 0, 0),
+    # many rows, a thread to each: all of k, widths that end inside 16 and 64, rows of several tiles, a stride
+    (21000, 100, 8, 0, 0), (30001, 17, 16, 0, 0), (20004, 512, 12, 0, 0), (24001, 65, 1, 72, 3), (19500, 130, 5, 136, 0)]
 
 
 @pytest.mark.parametrize("kind", ["bf16", "f16", "f32"])
@@ -76,7 +78,7 @@ def test_route(kind, normalise, case):
 
 
 @pytest.mark.parametrize("kind", ["bf16", "f32"])
-@pytest.mark.parametrize("rows", [1, 900])
+@pytest.mark.parametrize("rows", [1, 900, 20000])
 def test_all_experts_equal_and_signed_zeros(kind, rows):
     D = load_dbl()
     v = np.zeros((rows, 70))
@@ -87,10 +89,11 @@ def test_all_experts_equal_and_signed_zeros(kind, rows):
     assert (slots == np.arange(5) * rows + np.arange(rows)[:, None]).all()
 
 
-def test_bias_of_infinity_closes_an_expert_and_padding_may_hold_anything():
+@pytest.mark.parametrize("rows,experts", [(100, 12), (20000, 40)])
+def test_bias_of_infinity_closes_an_expert_and_padding_may_hold_anything(rows, experts):
     D = load_dbl()
     g = rng(4)
-    rows, experts, k = 100, 12, 4
+    k = 4
     v = g.standard_normal((rows, experts)).astype(np.float32)
     v[::5] = NAN
     bias, weight = np.zeros(experts), np.ones(rows)
@@ -106,7 +109,7 @@ def test_bias_of_infinity_closes_an_expert_and_padding_may_hold_anything():
     bias[:] = -INF
     bias[2] = 0
     got = run(D, "f32", z, k, True, bias, weight)
-    assert (got[0][1] == [2, -1, -1, -1]).all() and got[1][1].tolist() == [1, 0, 0, 0] and got[3][-1] == 80
+    assert (got[0][1] == [2, -1, -1, -1]).all() and got[1][1].tolist() == [1, 0, 0, 0] and got[3][-1] == rows * 4 // 5
 
 
 def test_the_same_bits_again_and_no_rows():
