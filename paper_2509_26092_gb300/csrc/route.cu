@@ -15,7 +15,7 @@ using namespace dbl::dev;
 constexpr int kMaxExperts = DBL_ROUTE_MAX_EXPERTS, kMaxK = DBL_ROUTE_MAX_K;
 constexpr int kMaxBlocks = 256;    // of the forward pass; the workspace holds one count for each block and expert
 constexpr int kOneBlockRows = 256;  // up to here one block chooses and places
-constexpr int kManyRows = 128;      // of a block: from here a thread takes a row
+constexpr int kManyRows = 64;       // of a block: from here a thread takes a row
 constexpr int kPlaceCounts = 8192;  // counts of a block's warps and experts in shared memory
 
 struct RouteArgs {
@@ -535,54 +535,78 @@ __global__ void __launch_bounds__(1024) route_place_kernel(const RouteArgs a)
     }
 }
 
-// A warp to a row: first what every expert gets, then the entries' experts.
+// What a lane has of a row: entry `lane`, and every 32nd expert's logit.
+template <int EPL>
+struct RouteRow {
+    int e;
+    float w, dw, z[EPL];
+};
+
+// A warp to a row, the next one's loads on their way: first what every expert gets, then the entries' experts.
 template <class T, int EPL>
 __global__ void __launch_bounds__(256) route_bwd_kernel(const void* logits, const int32_t* chosen, const float* weights,
                                                         const float* dweights, void* dlogits, int64_t rows, int experts,
                                                         int k, int normalise, int64_t ld, int64_t ld_grad)
 {
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    for (int64_t r = (int64_t)blockIdx.x * 8 + warp; r < rows; r += (int64_t)gridDim.x * 8) {
-        const T* z = static_cast<const T*>(logits) + r * ld;
-        T* dz = static_cast<T*>(dlogits) + r * ld_grad;
-        int e = lane < k ? chosen[r * k + lane] : -1;
-        if (e >= experts) e = -1;
-        const float w = lane < k ? weights[r * k + lane] : 0.f;
-        const float dw = e >= 0 ? dweights[r * k + lane] : 0.f;
-        float v[EPL];
+    const int lane = threadIdx.x & 31;
+    const auto load = [&](int64_t r) {
+        RouteRow<EPL> n;
+        const bool in = r < rows && lane < k;
+        n.e = in ? chosen[r * k + lane] : -1;
+        n.w = in ? weights[r * k + lane] : 0.f;
+        n.dw = in ? dweights[r * k + lane] : 0.f;
         if (!normalise) {
+            const T* z = static_cast<const T*>(logits) + (r < rows ? r : 0) * ld;
 #pragma unroll
-            for (int i = 0; i < EPL; ++i) v[i] = lane + 32 * i < experts ? elem_f(z[lane + 32 * i]) : -INFINITY;
+            for (int i = 0; i < EPL; ++i) n.z[i] = lane + 32 * i < experts ? elem_f(z[lane + 32 * i]) : -INFINITY;
         }
-        const bool nan = __any_sync(0xffffffffu, isnan(w)), some = __any_sync(0xffffffffu, e >= 0);
-        const float wd = e >= 0 ? w * dw : 0.f;
-        const float d = warp_sum(wd);
-        float peak = -INFINITY, sum = 0.f;
+        return n;
+    };
+    const int64_t step = (int64_t)gridDim.x * 8;
+    int64_t r = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
+    if (r >= rows) return;
+    for (RouteRow<EPL> row = load(r), next; r < rows; r += step, row = next) {
+        next = load(r + step);
+        T* dz = static_cast<T*>(dlogits) + r * ld_grad;
+        const int e = row.e < experts ? row.e : -1;
+        const bool nan = __any_sync(0xffffffffu, isnan(row.w)), some = __any_sync(0xffffffffu, e >= 0);
+        const float wd = e >= 0 ? row.w * row.dw : 0.f, d = warp_sum(wd);
+        float peak = -INFINITY, sum = 0.f, scale = 0.f;
         if (nan || !some || normalise) {
             const T fill = elem_from<T>(nan ? NAN : 0.f);
-            for (int i = lane; i < experts; i += 32) dz[i] = fill;
+#pragma unroll
+            for (int i = 0; i < EPL; ++i)
+                if (lane + 32 * i < experts) dz[lane + 32 * i] = fill;
             if (nan || !some) continue;
         } else {
 #pragma unroll
-            for (int i = 0; i < EPL; ++i) peak = fmaxf(peak, v[i]);
+            for (int i = 0; i < EPL; ++i) peak = fmaxf(peak, row.z[i]);
             peak = warp_max(peak);
 #pragma unroll
-            for (int i = 0; i < EPL; ++i) sum += v[i] = expf(v[i] - peak);
-            sum = warp_sum(sum);
-            const float scale = -d / sum;
+            for (int i = 0; i < EPL; ++i) sum += row.z[i] = expf(row.z[i] - peak);
+            scale = -d / warp_sum(sum);
 #pragma unroll
             for (int i = 0; i < EPL; ++i)
-                if (lane + 32 * i < experts) dz[lane + 32 * i] = elem_from<T>(v[i] * scale);
+                if (lane + 32 * i < experts) dz[lane + 32 * i] = elem_from<T>(row.z[i] * scale);
         }
-        float total = 0.f;  // of the row's entries of this lane's expert
-        const float term = normalise ? wd - w * d : wd;
+        const float mine = normalise ? wd - row.w * d : wd;
+        float term = 0.f;  // of the row's entries of this lane's expert: one, where no expert is named twice
         for (int i = 0; i < k; ++i) {
             const int other = __shfl_sync(0xffffffffu, e, i);
-            const float t = __shfl_sync(0xffffffffu, term, i);
-            if (other == e) total += t;
+            const float t = __shfl_sync(0xffffffffu, mine, i);
+            if (other == e) term += t;
         }
-        __syncwarp();
-        if (e >= 0) dz[e] = elem_from<T>(normalise ? total : total - d * (expf(elem_f(z[e]) - peak) / sum));
+        if (!normalise) {  // its expert's exponential, from the lane that has it
+            float p = 0.f;
+#pragma unroll
+            for (int i = 0; i < EPL; ++i) {
+                const float q = __shfl_sync(0xffffffffu, row.z[i], e & 31);
+                if (e >> 5 == i) p = q;
+            }
+            term = fmaf(p, scale, term);
+        }
+        __syncwarp();  // after the row's stores
+        if (e >= 0) dz[e] = elem_from<T>(term);
     }
 }
 
@@ -643,7 +667,7 @@ int launch_many(const RouteArgs& a, int blocks, cudaStream_t st, const char* wha
 template <class T>
 int launch_fwd(const RouteArgs& a, int blocks, cudaStream_t st, const char* what)
 {
-    const bool many = blocks > 1 && a.rows_per_block >= kManyRows && a.experts > 16 && a.experts <= kManyExperts && a.k <= 16;
+    const bool many = blocks > 1 && a.rows_per_block >= kManyRows && a.experts <= kManyExperts && a.k <= 16;
     int rc;
     if (many) {
         const auto go = [&](auto kt) {
