@@ -16,7 +16,6 @@ constexpr int kMaxExperts = DBL_ROUTE_MAX_EXPERTS, kMaxK = DBL_ROUTE_MAX_K;
 constexpr int kMaxBlocks = 256;    // of the forward pass; the workspace holds one count for each block and expert
 constexpr int kOneBlockRows = 256;  // up to here one block chooses and places
 constexpr int kManyRows = 64;       // of a block: from here a thread takes a row
-constexpr int kPlaceCounts = 8192;  // counts of a block's warps and experts in shared memory
 
 struct RouteArgs {
     const void* logits;
@@ -141,55 +140,39 @@ __device__ __forceinline__ int choose_row(const RouteArgs& a, int64_t r, int lan
 }
 
 // Gives the entries of rows r0 .. r1 - 1 their places among the block's entries of the same expert, in order, counted from
-// base[e].  counts: [warps][experts] in shared memory; the warps, which are so many that it fits, take parts of the entries in
-// order.
-__device__ __forceinline__ void place(const RouteArgs& a, int64_t r0, int64_t r1, const int* base, int* counts, int warps)
+// base[e], kPlaceRows rows at a time: a bit for each row in its expert's set; before a row are those of the words before and
+// the bits before.  sets: 2 * experts * kPlaceRows / 32 words of shared memory.
+constexpr int kPlaceRows = 128, kPlaceWords = kPlaceRows / 32;
+
+__device__ __forceinline__ void place(const RouteArgs& a, int64_t r0, int64_t r1, int* base, uint32_t* sets)
 {
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int64_t n = (r1 - r0) * a.k, part = (n + warps * 32 - 1) / (warps * 32) * 32;
-    const int32_t* chosen = a.chosen + r0 * a.k;
-    int32_t* slots = a.slots + r0 * a.k;
-    const int64_t i0 = min(n, warp * part), i1 = min(n, i0 + part);
-    for (int i = threadIdx.x; i < warps * a.experts; i += blockDim.x) counts[i] = 0;
-    __syncthreads();
-    int* mine = counts + warp * a.experts;
-    constexpr int AHEAD = 4;  // entries that a lane asks for at a time
-    if (warp < warps)
-        for (int64_t i = i0 + lane; i < i1; i += 32 * AHEAD) {
-            int e[AHEAD];
-#pragma unroll
-            for (int q = 0; q < AHEAD; ++q) e[q] = i + 32 * q < i1 ? chosen[i + 32 * q] : -1;
-#pragma unroll
-            for (int q = 0; q < AHEAD; ++q)
-                if (e[q] >= 0) atomicAdd(&mine[e[q]], 1);
+    uint32_t* before = sets + a.experts * kPlaceWords;
+    for (int64_t t0 = r0; t0 < r1; t0 += kPlaceRows) {
+        const int n = (int)min((int64_t)kPlaceRows, r1 - t0) * a.k;
+        const int32_t* chosen = a.chosen + t0 * a.k;
+        for (int i = threadIdx.x; i < a.experts * kPlaceWords; i += blockDim.x) sets[i] = 0;
+        __syncthreads();
+        for (int i = threadIdx.x; i < n; i += blockDim.x) {
+            const int e = chosen[i], row = i / a.k;
+            if (e >= 0) atomicOr(&sets[e * kPlaceWords + row / 32], 1u << (row & 31));
         }
-    __syncthreads();
-    for (int e = threadIdx.x; e < a.experts; e += blockDim.x) {
-        int at = base[e];
-#pragma unroll 8
-        for (int w = 0; w < warps; ++w) {
-            const int c = counts[w * a.experts + e];
-            counts[w * a.experts + e] = at;
-            at += c;
-        }
-    }
-    __syncthreads();
-    if (warp < warps)
-        for (int64_t i = i0 + lane; i - lane < i1; i += 32 * AHEAD) {
-            int e[AHEAD];
+        __syncthreads();
+        for (int e = threadIdx.x; e < a.experts; e += blockDim.x) {
+            int at = base[e];
 #pragma unroll
-            for (int q = 0; q < AHEAD; ++q) e[q] = i + 32 * q < i1 ? chosen[i + 32 * q] : -1;
-#pragma unroll
-            for (int q = 0; q < AHEAD; ++q) {
-                const uint32_t same = __match_any_sync(0xffffffffu, e[q]);
-                const int rank = __popc(same & ((1u << lane) - 1));
-                const int at = e[q] >= 0 ? mine[e[q]] + rank : -1;
-                __syncwarp();
-                if (e[q] >= 0 && rank == 0) mine[e[q]] += __popc(same);
-                __syncwarp();
-                if (i + 32 * q < i1) slots[i + 32 * q] = at;
+            for (int w = 0; w < kPlaceWords; ++w) {
+                before[e * kPlaceWords + w] = (uint32_t)at;
+                at += __popc(sets[e * kPlaceWords + w]);
             }
+            base[e] = at;
         }
+        __syncthreads();
+        for (int i = threadIdx.x; i < n; i += blockDim.x) {
+            const int e = chosen[i], row = i / a.k, at = e * kPlaceWords + row / 32;
+            a.slots[t0 * a.k + i] = e >= 0 ? (int)before[at] + __popc(sets[at] & ((1u << (row & 31)) - 1)) : -1;
+        }
+        __syncthreads();
+    }
 }
 
 // Exclusive sums of total[0 .. experts) into base, added to what is there, and the groups' bounds; by all threads.
@@ -223,25 +206,14 @@ __device__ __forceinline__ void bounds(const RouteArgs& a, const int* total, int
     }
 }
 
-// After the block's rows are chosen and its entries counted: their places in the block, or, where it is the only one, among all.
-__device__ __forceinline__ void finish_block(const RouteArgs& a, int64_t r0, int64_t r1, const int* total, int* base, int* part,
-                                             int* counts, int place_warps)
-{
-    if (gridDim.x > 1)
-        for (int e = threadIdx.x; e < a.experts; e += blockDim.x) a.counts[(int64_t)blockIdx.x * a.experts + e] = total[e];
-    else
-        bounds(a, total, base, part, true);
-    place(a, r0, r1, base, counts, place_warps);
-}
-
 template <int EPL>
 constexpr int choose_threads() { return EPL <= 8 ? 1024 : 512; }
 
 // Chooses the block's rows' experts and counts the entries of each; where there is one block, it places them too.
 template <class T, int EPL>
-__global__ void __launch_bounds__(choose_threads<EPL>()) route_choose_kernel(const RouteArgs a, int place_warps)
+__global__ void __launch_bounds__(choose_threads<EPL>()) route_choose_kernel(const RouteArgs a)
 {
-    extern __shared__ int counts[];  // one block: for place()
+    extern __shared__ uint32_t sets[];
     __shared__ int total[kMaxExperts], base[kMaxExperts], part[32];
     for (int e = threadIdx.x; e < a.experts; e += blockDim.x) total[e] = base[e] = 0;
     __syncthreads();
@@ -261,7 +233,12 @@ __global__ void __launch_bounds__(choose_threads<EPL>()) route_choose_kernel(con
         }
     }
     __syncthreads();
-    finish_block(a, r0, r1, total, base, part, counts, place_warps);
+    // its entries' places in the block, or, where it is the only one, among all
+    if (gridDim.x > 1)
+        for (int e = threadIdx.x; e < a.experts; e += blockDim.x) a.counts[(int64_t)blockIdx.x * a.experts + e] = total[e];
+    else
+        bounds(a, total, base, part, true);
+    place(a, r0, r1, base, sets);
 }
 
 // exp(x) for x <= 0, off by (1.5*|x| + 4)*2^-24 of it, and 0 below 2^-126: for sums that are divided by.
@@ -679,9 +656,7 @@ int launch_fwd(const RouteArgs& a, int blocks, cudaStream_t st, const char* what
     } else {
         rc = with_lanes(a.experts, [&](auto epl) {
             constexpr int EPL = decltype(epl)::value, threads = choose_threads<EPL>();
-            int warps = kPlaceCounts / a.experts;
-            if (warps > threads / 32) warps = threads / 32;
-            route_choose_kernel<T, EPL><<<blocks, threads, warps * a.experts * sizeof(int), st>>>(a, warps);
+            route_choose_kernel<T, EPL><<<blocks, threads, 2 * kPlaceWords * a.experts * sizeof(uint32_t), st>>>(a);
             return launch_check(what);
         });
     }
