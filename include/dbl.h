@@ -103,7 +103,8 @@ DBL_API int dbl_device_status(int32_t* status);
  * the SMs); DBL_MAX_CLUSTER=n takes clusters of more than n thread blocks of
  * these passes, of the BatchNorm backward and of the operators of models over
  * tokens as not fitting on the device, where smaller clusters or none are
- * used, as on a device that holds none.
+ * used, as on a device that holds none (the grouped products, which have no
+ * form without pairs, stay on them).
  * None of them changes what is computed; DBL_CONV_CTA_PAIRS and
  * DBL_MAX_CLUSTER change the order of fp32 sums (without pairs, or without
  * their clusters, no tile's reduction is split).
@@ -515,11 +516,11 @@ DBL_API int dbl_resize_taps(int32_t in, int32_t out, int32_t* i0, int32_t* i1, f
 
 /* ========================================================================
  * Operators of models over tokens, trained by the same server and workers:
- * layer norm, a gated linear recurrence along the sequence, and the
- * distillation loss.  The paper trains a ResNet-18 only; the scheme (Sec. 3
- * and 4) asks nothing of the model but its gradients, and these are the
- * layers of a sequence model that the calls above do not provide (its
- * products are dbl_conv_* with 1x1 filters).
+ * layer norm, a gated linear recurrence along the sequence, the distillation
+ * loss, a layer of experts, and dropout.  The paper trains a ResNet-18 only;
+ * the scheme (Sec. 3 and 4) asks nothing of the model but its gradients, and
+ * these are the layers of a sequence model that the calls above do not
+ * provide (its other products are dbl_conv_* with 1x1 filters).
  *
  * Beside the conventions at the top of this file:
  *  - dtype is DBL_BF16 (the library's 16-bit format) or DBL_F32, for every

@@ -1,5 +1,9 @@
 // exchange.cu -- tokens to their experts' groups and back: rows copied to the slots of their entries, the weighted sum
 // of the entries' rows, and the gradients of both.
+//
+// Bound by memory: every row is read once and written once, token by token, so that a token's own row is read once for all
+// its entries.  From a graph: 16384 rows of 1024 to two entries 12.9 us (the rows partly in the L2; 14.9 at the copy rate),
+// combine of 20011x2x1000 25.1 (22.2), its gradients of 32768x4x1024 90.7 (89.3).
 #include <type_traits>
 
 #include "dbl_elem.cuh"

@@ -1,5 +1,9 @@
 // route.cu -- the router of a layer of experts: the k experts of every token and their weights, the tokens' places
 // grouped by expert, and the gradient of the logits.
+//
+// The bytes are few (65536 tokens over 128 experts 23 MB, 3.4 us); what bounds the router is the selection's instructions and
+// the launches' latency.  The places are a counting sort without atomics on memory: a bit for each row in its expert's set gives
+// the places in a block, a second launch (one for few rows) adds what the blocks before and the smaller experts have.
 #include <float.h>
 #include <math.h>
 
@@ -268,8 +272,9 @@ constexpr int kTileThreads = 512, kTileBytes = 160 * 1024;
 
 // The same where there are many rows: a thread to a row, its logits in shared memory.  The row's experts form 16 classes,
 // every 16th expert one; the k-th largest of the classes' maxima is a bound that at least k experts reach and few others
-// (about 11 of 128 for k = 8), so that few enter the sorted list of KT.  81 instructions of a warp to a row where a warp to
-// a row takes 400.  KT: k or more.  N: elements of 16 bytes.
+// (about 11 of 128 for k = 8), so that few enter the sorted list of KT.  160 instructions of a warp to a row where a warp to
+// a row takes 400: 65536 rows of 128 with k = 8 21.5 us from a graph, both launches (47 before; 2 or 4 threads to a row, whose lists
+// are merged, 26).  KT: k or more.  N: elements of 16 bytes.
 template <class T, int KT, bool BIAS>
 __global__ void __launch_bounds__(kTileThreads) route_choose_many_kernel(const RouteArgs a, int tile, int pitch)
 {
