@@ -152,6 +152,7 @@ __device__ __forceinline__ void store_columns(uint32_t addr, uint32_t m0, uint32
 }
 
 // tmA: fwd, dgrad: the weights, wgrad: x; tmB: the tokens in boxes of 128, wgrad: dy; tmC: the tokens in boxes of 16.
+// The launch may begin before the kernel before it has ended (122 rows over 8 groups of 512x2048 in a loop of calls 10.2 -> 8.8 us).
 template <int PASS>
 __global__ void __launch_bounds__(Cfg::THREADS, 1)
     grouped_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
@@ -196,6 +197,7 @@ __global__ void __launch_bounds__(Cfg::THREADS, 1)
         tmem_relinquish_cg<2>();
     }
     if (warp == 0) {
+        grid_dependency_wait();  // what is above may overlap the kernel before; memory only after it
         load_offsets(p.offsets, p.groups, p.rows, off, lane);
         __syncwarp();
         if (PASS != kWgrad) {
@@ -217,6 +219,7 @@ __global__ void __launch_bounds__(Cfg::THREADS, 1)
     __syncthreads();
     cluster_sync_all();
     tc_fence_after();
+    grid_dependency_wait();
     const uint32_t tmem = tmem_slot;
     Walk<PASS> walk(p, first, unit0, nunits);
 
@@ -515,6 +518,7 @@ __global__ void __launch_bounds__(Cfg::THREADS, 1)
             }
         }
     }
+    grid_dependency_trigger();  // the next kernel's CTAs may be placed as these leave
     tc_fence_before();
     __syncthreads();
     // neither CTA of a pair leaves while the other may still signal its barriers or read its TMEM
@@ -637,16 +641,18 @@ int launch(const CUtensorMap (&maps)[3], const MmaArgs& p, int64_t most_tiles, c
     if (pairs < 1) pairs = sm_count() / 2;  // the device has not answered, or DBL_MAX_CLUSTER is 1: there is no other form
     if (pairs > most_tiles) pairs = (int)most_tiles;
     cudaLaunchConfig_t cfg = {};
-    cudaLaunchAttribute at[1];
+    cudaLaunchAttribute at[2];
     at[0].id = cudaLaunchAttributeClusterDimension;
     at[0].val.clusterDim.x = 2;
     at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+    at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.gridDim = dim3(2 * pairs);
     cfg.blockDim = dim3(C::THREADS);
     cfg.dynamicSmemBytes = C::SMEM;
     cfg.stream = st;
     cfg.attrs = at;
-    cfg.numAttrs = 1;
+    cfg.numAttrs = 2;
     const cudaError_t err = cudaLaunchKernelEx(&cfg, grouped_kernel<PASS>, maps[0], maps[1], maps[2], p);
     rc = launch_check(w);
     return err == cudaSuccess ? rc : cuda_check(err, w);
