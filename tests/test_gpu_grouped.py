@@ -152,6 +152,25 @@ def test_rows_of_other_groups_may_hold_anything(which):
     assert bool(out[:100].isfinite().all()) and bool(out[100:].isnan().all())
 
 
+@pytest.mark.parametrize("first", [1, 15, 16, 48, 63, 64, 65, 100, 600])
+def test_a_neighbours_rows_do_not_reach_a_weight_gradient(first):
+    """The last rows of a group are copied together with the next group's, here NaN and infinity."""
+    D = load_dbl()
+    rows, n_in, n_out = first + 70, 72, 136
+    g = rng(first)
+    x, dy = (torch.from_numpy(g.standard_normal((rows, c))).to(torch.bfloat16).cuda() for c in (n_in, n_out))
+    x[first:], dy[first:] = float("nan"), float("inf")
+    off = torch.tensor([0, first, rows], dtype=torch.int32, device="cuda")
+    dw = torch.empty((2, n_out, n_in), device="cuda")
+    shape = D.grouped_shape(rows, 2, n_in, n_out)
+    D.dbl_grouped_wgrad(shape, x, dy, off, dw, False, *scratch(D, shape, D.DBL_PASS_WGRAD))
+    xv, dv = (t[:first].double().cpu().numpy() for t in (x, dy))
+    size = np.abs(dv).T @ np.abs(xv)
+    assert_within(dw[0].double().cpu().numpy(), dv.T @ xv, sum_error(first, size), "dw")
+    assert bool(dw[1].isnan().all())
+    check_status(D)
+
+
 def test_relu_keeps_nan():
     D = load_dbl()
     off = torch.tensor([0, 8], dtype=torch.int32, device="cuda")
