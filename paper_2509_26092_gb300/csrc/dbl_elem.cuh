@@ -108,63 +108,92 @@ __device__ __forceinline__ float block_max(float v, float* red)
     return s;
 }
 
-// Rows that begin at any element, in units of 16 bytes.  A unit that is stored lies on a 16-byte boundary and holds the
-// row's elements from e on (N = 16 / sizeof(T) of them; e may be below 0 in the row's first unit, and the last may reach
-// past its end); a unit that is read for it lies anywhere, put together from the two on boundaries that it covers, of which
-// a lane loads one and takes the other from its neighbour.
+// Rows that begin at any element, in units of 16 bytes.  Unit u that is stored lies on a 16-byte boundary and holds the row's
+// elements u*N - lead to u*N - lead + N - 1 (N = 16 / sizeof(T); `lead` of the first are before the row, and the last may
+// reach past its end); what is read for it lies anywhere in memory, put together from the two units on boundaries that it
+// covers, of which a lane loads one and takes the other from its neighbour.
 template <class T>
 struct RowOf {
-    const T* row;
-    uintptr_t begin, end, low, high;  // bytes of the row, and of the tensor that it belongs to
+    const uint4* base;         // the boundary at or before the row
+    int c, units, low, high;   // units from the boundary that the row is in, and those that lie in the tensor as a whole
+    int first;                 // the row's first element, from the boundary on
+    int back;                  // 0 or -1: of unit 0 from the boundary
+    uint32_t shift;            // bytes of a unit read from its boundary
 
     // row r of [rows, c] at stride ld
-    __device__ __forceinline__ RowOf(const void* tensor, int64_t r, int64_t rows, int c, int64_t ld)
-        : row(static_cast<const T*>(tensor) + r * ld), begin(reinterpret_cast<uintptr_t>(row)), end(begin + (size_t)c * sizeof(T)),
-          low(reinterpret_cast<uintptr_t>(tensor)), high(low + ((size_t)(rows - 1) * ld + c) * sizeof(T))
+    __device__ __forceinline__ RowOf(const void* tensor, int64_t r, int64_t rows, int c, int64_t ld, int lead) : c(c)
     {
+        const uintptr_t first_byte = reinterpret_cast<uintptr_t>(tensor), begin = first_byte + (size_t)(r * ld) * sizeof(T);
+        const uintptr_t last = first_byte + ((size_t)(rows - 1) * ld + c) * sizeof(T);
+        const int d = (int)(begin & 15u), from = d - lead * (int)sizeof(T);
+        base = reinterpret_cast<const uint4*>(begin - d);
+        units = (int)((d + (size_t)c * sizeof(T) + 15) / 16);
+        low = begin - d < first_byte ? 1 : 0;
+        high = (begin - d) + (size_t)units * 16 > last ? units - 1 : units;
+        first = d / (int)sizeof(T);
+        back = from >> 4;
+        shift = (uint32_t)from & 15u;
     }
-    // The 16 bytes at a boundary: 0 where nothing of the row is in them, by elements where the tensor begins or ends in them.
-    __device__ __forceinline__ uint4 on_boundary(uintptr_t at) const
+    // M units u, u + 32, .. of what is stored: all lanes of a warp, u growing by 1 from lane to lane.  All loads go out first.
+    // The neighbour of lane 31 is lane 0 with the unit after; the last of those it loads for this alone.
+    template <int M>
+    __device__ __forceinline__ void load(int u, uint4 (&v)[M + 1]) const
     {
-        uint4 v = make_uint4(0, 0, 0, 0);
-        if (at + 16 <= begin || at >= end) return v;
-        if (at >= low && at + 16 <= high) return *reinterpret_cast<const uint4*>(at);
+        u += back;
+#pragma unroll
+        for (int m = 0; m <= M; ++m) {
+            const int at = u + 32 * m;
+            v[m] = at >= low && at < high && (m < M || (threadIdx.x & 31) == 0) ? base[at] : make_uint4(0, 0, 0, 0);
+        }
+    }
+    template <int M>
+    __device__ __forceinline__ void join(int u, uint4 (&v)[M + 1]) const
+    {
+        u += back;
+        if (low != 0 || high != units) {  // the tensor begins or ends in a unit of this row, which is read by elements
+#pragma unroll
+            for (int m = 0; m <= M; ++m) {
+                const int at = u + 32 * m;
+                if (at >= 0 && at < units && (at < low || at >= high)) v[m] = by_elements(at);
+            }
+        }
+        if (shift == 0) return;
+#pragma unroll
+        for (int m = 0; m < M; ++m) {
+            const bool after = (threadIdx.x & 31) == 0;
+            const int to = (threadIdx.x + 1) & 31;
+            uint32_t w[8] = {v[m].x, v[m].y, v[m].z, v[m].w};
+            w[4] = __shfl_sync(0xffffffffu, after ? v[m + 1].x : v[m].x, to);
+            w[5] = __shfl_sync(0xffffffffu, after ? v[m + 1].y : v[m].y, to);
+            w[6] = __shfl_sync(0xffffffffu, after ? v[m + 1].z : v[m].z, to);
+            w[7] = __shfl_sync(0xffffffffu, after ? v[m + 1].w : v[m].w, to);
+            if (shift & 8) {
+#pragma unroll
+                for (int i = 0; i < 6; ++i) w[i] = w[i + 2];
+            }
+            if (shift & 4) {
+#pragma unroll
+                for (int i = 0; i < 5; ++i) w[i] = w[i + 1];
+            }
+            if (sizeof(T) == 2) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) w[i] = __funnelshift_r(w[i], w[i + 1], (shift & 2) * 8);
+            }
+            v[m] = make_uint4(w[0], w[1], w[2], w[3]);
+        }
+    }
+    __device__ __forceinline__ uint4 by_elements(int at) const
+    {
+        constexpr int N = 16 / (int)sizeof(T);
         uint32_t w[4] = {0, 0, 0, 0};
 #pragma unroll
-        for (int i = 0; i < 16; i += (int)sizeof(T)) {
-            if (at + i < begin || at + i >= end) continue;
+        for (int i = 0; i < N; ++i) {
+            const int e = at * N + i - first;
+            if (e < 0 || e >= c) continue;
             if constexpr (sizeof(T) == 2)
-                w[i / 4] |= (uint32_t)*reinterpret_cast<const uint16_t*>(at + i) << (8 * (i & 3));
+                w[i / 2] |= (uint32_t)reinterpret_cast<const uint16_t*>(base)[at * N + i] << (16 * (i & 1));
             else
-                w[i / 4] = *reinterpret_cast<const uint32_t*>(at + i);
-        }
-        return make_uint4(w[0], w[1], w[2], w[3]);
-    }
-    // All lanes of a warp, with e growing by N from lane to lane.
-    __device__ __forceinline__ uint4 from(int e) const
-    {
-        const uintptr_t a = begin + (intptr_t)e * (intptr_t)sizeof(T), at = a & ~(uintptr_t)15;
-        const uint32_t d = (uint32_t)a & 15u;  // the same in all lanes
-        const uint4 v = on_boundary(at);
-        if (d == 0) return v;
-        uint4 n;
-        n.x = __shfl_down_sync(0xffffffffu, v.x, 1);
-        n.y = __shfl_down_sync(0xffffffffu, v.y, 1);
-        n.z = __shfl_down_sync(0xffffffffu, v.z, 1);
-        n.w = __shfl_down_sync(0xffffffffu, v.w, 1);
-        if ((threadIdx.x & 31) == 31) n = on_boundary(at + 16);
-        uint32_t w[8] = {v.x, v.y, v.z, v.w, n.x, n.y, n.z, n.w};
-        if (d & 8) {
-#pragma unroll
-            for (int i = 0; i < 6; ++i) w[i] = w[i + 2];
-        }
-        if (d & 4) {
-#pragma unroll
-            for (int i = 0; i < 5; ++i) w[i] = w[i + 1];
-        }
-        if (sizeof(T) == 2) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) w[i] = __funnelshift_r(w[i], w[i + 1], (d & 2) * 8);
+                w[i] = reinterpret_cast<const uint32_t*>(base)[at * N + i];
         }
         return make_uint4(w[0], w[1], w[2], w[3]);
     }

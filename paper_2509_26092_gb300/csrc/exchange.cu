@@ -245,11 +245,18 @@ __global__ void __launch_bounds__(256) expert_combine_bwd_kernel(const ExchangeA
 constexpr int kPart = 128;
 
 template <class T>
-__device__ __forceinline__ RowOf<T> token_row(const ExchangeArgs& a, const void* p, int64_t r) { return {p, r, a.rows, a.c, a.ld_rows}; }
+__device__ __forceinline__ RowOf<T> token_row(const ExchangeArgs& a, const void* p, int64_t r, int lead)
+{
+    return {p, r, a.rows, a.c, a.ld_rows, lead};
+}
 template <class T>
-__device__ __forceinline__ RowOf<T> grouped_row(const ExchangeArgs& a, const void* p, int64_t s) { return {p, s, a.grouped_rows, a.c, a.ld_grouped}; }
+__device__ __forceinline__ RowOf<T> grouped_row(const ExchangeArgs& a, const void* p, int64_t s, int lead)
+{
+    return {p, s, a.grouped_rows, a.c, a.ld_grouped, lead};
+}
 
-template <class T>
+// M units to a thread at a time.
+template <class T, int M>
 __global__ void __launch_bounds__(256) expert_scatter_any_kernel(const ExchangeArgs a, int parts)
 {
     constexpr int N = Chunk<T>::N;
@@ -257,21 +264,25 @@ __global__ void __launch_bounds__(256) expert_scatter_any_kernel(const ExchangeA
     const int64_t item = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5), r = item / parts;
     const int part = (int)(item - r * parts);
     if (r >= a.rows) return;
-    const RowOf<T> x = token_row<T>(a, a.a, r);
     for (int j = 0; j < a.k; ++j) {
         const int64_t s = slot_of(a, r * a.k + j);
         if (s < 0) continue;
         T* o = static_cast<T*>(a.out) + s * a.ld_grouped;
         const int lead = unit_lead(o), units = (a.c + lead + N - 1) / N, end = min(units, (part + 1) * kPart);
-        for (int u0 = part * kPart; u0 < end; u0 += 32) {
-            const int e = (u0 + lane) * N - lead;
-            const uint4 v = x.from(e);
-            if (u0 + lane < end) store_unit(o, a.c, e, v);
+        const RowOf<T> x = token_row<T>(a, a.a, r, lead);
+        for (int u0 = part * kPart; u0 < end; u0 += 32 * M) {
+            const int u = u0 + lane;
+            uint4 v[M + 1];
+            x.template load<M>(u, v);
+            x.template join<M>(u, v);
+#pragma unroll
+            for (int m = 0; m < M; ++m)
+                if (u + 32 * m < end) store_unit(o, a.c, (u + 32 * m) * N - lead, v[m]);
         }
     }
 }
 
-template <class T>
+template <class T, int M>
 __global__ void __launch_bounds__(256) expert_combine_any_kernel(const ExchangeArgs a, int parts)
 {
     constexpr int N = Chunk<T>::N;
@@ -281,70 +292,99 @@ __global__ void __launch_bounds__(256) expert_combine_any_kernel(const ExchangeA
     if (r >= a.rows) return;
     T* o = static_cast<T*>(a.out) + r * a.ld_rows;
     const int lead = unit_lead(o), units = (a.c + lead + N - 1) / N, end = min(units, (part + 1) * kPart);
-    for (int u0 = part * kPart; u0 < end; u0 += 32) {
-        const int e = (u0 + lane) * N - lead;
-        float sum[N] = {}, f[N];
+    for (int u0 = part * kPart; u0 < end; u0 += 32 * M) {
+        const int u = u0 + lane;
+        float sum[M][N] = {};
+        auto add = [&](const RowOf<T>& row, float w) {
+            uint4 v[M + 1];
+            row.template load<M>(u, v);
+            row.template join<M>(u, v);
+#pragma unroll
+            for (int m = 0; m < M; ++m) {
+                Chunk<T> y;
+                float f[N];
+                y.set(v[m]);
+                y.get(f);
+#pragma unroll
+                for (int i = 0; i < N; ++i) sum[m][i] = fmaf(w, f[i], sum[m][i]);
+            }
+        };
         for (int j = 0; j < a.k; ++j) {
             const int64_t s = slot_of(a, r * a.k + j);
             const float w = a.weights ? a.weights[r * a.k + j] : 1.f;
-            Chunk<T> y = {};
-            if (s >= 0) y.set(grouped_row<T>(a, a.a, s).from(e));
-            y.get(f);
+            if (s >= 0) {
+                add(grouped_row<T>(a, a.a, s, lead), w);
+            } else {  // w*0, which is not 0 for every w
 #pragma unroll
-            for (int i = 0; i < N; ++i) sum[i] = fmaf(w, f[i], sum[i]);
-        }
-        Chunk<T> t;
-        if (a.b) {
-            t.set(token_row<T>(a, a.b, r).from(e));
-            t.get(f);
+                for (int m = 0; m < M; ++m)
 #pragma unroll
-            for (int i = 0; i < N; ++i) sum[i] += f[i];
+                    for (int i = 0; i < N; ++i) sum[m][i] = fmaf(w, 0.f, sum[m][i]);
+            }
         }
-        t.put(sum);
-        if (u0 + lane < end) store_unit(o, a.c, e, t.vec());
+        if (a.b) add(token_row<T>(a, a.b, r, lead), 1.f);
+#pragma unroll
+        for (int m = 0; m < M; ++m) {
+            Chunk<T> t;
+            t.put(sum[m]);
+            if (u + 32 * m < end) store_unit(o, a.c, (u + 32 * m) * N - lead, t.vec());
+        }
     }
 }
 
-// G threads to a row.
-template <class T, int G>
-__global__ void __launch_bounds__(256) expert_combine_bwd_any_kernel(const ExchangeArgs a)
+// G threads to a row, M units to a thread at a time: eight rows of one warp to a block, or one row.
+template <class T, int G, int M>
+__global__ void __launch_bounds__(G == 32 ? 256 : G) expert_combine_bwd_any_kernel(const ExchangeArgs a)
 {
-    constexpr int N = Chunk<T>::N;
+    constexpr int N = Chunk<T>::N, R = G == 32 ? 8 : 1;
     __shared__ float red[32];
     const int lane = threadIdx.x & 31, warp = (threadIdx.x % G) >> 5;
-    const int64_t r = (int64_t)blockIdx.x * (256 / G) + threadIdx.x / G;
+    const int64_t r = (int64_t)blockIdx.x * R + threadIdx.x / G;
     if (r >= a.rows) return;
-    const RowOf<T> d = token_row<T>(a, a.a, r);
     for (int j = 0; j < a.k; ++j) {
         const int64_t s = slot_of(a, r * a.k + j);
         float dot = 0.f;
         if (s >= 0) {
             const float w = a.weights ? a.weights[r * a.k + j] : 1.f;
             T* o = static_cast<T*>(a.out) + s * a.ld_grouped;
-            const RowOf<T> y = grouped_row<T>(a, a.dweights ? a.b : a.out, s);
             const int lead = unit_lead(o), units = (a.c + lead + N - 1) / N;
-            for (int u0 = warp * 32; u0 < units; u0 += G) {
-                const int e = (u0 + lane) * N - lead;
-                Chunk<T> dv, yv;
-                float f[N], h[N];
-                dv.set(d.from(e));
-                dv.get(f);
+            const RowOf<T> d = token_row<T>(a, a.a, r, lead), y = grouped_row<T>(a, a.dweights ? a.b : a.out, s, lead);
+            for (int u0 = warp * 32 * M; u0 < units; u0 += G * M) {
+                const int u = u0 + lane;
+                uint4 dv[M + 1], yv[M + 1];
+                d.template load<M>(u, dv);
                 if (a.dweights) {
-                    yv.set(y.from(e));
-                    yv.get(h);
-                    // a row's first and last unit hold what is outside it
-#pragma unroll
-                    for (int i = 0; i < N; ++i)
-                        if (e + i >= 0 && e + i < a.c) dot = fmaf(f[i], h[i], dot);
+                    y.template load<M>(u, yv);
+                    y.template join<M>(u, yv);
                 }
+                d.template join<M>(u, dv);
 #pragma unroll
-                for (int i = 0; i < N; ++i) f[i] *= w;
-                dv.put(f);
-                if (u0 + lane < units) store_unit(o, a.c, e, dv.vec());
+                for (int m = 0; m < M; ++m) {
+                    const int e = (u + 32 * m) * N - lead;
+                    Chunk<T> c;
+                    float f[N], h[N];
+                    c.set(dv[m]);
+                    c.get(f);
+                    if (a.dweights) {
+                        c.set(yv[m]);
+                        c.get(h);
+                        if (e >= 0 && e + N <= a.c) {
+#pragma unroll
+                            for (int i = 0; i < N; ++i) dot = fmaf(f[i], h[i], dot);
+                        } else {  // a row's first and last unit hold what is outside it
+#pragma unroll
+                            for (int i = 0; i < N; ++i)
+                                if (e + i >= 0 && e + i < a.c) dot = fmaf(f[i], h[i], dot);
+                        }
+                    }
+#pragma unroll
+                    for (int i = 0; i < N; ++i) f[i] *= w;
+                    c.put(f);
+                    if (u + 32 * m < units) store_unit(o, a.c, e, c.vec());
+                }
             }
         }
         if (!a.dweights) continue;
-        dot = G == 256 ? block_sum(dot, red) : warp_sum(dot);
+        dot = G == 32 ? warp_sum(dot) : block_sum(dot, red);
         if (threadIdx.x % G == 0) a.dweights[r * a.k + j] = dot;
     }
 }
@@ -371,7 +411,7 @@ ExchangeArgs args(const dbl_exchange_shape* s, const void* a, const void* b, con
 
 // The bytes of a chunk: what the rows' addresses, strides and length have in common, 16 at most, an element at least; 0: long
 // rows that begin at any element, in units put together.  (30000 rows of 70 elements, two entries: combine 17 us by units, as a
-// warp has a row, 7 so; 8000 rows of 1001, four entries: scatter 32 us by elements, 21 by units, the gradients 68 and 52.)
+// warp has a row, 7 so; 8000 rows of 1001, four entries: scatter 32 us by elements, 15 by units, the gradients 68 and 39.)
 int chunk_bytes(const ExchangeArgs& a, size_t e)
 {
     uintptr_t bits = reinterpret_cast<uintptr_t>(a.a) | reinterpret_cast<uintptr_t>(a.b) | reinterpret_cast<uintptr_t>(a.out);
@@ -394,6 +434,11 @@ void with_bytes(int bytes, F f)
         f(std::integral_constant<int, 2>());
 }
 
+// Units of a row that begins anywhere up to which a thread has two at a time, not four.  (combine, 20000 rows of 333 with two
+// entries: 18 us with two, 27 with four; 8000 of 1001 with four 25.4 and 23.8, 3000 of 4001 with four 42 and 37; one unit at a
+// time 20, 29 and 51.)
+constexpr int kShort = 64;
+
 // Parts of a row that begins anywhere, and the blocks of eight warps that take them.
 template <class T>
 int row_parts(const ExchangeArgs& a) { return ((a.c + 2 * (Chunk<T>::N - 1)) / Chunk<T>::N + kPart - 1) / kPart; }
@@ -414,7 +459,10 @@ void launch_scatter(const ExchangeArgs& a, cudaStream_t st)
     const int bytes = chunk_bytes(a, sizeof(T));
     if (bytes == 0) {
         const int parts = row_parts<T>(a);
-        expert_scatter_any_kernel<T><<<part_blocks(a, parts), 256, 0, st>>>(a, parts);
+        if (a.c / Chunk<T>::N > kShort)
+            expert_scatter_any_kernel<T, 4><<<part_blocks(a, parts), 256, 0, st>>>(a, parts);
+        else
+            expert_scatter_any_kernel<T, 2><<<part_blocks(a, parts), 256, 0, st>>>(a, parts);
         return;
     }
     with_bytes<T>(bytes, [&](auto w) {
@@ -432,7 +480,10 @@ void launch_combine(const ExchangeArgs& a, cudaStream_t st)
     const int bytes = chunk_bytes(a, sizeof(T));
     if (bytes == 0) {
         const int parts = row_parts<T>(a);
-        expert_combine_any_kernel<T><<<part_blocks(a, parts), 256, 0, st>>>(a, parts);
+        if (a.c / Chunk<T>::N > kShort)
+            expert_combine_any_kernel<T, 4><<<part_blocks(a, parts), 256, 0, st>>>(a, parts);
+        else
+            expert_combine_any_kernel<T, 2><<<part_blocks(a, parts), 256, 0, st>>>(a, parts);
         return;
     }
     with_bytes<T>(bytes, [&](auto w) {
@@ -457,10 +508,14 @@ void launch_combine_bwd(const ExchangeArgs& a, cudaStream_t st)
 {
     const int bytes = chunk_bytes(a, sizeof(T));
     if (bytes == 0) {
-        if (a.c / Chunk<T>::N > 512)
-            expert_combine_bwd_any_kernel<T, 256><<<(unsigned)a.rows, 256, 0, st>>>(a);
+        // a row to a warp, or to a block of two or eight: 8000 rows of 1001, four entries, 43 us with a warp, 39 with two
+        const int units = a.c / Chunk<T>::N;
+        if (units > 512)
+            expert_combine_bwd_any_kernel<T, 256, 2><<<(unsigned)a.rows, 256, 0, st>>>(a);
+        else if (units > 96)
+            expert_combine_bwd_any_kernel<T, 64, 2><<<(unsigned)a.rows, 64, 0, st>>>(a);
         else
-            expert_combine_bwd_any_kernel<T, 32><<<(unsigned)((a.rows + 7) / 8), 256, 0, st>>>(a);
+            expert_combine_bwd_any_kernel<T, 32, 2><<<(unsigned)((a.rows + 7) / 8), 256, 0, st>>>(a);
         return;
     }
     with_bytes<T>(bytes, [&](auto w) {
