@@ -412,12 +412,16 @@ ExchangeArgs args(const dbl_exchange_shape* s, const void* a, const void* b, con
 // The bytes of a chunk: what the rows' addresses, strides and length have in common, 16 at most, an element at least; 0: long
 // rows that begin at any element, in units put together.  (30000 rows of 70 elements, two entries: combine 17 us by units, as a
 // warp has a row, 7 so; 8000 rows of 1001, four entries: scatter 32 us by elements, 15 by units, the gradients 68 and 39.)
-int chunk_bytes(const ExchangeArgs& a, size_t e)
+// Where they have four bytes in common, of more than `four` units: 8000 rows of 1001 in fp32 scatter 39 us by four bytes, 28 by
+// units, combine 50 and 47, the gradients 56 and 59; 3000 rows of 4001 have 60 and 39, 72 and 66, 136 and 84; and 8000 of 129,
+// 32 units, 7.7 and 8.5, 6.0 and 8.6, 6.8 and 15.
+int chunk_bytes(const ExchangeArgs& a, size_t e, size_t four)
 {
     uintptr_t bits = reinterpret_cast<uintptr_t>(a.a) | reinterpret_cast<uintptr_t>(a.b) | reinterpret_cast<uintptr_t>(a.out);
     bits |= (uintptr_t)a.c * e | (uintptr_t)a.ld_rows * e | (uintptr_t)a.ld_grouped * e;
     if (bits & 3) return a.c < 256 ? 2 : 0;
-    return bits & 4 ? 4 : bits & 8 ? 8 : 16;
+    if (bits & 4) return a.c * e / 16 > four ? 0 : 4;
+    return bits & 8 ? 8 : 16;
 }
 
 // f(bytes, as a value of their type)
@@ -456,7 +460,7 @@ int block_rows(const ExchangeArgs& a, int chunks)
 template <class T>
 void launch_scatter(const ExchangeArgs& a, cudaStream_t st)
 {
-    const int bytes = chunk_bytes(a, sizeof(T));
+    const int bytes = chunk_bytes(a, sizeof(T), 64);
     if (bytes == 0) {
         const int parts = row_parts<T>(a);
         if (a.c / Chunk<T>::N > kShort)
@@ -477,7 +481,7 @@ void launch_scatter(const ExchangeArgs& a, cudaStream_t st)
 template <class T>
 void launch_combine(const ExchangeArgs& a, cudaStream_t st)
 {
-    const int bytes = chunk_bytes(a, sizeof(T));
+    const int bytes = chunk_bytes(a, sizeof(T), 64);
     if (bytes == 0) {
         const int parts = row_parts<T>(a);
         if (a.c / Chunk<T>::N > kShort)
@@ -506,7 +510,7 @@ void launch_combine(const ExchangeArgs& a, cudaStream_t st)
 template <class T>
 void launch_combine_bwd(const ExchangeArgs& a, cudaStream_t st)
 {
-    const int bytes = chunk_bytes(a, sizeof(T));
+    const int bytes = chunk_bytes(a, sizeof(T), 256);
     if (bytes == 0) {
         // a row to a warp, or to a block of two or eight: 8000 rows of 1001, four entries, 43 us with a warp, 39 with two
         const int units = a.c / Chunk<T>::N;
