@@ -175,6 +175,7 @@ __global__ void __launch_bounds__(256) expert_combine_kernel(const ExchangeArgs 
 template <class T, int W, int G, int NC>
 __global__ void __launch_bounds__(256) expert_combine_bwd_kernel(const ExchangeArgs a)
 {
+    static_assert(G <= 32 || G == 256, "the sum over a row is a warp's or the block's");
     using V = Chunk<T, W>;
     constexpr int HELD = NC ? NC : 1;
     __shared__ float red[32];
@@ -413,8 +414,8 @@ ExchangeArgs args(const dbl_exchange_shape* s, const void* a, const void* b, con
 // rows that begin at any element, in units put together.  (30000 rows of 70 elements, two entries: combine 17 us by units, as a
 // warp has a row, 7 so; 8000 rows of 1001, four entries: scatter 32 us by elements, 15 by units, the gradients 68 and 39.)
 // Where they have four bytes in common, of more than `four` units: 8000 rows of 1001 in fp32 scatter 39 us by four bytes, 28 by
-// units, combine 50 and 47, the gradients 56 and 59; 3000 rows of 4001 have 60 and 39, 72 and 66, 136 and 84; and 8000 of 129,
-// 32 units, 7.7 and 8.5, 6.0 and 8.6, 6.8 and 15.
+// units, the gradients 56 and 59; 3000 rows of 4001 have 60 and 39, 136 and 84; and 8000 of 129, 32 units, 7.7 and 8.5, 6.8 and
+// 15.  combine, which adds in registers, is never faster by units: 32 and 46, 49 and 65, 6.0 and 8.6.
 int chunk_bytes(const ExchangeArgs& a, size_t e, size_t four)
 {
     uintptr_t bits = reinterpret_cast<uintptr_t>(a.a) | reinterpret_cast<uintptr_t>(a.b) | reinterpret_cast<uintptr_t>(a.out);
@@ -478,10 +479,14 @@ void launch_scatter(const ExchangeArgs& a, cudaStream_t st)
 
 // Threads to a row and chunks to a thread at a time of the forward pass.  More chunks of 16 bytes leave too few warps on an SM:
 // 20011 rows of 1000 with two entries 25.1 us with two, 27.8 with four (127 registers); 8000 of 512 in fp32 with eight 27 and 33.
+// Chunks of 8 bytes are the same (20000 of 1204 in bf16, two entries, 43 us with 256 threads to a row, 74 with 64 and eight
+// each).  Chunks of 4 want many to a thread: 8000 of 1001 in fp32, four entries, 32 us with 128 threads to a row and eight each,
+// 50 with 256 and one; 8000 of 1002 in bf16 17 with 64 and eight, 19 with 128 and four, 26 with 256 and one; 20000 of 333 in
+// fp32, two entries, 17.5 with 64 and six, 47 with 256 and one.
 template <class T>
 void launch_combine(const ExchangeArgs& a, cudaStream_t st)
 {
-    const int bytes = chunk_bytes(a, sizeof(T), 64);
+    const int bytes = chunk_bytes(a, sizeof(T), SIZE_MAX);
     if (bytes == 0) {
         const int parts = row_parts<T>(a);
         if (a.c / Chunk<T>::N > kShort)
@@ -502,6 +507,12 @@ void launch_combine(const ExchangeArgs& a, cudaStream_t st)
         if (chunks <= 32) return run(DBL_I(32), DBL_I(1));
         if (chunks <= 64) return run(DBL_I(32), DBL_I(2));
         if (chunks <= 256) return run(DBL_I(32), DBL_I(W == 16 ? 2 : 4));
+        if constexpr (W == 4) {
+            if (chunks <= 384) return run(DBL_I(64), DBL_I(6));
+            if (chunks <= 512) return run(DBL_I(64), DBL_I(8));
+            if (chunks <= 768) return run(DBL_I(256), DBL_I(3));
+            return run(DBL_I(128), DBL_I(8));
+        }
         run(DBL_I(256), DBL_I(1));
 #undef DBL_I
     });

@@ -14,8 +14,8 @@ CASES = [  # rows, k, c, stride of tokens, of grouped rows, offset, grouped rows
     (33, 3, 130, 136, 144, 0, 0), (33, 4, 136, 144, 152, 0, 100), (20, 2, 1000, 0, 0, 0, 0), (17, 5, 1001, 0, 0, 0, 0),
     (16, 2, 513, 520, 520, 1, 40), (9, 32, 256, 264, 0, 3, 0), (3, 2, 9000, 0, 0, 0, 0), (400, 2, 12, 0, 0, 0, 0),
     (50, 6, 36, 0, 40, 2, 200), (257, 1, 72, 0, 0, 0, 0), (11, 7, 4100, 0, 0, 0, 0),
-    (6, 3, 4001, 4003, 4005, 1, 0), (9, 4, 777, 779, 781, 3, 50), (5, 2, 2050, 2051, 2053, 5, 0), (70, 2, 270, 0, 271, 0, 0),
-    (4, 3, 1031, 1034, 1036, 2, 0), (12, 2, 515, 0, 0, 7, 30), (8, 3, 519, 522, 521, 0, 0)]
+    (42, 2, 1170, 0, 0, 4, 0), (9, 2, 1602, 1604, 0, 2, 0), (6, 3, 4001, 4003, 4005, 1, 0), (9, 4, 777, 779, 781, 3, 50),
+    (5, 2, 2050, 2051, 2053, 5, 0), (70, 2, 270, 0, 271, 0, 0), (4, 3, 1031, 1034, 1036, 2, 0), (12, 2, 515, 0, 0, 7, 30), (8, 3, 519, 522, 521, 0, 0)]
 
 
 def slots_of(g, rows, k, total):
