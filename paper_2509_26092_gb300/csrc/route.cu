@@ -281,7 +281,7 @@ __global__ void __launch_bounds__(kTileThreads) route_choose_many_kernel(const R
     constexpr int N = 16 / (int)sizeof(T);
     extern __shared__ __align__(16) uint8_t smem[];
     __shared__ int total[kManyExperts];
-    __shared__ float bias[BIAS ? kManyExperts : 1];
+    __shared__ __align__(16) float bias[BIAS ? kManyExperts : 1];  // read by 16 bytes
     for (int e = threadIdx.x; e < a.experts; e += blockDim.x) total[e] = 0;
     grid_dependency_trigger();
     const int padded = (a.experts + 15) / 16 * 16;
