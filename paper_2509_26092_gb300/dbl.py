@@ -113,7 +113,8 @@ class DropoutShape(ctypes.Structure):
 
 
 _libs = {}
-_precision = contextvars.ContextVar("dbl_precision", default="bf16")
+# the blocks of precision() that this context is in, outermost first
+_blocks = contextvars.ContextVar("dbl_precision", default=())
 PRECISIONS = ("bf16", "f16")
 _V = ctypes.c_void_p
 _I32 = ctypes.c_int32
@@ -123,32 +124,39 @@ _D = ctypes.c_double
 
 
 def lib_path(p=None):
-    return build_lib.library_path(p or _precision.get())
+    return build_lib.library_path(p or current_precision())
 
 
 class precision(contextlib.ContextDecorator):
-    """Route the calls made inside the block to the library of storage format p ("bf16" or "f16")."""
+    """Route the calls made inside the block, or inside the decorated function, to the library of storage format p ("bf16"
+    or "f16").  The blocks that are open belong to the context (a thread, a task), so that one object may be entered again and
+    in several threads at once."""
 
     def __init__(self, p):
         if p not in PRECISIONS:
             raise ValueError(f"precision must be one of {PRECISIONS}, not {p!r}")
-        self._p, self._tokens = p, []
+        self._p = p
 
     def __enter__(self):
-        self._tokens.append(_precision.set(self._p))
+        _blocks.set(_blocks.get() + (self,))
 
     def __exit__(self, *exc):
-        _precision.reset(self._tokens.pop())
+        blocks = _blocks.get()
+        last = max((i for i, b in enumerate(blocks) if b is self), default=None)
+        if last is None:
+            raise ValueError("a precision block is left in another context than it was entered in")
+        _blocks.set(blocks[:last] + blocks[last + 1:])
 
 
 def current_precision():
-    return _precision.get()
+    blocks = _blocks.get()
+    return blocks[-1]._p if blocks else "bf16"
 
 
 def lib(p=None):
     """Load the library of storage format p (default: the current one); it must have been built
     by ``build_lib.build()``."""
-    p = p or _precision.get()
+    p = p or current_precision()
     if p not in _libs:
         path = build_lib.library_path(p)
         if not os.path.exists(path):
