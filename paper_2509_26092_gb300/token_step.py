@@ -23,11 +23,16 @@ rows and back (``dbl_expert_*``) and the products of each expert's rows (``dbl_g
 residual additions run inside the norms, forward and backward.
 """
 import argparse
+import itertools
 
 import torch
 
 from . import dbl as D
 from .resnet18 import ACT_DTYPE, DualBatchIteration, FlatSpec, ServerState
+
+
+# the seeds of workers that are given none, far from those that programs give
+_next_seed = itertools.count(1 << 63)
 
 
 class TokenSpec(FlatSpec):
@@ -70,11 +75,12 @@ class TokenWorker:
     logits per token.  ``lengths`` ([n] int32, all t at first) ends sequences earlier; tokens past them count
     neither in the loss nor in the states nor, whatever their features hold, in a gradient, and go to no expert.
     ``dropout``: the rate of what each layer adds to the stream, its masks drawn from ``seed`` and ``step``, the
-    worker's count of its iterations on the device.  What a step reads (teacher, lengths, labels) is set on the
-    current stream, which the next iteration follows."""
+    worker's count of its iterations on the device.  Workers of the same seed have the same masks at the same step;
+    one that is given none has its own, the next in the order in which the program makes them.  What a step reads
+    (teacher, lengths, labels) is set on the current stream, which the next iteration follows."""
 
     def __init__(self, spec, n, t, k, temperature=2.0, alpha=0.5, device="cuda", eps=1e-5, precision="bf16",
-                 dropout=0.0, seed=0):
+                 dropout=0.0, seed=None):
         self.spec, self.batch, self.res, self.k, self.eps, self.precision = spec, n, t, k, eps, precision
         rows, w = n * t, spec.width
         self.rows = rows
@@ -121,6 +127,7 @@ class TokenWorker:
             self.down_shape = D.grouped_shape(rows * spec.chosen, spec.experts, spec.hidden, w)
             self.dhg, self.dr, self.dweights = entries(spec.hidden), act(spec.routed), vec(rows * spec.chosen)
         self.dropout, self.step = float(dropout), torch.zeros(1, dtype=torch.int64, device=device)
+        seed = next(_next_seed) if seed is None else seed
         self.drops = [D.dropout_shape(rows, w, dropout, seed ^ (0x9E3779B97F4A7C15 * (i + 1)))
                       for i in range(len(self.blocks) - 1)]
         self.dv = act(w) if self.dropout else None
