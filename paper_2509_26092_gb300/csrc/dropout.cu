@@ -114,6 +114,7 @@ __device__ __forceinline__ void store8(void* p, uint2 v)
 template <class T, int W>
 __global__ void __launch_bounds__(256) dropout_any_kernel(const DropArgs a, int rows_per_block)
 {
+    static_assert(sizeof(T) == 2 || W == 4, "wider accesses are pairs of 16-bit values");
     const unsigned per = ((unsigned)a.c + 3) / 4;
     const int64_t r0 = (int64_t)blockIdx.x * rows_per_block;
     const unsigned n = (unsigned)min((int64_t)rows_per_block, a.rows - r0) * per;
@@ -164,7 +165,7 @@ int launch(const DropArgs& a, cudaStream_t st, const char* what)
         dropout_any_kernel<T, (int)sizeof(T)><<<blocks, 256, 0, st>>>(a, rpb);
     else if (bits & 7)
         dropout_any_kernel<T, 4><<<blocks, 256, 0, st>>>(a, rpb);
-    else
+    else if constexpr (sizeof(T) == 2)
         dropout_any_kernel<T, 8><<<blocks, 256, 0, st>>>(a, rpb);
     return launch_check(what);
 }

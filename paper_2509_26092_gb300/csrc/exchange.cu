@@ -116,6 +116,7 @@ __global__ void __launch_bounds__(256) expert_scatter_kernel(const ExchangeArgs 
 template <class T, int W, int G, int NC>
 __global__ void __launch_bounds__(256) expert_combine_kernel(const ExchangeArgs a)
 {
+    static_assert(W > 2 || G <= 32, "rows go by single elements up to 255 of them");
     using V = Chunk<T, W>;
     const int chunks = a.c / V::N, g = threadIdx.x % G;
     const int64_t r = (int64_t)blockIdx.x * (256 / G) + threadIdx.x / G;
@@ -176,6 +177,7 @@ template <class T, int W, int G, int NC>
 __global__ void __launch_bounds__(256) expert_combine_bwd_kernel(const ExchangeArgs a)
 {
     static_assert(G <= 32 || G == 256, "the sum over a row is a warp's or the block's");
+    static_assert(W > 2 || G <= 32, "rows go by single elements up to 255 of them");
     using V = Chunk<T, W>;
     constexpr int HELD = NC ? NC : 1;
     __shared__ float red[32];
@@ -260,6 +262,7 @@ __device__ __forceinline__ RowOf<T> grouped_row(const ExchangeArgs& a, const voi
 template <class T, int M>
 __global__ void __launch_bounds__(256) expert_scatter_any_kernel(const ExchangeArgs a, int parts)
 {
+    static_assert(sizeof(T) == 2 || M == 4, "rows of fp32 come here with more than kShort units");
     constexpr int N = Chunk<T>::N;
     const int lane = threadIdx.x & 31;
     const int64_t item = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5), r = item / parts;
@@ -286,6 +289,7 @@ __global__ void __launch_bounds__(256) expert_scatter_any_kernel(const ExchangeA
 template <class T, int M>
 __global__ void __launch_bounds__(256) expert_combine_any_kernel(const ExchangeArgs a, int parts)
 {
+    static_assert(sizeof(T) == 2, "rows of fp32 go by four bytes at the least");
     constexpr int N = Chunk<T>::N;
     const int lane = threadIdx.x & 31;
     const int64_t item = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5), r = item / parts;
@@ -336,6 +340,7 @@ __global__ void __launch_bounds__(256) expert_combine_any_kernel(const ExchangeA
 template <class T, int G, int M>
 __global__ void __launch_bounds__(G == 32 ? 256 : G) expert_combine_bwd_any_kernel(const ExchangeArgs a)
 {
+    static_assert(sizeof(T) == 2 || G > 32, "rows of fp32 come here with more than 256 units");
     constexpr int N = Chunk<T>::N, R = G == 32 ? 8 : 1;
     __shared__ float red[32];
     const int lane = threadIdx.x & 31, warp = (threadIdx.x % G) >> 5;
@@ -461,13 +466,15 @@ int block_rows(const ExchangeArgs& a, int chunks)
 template <class T>
 void launch_scatter(const ExchangeArgs& a, cudaStream_t st)
 {
-    const int bytes = chunk_bytes(a, sizeof(T), 64);
+    const int bytes = chunk_bytes(a, sizeof(T), kShort);
     if (bytes == 0) {
         const int parts = row_parts<T>(a);
-        if (a.c / Chunk<T>::N > kShort)
-            expert_scatter_any_kernel<T, 4><<<part_blocks(a, parts), 256, 0, st>>>(a, parts);
-        else
-            expert_scatter_any_kernel<T, 2><<<part_blocks(a, parts), 256, 0, st>>>(a, parts);
+        if constexpr (sizeof(T) == 2)
+            if (a.c / Chunk<T>::N <= kShort) {
+                expert_scatter_any_kernel<T, 2><<<part_blocks(a, parts), 256, 0, st>>>(a, parts);
+                return;
+            }
+        expert_scatter_any_kernel<T, 4><<<part_blocks(a, parts), 256, 0, st>>>(a, parts);
         return;
     }
     with_bytes<T>(bytes, [&](auto w) {
@@ -487,14 +494,15 @@ template <class T>
 void launch_combine(const ExchangeArgs& a, cudaStream_t st)
 {
     const int bytes = chunk_bytes(a, sizeof(T), SIZE_MAX);
-    if (bytes == 0) {
-        const int parts = row_parts<T>(a);
-        if (a.c / Chunk<T>::N > kShort)
-            expert_combine_any_kernel<T, 4><<<part_blocks(a, parts), 256, 0, st>>>(a, parts);
-        else
-            expert_combine_any_kernel<T, 2><<<part_blocks(a, parts), 256, 0, st>>>(a, parts);
-        return;
-    }
+    if constexpr (sizeof(T) == 2)
+        if (bytes == 0) {
+            const int parts = row_parts<T>(a);
+            if (a.c / Chunk<T>::N > kShort)
+                expert_combine_any_kernel<T, 4><<<part_blocks(a, parts), 256, 0, st>>>(a, parts);
+            else
+                expert_combine_any_kernel<T, 2><<<part_blocks(a, parts), 256, 0, st>>>(a, parts);
+            return;
+        }
     with_bytes<T>(bytes, [&](auto w) {
         constexpr int W = decltype(w)::value;
         const int chunks = a.c / Chunk<T, W>::N;
@@ -511,9 +519,10 @@ void launch_combine(const ExchangeArgs& a, cudaStream_t st)
             if (chunks <= 384) return run(DBL_I(64), DBL_I(6));
             if (chunks <= 512) return run(DBL_I(64), DBL_I(8));
             if (chunks <= 768) return run(DBL_I(256), DBL_I(3));
-            return run(DBL_I(128), DBL_I(8));
+            run(DBL_I(128), DBL_I(8));
+        } else if constexpr (W > 4) {
+            run(DBL_I(256), DBL_I(1));
         }
-        run(DBL_I(256), DBL_I(1));
 #undef DBL_I
     });
 }
@@ -527,9 +536,9 @@ void launch_combine_bwd(const ExchangeArgs& a, cudaStream_t st)
         const int units = a.c / Chunk<T>::N;
         if (units > 512)
             expert_combine_bwd_any_kernel<T, 256, 2><<<(unsigned)a.rows, 256, 0, st>>>(a);
-        else if (units > 96)
+        else if (sizeof(T) == 4 || units > 96)
             expert_combine_bwd_any_kernel<T, 64, 2><<<(unsigned)a.rows, 64, 0, st>>>(a);
-        else
+        else if constexpr (sizeof(T) == 2)
             expert_combine_bwd_any_kernel<T, 32, 2><<<(unsigned)((a.rows + 7) / 8), 256, 0, st>>>(a);
         return;
     }
@@ -547,10 +556,11 @@ void launch_combine_bwd(const ExchangeArgs& a, cudaStream_t st)
         if (chunks <= 64) return run(DBL_I(32), DBL_I(2));
         if (chunks <= 128) return run(DBL_I(32), DBL_I(4));
         if (chunks <= 256) return run(DBL_I(32), DBL_I(8));
-        if (W < 16 && chunks <= 512) return run(DBL_I(32), DBL_I(16));
-        if (chunks <= 512) return run(DBL_I(256), DBL_I(2));
-        if (chunks <= 1024) return run(DBL_I(256), DBL_I(4));
-        run(DBL_I(256), DBL_I(0));
+        if constexpr (W > 2) {
+            if (chunks <= 512) return run(DBL_I(W < 16 ? 32 : 256), DBL_I(W < 16 ? 16 : 2));
+            if (chunks <= 1024) return run(DBL_I(256), DBL_I(4));
+            run(DBL_I(256), DBL_I(0));
+        }
 #undef DBL_I
     });
 }
