@@ -724,8 +724,10 @@ DBL_API int dbl_route_bwd(const dbl_route_shape* shape, const void* logits, cons
  *     (dx[r] = sum_j dxg[slots[r][j]] [+ dskip[r]]).
  *   combine_bwd: dyg[slots[r][j]] = weights[r][j]*dout[r] (weights = NULL: 1),
  *     dweights[r][j] = sum_c dout[r]*yg[slots[r][j]] (0 for an absent entry);
- *     dweights may be NULL, yg too then.  dyg may be yg's own buffer.
- * Two entries of the same slot: scatter and combine_bwd leave either's row. */
+ *     dweights may be NULL, yg too then.  dyg may be yg's own buffer, where no
+ *     two entries have the same slot.
+ * Two entries of the same slot: scatter and combine_bwd leave in each element
+ * of the row what either's has there (two tokens' rows may be mixed). */
 typedef struct {
     int64_t rows;
     int32_t k, c;
