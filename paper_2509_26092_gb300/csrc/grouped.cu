@@ -674,10 +674,10 @@ int64_t part_elements(const dbl_grouped_shape* s, int pass)
 }
 
 // Parts of a tile's reduction, which a second launch adds, where there are few tiles.  fwd, dgrad: as many as fill the pairs, with
-// eight stages each at least: 8 rows of one group of 4096x4096 24.8 -> 14.7 us.  wgrad: the least modelled time in us, a stage
-// taking 0.3, an item's end 2, the second launch 3 and what it reads and the parts are written at 5 TB/s; the groups are taken as
-// of the same length.  65000 rows of one group of 512x512 312 -> 41 us, 40000 of two of 2048x256 105 -> 47, 48000 rows of
-// one of 664x3424 (42 tiles for 76 pairs) 238 -> 208.
+// eight stages each at least: 8 rows of one group of 4096x4096 21.2 us whole, 12.2 in parts.  wgrad: the least modelled time in
+// us, a stage taking 0.3, an item's end 2, the second launch 3 and what it reads and the parts are written at 5 TB/s; the groups
+// are taken as of the same length, so that one long group among empty ones stays whole.  65000 rows of one group of 512x512 307 us
+// whole, 39 in parts, 40000 of two of 2048x256 111 and 46, 48000 rows of one of 664x3424 (42 tiles for 76 pairs) 236 and 208.
 int parts_of(const dbl_grouped_shape* s, int pass)
 {
     const int64_t tiles = tiles_of(s, pass), pairs = sm_count() / 2;
@@ -690,7 +690,7 @@ int parts_of(const dbl_grouped_shape* s, int pass)
     const double bytes = 4.0 * (double)part_elements(s, pass);
     int best = 1;
     double least = 0.0;
-    for (int n = 1; n <= 76 && (n == 1 || stages / n >= 8); ++n) {
+    for (int n = 1; n <= pairs && (n == 1 || stages / n >= 8); ++n) {
         const double rounds = (double)((tiles * n + pairs - 1) / pairs);
         const double us = rounds * (0.3 * (double)stages / n + 2.0) + (n > 1 ? 3.0 + 2 * n * bytes / 5e6 : 0.0);
         if (n == 1 || us < least) least = us, best = n;
