@@ -113,8 +113,8 @@ class DropoutShape(ctypes.Structure):
 
 
 _libs = {}
-# the blocks of precision() that this context is in, outermost first
-_blocks = contextvars.ContextVar("dbl_precision", default=())
+# the innermost block of precision() that this context is in: (its format, its object, the block around it)
+_block = contextvars.ContextVar("dbl_precision", default=("bf16", None, None))
 PRECISIONS = ("bf16", "f16")
 _V = ctypes.c_void_p
 _I32 = ctypes.c_int32
@@ -138,25 +138,28 @@ class precision(contextlib.ContextDecorator):
         self._p = p
 
     def __enter__(self):
-        _blocks.set(_blocks.get() + (self,))
+        _block.set((self._p, self, _block.get()))
 
     def __exit__(self, *exc):
-        blocks = _blocks.get()
-        last = max((i for i, b in enumerate(blocks) if b is self), default=None)
-        if last is None:
+        block = _block.get()
+        _block.set(block[2] if block[1] is self else self._without(block))
+
+    def _without(self, block):
+        """The open blocks without this object's innermost one, where blocks do not nest (as of two generators)."""
+        p, other, outer = block
+        if outer is None:
             raise ValueError("a precision block is left in another context than it was entered in")
-        _blocks.set(blocks[:last] + blocks[last + 1:])
+        return outer if other is self else (p, other, self._without(outer))
 
 
 def current_precision():
-    blocks = _blocks.get()
-    return blocks[-1]._p if blocks else "bf16"
+    return _block.get()[0]
 
 
 def lib(p=None):
     """Load the library of storage format p (default: the current one); it must have been built
     by ``build_lib.build()``."""
-    p = p or current_precision()
+    p = p or _block.get()[0]
     if p not in _libs:
         path = build_lib.library_path(p)
         if not os.path.exists(path):
