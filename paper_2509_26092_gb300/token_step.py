@@ -45,7 +45,7 @@ class TokenSpec(FlatSpec):
         if width % 64:
             raise ValueError("width must be a multiple of 64")
         hidden = hidden or 4 * width
-        if experts and (hidden % 8 or not 1 <= chosen <= min(experts, D.DBL_ROUTE_MAX_K)
+        if experts and (hidden < 8 or hidden % 8 or not 1 <= chosen <= min(experts, D.DBL_ROUTE_MAX_K)
                         or experts > D.DBL_ROUTE_MAX_EXPERTS):
             raise ValueError(f"a layer of experts has 1 to {D.DBL_ROUTE_MAX_EXPERTS} experts, 1 to "
                              f"{D.DBL_ROUTE_MAX_K} of them for a token, and a multiple of 8 hidden channels")
