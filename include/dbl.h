@@ -682,6 +682,11 @@ DBL_API int dbl_distill_fwd_bwd(const dbl_distill_shape* shape, const void* logi
  * +infinity among its logits has no distribution: its entries are absent and
  * their weights NaN.  row_weight (or NULL): [rows] fp32; a row of weight 0
  * (padding) has no entries, and weights of 0, whatever it holds.
+ * With many rows (64 and more for each SM, at most 512 experts and k = 16) the
+ * exponentials of the sum over all experts are the hardware's, each off by
+ * (1.5*|x| + 4)*2^-24 of itself, x being the logit less the row's largest, so
+ * that the weights of normalise = 0 may differ in their last digits from the
+ * same row's in a call of few rows.  The choice and the places are the same.
  * select_bias (or NULL): [experts] fp32, added for the choice alone, to even
  * out the experts' loads; it has no gradient.
  * slots: the entries' places in the order of expert, then row, then j.

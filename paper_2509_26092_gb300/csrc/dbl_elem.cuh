@@ -1,5 +1,5 @@
-// dbl_elem.cuh -- element types and block sums of the token operators (ln.cu, scan.cu, distill.cu), whose
-// tensors are fp32 or the library's 16-bit format.
+// dbl_elem.cuh -- element types, launches, block sums and rows that begin anywhere, of the token operators (ln.cu, scan.cu,
+// distill.cu, route.cu, exchange.cu, grouped.cu, dropout.cu), whose tensors are fp32 or the library's 16-bit format.
 #pragma once
 
 #include "dbl_internal.cuh"

@@ -421,6 +421,10 @@ ExchangeArgs args(const dbl_exchange_shape* s, const void* a, const void* b, con
 // Where they have four bytes in common, of more than `four` units: 8000 rows of 1001 in fp32 scatter 39 us by four bytes, 28 by
 // units, the gradients 56 and 59; 3000 rows of 4001 have 60 and 39, 136 and 84; and 8000 of 129, 32 units, 7.7 and 8.5, 6.8 and
 // 15.  combine, which adds in registers, is never faster by units: 32 and 46, 49 and 65, 6.0 and 8.6.
+// Where they have two bytes in common, from 256 columns on.  20000 rows of 129, 199 and 255 in bf16, two entries: scatter 10.0,
+// 14.2 and 17.0 us by elements, 12.1, 12.2 and 13.5 by units; combine 9.3, 9.6 and 9.7, 16.4, 16.5 and 17.5; the gradients 8.1, 8.5
+// and 9.1, 22.9, 22.9 and 24.9.  One border for the three, scatter's and long rows': at 257 and 511 combine takes 13.2 and 18.4 by
+// elements, 17.5 and 27.6 by units, the gradients 13.3 and 20.5, 24.8 and 38.3.
 int chunk_bytes(const ExchangeArgs& a, size_t e, size_t four)
 {
     uintptr_t bits = reinterpret_cast<uintptr_t>(a.a) | reinterpret_cast<uintptr_t>(a.b) | reinterpret_cast<uintptr_t>(a.out);
